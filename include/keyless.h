@@ -57,7 +57,10 @@ typedef enum kl_status {
 #define KL_FLAG_BAD_LENGTH 0x4   /* seq_len outside [0, max_pages_per_seq * P] */
 #define KL_FLAG_TIMEOUT 0x8      /* a bounded pipeline wait gave up (output invalid) */
 #define KL_FLAG_RANGE 0x10       /* a non-finite output of kl_prefill_attention (a cached value
-                                    beyond its fp16 range, or a non-finite input) */
+                                    beyond its fp16 range, or a non-finite input); a NaN or +inf
+                                    logit in kl_token_logprobs */
+#define KL_FLAG_BAD_TREE 0x20    /* a parent, or an accepted path, that is not in its sequence's tree */
+#define KL_FLAG_BAD_TOKEN 0x40   /* a token id outside [-1, vocab) */
 
 typedef enum kl_dtype { KL_BF16 = 0, KL_FP32 = 1 } kl_dtype;
 
@@ -252,6 +255,93 @@ kl_status kl_prefill_attention(const kl_shape *shape, const void *q, const void 
                                const int32_t *seq_lens, const int32_t *cu_q_lens,
                                int32_t total_q, int32_t max_q_len, void *out, kl_dtype out_dtype,
                                int32_t *err, kl_stream_t stream);
+
+/* ---- Verification of drafted tokens (speculative decoding) ------------------------------------
+ *
+ * A server drafts several continuations of each sequence as a tree, appends the drafted tokens' value
+ * rows behind the committed ones (kl_append_v_chunk), attends for all of them in one call
+ * (kl_tree_attention), reads the model's logits for them (kl_token_logprobs), chooses a path and keeps
+ * its rows (kl_tree_commit). The paper has no counterpart: the scores and outputs are those of its
+ * decode formula over the tokens that each draft sees. */
+
+/* Most drafted tokens per sequence. */
+#define KL_TREE_MAX_DRAFTS 128
+
+/* Bytes of device workspace kl_tree_attention needs (0 when it needs none, or on an invalid shape).
+ * The contract of kl_decode_workspace_size: zero-filled before its first use, then shared by any
+ * sequence of calls and shapes, decodes included. */
+size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len,
+                              int32_t num_splits);
+
+/*
+ * Attention of a tree of drafted tokens over the paged Value-Only Cache (Section 3's decode formula with
+ * the routing of Section 2.2). Sequence b's n_b = cu_q_lens[b + 1] - cu_q_lens[b] drafts are its last n_b
+ * cached rows (seq_lens[b] includes them; append them first). Draft i (row r = cu_q_lens[b] + i of q,
+ * out and parents) follows draft parents[r] of the same sequence (0 <= parents[r] < i), or the last
+ * committed token (-1), and sees the seq_lens[b] - n_b committed tokens, itself and its ancestors:
+ *   q_r = q[r][h] W^R[w(h)],  s_t = scale * <q_r, v_t>,  out[r][h] = sum_t softmax(s)_t v_t
+ * over these tokens. n_b = 1 is the decode step; parents[r] = i - 1 is the causal chunk.
+ * q, out: [total_q][Hq][D] (q bf16, out of out_dtype); cu_q_lens: [B + 1] int32 on the device,
+ * non-decreasing from 0; parents: [total_q] int32; max_q_len: a host-side bound on every n_b, at most
+ * KL_TREE_MAX_DRAFTS; w_r (NULL: q is the composed query), v_cache, block_table, seq_lens, num_splits as
+ * in kl_decode_attention. Workspace: kl_tree_workspace_size bytes of the same arguments, 256-byte
+ * aligned. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3 (KL_ERR_UNSUPPORTED
+ * otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <=
+ * max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine: nothing is
+ * written); a parent outside [-1, i) raises KL_FLAG_BAD_TREE and counts as -1; a bad page id leaves the
+ * affected outputs unspecified. A drafted row that is not finite reaches the drafts that see it
+ * alone. fp32 accumulation; the routed query and the softmax weights carry about 16 significant bits.
+ */
+kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
+                            const int32_t *block_table, const int32_t *seq_lens,
+                            const int32_t *cu_q_lens, const int32_t *parents, int32_t total_q,
+                            int32_t max_q_len, int32_t num_splits, void *out, kl_dtype out_dtype,
+                            void *workspace, size_t workspace_bytes, int32_t *err, kl_stream_t stream);
+
+/*
+ * Keep the accepted path of every tree: path[b][0 .. path_lens[b] - 1] are drafts of sequence b, strictly
+ * increasing (a path from the root down is); their value rows move to the front of the drafted region,
+ *   row seq_lens[b] - n_b + path[b][j]  ->  row seq_lens[b] - n_b + j   of every value head,
+ * and new_lens[b] = seq_lens[b] - n_b + path_lens[b] (new_lens may be seq_lens). path: [B][max_path]
+ * int32 (entries past path_lens[b] are not read); v_cache: [num_pages][Hkv][P][D] bf16, in place. A
+ * sequence whose lengths break 0 <= n_b <= min(KL_TREE_MAX_DRAFTS, seq_lens[b]) or seq_lens[b] <=
+ * max_pages_per_seq * P (KL_FLAG_BAD_LENGTH), whose path is longer than n_b or max_path or not strictly
+ * increasing within [0, n_b) (KL_FLAG_BAD_TREE), or whose pages lie outside the pool (KL_FLAG_BAD_PAGE)
+ * is left as it is, its new_lens entry included.
+ */
+kl_status kl_tree_commit(const kl_shape *shape, const int32_t *cu_q_lens, const int32_t *path,
+                         const int32_t *path_lens, int32_t max_path, const int32_t *block_table,
+                         const int32_t *seq_lens, int32_t *new_lens, void *v_cache, int32_t *err,
+                         kl_stream_t stream);
+
+/* Most alternatives per row of kl_token_logprobs. */
+#define KL_LOGPROBS_MAX_TOP 32
+
+/* Bytes of device workspace kl_token_logprobs needs (for either type of logits; 0 on bad arguments); the
+ * contract of kl_decode_workspace_size, and the same workspace may serve both. */
+size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top);
+
+/*
+ * Log probabilities under x = scale * logits (scale <= 0 selects 1; 1 / temperature otherwise). For row
+ * r, with z = sum_j exp(x_j):
+ *   logprobs[r][k]      = x_t - log z,  t = tokens[r][k]   (-1: no token, 0 is written)
+ *   entropy[r]          = -sum_j p_j log p_j, p = exp(x) / z           (in nats; NULL: not wanted)
+ *   top_ids[r][0 ..]    = the num_top largest logits, largest first, ties to the lowest index
+ *   top_logprobs[r][0 ..] = their log probabilities
+ * logits: [num_rows][row_stride] of logits_dtype, the first `vocab` of each row, row_stride >= vocab
+ * elements, aligned to their own size alone; tokens: [num_rows][tokens_per_row] int32; outputs fp32 and
+ * int32, dense; num_top <= min(vocab, KL_LOGPROBS_MAX_TOP), 0 for none (top_* are then not written),
+ * tokens_per_row may be 0. A token id outside [-1, vocab) raises KL_FLAG_BAD_TOKEN and gets NaN. Logits of
+ * -inf have probability 0; a row of -inf alone gives log probabilities of -inf and entropy 0. A NaN
+ * or +inf logit makes the row's log probabilities and entropy NaN and raises KL_FLAG_RANGE; NaN is never
+ * among the largest (an id of -1 stands where no logit is left). fp32 sums. One launch; the workspace
+ * holds kl_logprobs_workspace_size bytes, 256-byte aligned.
+ */
+kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride, const void *logits,
+                            kl_dtype logits_dtype, float scale, const int32_t *tokens,
+                            int32_t tokens_per_row, int32_t num_top, float *logprobs, float *entropy,
+                            float *top_logprobs, int32_t *top_ids, void *workspace,
+                            size_t workspace_bytes, int32_t *err, kl_stream_t stream);
 
 /*
  * Shape of a decode over a latent value-only cache (Section 3, "Multihead with Latent Value-only

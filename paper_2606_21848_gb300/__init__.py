@@ -19,4 +19,7 @@ from ._lib import (  # noqa: F401
     kl_latent_decode_step,
     kl_append_v_fp8, kl_decode_attention_fp8, kl_decode_step_fp8, kl_quantize_cache_fp8,
     kl_set_wait_timeout_ns,
+    KL_FLAG_BAD_TOKEN, KL_FLAG_BAD_TREE, KL_LOGPROBS_MAX_TOP, KL_TREE_MAX_DRAFTS,
+    kl_logprobs_workspace_size, kl_token_logprobs, kl_tree_attention, kl_tree_commit,
+    kl_tree_workspace_size,
 )

@@ -21,7 +21,9 @@ KL_OK, KL_ERR_INVALID_ARG, KL_ERR_UNSUPPORTED, KL_ERR_WORKSPACE, KL_ERR_CUDA = r
 KL_BF16, KL_FP32 = 0, 1
 KL_KERNEL_AUTO, KL_KERNEL_TENSOR, KL_KERNEL_SIMT = 0, 1, 2
 KL_FLAG_BAD_PAGE, KL_FLAG_BAD_POSITION, KL_FLAG_BAD_LENGTH, KL_FLAG_TIMEOUT, KL_FLAG_RANGE = 1, 2, 4, 8, 16
+KL_FLAG_BAD_TREE, KL_FLAG_BAD_TOKEN = 32, 64
 KL_NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024
+KL_TREE_MAX_DRAFTS, KL_LOGPROBS_MAX_TOP = 128, 32
 
 HEADER = os.path.join(_build.INCLUDE, "keyless.h")
 
@@ -71,6 +73,7 @@ def load() -> ctypes.CDLL:
         raise RuntimeError(f"libkeyless is not built ({_build.LIB} missing); call build() first")
     lib = ctypes.CDLL(_build.LIB)
     P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    I64, F32 = ctypes.c_int64, ctypes.c_float
     SH = ctypes.POINTER(kl_shape)
     OP = ctypes.POINTER(kl_decode_options)
     LS = ctypes.POINTER(kl_latent_shape)
@@ -95,6 +98,11 @@ def load() -> ctypes.CDLL:
         "kl_latent_decode": ([LS, P, P, P, P, P, P, I32, P, I32, P, SZ, P, P], I32),
         "kl_latent_decode_step": ([LS, P, P, P, P, P, P, P, P, I32, P, I32, P, SZ, P, P], I32),
         "kl_prefill_attention": ([SH, P, P, P, P, P, P, I32, I32, P, I32, P, P], I32),
+        "kl_tree_workspace_size": ([SH, I32, I32, I32], SZ),
+        "kl_tree_attention": ([SH, P, P, P, P, P, P, P, I32, I32, I32, P, I32, P, SZ, P, P], I32),
+        "kl_tree_commit": ([SH, P, P, P, I32, P, P, P, P, P, P], I32),
+        "kl_logprobs_workspace_size": ([I32, I32, I32], SZ),
+        "kl_token_logprobs": ([I32, I32, I64, P, I32, F32, P, I32, I32, P, P, P, P, P, SZ, P, P], I32),
         "kl_set_wait_timeout_ns": ([ctypes.c_uint64], ctypes.c_uint64),
         "kl_status_string": ([I32], ctypes.c_char_p),
     }
@@ -151,7 +159,7 @@ class _Ctypes:
                     out.append(self._stream(x))
                 elif t is ctypes.c_void_p:
                     out.append(self._address(x))
-                elif t is ctypes.c_int32 or (x is None and t is ctypes.POINTER(kl_decode_options)):
+                elif t in (ctypes.c_int32, ctypes.c_int64, ctypes.c_float) or (x is None and t is ctypes.POINTER(kl_decode_options)):
                     out.append(x)
                 else:
                     out.append(ctypes.byref(x))
@@ -312,6 +320,38 @@ def kl_latent_decode_step(shape, q, w_r, w_post, v_new, positions, v_lat, block_
     _check(_call().kl_latent_decode_step(shape, q, w_r, w_post, v_new, positions, v_lat,
                                          block_table, seq_lens, num_splits, out, out_dtype,
                                          workspace, err, stream), "kl_latent_decode_step")
+
+
+def kl_tree_workspace_size(shape, total_q, max_q_len, num_splits=0) -> int:
+    return int(load().kl_tree_workspace_size(ctypes.byref(shape), total_q, max_q_len, num_splits))
+
+
+def kl_tree_attention(shape, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, parents, total_q,
+                      max_q_len, num_splits, out, out_dtype, workspace, err=None, stream=None):
+    """Attention of a tree of drafted tokens: each sees the committed tokens, itself, its ancestors."""
+    _check(_call().kl_tree_attention(shape, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, parents,
+                                     total_q, max_q_len, num_splits, out, out_dtype, workspace, err,
+                                     stream), "kl_tree_attention")
+
+
+def kl_tree_commit(shape, cu_q_lens, path, path_lens, max_path, block_table, seq_lens, new_lens,
+                   v_cache, err=None, stream=None):
+    """Move the accepted path's rows to the front of the drafted region and set the new lengths."""
+    _check(_call().kl_tree_commit(shape, cu_q_lens, path, path_lens, max_path, block_table, seq_lens,
+                                  new_lens, v_cache, err, stream), "kl_tree_commit")
+
+
+def kl_logprobs_workspace_size(num_rows, vocab, num_top=0) -> int:
+    return int(load().kl_logprobs_workspace_size(num_rows, vocab, num_top))
+
+
+def kl_token_logprobs(num_rows, vocab, row_stride, logits, logits_dtype, scale, tokens, tokens_per_row,
+                      num_top, logprobs, entropy, top_logprobs, top_ids, workspace, err=None,
+                      stream=None):
+    """Log probabilities of given tokens, entropy and the largest logits of each row of logits."""
+    _check(_call().kl_token_logprobs(num_rows, vocab, row_stride, logits, logits_dtype, scale, tokens,
+                                     tokens_per_row, num_top, logprobs, entropy, top_logprobs, top_ids,
+                                     workspace, err, stream), "kl_token_logprobs")
 
 
 def kl_decode_kernel_available(shape, kernel, standard=False) -> bool:

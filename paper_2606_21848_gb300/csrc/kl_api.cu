@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "kl_internal.cuh"
+#include "kl_tree_plan.cuh"
 
 namespace kl {
 
@@ -346,6 +347,179 @@ kl_status kl_prefill_attention(const kl_shape *shape, const void *q, const void 
     a.err = err;
     a.stream = reinterpret_cast<cudaStream_t>(stream);
     return from_cuda(launch_prefill_tc(a));
+}
+
+}  // extern "C"
+
+namespace {
+
+// Counters in the front region that every workspace shares (layout()), then the states.
+struct SharedLayout {
+    size_t states, extra, total;
+};
+SharedLayout shared_layout(size_t counters, size_t state_bytes, size_t extra_bytes) {
+    SharedLayout w;
+    w.states = round_up((counters > kCounterFloor ? counters : kCounterFloor) * sizeof(unsigned int), 256);
+    w.extra = w.states + round_up(state_bytes, 256);
+    w.total = w.extra + round_up(extra_bytes, 256);
+    return w;
+}
+
+// Geometry, layout and workspace of a tree-attention call; KL_OK with total 0: no workspace needed.
+kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t num_splits,
+                         bool fp32, Geometry *g, TreePlan *p, SharedLayout *w) {
+    const kl_status st = resolve(shape, -1, g);
+    if (st != KL_OK) return st;
+    if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits) return KL_ERR_INVALID_ARG;
+    if (max_q_len > KL_TREE_MAX_DRAFTS) return KL_ERR_UNSUPPORTED;
+    *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P, num_splits,
+                   fp32, device_sm_count());
+    const size_t rows = (size_t)total_q * g->Hq * p->S;
+    *w = shared_layout((size_t)g->B * g->Hkv * p->blocks, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
+    if (p->S == 1 || rows == 0) w->total = 0;
+    return KL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len,
+                              int32_t num_splits) {
+    Geometry g;
+    TreePlan p;
+    SharedLayout w16, w32;
+    if (plan_tree_call(shape, total_q, max_q_len, num_splits, false, &g, &p, &w16) != KL_OK ||
+        plan_tree_call(shape, total_q, max_q_len, num_splits, true, &g, &p, &w32) != KL_OK)
+        return 0;
+    return w16.total > w32.total ? w16.total : w32.total;
+}
+
+kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
+                            const int32_t *block_table, const int32_t *seq_lens,
+                            const int32_t *cu_q_lens, const int32_t *parents, int32_t total_q,
+                            int32_t max_q_len, int32_t num_splits, void *out, kl_dtype out_dtype,
+                            void *workspace, size_t workspace_bytes, int32_t *err, kl_stream_t stream) {
+    if (out_dtype != KL_BF16 && out_dtype != KL_FP32) return KL_ERR_INVALID_ARG;
+    Geometry g;
+    TreePlan p;
+    SharedLayout w;
+    const kl_status st =
+        plan_tree_call(shape, total_q, max_q_len, num_splits, out_dtype == KL_FP32, &g, &p, &w);
+    if (st != KL_OK) return st;
+    if (!prefill_tc_supported(g)) return KL_ERR_UNSUPPORTED;
+    if (g.B == 0 || total_q == 0 || max_q_len == 0) return KL_OK;
+    if (!q || !v_cache || !block_table || !seq_lens || !cu_q_lens || !parents || !out)
+        return KL_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || (w_r && !aligned(w_r, 16)) || !aligned(v_cache, 16) || !aligned(out, 16))
+        return KL_ERR_INVALID_ARG;
+    if (w.total > 0 && (!workspace || workspace_bytes < w.total || !aligned(workspace, 256)))
+        return KL_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    TreeArgs a;
+    a.geo = g;
+    a.total_q = total_q;
+    a.max_q = max_q_len;
+    a.hp = p.hp;
+    a.rpb = p.rpb;
+    a.blocks = p.blocks;
+    a.S = p.S;
+    a.chunk = p.chunk;
+    a.q = static_cast<const uint16_t *>(q);
+    a.w_r = static_cast<const uint16_t *>(w_r);
+    a.v_cache = static_cast<const uint16_t *>(v_cache);
+    a.block_table = block_table;
+    a.seq_lens = seq_lens;
+    a.cu_q = cu_q_lens;
+    a.parents = parents;
+    a.part_o = w.total ? reinterpret_cast<float *>(ws + w.states) : nullptr;
+    a.part_ml = w.total ? reinterpret_cast<float *>(ws + w.extra) : nullptr;
+    a.counters = w.total ? reinterpret_cast<unsigned int *>(ws) : nullptr;
+    a.out = out;
+    a.out_dtype = out_dtype;
+    a.err = err;
+    a.stream = reinterpret_cast<cudaStream_t>(stream);
+    return from_cuda(launch_tree_tc(a));
+}
+
+kl_status kl_tree_commit(const kl_shape *shape, const int32_t *cu_q_lens, const int32_t *path,
+                         const int32_t *path_lens, int32_t max_path, const int32_t *block_table,
+                         const int32_t *seq_lens, int32_t *new_lens, void *v_cache, int32_t *err,
+                         kl_stream_t stream) {
+    Geometry g;
+    const kl_status st = resolve(shape, -1, &g);
+    if (st != KL_OK) return st;
+    if (max_path < 0) return KL_ERR_INVALID_ARG;
+    if (g.B == 0) return KL_OK;
+    if (!cu_q_lens || (!path && max_path > 0) || !path_lens || !block_table || !seq_lens || !new_lens || !v_cache)
+        return KL_ERR_INVALID_ARG;
+    if (!aligned(v_cache, 16)) return KL_ERR_INVALID_ARG;
+    return from_cuda(launch_tree_commit(g, cu_q_lens, path, path_lens, max_path, block_table, seq_lens,
+                                        new_lens, static_cast<uint16_t *>(v_cache), err,
+                                        reinterpret_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+SharedLayout logprobs_layout(int32_t rows, int chunks, int32_t top) {
+    const size_t slots = (size_t)rows * chunks;
+    SharedLayout w = shared_layout((size_t)rows, slots * sizeof(float4), slots * top * sizeof(uint64_t));
+    if (chunks <= 1) w.total = 0;
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top) {
+    if (num_rows < 0 || vocab <= 0 || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
+    return logprobs_layout(num_rows, logprob_chunks(vocab, KL_FP32), num_top).total;
+}
+
+kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride, const void *logits,
+                            kl_dtype logits_dtype, float scale, const int32_t *tokens,
+                            int32_t tokens_per_row, int32_t num_top, float *logprobs, float *entropy,
+                            float *top_logprobs, int32_t *top_ids, void *workspace,
+                            size_t workspace_bytes, int32_t *err, kl_stream_t stream) {
+    if (logits_dtype != KL_BF16 && logits_dtype != KL_FP32) return KL_ERR_INVALID_ARG;
+    if (num_rows < 0 || vocab <= 0 || row_stride < vocab || tokens_per_row < 0 || num_top < 0 || num_top > vocab)
+        return KL_ERR_INVALID_ARG;
+    if (!(scale == scale) || scale > 3e38f) return KL_ERR_INVALID_ARG;     // NaN, infinity
+    if (num_top > KL_LOGPROBS_MAX_TOP) return KL_ERR_UNSUPPORTED;
+    const int chunks = logprob_chunks(vocab, logits_dtype);
+    if ((int64_t)num_rows * chunks > (int64_t)INT32_MAX) return KL_ERR_UNSUPPORTED;
+    if (num_rows == 0) return KL_OK;
+    if (!logits || (tokens_per_row > 0 && (!tokens || !logprobs)) || (num_top > 0 && (!top_logprobs || !top_ids)))
+        return KL_ERR_INVALID_ARG;
+    if (!aligned(logits, logits_dtype == KL_FP32 ? 4 : 2)) return KL_ERR_INVALID_ARG;
+    const SharedLayout w = logprobs_layout(num_rows, chunks, num_top);
+    if (w.total > 0 && (!workspace || workspace_bytes < w.total || !aligned(workspace, 256)))
+        return KL_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    LogprobArgs a;
+    a.rows = num_rows;
+    a.vocab = vocab;
+    a.stride = row_stride;
+    a.logits = logits;
+    a.dtype = logits_dtype;
+    a.scale = scale > 0.f ? scale : 1.f;
+    a.tokens = tokens;
+    a.per_row = tokens_per_row;
+    a.top = num_top;
+    a.chunks = chunks;
+    a.logprobs = logprobs;
+    a.entropy = entropy;
+    a.top_logprobs = top_logprobs;
+    a.top_ids = top_ids;
+    a.counters = w.total ? reinterpret_cast<unsigned int *>(ws) : nullptr;
+    a.part = w.total ? reinterpret_cast<float4 *>(ws + w.states) : nullptr;
+    a.part_top = w.total ? reinterpret_cast<uint64_t *>(ws + w.extra) : nullptr;
+    a.err = err;
+    a.stream = reinterpret_cast<cudaStream_t>(stream);
+    return from_cuda(launch_logprobs(a));
 }
 
 }  // extern "C"

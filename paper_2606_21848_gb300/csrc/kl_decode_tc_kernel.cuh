@@ -260,21 +260,6 @@ __device__ __forceinline__ uint32_t qr_offset(int n, int k) {
            ((kk & 7) << 1);
 }
 
-// Arrival of one split of a (b, g) unit on its counter in the workspace: true for the last of
-// the unit's n splits. The increment wraps the counter back to zero on that arrival, so the
-// workspace is ready for the next call without any reset; one atomic per split, no retry.
-// Acquire-release at GPU scope: it publishes the split state that this CTA's threads wrote
-// before the CTA barrier that precedes it, and, for the last arrival, makes every other
-// split's state visible to the threads that synchronize with this one afterwards.
-__device__ __forceinline__ bool arrive_last(unsigned int *counter, int n) {
-    unsigned int old;
-    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;"
-                 : "=r"(old)
-                 : "l"(counter), "r"((unsigned int)(n - 1))
-                 : "memory");
-    return old == (unsigned int)(n - 1);
-}
-
 // Merge of the n_u split states of (b, g) by the compute warps of the CTA that finished last
 // (t = the thread's index among them)
 // (kl_combine's formula). Up to eight splits: direct loads. More: the cache ring is idle by

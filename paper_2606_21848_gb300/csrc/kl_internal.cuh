@@ -101,12 +101,73 @@ struct PrefillArgs {
     cudaStream_t stream;
 };
 
+// Arguments of a tree-attention launch (kl_tree_attention). Sequence b's drafts are rows cu_q[b] ..
+// cu_q[b + 1] - 1 of q / out ([total_q][Hq][D]), its last n_b cached rows.
+struct TreeArgs {
+    Geometry geo;             // S and chunk unused
+    int total_q;              // rows of q and out
+    int max_q;                // host bound on n_b
+    int hp, rpb, blocks, S, chunk;   // layout (plan_tree)
+    const uint16_t *q;        // [total_q][Hq][D] bf16
+    const uint16_t *w_r;      // [Hw][D][D] bf16, or nullptr: q is the composed query
+    const uint16_t *v_cache;  // [num_pages][Hkv][P][D] bf16
+    const int32_t *block_table;
+    const int32_t *seq_lens;
+    const int32_t *cu_q;      // [B + 1]
+    const int32_t *parents;   // [total_q]
+    float *part_o;            // [total_q][Hq][S][D] states of the runs, not normalized (S > 1)
+    float *part_ml;           // [total_q][Hq][S][2] {m (base 2), l}
+    unsigned int *counters;   // [B][Hkv][blocks] arrivals of the current call (zero between calls)
+    void *out;                // [total_q][Hq][D]
+    kl_dtype out_dtype;
+    int32_t *err;
+    cudaStream_t stream;
+};
+
+// Arguments of a kl_token_logprobs launch.
+struct LogprobArgs {
+    int rows;                 // T
+    int vocab;                // V
+    int64_t stride;           // elements between two rows of logits
+    const void *logits;       // [T][stride], the first V of each row
+    kl_dtype dtype;
+    float scale;
+    const int32_t *tokens;    // [T][per_row]
+    int per_row;
+    int top;                  // largest logits wanted
+    int chunks;               // CTAs per row
+    float *logprobs;          // [T][per_row]
+    float *entropy;           // [T] or nullptr
+    float *top_logprobs;      // [T][top]
+    int32_t *top_ids;         // [T][top]
+    unsigned int *counters;   // [T] arrivals (zero between calls); chunks > 1
+    float4 *part;             // [T][chunks] {maximum, sum, weighted sum, -}
+    uint64_t *part_top;       // [T][chunks][top] keys, largest first
+    int32_t *err;
+    cudaStream_t stream;
+};
+
 // bf16 bit helpers (a bf16 value is the upper half of a binary32 value).
 __device__ __forceinline__ float bf16lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 __device__ __forceinline__ void raise_flag(int32_t *err, int32_t bits) {
     if (err) atomicOr(err, bits);
+}
+
+// Arrival of one split of a (b, g) unit on its counter in the workspace: true for the last of
+// the unit's n splits. The increment wraps the counter back to zero on that arrival, so the
+// workspace is ready for the next call without any reset; one atomic per split, no retry.
+// Acquire-release at GPU scope: it publishes the split state that this CTA's threads wrote
+// before the CTA barrier that precedes it, and, for the last arrival, makes every other
+// split's state visible to the threads that synchronize with this one afterwards.
+__device__ __forceinline__ bool arrive_last(unsigned int *counter, int n) {
+    unsigned int old;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;"
+                 : "=r"(old)
+                 : "l"(counter), "r"((unsigned int)(n - 1))
+                 : "memory");
+    return old == (unsigned int)(n - 1);
 }
 
 // Programmatic dependent launch. A kernel launched with programmatic stream serialization may
@@ -176,6 +237,18 @@ cudaError_t launch_append_chunk(const Geometry &g, int total_q, int max_q, const
                                 const int32_t *block_table, const int32_t *seq_lens,
                                 const int32_t *cu_q, uint16_t *v_cache, int32_t *err,
                                 cudaStream_t stream);
+
+// Attention of a tree of drafted tokens (the geometry of the prefill), and the move of the accepted
+// path's rows.
+cudaError_t launch_tree_tc(const TreeArgs &a);
+cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
+                               const int32_t *path_lens, int max_path, const int32_t *block_table,
+                               const int32_t *seq_lens, int32_t *new_lens, uint16_t *v_cache,
+                               int32_t *err, cudaStream_t stream);
+
+// Log probabilities, entropy and largest logits of rows of logits; the CTAs per row.
+int logprob_chunks(int vocab, kl_dtype dtype);
+cudaError_t launch_logprobs(const LogprobArgs &a);
 
 // FP8 value cache (E4M3 codes [num_pages][Hkv][P][D] with fp32 row scales [num_pages][Hkv][P]):
 // the decode on the tensor cores (a.v_cache holds the codes; states or direct output, merged by

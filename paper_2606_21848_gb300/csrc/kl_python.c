@@ -30,7 +30,7 @@ static PyObject *g_initialized, *g_get_device, *g_raw_stream, *g_current_stream;
     X(route_query) X(append_v) X(decode_attention) X(decode_attention_ex) X(decode_step) X(combine) \
     X(standard_decode) X(decode_attention_noalloc) X(append_v_chunk) X(prefill_attention) \
     X(append_v_fp8) X(quantize_cache_fp8) X(decode_attention_fp8) X(decode_step_fp8) \
-    X(latent_decode) X(latent_decode_step)
+    X(latent_decode) X(latent_decode_step) X(tree_attention) X(tree_commit) X(token_logprobs)
 #define POINTER(n) static __typeof__(kl_##n) *f_##n;
 ENTRIES(POINTER)
 #define SLOT(n) {"kl_" #n, &f_##n},
@@ -88,6 +88,29 @@ static int get_i32(PyObject *o, int32_t *out) {
     }
     Py_DECREF(v);
     return ok;
+}
+
+static int get_i64(PyObject *o, int64_t *out) {
+    PyObject *v = PyNumber_Index(o);
+    if (!v) {
+        PyErr_Clear();
+        PyErr_Format(g_argument_error, "expected an int, got %.100s", Py_TYPE(o)->tp_name);
+        return 0;
+    }
+    *out = (int64_t)PyLong_AsUnsignedLongLongMask(v);
+    Py_DECREF(v);
+    return !(*out == -1 && PyErr_Occurred());
+}
+
+/* A float or an int, as ctypes takes it for a c_float. */
+static int get_f32(PyObject *o, float *out) {
+    if (!PyFloat_Check(o) && !PyLong_Check(o)) {
+        PyErr_Format(g_argument_error, "expected a float, got %.100s", Py_TYPE(o)->tp_name);
+        return 0;
+    }
+    const double v = PyFloat_AsDouble(o);
+    *out = (float)v;
+    return !(v == -1.0 && PyErr_Occurred());
 }
 
 /* The contents of an instance of the ctypes structure `type` (`size` bytes, or a subclass's more). */
@@ -221,6 +244,8 @@ static int get_stream(PyObject *o, kl_stream_t *out) {
 #define LATENT(i) kl_latent_shape sh; if (!get_struct(a[i], &sh, sizeof sh, g_latent)) return NULL
 #define PTR(i, x) void *x; if (!get_addr(a[i], &x)) return NULL
 #define INT(i, x) int32_t x; if (!get_i32(a[i], &x)) return NULL
+#define LONG(i, x) int64_t x; if (!get_i64(a[i], &x)) return NULL
+#define FLOAT(i, x) float x; if (!get_f32(a[i], &x)) return NULL
 #define OPTS(i) kl_decode_options o; const int has_o = a[i] != Py_None; \
     if (has_o && !get_struct(a[i], &o, sizeof o, g_options)) return NULL
 #define WORK(i) void *ws; size_t wsn; if (!get_addr(a[i], &ws) || !get_nbytes(a[i], &wsn)) return NULL
@@ -290,6 +315,18 @@ CALL(f_latent_decode(&sh, q, w, wp, c, bt, sl, ns, out, (kl_dtype)dt, ws, wsn, e
 FN(latent_decode_step, 15) LATENT(0); PTR(1, q); PTR(2, w); PTR(3, wp); PTR(4, v); PTR(5, pos); PTR(6, c);
 PTR(7, bt); PTR(8, sl); INT(9, ns); PTR(10, out); INT(11, dt); WORK(12); PTR(13, e); STREAM(14);
 CALL(f_latent_decode_step(&sh, q, w, wp, v, pos, c, bt, sl, ns, out, (kl_dtype)dt, ws, wsn, e, st))
+
+FN(tree_attention, 16) SHAPE(0); PTR(1, q); PTR(2, w); PTR(3, c); PTR(4, bt); PTR(5, sl); PTR(6, cu);
+PTR(7, pa); INT(8, tq); INT(9, mq); INT(10, ns); PTR(11, out); INT(12, dt); WORK(13); PTR(14, e); STREAM(15);
+CALL(f_tree_attention(&sh, q, w, c, bt, sl, cu, pa, tq, mq, ns, out, (kl_dtype)dt, ws, wsn, e, st))
+
+FN(tree_commit, 11) SHAPE(0); PTR(1, cu); PTR(2, pa); PTR(3, pl); INT(4, mp); PTR(5, bt); PTR(6, sl);
+PTR(7, nl); PTR(8, c); PTR(9, e); STREAM(10);
+CALL(f_tree_commit(&sh, cu, pa, pl, mp, bt, sl, nl, c, e, st))
+
+FN(token_logprobs, 16) INT(0, nr); INT(1, vo); LONG(2, rs); PTR(3, lg); INT(4, dt); FLOAT(5, sc); PTR(6, tk);
+INT(7, tr); INT(8, nt); PTR(9, lp); PTR(10, en); PTR(11, tl); PTR(12, ti); WORK(13); PTR(14, e); STREAM(15);
+CALL(f_token_logprobs(nr, vo, rs, lg, (kl_dtype)dt, sc, tk, tr, nt, lp, en, tl, ti, ws, wsn, e, st))
 
 #define M(name) {"kl_" #name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL},
 static PyMethodDef methods[] = {

@@ -35,6 +35,74 @@ __global__ void __launch_bounds__(128) append_kernel(int Hkv, int D, int P, int 
     }
 }
 
+// The accepted path of a tree of drafts becomes the end of the sequence: row L - n + path[j] moves to
+// row L - n + j. One CTA per sequence (which may also replace its own length), thread = 16-byte chunk of a
+// (head, row). A path increases, so path[j] >= j: a row is written only after the rows that the same
+// thread read in this batch and in all later ones have a higher position. kMoves loads are in flight
+// (8 x 4096 tokens, 8 heads: latency alone).
+constexpr int kMoves = 8;
+
+__global__ void __launch_bounds__(256) tree_commit_kernel(int Hkv, int D, int P, int num_pages, int max_pages,
+                                                          const int32_t *cu_q, const int32_t *path,
+                                                          const int32_t *path_lens, int max_path,
+                                                          const int32_t *block_table,
+                                                          const int32_t *seq_lens, int32_t *new_lens,
+                                                          uint4 *v_cache, int32_t *err) {
+    __shared__ int64_t from[KL_TREE_MAX_DRAFTS], to[KL_TREE_MAX_DRAFTS];   // first 16-byte chunk of head 0
+    __shared__ int bad;
+    grid_dep_wait();
+    grid_dep_launch();
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int n = cu_q[b + 1] - cu_q[b], L = seq_lens[b], m = path_lens[b];
+    const int base = L - n;
+    if (tid == 0) bad = 0;
+    __syncthreads();
+    if (n < 0 || n > KL_TREE_MAX_DRAFTS || base < 0 || L > max_pages * P) {
+        if (tid == 0) raise_flag(err, KL_FLAG_BAD_LENGTH);
+        return;
+    }
+    if (m < 0 || m > n || m > max_path) {
+        if (tid == 0) raise_flag(err, KL_FLAG_BAD_TREE);
+        return;
+    }
+    const int cpr = D / 8;                      // 16-byte chunks per row
+    if (tid < m) {
+        const int32_t *pb = path + (size_t)b * max_path;
+        const int i = pb[tid], before = tid > 0 ? pb[tid - 1] : -1;
+        if (i <= before || i >= n) {
+            bad = KL_FLAG_BAD_TREE;
+        } else {
+            const int32_t *bt = block_table + (size_t)b * max_pages;
+            const int src = base + i, dst = base + tid;
+            const int ps = bt[src / P], pd = bt[dst / P];
+            if (ps < 0 || ps >= num_pages || pd < 0 || pd >= num_pages) {
+                bad = KL_FLAG_BAD_PAGE;
+            } else {
+                from[tid] = ((int64_t)ps * Hkv * P + src % P) * cpr;
+                to[tid] = ((int64_t)pd * Hkv * P + dst % P) * cpr;
+            }
+        }
+    }
+    __syncthreads();
+    if (bad) {                                  // nothing of the sequence is changed
+        if (tid == 0) raise_flag(err, bad);
+        return;
+    }
+    if (tid == 0) new_lens[b] = base + m;
+    for (int c = tid; c < Hkv * cpr; c += blockDim.x) {
+        const int64_t off = (int64_t)(c / cpr) * P * cpr + c % cpr;
+        for (int j = 0; j < m; j += kMoves) {
+            uint4 v[kMoves];
+#pragma unroll
+            for (int k = 0; k < kMoves; ++k)
+                if (j + k < m) v[k] = v_cache[from[j + k] + off];
+#pragma unroll
+            for (int k = 0; k < kMoves; ++k)
+                if (j + k < m) v_cache[to[j + k] + off] = v[k];
+        }
+    }
+}
+
 // Routing projection (Section 2.2): one CTA per (h, b), thread j computes
 // q_r[j] = sum_k q[k] W^R[k][j]; the W^R reads of a k step are one coalesced row.
 __global__ void route_kernel(int Hq, int G, int D, int wr_per_qh, const uint16_t *__restrict__ q,
@@ -140,6 +208,21 @@ cudaError_t launch_append(const Geometry &g, const uint16_t *v_new, const int32_
     const OverlapAttr overlap(cfg);
     return cudaLaunchKernelEx(&cfg, append_kernel, g.Hkv, g.D, g.P, g.num_pages, g.max_pages,
                               reinterpret_cast<const uint4 *>(v_new), block_table, positions,
+                              reinterpret_cast<uint4 *>(v_cache), err);
+}
+
+cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
+                               const int32_t *path_lens, int max_path, const int32_t *block_table,
+                               const int32_t *seq_lens, int32_t *new_lens, uint16_t *v_cache,
+                               int32_t *err, cudaStream_t stream) {
+    if (g.B == 0) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(g.B);
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    const OverlapAttr overlap(cfg);
+    return cudaLaunchKernelEx(&cfg, tree_commit_kernel, g.Hkv, g.D, g.P, g.num_pages, g.max_pages, cu_q,
+                              path, path_lens, max_path, block_table, seq_lens, new_lens,
                               reinterpret_cast<uint4 *>(v_cache), err);
 }
 
