@@ -330,7 +330,7 @@ size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_t
  *   top_logprobs[r][0 ..] = their log probabilities
  * logits: [num_rows][row_stride] of logits_dtype, the first `vocab` of each row, row_stride >= vocab
  * elements, aligned to their own size alone; tokens: [num_rows][tokens_per_row] int32; outputs fp32 and
- * int32, dense; num_top <= min(vocab, KL_LOGPROBS_MAX_TOP), 0 for none (top_* are then not written),
+ * int32, dense; num_top <= min(vocab, KL_LOGPROBS_MAX_TOP), vocab <= 2^30; num_top 0: none (top_* are then not written),
  * tokens_per_row may be 0. A token id outside [-1, vocab) raises KL_FLAG_BAD_TOKEN and gets NaN. Logits of
  * -inf have probability 0; a row of -inf alone gives log probabilities of -inf and entropy 0. A NaN
  * or +inf logit makes the row's log probabilities and entropy NaN and raises KL_FLAG_RANGE; NaN is never

@@ -475,7 +475,7 @@ SharedLayout logprobs_layout(int32_t rows, int chunks, int32_t top) {
 extern "C" {
 
 size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top) {
-    if (num_rows < 0 || vocab <= 0 || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
+    if (num_rows < 0 || vocab <= 0 || vocab > (1 << 30) || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
     return logprobs_layout(num_rows, logprob_chunks(vocab, KL_FP32), num_top).total;
 }
 
@@ -488,7 +488,7 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     if (num_rows < 0 || vocab <= 0 || row_stride < vocab || tokens_per_row < 0 || num_top < 0 || num_top > vocab)
         return KL_ERR_INVALID_ARG;
     if (!(scale == scale) || scale > 3e38f) return KL_ERR_INVALID_ARG;     // NaN, infinity
-    if (num_top > KL_LOGPROBS_MAX_TOP) return KL_ERR_UNSUPPORTED;
+    if (num_top > KL_LOGPROBS_MAX_TOP || vocab > (1 << 30)) return KL_ERR_UNSUPPORTED;
     const int chunks = logprob_chunks(vocab, logits_dtype);
     if ((int64_t)num_rows * chunks > (int64_t)INT32_MAX) return KL_ERR_UNSUPPORTED;
     if (num_rows == 0) return KL_OK;

@@ -14,11 +14,14 @@
 // s2 += 2^d (s2_c + d s1_c); then log z = log2(s1) ln 2 above scale * M and H = (log2 s1 - s2 / s1) ln 2.
 //
 // Selection: a logit among the row's largest is among its chunk's. Each thread has the maximum of its own
-// logits; with `top` threads' maxima known to be >= t, so are `top` logits, and only logits above such a
-// bound t go on: t is the larger of (the smallest, over the 8 warps, of the ceil(top / 8)-th largest
-// maximum) and (the largest over the warps of the top-th). Those few are ranked by counting; if they are
-// fewer than `top`, the rest are the lowest-indexed logits equal to t.
+// logits; with `top` threads' maxima known to be >= t, so are `top` logits, and only logits from such a
+// bound t on are candidates: t is the larger of (the smallest, over the 8 warps, of the ceil(top / 8)-th largest
+// maximum) and (the largest over the warps of the top-th). Those few are ranked by counting. Masked and tied rows,
+// where the bound leaves too few or too many, read their chunk a second time.
+#include <float.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "kl_internal.cuh"
 
@@ -60,12 +63,52 @@ __device__ __forceinline__ float lp_ex2(float x) {
     return y;
 }
 
-// Element e of a 16-byte vector.
+// The 32-bit word w as logits: two bf16 (x the lower half) or one fp32 (x).
 template <typename T>
-__device__ __forceinline__ float lp_get(const uint4 &v, int e) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
-    else return (e & 1) ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
+__device__ __forceinline__ float2 lp_unpack(uint32_t w) {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w), -INFINITY);
+    else return make_float2(bf16lo(w), bf16hi(w));
+}
+
+// Packed fp32 pairs (one instruction for two logits).
+__device__ __forceinline__ float2 lp_add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 lp_mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 lp_fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mov.b64 z, {%6, %7};\n\tfma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
+// max of two packed bf16 pairs (a NaN loses).
+__device__ __forceinline__ uint32_t lp_max_bf16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// The registers of the chunk as the compiler may not know them from before: each phase unpacks them anew
+// instead of keeping 64 unpacked logits (which spilled).
+template <int N>
+__device__ __forceinline__ void lp_forget(uint32_t (&w)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(w[i]));
 }
 
 template <typename T>
@@ -74,16 +117,25 @@ __device__ __forceinline__ float lp_load(const void *row, int idx) {
     else return bf16lo((uint32_t)static_cast<const uint16_t *>(row)[idx]);
 }
 
-// Sum over the block of one value per thread (every thread gets it).
-__device__ __forceinline__ float block_sum(float v, float *red, int warp, int lane) {
+// Sum over each warp of s1 and s2, to the warps' slots (block_sums() after the next barrier).
+__device__ __forceinline__ void warp_sums(LogprobSmem &sm, float s1, float s2, int warp, int lane) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (lane == 0) red[warp] = v;
-    __syncthreads();
-    float t = 0.f;
+    for (int o = 16; o > 0; o >>= 1) {
+        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (lane == 0) {
+        sm.s1[warp] = s1;
+        sm.s2[warp] = s2;
+    }
+}
+__device__ __forceinline__ void block_sums(const LogprobSmem &sm, float &s1, float &s2) {
+    s1 = s2 = 0.f;
 #pragma unroll
-    for (int w = 0; w < kLpWarps; ++w) t += red[w];
-    return t;
+    for (int w = 0; w < kLpWarps; ++w) {
+        s1 += sm.s1[w];
+        s2 += sm.s2[w];
+    }
 }
 
 // The keys cand[0 .. n - 1] (all different), ranked: the largest `top` of them to list. n <= kLpCap.
@@ -128,7 +180,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
     const char *rp = static_cast<const char *>(a.logits) + (size_t)row * a.stride * sizeof(T);
     // vectors from the 16-byte boundary at or before the row's start; logit i is element off + i
     const int off = (int)((reinterpret_cast<uintptr_t>(rp) & 15) / sizeof(T));
-    const int64_t v0 = (int64_t)chunk * per_chunk;
+    const int v0 = chunk * per_chunk;
     const float c = a.scale * kLog2e;
     const int top = a.top;
     if (tid < KL_LOGPROBS_MAX_TOP) sm.list[tid] = 0;
@@ -136,39 +188,51 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
     grid_dep_wait();
     grid_dep_launch();
 
-    uint4 v[kLpVecs];
-    // logits outside the row (the edges' other elements, vectors past the end) count as -inf
-    auto index_of = [&](int i, int e) -> int64_t { return (v0 + i * kLpThreads + tid) * VEC + e - off; };
+    // logit of word k of vector i (its lower half)
+    auto index_of = [&](int i, int k) { return (v0 + i * kLpThreads + tid) * VEC + k * (VEC / 4) - off; };
+    // Logits outside the row (the edges' other elements, vectors past the end) count as -inf.
+    uint32_t v[4 * kLpVecs];
+    bool edge = false;                                   // the thread holds some of those
 #pragma unroll
     for (int i = 0; i < kLpVecs; ++i) {
-        const int64_t j0 = index_of(i, 0);
+        const int j0 = index_of(i, 0);
         const bool inside = i * kLpThreads + tid < per_chunk;
         if (inside && j0 >= 0 && j0 + VEC <= a.vocab) {
-            v[i] = __ldcs(reinterpret_cast<const uint4 *>(rp + j0 * (int64_t)sizeof(T)));
+            const uint4 x = __ldcs(reinterpret_cast<const uint4 *>(rp + (int64_t)j0 * (int)sizeof(T)));
+            v[4 * i] = x.x;
+            v[4 * i + 1] = x.y;
+            v[4 * i + 2] = x.z;
+            v[4 * i + 3] = x.w;
         } else {
-            uint32_t w[4];
+            edge = true;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+            for (int k = 0; k < 4; ++k) v[4 * i + k] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
             if (inside && j0 < a.vocab)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const int64_t j = j0 + e;
+                    const int j = j0 + e;
                     if (j < 0 || j >= a.vocab) continue;
                     if constexpr (sizeof(T) == 4) {
-                        w[e] = reinterpret_cast<const uint32_t *>(rp)[j];
+                        v[4 * i + e] = reinterpret_cast<const uint32_t *>(rp)[j];
                     } else {
+                        uint32_t &w = v[4 * i + (e >> 1)];
                         const uint32_t x = reinterpret_cast<const uint16_t *>(rp)[j];
-                        w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xffffu) | x << 16 : (w[e >> 1] & 0xffff0000u) | x;
+                        w = (e & 1) ? (w & 0xffffu) | x << 16 : (w & 0xffff0000u) | x;
                     }
                 }
-            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    float tmax = -INFINITY;                              // (NaN does not take part)
+    float tmax;                                          // (NaN does not take part)
+    if constexpr (sizeof(T) == 4) {
+        tmax = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kLpVecs; ++i)
+        for (int i = 0; i < 4 * kLpVecs; ++i) tmax = fmaxf(tmax, __uint_as_float(v[i]));
+    } else {
+        uint32_t t = 0xff80ff80u;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) tmax = fmaxf(tmax, lp_get<T>(v[i], e));
+        for (int i = 0; i < 4 * kLpVecs; ++i) t = lp_max_bf16(t, v[i]);
+        tmax = fmaxf(bf16lo(t), bf16hi(t));
+    }
 
     // the block's maximum, and the warps' bounds for the selection: the maxima sorted over the lanes
     float s = tmax;
@@ -203,102 +267,121 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
         bound = fmaxf(bound, lowest);
     }
 
-    // the sums against the chunk's maximum (0 where nothing is above -inf)
-    const float mr = m == -INFINITY ? 0.f : m;
-    float s1 = 0.f, s2 = 0.f;
+    // logits from the bound on (above it, where it is -inf)
+    lp_forget(v);
+    const float from = bound == -INFINITY ? -FLT_MAX : bound;
+    if (top > 0 && tmax >= from) {
 #pragma unroll
-    for (int i = 0; i < kLpVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float y = (lp_get<T>(v[i], e) - mr) * c;
-            const float p = lp_ex2(y);
-            s1 += p;
-            s2 = fmaf(p, fmaxf(y, -1e30f), s2);          // (a weight of 0 at y = -inf adds 0)
+        for (int i = 0; i < 4 * kLpVecs; ++i) {
+            const float2 x = lp_unpack<T>(v[i]);
+            if (fmaxf(x.x, x.y) >= from) {
+                const int j = index_of(i >> 2, i & 3);
+                if (x.x >= from) {
+                    const int at = atomicAdd(&sm.count, 1);
+                    if (at < kLpCap) sm.cand[at] = make_key(x.x, j);
+                }
+                if (x.y >= from) {
+                    const int at = atomicAdd(&sm.count, 1);
+                    if (at < kLpCap) sm.cand[at] = make_key(x.y, j + 1);
+                }
+            }
         }
-    s1 = block_sum(s1, sm.s1, warp, lane);
-    s2 = block_sum(s2, sm.s2, warp, lane);
+        lp_forget(v);
+    }
+
+    // The sums against the chunk's maximum (0 where nothing is above -inf). A weight of 0 at y = -inf has
+    // to add 0 to s2, not NaN: the clamp for that is left out where the thread's logits do without.
+    const float mr = m == -INFINITY ? 0.f : m;
+    const float2 neg_m = make_float2(-mr, -mr), cc = make_float2(c, c);
+    float s1, s2;
+    auto sums = [&](auto clamp) {
+        float2 a1 = make_float2(0.f, 0.f), a2 = a1;
+#pragma unroll
+        for (int i = 0; i < 4 * kLpVecs; i += VEC == 4 ? 2 : 1) {
+            float2 x;
+            if constexpr (VEC == 4) x = make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+            else x = lp_unpack<T>(v[i]);
+            float2 y = lp_mul2(lp_add2(x, neg_m), cc);
+            const float2 p = make_float2(lp_ex2(y.x), lp_ex2(y.y));
+            if constexpr (decltype(clamp)::value) y = make_float2(fmaxf(y.x, -1e30f), fmaxf(y.y, -1e30f));
+            a1 = lp_add2(a1, p);
+            a2 = lp_fma2(p, y, a2);
+        }
+        s1 = a1.x + a1.y;
+        s2 = a2.x + a2.y;
+    };
+    if (!edge) sums(std::false_type{});
+    if (edge || (s2 != s2 && s1 == s1)) {
+        lp_forget(v);
+        sums(std::true_type{});
+    }
+    warp_sums(sm, s1, s2, warp, lane);
+    __syncthreads();
+    block_sums(sm, s1, s2);
 
     if (top > 0) {
-        // logits above the bound
-        if (tmax > bound) {
-#pragma unroll
-            for (int i = 0; i < kLpVecs; ++i)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float x = lp_get<T>(v[i], e);
+        int n = sm.count;
+        if (n >= top && n <= kLpCap) {
+            rank_keys(sm, n, top, tid);
+        } else {
+            // Too few (the bound is -inf) or too many (ties at the bound, or a chunk whose large logits lie
+            // in a few threads): the chunk is read once more.
+            const int j0 = max(0, v0 * VEC - off), j1 = min(a.vocab, (v0 + per_chunk) * VEC - off);
+            __syncthreads();
+            if (n > kLpCap) {
+                if (tid == 0) sm.count = 0;
+                __syncthreads();
+                for (int j = j0 + tid; j < j1; j += kLpThreads) {
+                    const float x = lp_load<T>(rp, j);
                     if (x > bound) {
                         const int at = atomicAdd(&sm.count, 1);
-                        if (at < kLpCap) sm.cand[at] = make_key(x, (int)index_of(i, e));
+                        if (at < kLpCap) sm.cand[at] = make_key(x, j);
                     }
                 }
-        }
-        __syncthreads();
-        const int n = sm.count;
-        if (n <= kLpCap) {
-            rank_keys(sm, n, top, tid);
-            // too few: the first logits equal to the bound, in order
-            int have = n;
-#pragma unroll
-            for (int i = 0; i < kLpVecs; ++i) {
-                if (have >= top) continue;               // (uniform: `have` is the block's)
-                int mine = 0;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const int64_t j = index_of(i, e);
-                    mine += lp_get<T>(v[i], e) == bound && j >= 0 && j < a.vocab &&
-                            i * kLpThreads + tid < per_chunk;
-                }
-                int before = mine;                       // inclusive prefix over the warp
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int x = __shfl_up_sync(0xffffffffu, before, o);
-                    if (lane >= o) before += x;
-                }
-                if (lane == 31) sm.wcount[warp] = before;
                 __syncthreads();
-                int at = have + before - mine, all = 0;
-#pragma unroll
-                for (int w = 0; w < kLpWarps; ++w) {
-                    if (w < warp) at += sm.wcount[w];
-                    all += sm.wcount[w];
-                }
-                if (mine > 0)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const int64_t j = index_of(i, e);
-                        if (lp_get<T>(v[i], e) == bound && j >= 0 && j < a.vocab) {
-                            if (at < top) sm.list[at] = make_key(bound, (int)j);
-                            ++at;
-                        }
-                    }
-                have += all;
-                __syncthreads();
+                n = sm.count;
             }
-        } else {
-            take_keys(sm, top, tid, [&](uint64_t prev) {
-                uint64_t k = 0;
+            if (n <= kLpCap) {
+                rank_keys(sm, n, top, tid);
+                // then the first logits equal to the bound, in order
+                for (int jb = j0; jb < j1 && n < top; jb += kLpThreads) {
+                    const int j = jb + tid;
+                    const bool mine = j < j1 && lp_load<T>(rp, j) == bound;
+                    const unsigned votes = __ballot_sync(0xffffffffu, mine);
+                    if (lane == 0) sm.wcount[warp] = __popc(votes);
+                    __syncthreads();
+                    int at = n + __popc(votes & ((1u << lane) - 1));
 #pragma unroll
-                for (int i = 0; i < kLpVecs; ++i)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float x = lp_get<T>(v[i], e);
-                        if (x > bound) {
-                            const uint64_t y = make_key(x, (int)index_of(i, e));
-                            if (y < prev && y > k) k = y;
-                        }
+                    for (int w = 0; w < kLpWarps; ++w) {
+                        if (w < warp) at += sm.wcount[w];
+                        n += sm.wcount[w];
                     }
-                return k;
-            });
+                    if (mine && at < top) sm.list[at] = make_key(bound, j);
+                    __syncthreads();
+                }
+            } else {
+                take_keys(sm, top, tid, [&](uint64_t prev) {
+                    uint64_t k = 0;
+                    for (int j = j0 + tid; j < j1; j += kLpThreads) {
+                        const float x = lp_load<T>(rp, j);
+                        const uint64_t y = x > bound ? make_key(x, j) : 0;
+                        if (y < prev && y > k) k = y;
+                    }
+                    return k;
+                });
+            }
         }
         __syncthreads();
     }
 
     if (a.chunks > 1) {
         const size_t slot = (size_t)row * a.chunks + chunk;
-        if (tid == 0) a.part[slot] = make_float4(m, s1, s2, 0.f);
-        if (tid < top) a.part_top[slot * top + tid] = sm.list[tid];
-        __syncthreads();
-        if (tid == 0) sm.is_last = arrive_last(a.counters + row, a.chunks);
+        if (warp == 0) {
+            if (lane == 0) a.part[slot] = make_float4(m, s1, s2, 0.f);
+            if (lane < top) a.part_top[slot * top + lane] = sm.list[lane];
+            __syncwarp();
+            if (lane == 0) sm.is_last = arrive_last(a.counters + row, a.chunks);
+        }
         __syncthreads();
         if (!sm.is_last) return;
         // join the row's chunks
@@ -323,8 +406,9 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
                 s2 = fmaf(f, fmaf(d, q.y, q.z), s2);
             }
         }
-        s1 = block_sum(s1, sm.s1, warp, lane);
-        s2 = block_sum(s2, sm.s2, warp, lane);
+        warp_sums(sm, s1, s2, warp, lane);
+        __syncthreads();
+        block_sums(sm, s1, s2);
         if (top > 0) {
             // every chunk's last key is a bound; the largest of them leaves few
             const uint64_t *keys = a.part_top + (size_t)row * a.chunks * top;
