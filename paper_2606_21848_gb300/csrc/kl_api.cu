@@ -476,7 +476,7 @@ extern "C" {
 
 size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top) {
     if (num_rows < 0 || vocab <= 0 || vocab > (1 << 30) || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
-    return logprobs_layout(num_rows, logprob_chunks(vocab, KL_FP32), num_top).total;
+    return logprobs_layout(num_rows, logprob_chunks(num_rows, vocab, KL_FP32), num_top).total;
 }
 
 kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride, const void *logits,
@@ -489,9 +489,8 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
         return KL_ERR_INVALID_ARG;
     if (!(scale == scale) || scale > 3e38f) return KL_ERR_INVALID_ARG;     // NaN, infinity
     if (num_top > KL_LOGPROBS_MAX_TOP || vocab > (1 << 30)) return KL_ERR_UNSUPPORTED;
-    const int chunks = logprob_chunks(vocab, logits_dtype);
-    if ((int64_t)num_rows * chunks > (int64_t)INT32_MAX) return KL_ERR_UNSUPPORTED;
     if (num_rows == 0) return KL_OK;
+    const int chunks = logprob_chunks(num_rows, vocab, logits_dtype);
     if (!logits || (tokens_per_row > 0 && (!tokens || !logprobs)) || (num_top > 0 && (!top_logprobs || !top_ids)))
         return KL_ERR_INVALID_ARG;
     if (!aligned(logits, logits_dtype == KL_FP32 ? 4 : 2)) return KL_ERR_INVALID_ARG;
@@ -509,7 +508,7 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     a.tokens = tokens;
     a.per_row = tokens_per_row;
     a.top = num_top;
-    a.chunks = chunks;
+    a.chunks = a.slots = chunks;
     a.logprobs = logprobs;
     a.entropy = entropy;
     a.top_logprobs = top_logprobs;

@@ -135,14 +135,15 @@ struct LogprobArgs {
     const int32_t *tokens;    // [T][per_row]
     int per_row;
     int top;                  // largest logits wanted
-    int chunks;               // CTAs per row
+    int chunks;               // pieces of a row (logprob_chunks)
+    int slots;                // of a row in part and part_top: at least its chunks
     float *logprobs;          // [T][per_row]
     float *entropy;           // [T] or nullptr
     float *top_logprobs;      // [T][top]
     int32_t *top_ids;         // [T][top]
     unsigned int *counters;   // [T] arrivals (zero between calls); chunks > 1
-    float4 *part;             // [T][chunks] {maximum, sum, weighted sum, -}
-    uint64_t *part_top;       // [T][chunks][top] keys, largest first
+    float4 *part;             // [T][slots] {maximum, sum, weighted sum, -}
+    uint64_t *part_top;       // [T][slots][top] keys, largest first
     int32_t *err;
     cudaStream_t stream;
 };
@@ -246,8 +247,8 @@ cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int
                                const int32_t *seq_lens, int32_t *new_lens, uint16_t *v_cache,
                                int32_t *err, cudaStream_t stream);
 
-// Log probabilities, entropy and largest logits of rows of logits; the CTAs per row.
-int logprob_chunks(int vocab, kl_dtype dtype);
+// Log probabilities, entropy and largest logits of rows of logits; the pieces of a row.
+int logprob_chunks(int rows, int vocab, kl_dtype dtype);
 cudaError_t launch_logprobs(const LogprobArgs &a);
 
 // FP8 value cache (E4M3 codes [num_pages][Hkv][P][D] with fp32 row scales [num_pages][Hkv][P]):

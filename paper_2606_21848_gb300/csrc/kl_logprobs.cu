@@ -2,48 +2,55 @@
 //
 // With x = scale * logits, z = sum_j exp(x_j) and p = exp(x) / z:
 //   logprob(t) = x_t - log z,   H = - sum_j p_j log p_j = log z - sum_j p_j x_j,
-// and the `top` largest logits, ties to the lowest index. A row is cut into chunks of up to 2048 16-byte
-// vectors, one CTA each: the chunk stays in registers (8 vectors per thread, all loads in flight at
-// once), so that the maximum, the sums against it, and the selection read HBM once. The CTA that
-// finishes last joins the row's chunks. Bound by HBM: 6 to 7 instructions per logit leave the issue
-// slots two thirds busy at full bandwidth.
+// and the `top` largest logits, ties to the lowest index. Bound by HBM: every logit is read once; 5 to 6
+// instructions per bf16 logit leave the issue slots half busy at full bandwidth.
 //
-// Sums are held in fp32 against the chunk's largest logit m: y = (x - m) scale log2 e (the difference
-// first, so that rows of huge or lowest values neither overflow nor cancel), s1 = sum 2^y, s2 = sum y 2^y.
-// Chunks join as softmax states do: with d = (m_c - M) scale log2 e, s1 += 2^d s1_c,
-// s2 += 2^d (s2_c + d s1_c); then log z = log2(s1) ln 2 above scale * M and H = (log2 s1 - s2 / s1) ln 2.
+// The rows are cut into chunks of up to 32 KiB. Each CTA, three per SM, takes an equal run of consecutive
+// chunks and streams them through a ring of bulk copies, so that loads stay in flight whatever the
+// threads do. A thread keeps its own state over the chunks of a row, in fp32: its largest logit m, and
+// with y = (x - m) scale log2 e (the difference first, so that rows of huge or lowest values neither
+// overflow nor cancel) s1 = sum 2^y and s2 = sum y 2^y. States join as softmax states do: with d =
+// (m - M) scale log2 e, s1' = 2^d s1, s2' = 2^d s2 + d s1'; at last log z = log2(s1) ln 2 above scale * M
+// and H = (log2 s1 - s2 / s1) ln 2. A row that lies in several CTAs' runs is joined by the last of them.
 //
-// Selection: a logit among the row's largest is among its chunk's. Each thread has the maximum of its own
-// logits; with `top` threads' maxima known to be >= t, so are `top` logits, and only logits from such a
-// bound t on are candidates: t is the larger of (the smallest, over the 8 warps, of the ceil(top / 8)-th largest
-// maximum) and (the largest over the warps of the top-th). Those few are ranked by counting. Masked and tied rows,
-// where the bound leaves too few or too many, read their chunk a second time.
+// Selection: keys (value, lowest index first) above the smallest of the `top` best so far go to a list of
+// candidates in shared memory, which is ranked by counting and cut to `top` after the row's first chunk,
+// when it fills up and at the row's end. The first chunk's bound comes from the threads' maxima: with `top` of them known to be >= t, so are `top` logits; t is the larger of (the smallest, over the
+// 8 warps, of the ceil(top / 8)-th largest maximum) and (the largest over the warps of the top-th).
 #include <float.h>
 #include <math.h>
 
 #include <type_traits>
 
 #include "kl_internal.cuh"
+#include "kl_tc_ptx.cuh"
 
 namespace kl {
 namespace {
 
 constexpr int kLpThreads = 256, kLpWarps = 8;
-constexpr int kLpVecs = 8;                               // 16-byte vectors per thread
+constexpr int kLpVecs = 8;                               // 16-byte vectors per thread and chunk
 constexpr int kLpChunk = kLpThreads * kLpVecs;           // vectors per chunk, at most
-constexpr int kLpCap = 1024;                             // candidates ranked in shared memory
+constexpr int kLpMinChunk = 512;                         // vectors per chunk where rows are few
+constexpr int kLpStages = 2;
+constexpr int kLpCtas = 3;                               // per SM
+constexpr int kLpCap = 1024;                             // candidates in shared memory,
+constexpr int kLpExtra = 16;                             // room among them for a row's head and tail
 static_assert(KL_LOGPROBS_MAX_TOP <= 32, "a warp's sorted maxima bound the selection");
 
-struct LogprobSmem {
+struct __align__(16) LogprobSmem {
+    uint8_t ring[kLpStages][kLpChunk * 16];
+    uint64_t full[kLpStages];
     uint64_t cand[kLpCap];
     uint64_t list[KL_LOGPROBS_MAX_TOP];                  // keys, largest first
+    uint64_t wkey[kLpWarps];
     float wmax[kLpWarps], wnth[kLpWarps], wtop[kLpWarps];
     float s1[kLpWarps], s2[kLpWarps];
-    uint64_t wkey[kLpWarps];
     int wcount[kLpWarps];
-    int count;
+    int added[3];                                        // candidates of a chunk, by chunk number % 3
     int is_last;
 };
+static_assert(sizeof(LogprobSmem) * kLpCtas <= (228 - kLpCtas) * 1024, "CTAs per SM");
 
 // Keys order logits by value, then by lowest index; 0 is below every key. (-0 counts as +0.)
 __device__ __forceinline__ uint64_t make_key(float x, int idx) {
@@ -55,12 +62,6 @@ __device__ __forceinline__ int key_index(uint64_t k) { return (int)~(uint32_t)k;
 __device__ __forceinline__ float key_value(uint64_t k) {
     const int b = (int)((uint32_t)(k >> 32) ^ 0x80000000u);
     return __int_as_float(b >= 0 ? b : b ^ 0x7FFFFFFF);
-}
-
-__device__ __forceinline__ float lp_ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 
 // The 32-bit word w as logits: two bf16 (x the lower half) or one fp32 (x).
@@ -101,14 +102,6 @@ __device__ __forceinline__ uint32_t lp_max_bf16(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
-}
-
-// The registers of the chunk as the compiler may not know them from before: each phase unpacks them anew
-// instead of keeping 64 unpacked logits (which spilled).
-template <int N>
-__device__ __forceinline__ void lp_forget(uint32_t (&w)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(w[i]));
 }
 
 template <typename T>
@@ -171,297 +164,130 @@ __device__ __forceinline__ void take_keys(LogprobSmem &sm, int top, int tid, F &
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobArgs a, const int per_chunk) {
-    constexpr int VEC = 16 / sizeof(T);                  // logits per vector
-    __shared__ LogprobSmem sm;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
-    const char *rp = static_cast<const char *>(a.logits) + (size_t)row * a.stride * sizeof(T);
-    // vectors from the 16-byte boundary at or before the row's start; logit i is element off + i
-    const int off = (int)((reinterpret_cast<uintptr_t>(rp) & 15) / sizeof(T));
-    const int v0 = chunk * per_chunk;
-    const float c = a.scale * kLog2e;
-    const int top = a.top;
-    if (tid < KL_LOGPROBS_MAX_TOP) sm.list[tid] = 0;
-    if (tid == 0) sm.count = 0;
-    grid_dep_wait();
-    grid_dep_launch();
-
-    // logit of word k of vector i (its lower half)
-    auto index_of = [&](int i, int k) { return (v0 + i * kLpThreads + tid) * VEC + k * (VEC / 4) - off; };
-    // Logits outside the row (the edges' other elements, vectors past the end) count as -inf.
-    uint32_t v[4 * kLpVecs];
-    bool edge = false;                                   // the thread holds some of those
+// Largest of `n` values over the block by warps (each thread gets it after the barrier inside).
+__device__ __forceinline__ float block_max(LogprobSmem &sm, float x, int warp, int lane) {
 #pragma unroll
-    for (int i = 0; i < kLpVecs; ++i) {
-        const int j0 = index_of(i, 0);
-        const bool inside = i * kLpThreads + tid < per_chunk;
-        if (inside && j0 >= 0 && j0 + VEC <= a.vocab) {
-            const uint4 x = __ldcs(reinterpret_cast<const uint4 *>(rp + (int64_t)j0 * (int)sizeof(T)));
-            v[4 * i] = x.x;
-            v[4 * i + 1] = x.y;
-            v[4 * i + 2] = x.z;
-            v[4 * i + 3] = x.w;
-        } else {
-            edge = true;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[4 * i + k] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-            if (inside && j0 < a.vocab)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const int j = j0 + e;
-                    if (j < 0 || j >= a.vocab) continue;
-                    if constexpr (sizeof(T) == 4) {
-                        v[4 * i + e] = reinterpret_cast<const uint32_t *>(rp)[j];
-                    } else {
-                        uint32_t &w = v[4 * i + (e >> 1)];
-                        const uint32_t x = reinterpret_cast<const uint16_t *>(rp)[j];
-                        w = (e & 1) ? (w & 0xffffu) | x << 16 : (w & 0xffff0000u) | x;
-                    }
-                }
-        }
-    }
-    float tmax;                                          // (NaN does not take part)
-    if constexpr (sizeof(T) == 4) {
-        tmax = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4 * kLpVecs; ++i) tmax = fmaxf(tmax, __uint_as_float(v[i]));
-    } else {
-        uint32_t t = 0xff80ff80u;
-#pragma unroll
-        for (int i = 0; i < 4 * kLpVecs; ++i) t = lp_max_bf16(t, v[i]);
-        tmax = fmaxf(bf16lo(t), bf16hi(t));
-    }
-
-    // the block's maximum, and the warps' bounds for the selection: the maxima sorted over the lanes
-    float s = tmax;
-    if (top > 0) {
-#pragma unroll
-        for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-            for (int j = k >> 1; j > 0; j >>= 1) {
-                const float o = __shfl_xor_sync(0xffffffffu, s, j);
-                const bool larger = ((lane & j) == 0) == ((lane & k) == 0);   // descending overall
-                s = larger ? fmaxf(s, o) : fminf(s, o);
-            }
-        if (lane == (top + kLpWarps - 1) / kLpWarps - 1) sm.wnth[warp] = s;
-        if (lane == top - 1) sm.wtop[warp] = s;
-    } else {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
-    }
-    if (lane == 0) sm.wmax[warp] = s;
+    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    if (lane == 0) sm.wmax[warp] = x;
     __syncthreads();
-    float m = sm.wmax[0], bound = -INFINITY;
+    x = sm.wmax[0];
 #pragma unroll
-    for (int w = 1; w < kLpWarps; ++w) m = fmaxf(m, sm.wmax[w]);
-    if (top > 0) {
-        float lowest = sm.wnth[0];
-        bound = sm.wtop[0];
-#pragma unroll
-        for (int w = 1; w < kLpWarps; ++w) {
-            lowest = fminf(lowest, sm.wnth[w]);
-            bound = fmaxf(bound, sm.wtop[w]);
-        }
-        bound = fmaxf(bound, lowest);
-    }
+    for (int w = 1; w < kLpWarps; ++w) x = fmaxf(x, sm.wmax[w]);
+    return x;
+}
 
-    // logits from the bound on (above it, where it is -inf)
-    lp_forget(v);
-    const float from = bound == -INFINITY ? -FLT_MAX : bound;
-    if (top > 0 && tmax >= from) {
+// A state (m, s1, s2) moves to the reference M >= m. (One so low that its factor is 0 keeps only NaN.)
+__device__ __forceinline__ void move_state(float m, float M, float c, float &s1, float &s2) {
+    const float d = (m - M) * c, f = m == -INFINITY ? 1.f : ptx::ex2(d);   // (m = -inf: the sums are 0 or NaN)
+    s1 *= f;
+    s2 = f == 0.f || m == -INFINITY ? s1 : fmaf(d, s1, f * s2);
+}
+
+// Where a row's chunks lie. The row starts with `head` logits ahead of a 16-byte boundary, then `vecs`
+// vectors, then `tail` logits.
+template <typename T>
+struct LogprobRow {
+    static constexpr int VEC = 16 / sizeof(T);
+    const char *p;
+    int head, vecs, tail;
+    __device__ LogprobRow(const LogprobArgs &a, int row) {
+        p = static_cast<const char *>(a.logits) + (size_t)row * a.stride * sizeof(T);
+        head = min(a.vocab, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) % 16 / sizeof(T)));
+        vecs = (a.vocab - head) / VEC;
+        tail = a.vocab - head - vecs * VEC;
+    }
+};
+
+// A copy that has not landed at the first look: bounded (about one second).
+__device__ __noinline__ void wait_slow(uint64_t *bar, uint32_t phase, int32_t *err) {
+    const uint64_t t0 = ptx::globaltimer();
+    while (!ptx::mbar_try_wait(bar, phase))
+        if (ptx::globaltimer() - t0 > kDefaultWaitNs) {
+            raise_flag(err, KL_FLAG_TIMEOUT);
+            return;
+        }
+}
+
+// The CTA whose run of chunks holds chunk i: runs start at floor(c * n / ctas).
+__device__ __forceinline__ int run_of(int64_t i, int64_t n, int ctas) { return (int)(((i + 1) * ctas - 1) / n); }
+
+// The parts of a row, joined by the CTA that arrived last: the sums to every thread, the keys to the list.
+__device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int row, int parts, float c, float &m,
+                           float &s1, float &s2) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, top = a.top;
+    const float4 *part = a.part + (size_t)row * a.slots;
+    const uint64_t *keys = a.part_top + (size_t)row * a.slots * top;
+    // every part's last key is a bound; the largest of them leaves few
+    float M = -INFINITY;
+    uint64_t least = 0;
+    for (int i = tid; i < parts; i += kLpThreads) {
+        M = fmaxf(M, __ldcg(part + i).x);
+        if (top > 0) {
+            const uint64_t x = __ldcg(keys + (size_t)i * top + top - 1);
+            if (x > least) least = x;
+        }
+    }
 #pragma unroll
-        for (int i = 0; i < 4 * kLpVecs; ++i) {
-            const float2 x = lp_unpack<T>(v[i]);
-            if (fmaxf(x.x, x.y) >= from) {
-                const int j = index_of(i >> 2, i & 3);
-                if (x.x >= from) {
-                    const int at = atomicAdd(&sm.count, 1);
-                    if (at < kLpCap) sm.cand[at] = make_key(x.x, j);
-                }
-                if (x.y >= from) {
-                    const int at = atomicAdd(&sm.count, 1);
-                    if (at < kLpCap) sm.cand[at] = make_key(x.y, j + 1);
-                }
+    for (int o = 16; o > 0; o >>= 1) {
+        const uint64_t x = __shfl_xor_sync(0xffffffffu, least, o);
+        if (x > least) least = x;
+    }
+    if (lane == 0) sm.wkey[warp] = least;
+    if (tid < KL_LOGPROBS_MAX_TOP) sm.list[tid] = 0;
+    if (tid == 0) sm.wcount[0] = 0;
+    M = block_max(sm, M, warp, lane);
+    float a1 = 0.f, a2 = 0.f;
+    for (int i = tid; i < parts; i += kLpThreads) {
+        const float4 q = __ldcg(part + i);
+        float p1 = q.y, p2 = q.z;
+        move_state(q.x, M, c, p1, p2);
+        a1 += p1;
+        a2 += p2;
+    }
+    warp_sums(sm, a1, a2, warp, lane);
+    if (top > 0) {
+        least = 0;
+#pragma unroll
+        for (int w = 0; w < kLpWarps; ++w)
+            if (sm.wkey[w] > least) least = sm.wkey[w];
+        for (int i = tid; i < parts * top; i += kLpThreads) {
+            const uint64_t x = __ldcg(keys + i);
+            if (x != 0 && x >= least) {
+                const int at = atomicAdd(&sm.wcount[0], 1);
+                if (at < kLpCap) sm.cand[at] = x;
             }
         }
-        lp_forget(v);
     }
-
-    // The sums against the chunk's maximum (0 where nothing is above -inf). A weight of 0 at y = -inf has
-    // to add 0 to s2, not NaN: the clamp for that is left out where the thread's logits do without.
-    const float mr = m == -INFINITY ? 0.f : m;
-    const float2 neg_m = make_float2(-mr, -mr), cc = make_float2(c, c);
-    float s1, s2;
-    auto sums = [&](auto clamp) {
-        float2 a1 = make_float2(0.f, 0.f), a2 = a1;
-#pragma unroll
-        for (int i = 0; i < 4 * kLpVecs; i += VEC == 4 ? 2 : 1) {
-            float2 x;
-            if constexpr (VEC == 4) x = make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-            else x = lp_unpack<T>(v[i]);
-            float2 y = lp_mul2(lp_add2(x, neg_m), cc);
-            const float2 p = make_float2(lp_ex2(y.x), lp_ex2(y.y));
-            if constexpr (decltype(clamp)::value) y = make_float2(fmaxf(y.x, -1e30f), fmaxf(y.y, -1e30f));
-            a1 = lp_add2(a1, p);
-            a2 = lp_fma2(p, y, a2);
-        }
-        s1 = a1.x + a1.y;
-        s2 = a2.x + a2.y;
-    };
-    if (!edge) sums(std::false_type{});
-    if (edge || (s2 != s2 && s1 == s1)) {
-        lp_forget(v);
-        sums(std::true_type{});
-    }
-    warp_sums(sm, s1, s2, warp, lane);
     __syncthreads();
     block_sums(sm, s1, s2);
-
+    m = M;
     if (top > 0) {
-        int n = sm.count;
-        if (n >= top && n <= kLpCap) {
+        const int n = sm.wcount[0];
+        if (n <= kLpCap) {
             rank_keys(sm, n, top, tid);
         } else {
-            // Too few (the bound is -inf) or too many (ties at the bound, or a chunk whose large logits lie
-            // in a few threads): the chunk is read once more.
-            const int j0 = max(0, v0 * VEC - off), j1 = min(a.vocab, (v0 + per_chunk) * VEC - off);
-            __syncthreads();
-            if (n > kLpCap) {
-                if (tid == 0) sm.count = 0;
-                __syncthreads();
-                for (int j = j0 + tid; j < j1; j += kLpThreads) {
-                    const float x = lp_load<T>(rp, j);
-                    if (x > bound) {
-                        const int at = atomicAdd(&sm.count, 1);
-                        if (at < kLpCap) sm.cand[at] = make_key(x, j);
-                    }
+            take_keys(sm, top, tid, [&](uint64_t prev) {
+                uint64_t best = 0;
+                for (int i = tid; i < parts * top; i += kLpThreads) {
+                    const uint64_t x = __ldcg(keys + i);
+                    if (x < prev && x > best) best = x;
                 }
-                __syncthreads();
-                n = sm.count;
-            }
-            if (n <= kLpCap) {
-                rank_keys(sm, n, top, tid);
-                // then the first logits equal to the bound, in order
-                for (int jb = j0; jb < j1 && n < top; jb += kLpThreads) {
-                    const int j = jb + tid;
-                    const bool mine = j < j1 && lp_load<T>(rp, j) == bound;
-                    const unsigned votes = __ballot_sync(0xffffffffu, mine);
-                    if (lane == 0) sm.wcount[warp] = __popc(votes);
-                    __syncthreads();
-                    int at = n + __popc(votes & ((1u << lane) - 1));
-#pragma unroll
-                    for (int w = 0; w < kLpWarps; ++w) {
-                        if (w < warp) at += sm.wcount[w];
-                        n += sm.wcount[w];
-                    }
-                    if (mine && at < top) sm.list[at] = make_key(bound, j);
-                    __syncthreads();
-                }
-            } else {
-                take_keys(sm, top, tid, [&](uint64_t prev) {
-                    uint64_t k = 0;
-                    for (int j = j0 + tid; j < j1; j += kLpThreads) {
-                        const float x = lp_load<T>(rp, j);
-                        const uint64_t y = x > bound ? make_key(x, j) : 0;
-                        if (y < prev && y > k) k = y;
-                    }
-                    return k;
-                });
-            }
+                return best;
+            });
         }
         __syncthreads();
     }
+}
 
-    if (a.chunks > 1) {
-        const size_t slot = (size_t)row * a.chunks + chunk;
-        if (warp == 0) {
-            if (lane == 0) a.part[slot] = make_float4(m, s1, s2, 0.f);
-            if (lane < top) a.part_top[slot * top + lane] = sm.list[lane];
-            __syncwarp();
-            if (lane == 0) sm.is_last = arrive_last(a.counters + row, a.chunks);
-        }
-        __syncthreads();
-        if (!sm.is_last) return;
-        // join the row's chunks
-        const float4 *part = a.part + (size_t)row * a.chunks;
-        float M = -INFINITY;
-        for (int i = tid; i < a.chunks; i += kLpThreads) M = fmaxf(M, __ldcg(part + i).x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-        if (lane == 0) sm.wmax[warp] = M;
-        if (tid == 0) sm.count = 0;
-        __syncthreads();
-        m = sm.wmax[0];
-#pragma unroll
-        for (int w = 1; w < kLpWarps; ++w) m = fmaxf(m, sm.wmax[w]);
-        s1 = s2 = 0.f;
-        for (int i = tid; i < a.chunks; i += kLpThreads) {
-            const float4 q = __ldcg(part + i);
-            const float d = (q.x - m) * c, f = lp_ex2(d);
-            // (a chunk of -inf has s1 = 0 and d = NaN or -inf; one so low that f is 0 adds nothing but NaN)
-            if (q.y != 0.f && (f != 0.f || q.y != q.y)) {
-                s1 = fmaf(f, q.y, s1);
-                s2 = fmaf(f, fmaf(d, q.y, q.z), s2);
-            }
-        }
-        warp_sums(sm, s1, s2, warp, lane);
-        __syncthreads();
-        block_sums(sm, s1, s2);
-        if (top > 0) {
-            // every chunk's last key is a bound; the largest of them leaves few
-            const uint64_t *keys = a.part_top + (size_t)row * a.chunks * top;
-            uint64_t k = 0;
-            for (int i = tid; i < a.chunks; i += kLpThreads) {
-                const uint64_t x = __ldcg(keys + (size_t)i * top + top - 1);
-                if (x > k) k = x;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                const uint64_t x = __shfl_xor_sync(0xffffffffu, k, o);
-                if (x > k) k = x;
-            }
-            if (lane == 0) sm.wkey[warp] = k;
-            if (tid < KL_LOGPROBS_MAX_TOP) sm.list[tid] = 0;
-            __syncthreads();
-            k = 0;
-#pragma unroll
-            for (int w = 0; w < kLpWarps; ++w)
-                if (sm.wkey[w] > k) k = sm.wkey[w];
-            const int64_t all = (int64_t)a.chunks * top;
-            for (int64_t i = tid; i < all; i += kLpThreads) {
-                const uint64_t x = __ldcg(keys + i);
-                if (x != 0 && x >= k) {
-                    const int at = atomicAdd(&sm.count, 1);
-                    if (at < kLpCap) sm.cand[at] = x;
-                }
-            }
-            __syncthreads();
-            const int n = sm.count;
-            if (n <= kLpCap) {
-                rank_keys(sm, n, top, tid);
-            } else {
-                take_keys(sm, top, tid, [&](uint64_t prev) {
-                    uint64_t best = 0;
-                    for (int64_t i = tid; i < all; i += kLpThreads) {
-                        const uint64_t x = __ldcg(keys + i);
-                        if (x < prev && x > best) best = x;
-                    }
-                    return best;
-                });
-            }
-            __syncthreads();
-        }
-    }
-
-    // Results. A row of -inf alone has no distribution: log probabilities of -inf, entropy 0. A NaN or
-    // +inf logit makes the sums, and with them everything but the ids, NaN.
+// The results of a row. One of -inf alone has no distribution: log probabilities of -inf, entropy 0. A NaN
+// or +inf logit makes the sums, and with them everything but the ids, NaN.
+template <typename T>
+__device__ void finish_row(LogprobSmem &sm, const LogprobArgs &a, const char *rp, int row, float c, float m,
+                           float s1, float s2) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, top = a.top;
     const bool none = s1 == 0.f;
     const float lz = log2f(s1);
     auto logprob = [&](float x) { return none ? -INFINITY : ((x - m) * c - lz) * kLn2; };
-    if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : (lz - s2 / s1) * kLn2;
-    if (tid == 0 && s1 != s1) raise_flag(a.err, KL_FLAG_RANGE);
     for (int i = tid; i < a.per_row; i += kLpThreads) {
         const int id = a.tokens[(size_t)row * a.per_row + i];
         float lp = 0.f;                                  // -1: no token
@@ -473,6 +299,29 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
         }
         a.logprobs[(size_t)row * a.per_row + i] = lp;
     }
+    if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : (lz - s2 / s1) * kLn2;
+    if (tid == 0 && s1 != s1) raise_flag(a.err, KL_FLAG_RANGE);
+    if (top > 0 && sm.list[top - 1] == 0) {
+        // fewer than `top` logits above -inf: the first of the others, in order
+        int n = 0;
+        while (sm.list[n] != 0) ++n;
+        __syncthreads();
+        for (int jb = 0; jb < a.vocab && n < top; jb += kLpThreads) {
+            const int j = jb + tid;
+            const bool mine = j < a.vocab && lp_load<T>(rp, j) == -INFINITY;
+            const unsigned votes = __ballot_sync(0xffffffffu, mine);
+            if (lane == 0) sm.wcount[warp] = __popc(votes);
+            __syncthreads();
+            int at = n + __popc(votes & ((1u << lane) - 1));
+#pragma unroll
+            for (int w = 0; w < kLpWarps; ++w) {
+                if (w < warp) at += sm.wcount[w];
+                n += sm.wcount[w];
+            }
+            if (mine && at < top) sm.list[at] = make_key(-INFINITY, j);
+            __syncthreads();
+        }
+    }
     if (tid < top) {
         const uint64_t k = sm.list[tid];
         a.top_ids[(size_t)row * top + tid] = k ? key_index(k) : -1;
@@ -480,32 +329,338 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
     }
 }
 
-// 16-byte vectors that a row of `vocab` logits can touch, whatever its alignment.
-int64_t row_vectors(int vocab, int vec, bool aligned) {
-    return ((int64_t)vocab + (aligned ? 0 : vec - 1) + vec - 1) / vec;
+template <typename T>
+__global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const LogprobArgs a, const int per_chunk) {
+    using Row = LogprobRow<T>;
+    constexpr int VEC = Row::VEC;
+    extern __shared__ __align__(16) uint8_t lp_smem[];
+    LogprobSmem &sm = *reinterpret_cast<LogprobSmem *>(lp_smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int top = a.top;
+    const float c = a.scale * kLog2e;
+    const int64_t total = (int64_t)a.rows * a.chunks;
+    const int64_t it0 = total * blockIdx.x / gridDim.x, it1 = total * (blockIdx.x + 1) / gridDim.x;
+    const int steps = (int)(it1 - it0);
+    if (tid == 0) {
+        for (int s = 0; s < kLpStages; ++s) ptx::mbar_init(&sm.full[s], 1);
+        ptx::fence_mbar_init();
+    }
+    if (tid < 3) sm.added[tid] = 0;
+    __syncthreads();
+    grid_dep_wait();
+    grid_dep_launch();
+
+    // thread 0: the copy of the run's chunk k into its slot (called for k = 0, 1, 2, ...)
+    int row = (int)(it0 / a.chunks), ch = (int)(it0 - (int64_t)row * a.chunks);
+    int frow = row, fch = ch;
+    auto fetch = [&](int k) {
+        const Row r(a, frow);
+        const int q0 = fch * per_chunk, nv = max(0, min(per_chunk, r.vecs - q0));
+        if (++fch == a.chunks) {
+            fch = 0;
+            ++frow;
+        }
+        uint64_t *bar = &sm.full[k % kLpStages];
+        if (nv == 0) {
+            ptx::mbar_arrive(bar);
+            return;
+        }
+        ptx::mbar_arrive_expect_tx(bar, (uint32_t)nv * 16u);
+        ptx::bulk_load(sm.ring[k % kLpStages], r.p + (size_t)r.head * sizeof(T) + (size_t)q0 * 16, (uint32_t)nv * 16u, bar);
+    };
+    if (tid == 0)
+        for (int k = 0; k < kLpStages && k < steps; ++k) fetch(k);
+
+    float m = -INFINITY, s1 = 0.f, s2 = 0.f;             // this thread's state of the row
+    float extra = -INFINITY;                             // its logit of the row's head or tail
+    int extra_at = -1;
+    int kept = 0;                                        // candidates known to all threads
+    float from = -FLT_MAX;                               // logits below do not matter
+    uint64_t above = 0;                                  // nor do keys up to this one
+    Row r(a, row);
+    // The candidates that chunk k added become known: cut to the `top` largest when they are the row's
+    // first (which gives the bound for the rest) or fill half of the list, or at the end. Where they
+    // overflowed it (ties; rising rows), the chunk is read once more. All threads, after a barrier behind
+    // the chunk's adds; ends behind a barrier if it cut.
+    auto settle = [&](int k, bool all) {
+        const int n = kept + sm.added[k % 3];
+        if (tid == 0) sm.added[(k + 2) % 3] = 0;         // chunk k - 1's: read by all before that barrier
+        if (n <= kLpCap - kLpExtra) {
+            if (!all && (above != 0 || n < top) && n <= kLpCap / 2) {
+                kept = n;
+                return;
+            }
+            rank_keys(sm, n, top, tid);
+            __syncthreads();
+        } else {
+            const int c = ch - (all ? 0 : 1);            // the chunk's number in the row
+            const int j0 = r.head + c * per_chunk * VEC, j1 = r.head + min(r.vecs, (c + 1) * per_chunk) * VEC;
+            take_keys(sm, top, tid, [&](uint64_t prev) {
+                uint64_t best = 0;
+                for (int i = tid; i < kept; i += kLpThreads)
+                    if (sm.cand[i] < prev && sm.cand[i] > best) best = sm.cand[i];
+                for (int j = j0 + tid; j < j1; j += kLpThreads) {
+                    const float x = lp_load<T>(r.p, j);
+                    const uint64_t y = x >= from ? make_key(x, j) : 0;
+                    if (y < prev && y > best) best = y;
+                }
+                return best;
+            });
+        }
+        kept = min(n, top);
+        if (kept == top) {
+            above = sm.list[top - 1];
+            from = key_value(above);
+        }
+        if (tid < kept) sm.cand[tid] = sm.list[tid];
+        if (tid == 0) sm.added[k % 3] = 0;
+        __syncthreads();
+    };
+    int slot = 0;                                        // of chunk k, and the phase of its copy
+    uint32_t phase = 0;
+
+    for (int k = 0; k < steps; ++k, ++ch) {
+        if (ch == a.chunks) {
+            ch = 0;
+            ++row;
+        }
+        const bool first = k == 0 || ch == 0, last = k == steps - 1 || ch == a.chunks - 1;
+        if (first) {
+            r = Row(a, row);
+            m = -INFINITY;
+            s1 = s2 = 0.f;
+            kept = 0;
+            from = -FLT_MAX;
+            above = 0;
+            // the logits outside the vectors: the first chunk's CTA takes the head, the last one's the tail
+            const bool in_head = tid < r.head && ch == 0;
+            const bool in_tail = tid >= 32 && tid - 32 < r.tail && it1 >= ((int64_t)row + 1) * a.chunks;
+            extra_at = in_head ? tid : in_tail ? a.vocab - r.tail + tid - 32 : -1;
+            extra = extra_at >= 0 ? lp_load<T>(r.p, extra_at) : -INFINITY;
+        }
+        // Everyone has read the last chunk's slot, and its candidates are complete.
+        __syncthreads();
+        if (tid == 0 && k > 0 && k - 1 + kLpStages < steps) fetch(k - 1 + kLpStages);
+        if (top > 0 && !first) settle(k - 1, false);
+        // the chunk: vector i of the thread is i * 256 + tid
+        const int q0 = ch * per_chunk, nv = min(per_chunk, r.vecs - q0);
+        if (!ptx::mbar_try_wait(&sm.full[slot], phase)) wait_slow(&sm.full[slot], phase, a.err);
+        // (read from shared memory once for the maximum and once for the sums: 64 logits held in between
+        // spilled)
+        const uint4 *const data = reinterpret_cast<const uint4 *>(sm.ring[slot]) + tid;
+        const int mine = nv > tid ? (nv - tid + kLpThreads - 1) / kLpThreads : 0;   // vectors of this thread
+        float tmax = -INFINITY;                          // (NaN does not take part)
+        {
+            uint32_t t = 0xff80ff80u;
+            auto look = [&](const uint4 &x) {
+                if constexpr (sizeof(T) == 4) {
+                    tmax = fmaxf(fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), __uint_as_float(x.z)),
+                                 fmaxf(tmax, __uint_as_float(x.w)));
+                } else {
+                    t = lp_max_bf16(lp_max_bf16(lp_max_bf16(x.x, x.y), lp_max_bf16(x.z, x.w)), t);
+                }
+            };
+            if (mine == kLpVecs) {
+#pragma unroll
+                for (int i = 0; i < kLpVecs; ++i) look(data[i * kLpThreads]);
+            } else {
+                for (int i = 0; i < mine; ++i) look(data[i * kLpThreads]);
+            }
+            if constexpr (sizeof(T) == 2) tmax = fmaxf(bf16lo(t), bf16hi(t));
+        }
+
+        if (top > 0) {
+            float bound = from;
+            if (first) {
+                // the bound: the threads' maxima sorted over the lanes (descending)
+                float s = tmax;
+#pragma unroll
+                for (int g = 2; g <= 32; g <<= 1)
+#pragma unroll
+                    for (int j = g >> 1; j > 0; j >>= 1) {
+                        const float o = __shfl_xor_sync(0xffffffffu, s, j);
+                        const bool larger = ((lane & j) == 0) == ((lane & g) == 0);
+                        s = larger ? fmaxf(s, o) : fminf(s, o);
+                    }
+                if (lane == (top + kLpWarps - 1) / kLpWarps - 1) sm.wnth[warp] = s;
+                if (lane == top - 1) sm.wtop[warp] = s;
+                __syncthreads();
+                float lowest = sm.wnth[0], best = sm.wtop[0];
+#pragma unroll
+                for (int w = 1; w < kLpWarps; ++w) {
+                    lowest = fminf(lowest, sm.wnth[w]);
+                    best = fmaxf(best, sm.wtop[w]);
+                }
+                bound = fmaxf(-FLT_MAX, fmaxf(best, lowest));
+            }
+            if (tmax >= bound) {
+#pragma unroll 1
+                for (int i = 0; i < mine; ++i) {
+                    const uint4 x = data[i * kLpThreads];
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    const int j = r.head + (q0 + i * kLpThreads + tid) * VEC;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 y = lp_unpack<T>(w[e]);
+                        if (fmaxf(y.x, y.y) >= bound) {
+                            auto add = [&](float z, int at) {
+                                const uint64_t key = make_key(z, at);
+                                if (z >= bound && key > above) {
+                                    const int o = kept + atomicAdd(&sm.added[k % 3], 1);
+                                    if (o < kLpCap) sm.cand[o] = key;
+                                }
+                            };
+                            add(y.x, j + e * (VEC / 4));
+                            if (VEC == 8) add(y.y, j + e * 2 + 1);
+                        }
+                    }
+                }
+            }
+        }
+
+        // the sums, at the thread's reference
+        // (moved when a weight would pass 2^16: m need not be the largest logit itself)
+        if ((tmax - m) * c > 16.f) {
+            move_state(m, tmax, c, s1, s2);
+            m = tmax;
+        }
+        {
+            // (a weight of 0 at y = -inf has to add 0 to s2, not NaN: with the clamp, where it came up)
+            const float mr = m == -INFINITY ? 0.f : m;
+            const float2 neg_m = make_float2(-mr, -mr), cc = make_float2(c, c);
+            const float b1 = s1, b2 = s2;
+            auto sums = [&](auto clamp) {
+                float2 a1 = make_float2(b1, 0.f), a2 = make_float2(b2, 0.f);
+                auto pair = [&](float2 x) {
+                    float2 y = lp_mul2(lp_add2(x, neg_m), cc);
+                    const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
+                    if constexpr (decltype(clamp)::value) y = make_float2(fmaxf(y.x, -1e30f), fmaxf(y.y, -1e30f));
+                    a1 = lp_add2(a1, p);
+                    a2 = lp_fma2(p, y, a2);
+                };
+                auto vec = [&](const uint4 &x) {
+                    if constexpr (VEC == 4) {
+                        pair(make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
+                        pair(make_float2(__uint_as_float(x.z), __uint_as_float(x.w)));
+                    } else {
+                        pair(lp_unpack<T>(x.x));
+                        pair(lp_unpack<T>(x.y));
+                        pair(lp_unpack<T>(x.z));
+                        pair(lp_unpack<T>(x.w));
+                    }
+                };
+                if (mine == kLpVecs && !decltype(clamp)::value) {
+#pragma unroll
+                    for (int i = 0; i < kLpVecs; ++i) vec(data[i * kLpThreads]);
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < mine; ++i) vec(data[i * kLpThreads]);
+                }
+                s1 = a1.x + a1.y;
+                s2 = a2.x + a2.y;
+            };
+            sums(std::false_type{});
+            if (s2 != s2 && s1 == s1) sums(std::true_type{});
+        }
+        if (++slot == kLpStages) {
+            slot = 0;
+            phase ^= 1;
+        }
+        if (!last) continue;
+
+        // ------------------------------------------------------- the row, or its part in this run ----
+        if (extra_at >= 0) {
+            if ((extra - m) * c > 16.f) {
+                move_state(m, extra, c, s1, s2);
+                m = extra;
+            }
+            const float y = (extra - (m == -INFINITY ? 0.f : m)) * c, p = ptx::ex2(y);
+            s1 += p;
+            s2 = fmaf(p, fmaxf(y, -1e30f), s2);
+        }
+        const float M = block_max(sm, m, warp, lane);    // (the barrier: the last candidates are there)
+        move_state(m, M, c, s1, s2);
+        m = M;
+        warp_sums(sm, s1, s2, warp, lane);
+        __syncthreads();
+        block_sums(sm, s1, s2);
+        if (top > 0) {
+            settle(k, true);
+            // the candidates outside the vectors
+            if (extra_at >= 0 && extra >= from) {
+                const uint64_t key = make_key(extra, extra_at);
+                if (key > above) sm.cand[kept + atomicAdd(&sm.added[k % 3], 1)] = key;
+            }
+            if (tid >= kept && tid < KL_LOGPROBS_MAX_TOP) sm.list[tid] = 0;
+            __syncthreads();
+            const int n = kept + sm.added[k % 3];
+            if (n > kept) rank_keys(sm, n, top, tid);
+            __syncthreads();
+            if (tid < 3) sm.added[tid] = 0;
+        }
+        const int64_t row0 = (int64_t)row * a.chunks;
+        const int c0 = run_of(row0, total, gridDim.x);
+        const int parts = run_of(row0 + a.chunks - 1, total, gridDim.x) - c0 + 1;
+        if (parts > 1) {
+            const size_t at = (size_t)row * a.slots + (blockIdx.x - c0);
+            if (warp == 0) {
+                if (lane == 0) a.part[at] = make_float4(m, s1, s2, 0.f);
+                if (lane < top) a.part_top[at * top + lane] = sm.list[lane];
+                __syncwarp();
+                if (lane == 0) sm.is_last = arrive_last(a.counters + row, parts);
+            }
+            __syncthreads();
+            if (!sm.is_last) continue;
+            join_parts(sm, a, row, parts, c, m, s1, s2);
+        }
+        finish_row<T>(sm, a, r.p, row, c, m, s1, s2);
+        __syncthreads();
+    }
+}
+
+// Vectors per chunk when a row of `vecs` vectors is cut into `chunks`: a multiple of the threads, so that only
+// a row's last chunk leaves some of them without a vector.
+int chunk_vectors(int64_t vecs, int chunks) {
+    const int64_t each = (vecs + chunks - 1) / chunks;
+    return (int)((each + kLpThreads - 1) / kLpThreads * kLpThreads);
+}
+
+// Chunks of a row of `vecs` 16-byte vectors: of kLpChunk vectors, or smaller (kLpMinChunk) while the rows
+// leave CTAs idle.
+int chunks_of(int64_t rows, int64_t vecs) {
+    const int64_t ctas = (int64_t)kLpCtas * device_sm_count();
+    int64_t n = (vecs + kLpChunk - 1) / kLpChunk;
+    if (rows * n < ctas) {
+        const int64_t want = (ctas + rows - 1) / rows, most = (vecs + kLpMinChunk - 1) / kLpMinChunk;
+        n = max(n, min(want, most));
+    }
+    if (n < 1) return 1;
+    const int64_t each = chunk_vectors(vecs, (int)n);
+    return (int)max((vecs + each - 1) / each, (int64_t)1);
 }
 
 }  // namespace
 
-int logprob_chunks(int vocab, kl_dtype dtype) {
-    return (int)((row_vectors(vocab, dtype == KL_FP32 ? 4 : 8, false) + kLpChunk - 1) / kLpChunk);
+int logprob_chunks(int rows, int vocab, kl_dtype dtype) {
+    return chunks_of(rows, vocab / (dtype == KL_FP32 ? 4 : 8));
 }
 
 cudaError_t launch_logprobs(const LogprobArgs &a) {
-    LogprobArgs la = a;
-    const int es = a.dtype == KL_FP32 ? 4 : 2;
-    const bool aligned = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
-                         (a.rows == 1 || (a.stride * es) % 16 == 0);
-    const int64_t vecs = row_vectors(a.vocab, 16 / es, aligned);
-    la.chunks = (int)((vecs + kLpChunk - 1) / kLpChunk);
-    const int per_chunk = (int)((vecs + la.chunks - 1) / la.chunks);
+    const int per_chunk = chunk_vectors(a.vocab / (a.dtype == KL_FP32 ? 4 : 8), a.chunks);
+    const int64_t total = (int64_t)a.rows * a.chunks, ctas = (int64_t)kLpCtas * device_sm_count();
+    const auto kernel = a.dtype == KL_FP32 ? logprobs_kernel<float> : logprobs_kernel<uint16_t>;
+    static PerDeviceOnce once[2];
+    const cudaError_t e = once[a.dtype == KL_FP32].run([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LogprobSmem));
+    });
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((int64_t)a.rows * la.chunks));
+    cfg.gridDim = dim3((unsigned)(total < ctas ? total : ctas));
     cfg.blockDim = dim3(kLpThreads);
+    cfg.dynamicSmemBytes = sizeof(LogprobSmem);
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
-    return a.dtype == KL_FP32 ? cudaLaunchKernelEx(&cfg, logprobs_kernel<float>, la, per_chunk)
-                              : cudaLaunchKernelEx(&cfg, logprobs_kernel<uint16_t>, la, per_chunk);
+    return cudaLaunchKernelEx(&cfg, kernel, a, per_chunk);
 }
 
 }  // namespace kl
