@@ -178,9 +178,10 @@ __device__ __forceinline__ float block_max(LogprobSmem &sm, float x, int warp, i
 
 // A state (m, s1, s2) moves to the reference M >= m. (One so low that its factor is 0 keeps only NaN.)
 __device__ __forceinline__ void move_state(float m, float M, float c, float &s1, float &s2) {
-    const float d = (m - M) * c, f = m == -INFINITY ? 1.f : ptx::ex2(d);   // (m = -inf: the sums are 0 or NaN)
+    if (m == -INFINITY || m == M) return;                // (the sums are 0 or NaN; nothing moves)
+    const float d = (m - M) * c, f = ptx::ex2(d);
     s1 *= f;
-    s2 = f == 0.f || m == -INFINITY ? s1 : fmaf(d, s1, f * s2);
+    s2 = f == 0.f ? s1 : fmaf(d, s1, f * s2);
 }
 
 // Where a row's chunks lie. The row starts with `head` logits ahead of a 16-byte boundary, then `vecs`
@@ -493,36 +494,34 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
                 }
                 bound = fmaxf(-FLT_MAX, fmaxf(best, lowest));
             }
-            if (tmax >= bound) {
-#pragma unroll 1
-                for (int i = 0; i < mine; ++i) {
-                    const uint4 x = data[i * kLpThreads];
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                    const int j = r.head + (q0 + i * kLpThreads + tid) * VEC;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 y = lp_unpack<T>(w[e]);
-                        if (fmaxf(y.x, y.y) >= bound) {
-                            auto add = [&](float z, int at) {
-                                const uint64_t key = make_key(z, at);
-                                if (z >= bound && key > above) {
-                                    const int o = kept + atomicAdd(&sm.added[k % 3], 1);
-                                    if (o < kLpCap) sm.cand[o] = key;
-                                }
-                            };
-                            add(y.x, j + e * (VEC / 4));
-                            if (VEC == 8) add(y.y, j + e * 2 + 1);
+            // For each thread with a hit its warp looks at the thread's 32 words, one per lane.
+            static_assert(kLpVecs * 4 == 32, "a word per lane");
+            for (unsigned left = __ballot_sync(0xffffffffu, tmax >= bound); left; left &= left - 1) {
+                const int at = (lane >> 2) * kLpThreads + warp * 32 + __ffs(left) - 1;   // vector
+                if (at < nv) {
+                    const float2 x = lp_unpack<T>(reinterpret_cast<const uint32_t *>(sm.ring[slot])[4 * at + (lane & 3)]);
+                    const int j = r.head + (q0 + at) * VEC + (lane & 3) * (VEC / 4);
+                    auto add = [&](float y, int index) {
+                        const uint64_t key = make_key(y, index);
+                        if (y >= bound && key > above) {
+                            const int o = kept + atomicAdd(&sm.added[k % 3], 1);
+                            if (o < kLpCap) sm.cand[o] = key;
                         }
-                    }
+                    };
+                    add(x.x, j);
+                    if (VEC == 8) add(x.y, j + 1);
                 }
+                __syncwarp();
             }
         }
 
         // the sums, at the thread's reference
         // (moved when a weight would pass 2^16: m need not be the largest logit itself)
-        if ((tmax - m) * c > 16.f) {
-            move_state(m, tmax, c, s1, s2);
-            m = tmax;
+        const bool moves = (tmax - m) * c > 16.f;
+        if (__any_sync(0xffffffffu, moves)) {
+            const float to = moves ? tmax : m;
+            move_state(m, to, c, s1, s2);
+            m = to;
         }
         {
             // (a weight of 0 at y = -inf has to add 0 to s2, not NaN: with the clamp, where it came up)
@@ -560,7 +559,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
                 s2 = a2.x + a2.y;
             };
             sums(std::false_type{});
-            if (s2 != s2 && s1 == s1) sums(std::true_type{});
+            if (__any_sync(0xffffffffu, s2 != s2 && s1 == s1)) sums(std::true_type{});
         }
         if (++slot == kLpStages) {
             slot = 0;
