@@ -365,18 +365,17 @@ SharedLayout shared_layout(size_t counters, size_t state_bytes, size_t extra_byt
     return w;
 }
 
-// Geometry, layout and workspace of a tree-attention call; KL_OK with total 0: no workspace needed.
+// Geometry and layout of a tree-attention call, and the workspace behind the shared front region: the
+// runs' entries for the merge, then their states (none of which a decode's counters ever share).
 kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t num_splits,
-                         bool fp32, Geometry *g, TreePlan *p, SharedLayout *w) {
+                         Geometry *g, TreePlan *p, SharedLayout *w) {
     const kl_status st = resolve(shape, -1, g);
     if (st != KL_OK) return st;
     if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits) return KL_ERR_INVALID_ARG;
     if (max_q_len > KL_TREE_MAX_DRAFTS) return KL_ERR_UNSUPPORTED;
-    *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P, num_splits,
-                   fp32, device_sm_count());
-    const size_t rows = (size_t)total_q * g->Hq * p->S;
-    *w = shared_layout((size_t)g->B * g->Hkv * p->blocks, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
-    if (p->S == 1 || rows == 0) w->total = 0;
+    *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P,
+                   device_sm_count());
+    *w = shared_layout(0, p->ctas * sizeof(TreeMerge), p->ctas * 2 * kTreeStateBytes);
     return KL_OK;
 }
 
@@ -388,11 +387,8 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
                               int32_t num_splits) {
     Geometry g;
     TreePlan p;
-    SharedLayout w16, w32;
-    if (plan_tree_call(shape, total_q, max_q_len, num_splits, false, &g, &p, &w16) != KL_OK ||
-        plan_tree_call(shape, total_q, max_q_len, num_splits, true, &g, &p, &w32) != KL_OK)
-        return 0;
-    return w16.total > w32.total ? w16.total : w32.total;
+    SharedLayout w;
+    return plan_tree_call(shape, total_q, max_q_len, num_splits, &g, &p, &w) == KL_OK ? w.total : 0;
 }
 
 kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
@@ -404,8 +400,7 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     Geometry g;
     TreePlan p;
     SharedLayout w;
-    const kl_status st =
-        plan_tree_call(shape, total_q, max_q_len, num_splits, out_dtype == KL_FP32, &g, &p, &w);
+    const kl_status st = plan_tree_call(shape, total_q, max_q_len, num_splits, &g, &p, &w);
     if (st != KL_OK) return st;
     if (!prefill_tc_supported(g)) return KL_ERR_UNSUPPORTED;
     if (g.B == 0 || total_q == 0 || max_q_len == 0) return KL_OK;
@@ -413,8 +408,7 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
         return KL_ERR_INVALID_ARG;
     if (!aligned(q, 16) || (w_r && !aligned(w_r, 16)) || !aligned(v_cache, 16) || !aligned(out, 16))
         return KL_ERR_INVALID_ARG;
-    if (w.total > 0 && (!workspace || workspace_bytes < w.total || !aligned(workspace, 256)))
-        return KL_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < w.total || !aligned(workspace, 256)) return KL_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     TreeArgs a;
     a.geo = g;
@@ -422,9 +416,8 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     a.max_q = max_q_len;
     a.hp = p.hp;
     a.rpb = p.rpb;
-    a.blocks = p.blocks;
-    a.S = p.S;
-    a.chunk = p.chunk;
+    a.ctas = p.ctas;
+    a.num_splits = num_splits;
     a.q = static_cast<const uint16_t *>(q);
     a.w_r = static_cast<const uint16_t *>(w_r);
     a.v_cache = static_cast<const uint16_t *>(v_cache);
@@ -432,9 +425,8 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     a.seq_lens = seq_lens;
     a.cu_q = cu_q_lens;
     a.parents = parents;
-    a.part_o = w.total ? reinterpret_cast<float *>(ws + w.states) : nullptr;
-    a.part_ml = w.total ? reinterpret_cast<float *>(ws + w.extra) : nullptr;
-    a.counters = w.total ? reinterpret_cast<unsigned int *>(ws) : nullptr;
+    a.merge = reinterpret_cast<TreeMerge *>(ws + w.states);
+    a.states = reinterpret_cast<uint8_t *>(ws + w.extra);
     a.out = out;
     a.out_dtype = out_dtype;
     a.err = err;

@@ -101,13 +101,23 @@ struct PrefillArgs {
     cudaStream_t stream;
 };
 
+// A unit that lies in several runs, for the merge of its parts (written by the first run that starts inside
+// it; rows 0: none).
+struct TreeMerge {
+    int64_t unit0, total;     // its first tile among all units' tiles, and their number
+    int tiles, step;          // its tiles, and what cuts fall on multiples of
+    int runs, last;           // runs of the call, and the last that holds some of the unit
+    int row0, rows, h, hn;    // its drafts (rows of q and out) and heads
+};
+
 // Arguments of a tree-attention launch (kl_tree_attention). Sequence b's drafts are rows cu_q[b] ..
 // cu_q[b + 1] - 1 of q / out ([total_q][Hq][D]), its last n_b cached rows.
 struct TreeArgs {
     Geometry geo;             // S and chunk unused
     int total_q;              // rows of q and out
     int max_q;                // host bound on n_b
-    int hp, rpb, blocks, S, chunk;   // layout (plan_tree)
+    int hp, rpb, ctas;        // layout (plan_tree)
+    int num_splits;           // most parts of a unit; 0: no such limit
     const uint16_t *q;        // [total_q][Hq][D] bf16
     const uint16_t *w_r;      // [Hw][D][D] bf16, or nullptr: q is the composed query
     const uint16_t *v_cache;  // [num_pages][Hkv][P][D] bf16
@@ -115,14 +125,35 @@ struct TreeArgs {
     const int32_t *seq_lens;
     const int32_t *cu_q;      // [B + 1]
     const int32_t *parents;   // [total_q]
-    float *part_o;            // [total_q][Hq][S][D] states of the runs, not normalized (S > 1)
-    float *part_ml;           // [total_q][Hq][S][2] {m (base 2), l}
-    unsigned int *counters;   // [B][Hkv][blocks] arrivals of the current call (zero between calls)
+    TreeMerge *merge;         // [ctas]
+    uint8_t *states;          // [ctas][2] states of kTreeStateBytes
     void *out;                // [total_q][Hq][D]
     kl_dtype out_dtype;
     int32_t *err;
     cudaStream_t stream;
 };
+
+// A segment: the part of a unit (sequence b, its block `unit`) that lies in a run.
+struct TreeSegment {
+    int b, unit, tile0, n_tiles;
+    int q0, n, L, tiles, units;   // of the sequence: drafts, length, tiles per unit, units
+};
+
+// A unit's block: value head g, drafts m0 .. m0 + rows - 1, query heads h .. h + hn - 1.
+struct TreeBlock {
+    int g, m0, rows, h, hn;
+};
+__device__ __forceinline__ TreeBlock tree_block(const TreeArgs &a, const TreeSegment &s) {
+    const int nhg = (a.geo.G + a.hp - 1) / a.hp, nm = (s.n + a.rpb - 1) / a.rpb;
+    const int hg = s.unit % nhg, rest = s.unit / nhg;
+    TreeBlock k;
+    k.g = rest / nm;
+    k.m0 = rest % nm * a.rpb;
+    k.rows = min(a.rpb, s.n - k.m0);
+    k.h = k.g * a.geo.G + hg * a.hp;
+    k.hn = min(a.hp, a.geo.G - hg * a.hp);
+    return k;
+}
 
 // Arguments of a kl_token_logprobs launch.
 struct LogprobArgs {

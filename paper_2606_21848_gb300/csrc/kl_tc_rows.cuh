@@ -50,6 +50,25 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t &hi, uint32_
     lo = *reinterpret_cast<const uint32_t *>(&l);
 }
 
+// The leading bf16 term of two fp32 values, packed; the values become what is left.
+__device__ __forceinline__ uint32_t take_term(uint32_t &x0, uint32_t &x1) {
+    const float a = __uint_as_float(x0), b = __uint_as_float(x1);
+    const uint32_t t = pack2(a, b);
+    x0 = __float_as_uint(a - bf16lo(t));
+    x1 = __float_as_uint(b - bf16hi(t));
+    return t;
+}
+
+// Whether one of two packed bf16 values is infinite or NaN.
+__device__ __forceinline__ bool not_finite(uint32_t v) {
+    return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+}
+
+// Whether one of two packed bf16 values has no finite fp16 form (a magnitude of 65536 or more).
+__device__ __forceinline__ bool past_fp16(uint32_t v) {
+    return (v & 0x7fffu) >= 0x4780u || (v & 0x7fff0000u) >= 0x47800000u;
+}
+
 // Instruction descriptor of kind::f16 with fp16 A and B (A and B formats 0), fp32 accumulator,
 // operand majorness (0 = K-major, 1 = MN-major), N and M.
 __host__ __device__ constexpr uint32_t idesc_f16(uint32_t M, uint32_t N, bool a_mn, bool b_mn) {

@@ -7,21 +7,27 @@
 //   s_t = scale <q_r, v_t>,  out = sum_t softmax(s)_t v_t   over the tokens that the draft sees.
 // n = 1 is the decode step, a chain of drafts the causal chunk.
 //
-// The G heads of a value head's group times the n drafts read the same cache rows. A block holds up to
-// 128 of these (draft, head) rows; a block's cache tiles are cut over S CTAs, whose states are merged by
-// the CTA that finishes last. One CTA per SM:
+// The G heads of a value head's group times the n drafts read the same cache rows: a unit is a block of up
+// to 128 of these (draft, head) rows with the sequence's cache tiles. One CTA per SM; all units' tiles
+// are laid end to end and cut into equal runs, one per CTA, so that batches of any lengths fill the GPU
+// evenly. A unit that lies in several runs leaves a state (m, l, O) per part, which a second kernel
+// merges. For each segment (a unit's tiles within a run):
 //
 //   routing  Q_r = Q . W^R                             M = 128 rows, N = 128, K = 128
-//   scores   S   = Q_hi . V_t^T + Q_lo . V_t^T         M = 128 rows, N = 64 tokens, K = 2 x 128
-//   output   O  += P_hi . V_t + P_lo . V_t             M = 128 rows, N = 128 dims, K = 2 x 64
+//   scores   S   = sum_i Q_i . V_t^T                   M = 128 rows, N = 64 tokens, K = 128 per term
+//   output   O  += sum_i P_i . V_t                     M = 128 rows, N = 128 dims, K = 64 per term
 //
 // Each cached tile V_t [128 tokens x 128 dims] arrives once by TMA (one box per page and 64 dims) and
 // feeds both products from the same shared-memory copy, as the K-major B operand of the scores and the
-// MN-major one of the output. Q and P are A operands in tensor memory (512 columns: 4 x 64 of scores,
-// then weights; O 128; Q_hi | Q_lo 64 + 64). Both are pairs of bf16 operands, x = hi + lo (about 16
-// significant bits), so that fp32 outputs are good to about 3e-6 of their size.
+// MN-major one of the output. Q and P are A operands in tensor memory.
 //
-// The unit of the pipeline is a half tile of 64 tokens, four in flight, as in the prefill: thread = row
+// Precision. bf16 outputs (Half): the routed query is a pair of bf16 operands (16 significant bits), the
+// weights one fp16 operand (11 bits) against the tile converted to fp16 in place, as in the prefill:
+// three MMAs per tile; cached values of magnitude 65536 or more have no fp16 form (KL_FLAG_RANGE).
+// fp32 outputs (Full): query and weights are sums of three bf16 terms (24 bits), and since the tensor
+// core's adds truncate, O moves every 256 tokens to a sum that the softmax warps keep in shared memory.
+//
+// The unit of the pipeline is a half tile of 64 tokens, kSub in flight, as in the prefill: thread = row
 // = TMEM lane; two groups of four softmax warps take alternate half tiles and share each row's
 // reference maximum, which moves only when a half tile's maximum passes it by more than 2^7.
 //
@@ -40,45 +46,73 @@ namespace kl {
 namespace {
 
 constexpr int kD = 128;
-constexpr int kBM = kTreeRows;                    // rows per CTA
+constexpr int kBM = kTreeRows;                    // rows per block
 constexpr int kBN = kTreeTile;                    // cache rows per tile
 constexpr int kBS = 64;                           // cache rows per half tile
-constexpr int kSub = 4;                           // half tiles in flight
-constexpr int kStages = 5;
 constexpr int kComputeWarps = 8;                  // two per TMEM lane quarter
 constexpr int kProducerWarp = 8, kMmaWarp = 9, kPvWarp = 10;
 constexpr int kThreads = 11 * 32;
 constexpr uint32_t kTileBytes = kBN * kD * 2;     // 32 KiB
 constexpr uint32_t kHalfBytes = kTileBytes / 2;   // one 64-dim half: 128 rows x 128 B
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColS = 0;                     // S of half tile u: 64 (u % 4) .. + 63, then its P
-                                                  // (hi in the first 32, lo in the others); the
-                                                  // routed queries first land in 0 .. 255
-constexpr uint32_t kColO = 256;                   // O: columns 256 .. 383
-constexpr uint32_t kColQ = 384;                   // Q_hi: 384 .. 447, Q_lo: 448 .. 511
-constexpr uint32_t kLoCols = 64;                  // hi -> lo of the packed query
 constexpr float kRescaleLog2 = 7.f;
 constexpr uint64_t kTimeoutNs = kRowsTimeoutNs;
 constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 is __syncthreads)
 
+// Operand forms and the layout that they leave room for. Tensor memory: kSub buffers of kBuf columns (64
+// of scores, then the weights, 32 per term), O (128), the query's terms (64 each); the routed queries
+// first land in columns 0 .. 255, before anything else is there.
+struct Half {
+    static constexpr bool kFp16P = true, kFold = false;
+    static constexpr int kQTerms = 2, kPTerms = 1, kSub = 4, kStages = 5;
+    static constexpr uint32_t kBuf = 64, kColO = 256, kColQ = 384;
+};
+struct Full {
+    static constexpr bool kFp16P = false, kFold = true;
+    static constexpr int kQTerms = 3, kPTerms = 3, kSub = 2, kStages = 3;
+    static constexpr uint32_t kBuf = 96, kColO = 192, kColQ = 320;
+};
+constexpr int kFoldSub = 4;           // half tiles between two moves of O to the fp32 sum (Full)
+
+template <typename C>
 struct __align__(1024) TreeSmem {
     uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B]
     // Ring: the W^R matrices, then the cache tiles ([64-dim half][128 rows][128 B], SW128).
-    uint8_t tiles[kStages][kTileBytes];
-    uint64_t full[kStages], empty[kStages];
-    uint64_t s_full[kSub], s_free[kSub], p_full[kSub];
-    uint64_t turn[4][2];       // per lane quarter and parity: the references after a half tile
-    uint64_t first[4];         // per lane quarter: the maxima of half tile 1 are in lsum[1]
-    uint64_t r_full[2], r_free[2];   // routing results, alternating halves of the score columns
-    uint64_t qr_ready, drain, drain2;
+    uint8_t tiles[C::kStages][kTileBytes];
+    float sum[C::kFold ? kBM * kD : 4];    // Full: O of the half tiles folded so far, [row][128], its
+                                           // 16-byte chunks c at c ^ (row % 32)
+    // Barriers (set up anew for every segment): one completion per half tile u of its buffer u % kSub
+    // on s_full (its scores), p_full (its weights) and s_free (its output MMAs are done), and per
+    // lane quarter on turn[.][u % 2] (the references after it).
+    struct Bars {
+        uint64_t full[C::kStages], empty[C::kStages];
+        uint64_t s_full[C::kSub], s_free[C::kSub], p_full[C::kSub];
+        uint64_t turn[4][2];
+        uint64_t first[4];                 // per lane quarter: the maxima of half tile 1 are in lsum[1]
+        uint64_t r_full[2], r_free[2];     // routing results, alternating halves of columns 0 .. 255
+        uint64_t qr_ready, drain, drain2;
+    } bar;
     float mref[2][kBM];        // the rows' references after the last half tile of each parity
     float lsum[2][kBM];        // the two groups' shares of the row sums, for the epilogue
+    float fref[kBM];           // Full: the references of `sum`
     int32_t parent[KL_TREE_MAX_DRAFTS];
+    unsigned int over[KL_TREE_MAX_DRAFTS / 32];   // Half: drafts with a finite value beyond fp16's range
+    TreeSegment seg[2];        // this segment and the next
+    int64_t warp_sum[kThreads / 32];
+    int64_t x0, x1;            // this CTA's run
     uint32_t tmem_base;
-    int is_last;
     int abort;
 };
-static_assert(sizeof(TreeSmem) + 1024 <= 227 * 1024, "one CTA per SM");
+static_assert(sizeof(TreeSmem<Half>) + 1024 <= 227 * 1024 && sizeof(TreeSmem<Full>) + 1024 <= 227 * 1024, "");
+
+// Arrivals that complete a phase of barrier i (in the order of Bars).
+template <typename C>
+__device__ __forceinline__ uint32_t bar_count(int i) {
+    using B = typename TreeSmem<C>::Bars;
+    if (i >= (int)(offsetof(B, p_full) / 8) && i < (int)(offsetof(B, turn) / 8)) return kComputeWarps / 2;
+    if (i >= (int)(offsetof(B, r_free) / 8) && i <= (int)(offsetof(B, qr_ready) / 8)) return kComputeWarps;
+    return 1;
+}
 
 // The 64 bits off .. off + 63 of the 128-bit set (lo, hi), off in -63 .. 127; bits below 0 are ones.
 __device__ __forceinline__ uint64_t window64(uint64_t lo, uint64_t hi, int off) {
@@ -87,397 +121,543 @@ __device__ __forceinline__ uint64_t window64(uint64_t lo, uint64_t hi, int off) 
     return off < 64 ? (lo >> off) | (hi << (64 - off)) : hi >> (off - 64);
 }
 
+// ---------------------------------------------------------------------- runs and segments ----
+
+// Sequence b as the units see it: its drafts, length, tiles per unit and units (0 where it has none).
+struct TreeSeq {
+    int q0, n, L, tiles, units;
+};
+__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int b, bool report) {
+    TreeSeq s;
+    s.q0 = a.cu_q[b];
+    const int q1 = a.cu_q[b + 1];
+    s.L = a.seq_lens[b];
+    s.n = q1 - s.q0;
+    s.tiles = s.units = 0;
+    if (s.q0 < 0 || s.n < 0 || q1 > a.total_q || s.n > a.max_q || s.L < s.n ||
+        s.L > a.geo.max_pages * a.geo.P) {
+        if (report) raise_flag(a.err, KL_FLAG_BAD_LENGTH);
+    } else if (s.n > 0) {
+        s.tiles = (s.L + kBN - 1) / kBN;
+        s.units = a.geo.Hkv * ((a.geo.G + a.hp - 1) / a.hp) * ((s.n + a.rpb - 1) / a.rpb);
+    }
+    return s;
+}
+
+// Cuts inside a unit of `tiles` tiles fall on multiples of this.
+__device__ __forceinline__ int cut_step(const TreeArgs &a, int tiles) {
+    return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : kTreeCut;
+}
+
+// The start of run c of `runs` when `total` tiles are shared out, before it moves down to a cut.
+__device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { return total * c / runs; }
+
+// Finds this CTA's run: sm.x0, sm.x1 and the first segment; writes the CTA's entry for the merge. All
+// threads; ends behind a barrier. False if there is nothing to do.
+template <typename C>
+__device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = blockIdx.x;
+    const int B = a.geo.B, per = (B + kThreads - 1) / kThreads;
+    int64_t mine = 0;
+    for (int b = tid * per; b < min(B, (tid + 1) * per); ++b) {
+        const TreeSeq s = tree_seq(a, b, c == 0);
+        mine += (int64_t)s.tiles * s.units;
+    }
+    int64_t upto = mine;                             // inclusive prefix
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    if (lane == 31) sm.warp_sum[warp] = upto;
+    if (tid == 0) {
+        sm.seg[0].n_tiles = 0;
+        a.merge[c].rows = 0;
+    }
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) upto += sm.warp_sum[w];
+        total += sm.warp_sum[w];
+    }
+    const int64_t most = total / kTreeCut;
+    const int runs = (int)(most < 1 ? 1 : most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x);
+    if (total == 0 || c >= runs) return false;
+    // the threads whose sequences hold the run's two ends move them down to a cut
+    for (int end = 0; end < 2; ++end) {
+        int64_t x = run_start(total, c + end, runs);
+        if (x == total) {
+            if (tid == 0) sm.x1 = total;
+            continue;
+        }
+        if (x < upto - mine || x >= upto) continue;
+        int64_t start = upto - mine;
+        for (int b = tid * per; b < min(B, (tid + 1) * per); ++b) {
+            const TreeSeq s = tree_seq(a, b, false);
+            const int64_t all = (int64_t)s.tiles * s.units;
+            if (x < start + all) {
+                const int unit = (int)((x - start) / s.tiles);
+                const int64_t unit0 = start + (int64_t)unit * s.tiles;
+                const int step = cut_step(a, s.tiles), tile0 = (int)(x - unit0) / step * step;
+                if (end == 1) {
+                    sm.x1 = unit0 + tile0;
+                } else {
+                    sm.x0 = unit0 + tile0;
+                    sm.seg[0] = TreeSegment{b, unit, tile0, s.tiles - tile0, s.q0, s.n, s.L, s.tiles, s.units};
+                    // the first run that starts inside the unit announces its parts
+                    if (tile0 > 0 && run_start(total, c - 1, runs) < unit0 + step) {
+                        const TreeBlock k = tree_block(a, sm.seg[0]);
+                        a.merge[c] = TreeMerge{unit0, total, s.tiles, step, runs,
+                                               (int)(((unit0 + s.tiles) * runs - 1) / total), s.q0 + k.m0, k.rows,
+                                               k.h, k.hn};
+                    }
+                }
+                break;
+            }
+            start += all;
+        }
+    }
+    __syncthreads();
+    const int64_t left = sm.x1 - sm.x0;
+    if (left <= 0) return false;
+    return true;
+}
+
+// The segment after `s` (which ends at x of the run): the next unit's start, or none (n_tiles 0).
+__device__ __forceinline__ TreeSegment next_segment(const TreeArgs &a, const TreeSegment &s, int64_t left) {
+    TreeSegment t = s;
+    t.tile0 = 0;
+    if (left <= 0) {
+        t.n_tiles = 0;
+        return t;
+    }
+    if (++t.unit == s.units) {
+        t.unit = 0;
+        TreeSeq q;
+        do {
+            ++t.b;
+            q = tree_seq(a, t.b, false);
+        } while (q.units == 0);                      // (tiles are left, so a sequence follows)
+        t.q0 = q.q0;
+        t.n = q.n;
+        t.L = q.L;
+        t.tiles = q.tiles;
+        t.units = q.units;
+    }
+    t.n_tiles = (int)(left < t.tiles ? left : t.tiles);
+    return t;
+}
+
+// ------------------------------------------------------------------------------- kernel ----
+template <typename C>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_tc_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap wmap,
                    const __grid_constant__ CUtensorMap qmap, const TreeArgs a) {
+    constexpr int kSub = C::kSub, kStages = C::kStages;
+    constexpr uint32_t kColO = C::kColO, kColQ = C::kColQ;
+    using Smem = TreeSmem<C>;
     extern __shared__ uint8_t smem_raw[];
-    TreeSmem &sm = *reinterpret_cast<TreeSmem *>(
-        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const Geometry &geo = a.geo;
-    const int blk = blockIdx.x % a.blocks, split = blockIdx.x / a.blocks;
-    const int g = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int hp = a.hp, rpb = a.rpb;
 
     grid_dep_wait();
-    const int q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
-    const int L = a.seq_lens[b];
-    const int n = q1 - q0;
-    if (q0 < 0 || n < 0 || q1 > a.total_q || n > a.max_q || L < n || L > geo.max_pages * geo.P) {
-        if (tid == 0 && blockIdx.x == 0 && g == 0) raise_flag(a.err, KL_FLAG_BAD_LENGTH);
-        return;
-    }
-    // The block: drafts m0 .. m0 + rows - 1, heads h .. h + hn - 1 of the group; row r of the 128 is
-    // draft m0 + r / hp with head h + r % hp.
-    const int hp = a.hp, rpb = a.rpb;
-    const int nhg = (geo.G + hp - 1) / hp;       // blocks of heads
-    const int m0 = (blk / nhg) * rpb;
-    if (m0 >= n) return;
-    const int rows = min(rpb, n - m0);
-    const int h = g * geo.G + (blk % nhg) * hp;
-    const int hn = min(hp, (g + 1) * geo.G - h);
-    // This CTA's cache tiles: tile0 .. tile0 + n_tiles - 1, as half tiles 0 .. n_sub - 1 from there.
-    const int base = L - n;                      // committed tokens
-    const int seen = base + m0 + rows;           // no row sees a token from here on
-    const int share = a.chunk / kBN;
-    const int all_tiles = (seen + kBN - 1) / kBN;
-    const int runs = (all_tiles + share - 1) / share;
-    if (split >= runs) return;
-    const int tile0 = split * share;
-    const int n_tiles = min(share, all_tiles - tile0);
-    const int n_sub = min(2 * n_tiles, (seen + kBS - 1) / kBS - 2 * tile0);
-    const bool has_drafts = (tile0 + n_tiles) * kBN > base;
-    // ring positions of W^R matrices: one, one per head of the block, or none (composed query)
-    const int ro = a.w_r ? (geo.wr_per_qh ? hn : 1) : 0;
-
-    if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            ptx::mbar_init(&sm.full[s], 1);
-            ptx::mbar_init(&sm.empty[s], 1);
-        }
-        // One completion per half tile u of its buffer u % kSub on s_full (its scores), p_full (its
-        // weights) and s_free (its output MMAs are done), and per lane quarter on turn[.][u % 2].
-        for (int i = 0; i < kSub; ++i) {
-            ptx::mbar_init(&sm.s_full[i], 1);
-            ptx::mbar_init(&sm.s_free[i], 1);
-            ptx::mbar_init(&sm.p_full[i], kComputeWarps / 2);
-        }
-        for (int q = 0; q < 4; ++q) {
-            for (int i = 0; i < 2; ++i) ptx::mbar_init(&sm.turn[q][i], 1);
-            ptx::mbar_init(&sm.first[q], 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            ptx::mbar_init(&sm.r_full[i], 1);
-            ptx::mbar_init(&sm.r_free[i], kComputeWarps);
-        }
-        ptx::mbar_init(&sm.qr_ready, kComputeWarps);
-        ptx::mbar_init(&sm.drain, 1);
-        ptx::mbar_init(&sm.drain2, 1);
-        sm.abort = 0;
-        ptx::fence_mbar_init();
-    }
+    const bool any = find_run(sm, a);
+    if (!any) return;
+    if (tid == 0) sm.abort = 0;
     if (warp == kMmaWarp) {
         ptx::tmem_alloc(&sm.tmem_base, kTmemCols);
         ptx::tmem_relinquish();
     }
-    // (a parent that is not an earlier draft or -1 counts as -1)
-    if (has_drafts && tid < n) {
-        const int p = a.parents[q0 + tid];
-        const bool fine = p >= -1 && p < tid;
-        if (!fine) raise_flag(a.err, KL_FLAG_BAD_TREE);
-        sm.parent[tid] = fine ? p : -1;
+    if (warp == kProducerWarp && lane == 0) {
+        ptx::prefetch_tensormap(&vmap);
+        if (a.w_r) {
+            ptx::prefetch_tensormap(&wmap);
+            ptx::prefetch_tensormap(&qmap);
+        }
     }
     // rows of the query block that its box does not fill
-    if (ro > 0) {
+    if (a.w_r) {
         for (int i = tid; i < (kBM - hp * rpb) * 16; i += kThreads)
             *reinterpret_cast<uint4 *>(sm.q + (i & 8 ? kHalfBytes : 0) + (hp * rpb + (i >> 4)) * 128 +
                                        (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
         ptx::fence_proxy_async_smem();
     }
-    if (warp == kProducerWarp && lane == 0) {
-        ptx::prefetch_tensormap(&vmap);
-        if (ro > 0) {
-            ptx::prefetch_tensormap(&wmap);
-            ptx::prefetch_tensormap(&qmap);
-        }
-    }
-    ptx::tc_fence_before();
-    __syncthreads();
-    ptx::tc_fence_after();
-    grid_dep_launch();
-
-    const uint32_t tmem = sm.tmem_base;
+    const int64_t x1 = sm.x1;
+    int64_t x = sm.x0;
     const Waiter wait{&sm.abort, a.err};
+    uint32_t tmem = 0;
 
-    if (warp == kProducerWarp) {
-        // ------------------------------------------------------------------ producer ----
-        const int P = geo.P;
-        const int ppt = kBN / P;                          // pages per tile (<= 8)
-        const int seq_pages = (L + P - 1) / P;
-        const uint32_t page_bytes = (uint32_t)P * 128u;   // one half of one page
-        const int32_t *bt = a.block_table + (size_t)b * geo.max_pages;
-        int issued = 0;
-        bool bad = false, ok = true;
-        // W^R matrices (B operand of the routing MMAs); the first brings the query block along
-        for (int r = 0; r < ro; ++r) {
-            const int s = r % kStages;
-            if (r >= kStages && !(ok = wait(&sm.empty[s], ((r / kStages) & 1) ^ 1))) break;
-            if (lane == 0) {
-                const int wrow = (geo.wr_per_qh ? h + r : g) * kD;
-                ptx::mbar_arrive_expect_tx(&sm.full[s], kTileBytes + (r == 0 ? hp * rpb * kD * 2 : 0));
-                ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.full[s], 0, wrow);
-                ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.full[s], 64, wrow);
-                if (r == 0) {
-                    ptx::tma_load_3d(sm.q, &qmap, &sm.full[s], 0, h, q0 + m0);
-                    ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.full[s], 64, h, q0 + m0);
+    for (int si = 0;; ++si) {
+        TreeSegment sg = sm.seg[si & 1];
+        if (sg.n_tiles > x1 - x) sg.n_tiles = (int)(x1 - x);
+        // The block: drafts m0 .. m0 + rows - 1, heads h .. h + hn - 1 of the group; row r of the 128 is
+        // draft m0 + r / hp with head h + r % hp.
+        const TreeBlock blk = tree_block(a, sg);
+        const int m0 = blk.m0, rows = blk.rows, h = blk.h, hn = blk.hn, g = blk.g;
+        const int q0 = sg.q0, n = sg.n, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int base = L - n;                      // committed tokens
+        const int n_sub = min(2 * n_tiles, (L + kBS - 1) / kBS - 2 * tile0);   // half tiles
+        const bool has_drafts = (tile0 + n_tiles) * kBN > base;
+        const bool whole = n_tiles == sg.tiles;
+        // ring positions of W^R matrices: one, one per head of the block, or none (composed query)
+        const int ro = a.w_r ? (geo.wr_per_qh ? hn : 1) : 0;
+
+        uint64_t *const bars = reinterpret_cast<uint64_t *>(&sm.bar);
+        if (tid < (int)(sizeof(sm.bar) / 8)) {
+            if (si > 0) ptx::mbar_inval(bars + tid);
+            ptx::mbar_init(bars + tid, bar_count<C>(tid));
+            ptx::fence_mbar_init();
+        }
+        if (tid < KL_TREE_MAX_DRAFTS / 32) sm.over[tid] = 0;
+        // (a parent that is not an earlier draft or -1 counts as -1)
+        if (has_drafts && tid < n) {
+            const int p = a.parents[q0 + tid];
+            const bool fine = p >= -1 && p < tid;
+            if (!fine) raise_flag(a.err, KL_FLAG_BAD_TREE);
+            sm.parent[tid] = fine ? p : -1;
+        }
+        ptx::tc_fence_before();
+        __syncthreads();
+        ptx::tc_fence_after();
+        if (si == 0) {
+            grid_dep_launch();
+            tmem = sm.tmem_base;
+        }
+
+        if (warp == kProducerWarp) {
+            // -------------------------------------------------------------- producer ----
+            const int P = geo.P;
+            const int ppt = kBN / P;                          // pages per tile (<= 8)
+            const int seq_pages = (L + P - 1) / P;
+            const uint32_t page_bytes = (uint32_t)P * 128u;   // one half of one page
+            const int32_t *bt = a.block_table + (size_t)sg.b * geo.max_pages;
+            int issued = 0;
+            bool bad = false, ok = true;
+            // W^R matrices (B operand of the routing MMAs); the first brings the query block along
+            for (int r = 0; r < ro; ++r) {
+                const int s = r % kStages;
+                if (r >= kStages && !(ok = wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1))) break;
+                if (lane == 0) {
+                    const int wrow = (geo.wr_per_qh ? h + r : g) * kD;
+                    ptx::mbar_arrive_expect_tx(&sm.bar.full[s], kTileBytes + (r == 0 ? hp * rpb * kD * 2 : 0));
+                    ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.bar.full[s], 0, wrow);
+                    ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.bar.full[s], 64, wrow);
+                    if (r == 0) {
+                        ptx::tma_load_3d(sm.q, &qmap, &sm.bar.full[s], 0, h, q0 + m0);
+                        ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.bar.full[s], 64, h, q0 + m0);
+                    }
+                }
+                __syncwarp();
+                issued = r + 1;
+            }
+            for (int i = 0; ok && i < n_tiles; ++i) {
+                const int r = i + ro, s = r % kStages;
+                const int pg = (tile0 + i) * ppt + lane;      // page index within the sequence
+                const bool exists = lane < ppt && pg < seq_pages;
+                const int page = exists ? bt[pg] : -1;
+                if (r >= kStages && !wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1)) break;
+                const bool in_range = exists && page >= 0 && page < geo.num_pages;
+                if (exists && !in_range) bad = true;
+                const unsigned mask = __ballot_sync(0xffffffffu, in_range);
+                ptx::for_pages(
+                    (page * geo.Hkv + g) * P, mask,
+                    [&] { ptx::mbar_arrive_expect_tx(&sm.bar.full[s], __popc(mask) * page_bytes * 2u); },
+                    [&](int p, int row) {
+                        uint8_t *dst = sm.tiles[s] + p * page_bytes;
+                        ptx::tma_load_2d(dst, &vmap, &sm.bar.full[s], 0, row);
+                        ptx::tma_load_2d(dst + kHalfBytes, &vmap, &sm.bar.full[s], 64, row);
+                    });
+                issued = r + 1;
+            }
+            // the last commit of every slot lands before the barriers are set up anew
+            for (int i = max(0, ro + n_tiles - kStages); ok && i < ro + n_tiles; ++i)
+                ok = wait(&sm.bar.empty[i % kStages], (i / kStages) & 1);
+            if (__any_sync(0xffffffffu, bad) && lane == 0) raise_flag(a.err, KL_FLAG_BAD_PAGE);
+            if (sm.abort) {
+                // copies still in flight land before the CTA's shared memory goes away
+                for (int i = max(0, issued - kStages); i < issued; ++i) {
+                    const uint64_t t0 = ptx::globaltimer();
+                    while (!ptx::mbar_try_wait(&sm.bar.full[i % kStages], (i / kStages) & 1) &&
+                           ptx::globaltimer() - t0 < kTimeoutNs) {
+                    }
+                }
+            }
+        } else if (warp == kMmaWarp || warp == kPvWarp) {
+            // ------------------------------------------------------------ MMA issuers ----
+            // K-major SW128 operands step 32 B per 16 columns inside a 64-column half and jump a
+            // half (kHalfBytes) every 4 steps; MN-major SW128 operands step 16 rows = 2 KiB; TMEM
+            // A operands step 8 columns (16 packed 16-bit values).
+            constexpr uint32_t idesc_qk = ptx::idesc_bf16(128, kBS, false, false);
+            constexpr uint32_t idesc_route = ptx::idesc_bf16(128, 128, false, true);
+            constexpr uint32_t idesc_pv = C::kFp16P ? idesc_f16(128, 128, false, true) : idesc_route;
+            const uint64_t q_desc = ptx::smem_desc(ptx::smem_addr(sm.q), 16, 1024, ptx::kSwizzle128B);
+            const uint64_t k_desc = ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), 16, 1024, ptx::kSwizzle128B);
+            const uint64_t mn_desc =
+                ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), kHalfBytes, 1024, ptx::kSwizzle128B);
+            auto kstep = [](int kk) -> uint32_t { return ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4; };
+            if (warp == kMmaWarp) {
+                // Q_r = Q . W^R for all 128 rows, once per matrix, into alternating halves of columns
+                // 0 .. 255 (a row keeps the result of its head's matrix), then the scores
+                bool ok = true;
+                for (int r = 0; ok && r < ro; ++r) {
+                    const int s = r % kStages;
+                    ok = wait(&sm.bar.full[s], (r / kStages) & 1) &&
+                         (r < 2 || wait(&sm.bar.r_free[r & 1], ((r >> 1) - 1) & 1));
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    if (ptx::elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < kD / 16; ++kk)
+                            ptx::mma_bf16(tmem + (r & 1) * 128, q_desc + kstep(kk),
+                                          mn_desc + ((s * kTileBytes + kk * 2048) >> 4), idesc_route, kk > 0);
+                        ptx::mma_commit(&sm.bar.empty[s]);
+                        ptx::mma_commit(&sm.bar.r_full[r & 1]);
+                    }
+                    __syncwarp();
+                }
+                ok = ok && wait(&sm.bar.qr_ready, 0);
+                // (the loop by one lane: warp-wide waits between two half tiles leave the tensor cores idle)
+                if (ok && ptx::elect_one()) {
+                    ptx::tc_fence_after();
+                    for (int u = 0; u < n_sub; ++u) {
+                        const int r = (u >> 1) + ro, s = r % kStages, sb = u % kSub;
+                        if (!wait.one(&sm.bar.full[s], (r / kStages) & 1)) break;
+                        if (u >= kSub && !wait.one(&sm.bar.s_free[sb], (u / kSub - 1) & 1)) break;
+                        ptx::tc_fence_after();
+                        const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+#pragma unroll
+                        for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
+                            ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
+                                             idesc_qk, kk > 0);
+                        ptx::mma_commit(&sm.bar.s_full[sb]);
+                    }
+                }
+            } else if (ptx::elect_one()) {
+                // O += P . V; at a fold O starts over (its old value has been read by then)
+                for (int u = 0; u < n_sub; ++u) {
+                    const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
+                    if (!wait.one(&sm.bar.p_full[sb], (u / kSub) & 1)) break;
+                    ptx::tc_fence_after();
+                    const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+                    const bool more = C::kFold ? u % kFoldSub != 0 : u > 0;
+#pragma unroll
+                    for (int kk = 0; kk < C::kPTerms * kBS / 16; ++kk)
+                        ptx::mma_bf16_ts(tmem + kColO, tmem + sb * C::kBuf + kk * 8,
+                                         b0 + (((kk & 3) * 2048) >> 4), idesc_pv, (more || kk > 0) ? 1u : 0u);
+                    ptx::mma_commit(&sm.bar.s_free[sb]);
+                    if ((u & 1) || u == n_sub - 1) ptx::mma_commit(&sm.bar.empty[s]);
                 }
             }
             __syncwarp();
-            issued = r + 1;
-        }
-        for (int i = 0; ok && i < n_tiles; ++i) {
-            const int r = i + ro, s = r % kStages;
-            const int pg = (tile0 + i) * ppt + lane;      // page index within the sequence
-            const bool exists = lane < ppt && pg < seq_pages;
-            const int page = exists ? bt[pg] : -1;
-            if (r >= kStages && !wait(&sm.empty[s], ((r / kStages) & 1) ^ 1)) break;
-            const bool in_range = exists && page >= 0 && page < geo.num_pages;
-            if (exists && !in_range) bad = true;
-            const unsigned mask = __ballot_sync(0xffffffffu, in_range);
-            ptx::for_pages(
-                (page * geo.Hkv + g) * P, mask,
-                [&] { ptx::mbar_arrive_expect_tx(&sm.full[s], __popc(mask) * page_bytes * 2u); },
-                [&](int p, int row) {
-                    uint8_t *dst = sm.tiles[s] + p * page_bytes;
-                    ptx::tma_load_2d(dst, &vmap, &sm.full[s], 0, row);
-                    ptx::tma_load_2d(dst + kHalfBytes, &vmap, &sm.full[s], 64, row);
-                });
-            issued = r + 1;
-        }
-        if (__any_sync(0xffffffffu, bad) && lane == 0) raise_flag(a.err, KL_FLAG_BAD_PAGE);
-        if (sm.abort) {
-            // copies still in flight land before the CTA's shared memory goes away
-            for (int i = max(0, issued - kStages); i < issued; ++i) {
-                const uint64_t t0 = ptx::globaltimer();
-                while (!ptx::mbar_try_wait(&sm.full[i % kStages], (i / kStages) & 1) &&
-                       ptx::globaltimer() - t0 < kTimeoutNs) {
-                }
+            // every MMA this warp issued completes before the segment ends
+            uint64_t *drain = warp == kMmaWarp ? &sm.bar.drain : &sm.bar.drain2;
+            if (ptx::elect_one()) ptx::mma_commit(drain);
+            __syncwarp();
+            const uint64_t t0 = ptx::globaltimer();
+            while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer() - t0 < kTimeoutNs) {
             }
-        }
-    } else if (warp == kMmaWarp || warp == kPvWarp) {
-        // ---------------------------------------------------------------- MMA issuers ----
-        // K-major SW128 operands step 32 B per 16 columns inside a 64-column half and jump a
-        // half (kHalfBytes) every 4 steps; MN-major SW128 operands step 16 rows = 2 KiB; TMEM
-        // A operands step 8 columns (16 packed 16-bit values).
-        constexpr uint32_t idesc_qk = ptx::idesc_bf16(128, kBS, false, false);
-        constexpr uint32_t idesc_mn = ptx::idesc_bf16(128, 128, false, true);   // routing and output
-        const uint64_t q_desc = ptx::smem_desc(ptx::smem_addr(sm.q), 16, 1024, ptx::kSwizzle128B);
-        const uint64_t k_desc = ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), 16, 1024, ptx::kSwizzle128B);
-        const uint64_t mn_desc =
-            ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), kHalfBytes, 1024, ptx::kSwizzle128B);
-        auto kstep = [](int kk) -> uint32_t { return ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4; };
-        if (warp == kMmaWarp) {
-            // Q_r = Q . W^R for all 128 rows, once per matrix, into alternating halves of the score
-            // columns (a row keeps the result of its head's matrix), then the scores
+        } else {
+            // ----------------------------------------------------- softmax, epilogue ----
+            if (tid == 0) sm.seg[(si + 1) & 1] = next_segment(a, sg, x1 - x - n_tiles);
+            const int qd = warp & 3, hf = warp >> 2;     // lane quarter; group, and half of the columns
+            const int r = qd * 32 + lane;                // row = TMEM lane
+            const int ri = r / hp, hh = r - ri * hp;     // draft and head within the block
+            const bool live = ri < rows && hh < hn;
+            const int c0 = hf * 64;
+            const uint32_t lane_base = (uint32_t)(qd * 32) << 16;
+            const float sl2 = geo.scale * kLog2e;
+            const size_t row_id = (size_t)(q0 + m0 + ri) * geo.Hq + h + hh;   // of q and out
             bool ok = true;
-            for (int r = 0; ok && r < ro; ++r) {
-                const int s = r % kStages;
-                ok = wait(&sm.full[s], (r / kStages) & 1) &&
-                     (r < 2 || wait(&sm.r_free[r & 1], ((r >> 1) - 1) & 1));
-                if (!ok) break;
-                ptx::tc_fence_after();
-                if (ptx::elect_one()) {
-#pragma unroll
-                    for (int kk = 0; kk < kD / 16; ++kk)
-                        ptx::mma_bf16(tmem + kColS + (r & 1) * 128, q_desc + kstep(kk),
-                                      mn_desc + ((s * kTileBytes + kk * 2048) >> 4), idesc_mn, kk > 0);
-                    ptx::mma_commit(&sm.empty[s]);
-                    ptx::mma_commit(&sm.r_full[r & 1]);
-                }
-                __syncwarp();
-            }
-            ok = ok && wait(&sm.qr_ready, 0);
-            // (the loop by one lane: warp-wide waits between two half tiles leave the tensor cores idle)
-            if (ok && ptx::elect_one()) {
-                ptx::tc_fence_after();
-                for (int u = 0; u < n_sub; ++u) {
-                    const int r = (u >> 1) + ro, s = r % kStages, sb = u % kSub;
-                    if (!wait.one(&sm.full[s], (r / kStages) & 1)) break;
-                    if (u >= kSub && !wait.one(&sm.s_free[sb], (u / kSub - 1) & 1)) break;
-                    ptx::tc_fence_after();
-                    const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
-#pragma unroll
-                    for (int kk = 0; kk < 2 * kD / 16; ++kk)
-                        ptx::mma_bf16_ts(tmem + kColS + sb * kBS,
-                                         tmem + kColQ + (kk >= 8 ? kLoCols : 0u) + (kk & 7) * 8,
-                                         b0 + kstep(kk & 7), idesc_qk, kk > 0);
-                    ptx::mma_commit(&sm.s_full[sb]);
-                }
-            }
-        } else if (ptx::elect_one()) {
-            for (int u = 0; u < n_sub; ++u) {
-                const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
-                if (!wait.one(&sm.p_full[sb], (u / kSub) & 1)) break;
-                ptx::tc_fence_after();
-                const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
-                const uint32_t pa = tmem + kColS + sb * kBS;      // P_hi, then P_lo: 8 columns a step
-#pragma unroll
-                for (int kk = 0; kk < 2 * kBS / 16; ++kk)
-                    ptx::mma_bf16_ts(tmem + kColO, pa + kk * 8, b0 + (((kk & 3) * 2048) >> 4), idesc_mn,
-                                     (u > 0 || kk > 0) ? 1u : 0u);
-                ptx::mma_commit(&sm.s_free[sb]);
-                if ((u & 1) || u == n_sub - 1) ptx::mma_commit(&sm.empty[s]);
-            }
-        }
-        __syncwarp();
-        // every MMA this warp issued completes before TMEM is freed
-        uint64_t *drain = warp == kMmaWarp ? &sm.drain : &sm.drain2;
-        if (ptx::elect_one()) ptx::mma_commit(drain);
-        __syncwarp();
-        const uint64_t t0 = ptx::globaltimer();
-        while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer() - t0 < kTimeoutNs) {
-        }
-    } else {
-        // --------------------------------------------------------- softmax, epilogue ----
-        const int qd = warp & 3, hf = warp >> 2;     // lane quarter; group, and half of the columns
-        const int r = qd * 32 + lane;                // row = TMEM lane
-        const int ri = r / hp, hh = r - ri * hp;     // draft and head within the block
-        const bool live = ri < rows && hh < hn;
-        const int c0 = hf * 64;
-        const uint32_t lane_base = (uint32_t)(qd * 32) << 16;
-        const float sl2 = geo.scale * kLog2e;
-        const size_t row_id = (size_t)(q0 + m0 + ri) * geo.Hq + h + hh;   // of q, out and the states
-        bool ok = true;
 
-        // Routed query row, this warp's 64 columns, times scale * log2 e, as hi + lo bf16 pairs
-        {
-            uint32_t x[64];
-            if (ro == 0) {
-                // the composed query, as it is
-                const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row_id * kD + c0);
+            // Routed query row, this warp's 64 columns, times scale * log2 e, as bf16 terms
+            {
+                uint32_t q[64];
+                if (ro == 0) {
+                    // the composed query, as it is
+                    const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row_id * kD + c0);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    for (int c = 0; c < 8; ++c) {
+                        const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[8 * c + 2 * e] = w[e] << 16;
-                        x[8 * c + 2 * e + 1] = w[e] & 0xffff0000u;
+                        for (int e = 0; e < 4; ++e) {
+                            q[8 * c + 2 * e] = w[e] << 16;
+                            q[8 * c + 2 * e + 1] = w[e] & 0xffff0000u;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 64; ++e) q[e] = 0u;
+                    for (int i = 0; ok && i < ro; ++i) {
+                        ok = wait(&sm.bar.r_full[i & 1], (i >> 1) & 1);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+                        const bool mine = ro == 1 || hh == i;
+                        const uint32_t rc = tmem + (i & 1) * 128 + c0 + lane_base;
+#pragma unroll
+                        for (int c = 0; c < 64; c += 32) {
+                            uint32_t u[32];
+                            ptx::tmem_ld32(rc + c, u);
+                            ptx::tmem_wait_ld();
+                            ptx::reg_fence(u);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (mine) q[c + e] = u[e];
+                        }
+                        ptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(&sm.bar.r_free[i & 1]);
                     }
                 }
-            } else {
+                if (ok) {
 #pragma unroll
-                for (int e = 0; e < 64; ++e) x[e] = 0u;
-                for (int i = 0; ok && i < ro; ++i) {
-                    ok = wait(&sm.r_full[i & 1], (i >> 1) & 1);
-                    if (!ok) break;
-                    ptx::tc_fence_after();
-                    const bool mine = ro == 1 || hh == i;
-                    const uint32_t rc = tmem + kColS + (i & 1) * 128 + c0 + lane_base;
+                    for (int e = 0; e < 64; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * sl2);
 #pragma unroll
-                    for (int c = 0; c < 64; c += 32) {
-                        uint32_t u[32];
-                        ptx::tmem_ld32(rc + c, u);
-                        ptx::tmem_wait_ld();
-                        ptx::reg_fence(u);
+                    for (int t = 0; t < C::kQTerms; ++t) {
+                        uint32_t w[32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (mine) x[c + e] = u[e];
+                        for (int e = 0; e < 32; ++e) w[e] = take_term(q[2 * e], q[2 * e + 1]);
+                        ptx::tmem_st32(tmem + kColQ + 64 * t + c0 / 2 + lane_base, w);
                     }
+                    ptx::tmem_wait_st();
                     ptx::tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&sm.r_free[i & 1]);
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.qr_ready);
                 }
             }
-            if (ok) {
-                uint32_t hi[32], lo[32];
+
+            // the drafts that this row's draft sees: itself and its ancestors
+            uint64_t anc_lo = 0, anc_hi = 0;
+            if (has_drafts) {
+                for (int j = m0 + min(ri, rows - 1); j >= 0; j = sm.parent[j]) {
+                    if (j < 64) anc_lo |= 1ull << j;
+                    else anc_hi |= 1ull << (j - 64);
+                }
+            }
+
+            float m_used = -INFINITY;  // the reference of this thread's share of the row sum
+            float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
+            float m_sum = -INFINITY;   // Full: the reference of sm.sum (group 0)
+            bool okl = ok;
+            for (int u = hf; okl && u < n_sub; u += 2) {
+                const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
+                const uint32_t sbuf = tmem + (uint32_t)sb * C::kBuf + lane_base;   // S, then P
+                const int ring = (u >> 1) + ro, st = ring % kStages;
+                const bool drafts_here = t0 + kBS > base;
+                // This thread's half (64 dims) of a cache row of the half tile. Half: converted to fp16
+                // while the scores are on their way. Rows that not every draft sees must not reach the
+                // others through 0 * NaN: a row past the sequence's end, or a drafted one that is not
+                // finite in the output MMAs' operand, becomes zeros for them (the score MMAs have read it by
+                // then: a draft that sees a NaN or infinity has a NaN score; one that sees a finite value
+                // beyond fp16's range gets NaN by its bit in `over`). The lanes start at different 16-byte
+                // chunks so that a warp's accesses spread over all banks.
+                const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes +
+                                     (hf * kBS + (r & 63)) * 128;
+                const int vt = t0 + (r & 63);
+                uint32_t vr[C::kFp16P ? 32 : 1];
+                bool zero = vt >= L;
+                if (C::kFp16P || drafts_here) {
+                    okl = wait(&sm.bar.full[st], (ring / kStages) & 1);
+                    if (!okl) break;
+                }
+                if constexpr (C::kFp16P) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    split2(__uint_as_float(x[2 * e]) * sl2, __uint_as_float(x[2 * e + 1]) * sl2, hi[e], lo[e]);
-                ptx::tmem_st32(tmem + kColQ + c0 / 2 + lane_base, hi);
-                ptx::tmem_st32(tmem + kColQ + kLoCols + c0 / 2 + lane_base, lo);
-                ptx::tmem_wait_st();
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sm.qr_ready);
-            }
-        }
-
-        // the drafts that this row's draft sees: itself and its ancestors
-        uint64_t anc_lo = 0, anc_hi = 0;
-        if (has_drafts) {
-            for (int j = m0 + min(ri, rows - 1); j >= 0; j = sm.parent[j]) {
-                if (j < 64) anc_lo |= 1ull << j;
-                else anc_hi |= 1ull << (j - 64);
-            }
-        }
-
-        float m_used = -INFINITY;  // the reference of this thread's share of the row sum
-        float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
-        bool okl = ok;
-        for (int u = hf; okl && u < n_sub; u += 2) {
-            const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
-            const uint32_t sbuf = tmem + kColS + (uint32_t)sb * kBS + lane_base;   // S, then P
-            okl = wait(&sm.s_full[sb], (u / kSub) & 1);
-            if (!okl) break;
-            ptx::tc_fence_after();
-            uint32_t s0[32], s1[32];
-            ptx::tmem_ld32(sbuf, s0);
-            ptx::tmem_ld32(sbuf + 32, s1);
-            const bool drafts_here = t0 + kBS > base;
-            if (drafts_here) {
-                // Rows that not every draft sees must not reach the others through 0 * NaN: a row past
-                // the sequence's end, or one that is not finite, is zeroed for the output MMAs (the
-                // score MMAs have read it; a draft that sees such a row has a NaN score). Thread =
-                // (cache row, 64-dim half).
-                const int st = ((u >> 1) + ro) % kStages;
-                okl = wait(&sm.full[st], (((u >> 1) + ro) / kStages) & 1);   // (the copy: completed)
-                if (!okl) break;
-                const int tr = r & 63;
-                if (t0 + tr >= base) {
-                    const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes +
-                                         (hf * kBS + tr) * 128;
-                    bool zero = t0 + tr >= L;
+                    for (int c = 0; c < 8; ++c) ld_shared_v4(v_s + ((c + lane) & 7) * 16, vr + 4 * c);
+                    if (drafts_here && vt >= base) {
+                        bool over = false;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            zero |= not_finite(vr[e]);
+                            over |= past_fp16(vr[e]);
+                        }
+                        if (over && !zero) atomicOr(&sm.over[(vt - base) >> 5], 1u << ((vt - base) & 31));
+                        zero |= over;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float x = __uint_as_float(vr[e] << 16), y = __uint_as_float(vr[e] & 0xffff0000u);
+                        vr[e] = zero ? 0u : pack_f16(x, y);
+                    }
+                } else if (drafts_here && vt >= base) {
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         uint32_t v[4];
                         ld_shared_v4(v_s + ((c + lane) & 7) * 16, v);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            zero |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+                        for (int e = 0; e < 4; ++e) zero |= not_finite(v[e]);
                     }
-                    if (zero)
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) st_shared_v4(v_s + c * 16, 0u, 0u, 0u, 0u);
                 }
-            }
-            ptx::tmem_wait_ld();
-            ptx::reg_fence(s0);
-            ptx::reg_fence(s1);
-            if (drafts_here) {
-                const uint64_t vis = window64(anc_lo, anc_hi, t0 - base);
-                const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    if (!(v0 & (1u << c))) s0[c] = 0xff800000u;
-                    if (!(v1 & (1u << c))) s1[c] = 0xff800000u;
-                }
-            }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                mx[0] = max3(mx[0], __uint_as_float(s0[c]), __uint_as_float(s0[c + 1]));
-                mx[1] = max3(mx[1], __uint_as_float(s0[c + 2]), __uint_as_float(s0[c + 3]));
-                mx[2] = max3(mx[2], __uint_as_float(s1[c]), __uint_as_float(s1[c + 1]));
-                mx[3] = max3(mx[3], __uint_as_float(s1[c + 2]), __uint_as_float(s1[c + 3]));
-            }
-            float mt = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-            float m_ref = -INFINITY;
-            if (u == 0) {
-                // the row's first reference is the maximum of its first two half tiles
-                if (n_sub > 1) {
-                    okl = wait(&sm.first[qd], 0);
-                    if (!okl) break;
-                    mt = fmaxf(mt, sm.lsum[1][r]);
-                }
-            } else {
-                if (u == 1) {
-                    sm.lsum[1][r] = mt;
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&sm.first[qd]);
-                }
-                okl = wait(&sm.turn[qd][hf ^ 1], ((u - 1) >> 1) & 1);
+                okl = wait(&sm.bar.s_full[sb], (u / kSub) & 1);
                 if (!okl) break;
-                m_ref = sm.mref[hf ^ 1][r];
-            }
-            // a new reference when the maximum grew by more than 2^7 (or is the first finite)
-            const float m_new = fmaxf(m_ref, mt);
-            if (__any_sync(0xffffffffu, m_new > m_ref + kRescaleLog2)) {
-                const float f = (m_new == -INFINITY || m_ref == -INFINITY) ? 0.f : ptx::ex2(m_ref - m_new);
-                if (u > 0) {
-                    // O holds half tiles 0 .. u - 1 once the output MMAs of u - 1 are done
-                    okl = wait(&sm.s_free[(u - 1) % kSub], ((u - 1) / kSub) & 1);
+                ptx::tc_fence_after();
+                uint32_t s0[32], s1[32];
+                ptx::tmem_ld32(sbuf, s0);
+                ptx::tmem_ld32(sbuf + 32, s1);
+                if constexpr (C::kFp16P) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        st_shared_v4(v_s + ((c + lane) & 7) * 16, vr[4 * c], vr[4 * c + 1], vr[4 * c + 2],
+                                     vr[4 * c + 3]);
+                } else if (zero) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) st_shared_v4(v_s + c * 16, 0u, 0u, 0u, 0u);
+                }
+                ptx::tmem_wait_ld();
+                ptx::reg_fence(s0);
+                ptx::reg_fence(s1);
+                if (drafts_here) {
+                    const uint64_t vis = window64(anc_lo, anc_hi, t0 - base);
+                    const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        if (!(v0 & (1u << c))) s0[c] = 0xff800000u;
+                        if (!(v1 & (1u << c))) s1[c] = 0xff800000u;
+                    }
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    mx[0] = max3(mx[0], __uint_as_float(s0[c]), __uint_as_float(s0[c + 1]));
+                    mx[1] = max3(mx[1], __uint_as_float(s0[c + 2]), __uint_as_float(s0[c + 3]));
+                    mx[2] = max3(mx[2], __uint_as_float(s1[c]), __uint_as_float(s1[c + 1]));
+                    mx[3] = max3(mx[3], __uint_as_float(s1[c + 2]), __uint_as_float(s1[c + 3]));
+                }
+                float mt = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+                float m_ref = -INFINITY;
+                if (u == 0) {
+                    // the row's first reference is the maximum of its first two half tiles
+                    if (n_sub > 1) {
+                        okl = wait(&sm.bar.first[qd], 0);
+                        if (!okl) break;
+                        mt = fmaxf(mt, sm.lsum[1][r]);
+                    }
+                } else {
+                    if (u == 1) {
+                        sm.lsum[1][r] = mt;
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(&sm.bar.first[qd]);
+                    }
+                    okl = wait(&sm.bar.turn[qd][hf ^ 1], ((u - 1) >> 1) & 1);
+                    if (!okl) break;
+                    m_ref = sm.mref[hf ^ 1][r];
+                }
+                const float m_new = fmaxf(m_ref, mt);
+                const bool moves = __any_sync(0xffffffffu, m_new > m_ref + kRescaleLog2);
+                const bool fold = C::kFold && u > 0 && u % kFoldSub == 0;
+                if (u > 0 && (moves || fold)) {
+                    // O holds half tiles .. u - 1 once the output MMAs of u - 1 are done
+                    okl = wait(&sm.bar.s_free[(u - 1) % kSub], ((u - 1) / kSub) & 1);
                     if (!okl) break;
                     ptx::tc_fence_after();
+                }
+                if (fold) {
+                    // O, at reference m_ref, joins the sum; the output MMAs of u start over
+                    const float f = m_sum == -INFINITY ? 0.f : ptx::ex2(m_sum - m_ref);
+                    const bool had = u > kFoldSub;
+                    float4 *row = reinterpret_cast<float4 *>(sm.sum) + r * 32;
 #pragma unroll
                     for (int c = 0; c < 128; c += 32) {
                         uint32_t o[32];
@@ -485,156 +665,232 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ptx::tmem_wait_ld();
                         ptx::reg_fence(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        ptx::tmem_st32(tmem + kColO + c + lane_base, o);
+                        for (int e = 0; e < 8; ++e) {
+                            float4 &w = row[(c / 4 + e) ^ lane];
+                            float4 y = had ? w : make_float4(0.f, 0.f, 0.f, 0.f);
+                            y.x = fmaf(y.x, f, __uint_as_float(o[4 * e]));
+                            y.y = fmaf(y.y, f, __uint_as_float(o[4 * e + 1]));
+                            y.z = fmaf(y.z, f, __uint_as_float(o[4 * e + 2]));
+                            y.w = fmaf(y.w, f, __uint_as_float(o[4 * e + 3]));
+                            w = y;
+                        }
                     }
-                    ptx::tmem_wait_st();
+                    ptx::tc_fence_before();
+                    m_sum = m_ref;
+                    sm.fref[r] = m_ref;
                 }
-                m_ref = m_new;
-            }
-            sm.mref[hf][r] = m_ref;
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&sm.turn[qd][hf]);
-            // the group's sums move to this reference
-            if (__any_sync(0xffffffffu, m_ref != m_used)) {
-                const float f = m_used == -INFINITY ? 0.f : ptx::ex2(m_used - m_ref);
-                la = mul2(la, f);
-                lb = mul2(lb, f);
-                m_used = m_ref;
-            }
-            // the row's 64 weights -> 32 packed columns of P_hi and 32 of P_lo
-            const float mr = m_ref == -INFINITY ? 0.f : m_ref;
+                // a new reference when the maximum grew by more than 2^7 (or is the first finite)
+                if (moves) {
+                    if (u > 0 && !fold) {
+                        const float f =
+                            (m_new == -INFINITY || m_ref == -INFINITY) ? 0.f : ptx::ex2(m_ref - m_new);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                uint32_t *s = e < 16 ? s0 + 2 * e : s1 + 2 * (e - 16);
-                const float2 d = sub2(make_float2(__uint_as_float(s[0]), __uint_as_float(s[1])),
-                                      make_float2(mr, mr));
-                const float2 pe = make_float2(ptx::ex2(d.x), ptx::ex2(d.y));
-                if (e & 1) lb = add2(lb, pe); else la = add2(la, pe);
-                s[0] = __float_as_uint(pe.x);
-                s[1] = __float_as_uint(pe.y);
-            }
-            uint32_t hi[32];
+                        for (int c = 0; c < 128; c += 32) {
+                            uint32_t o[32];
+                            ptx::tmem_ld32(tmem + kColO + c + lane_base, o);
+                            ptx::tmem_wait_ld();
+                            ptx::reg_fence(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                uint32_t *s = e < 16 ? s0 + 2 * e : s1 + 2 * (e - 16);
-                uint32_t lo;
-                split2(__uint_as_float(s[0]), __uint_as_float(s[1]), hi[e], lo);
-                s0[e] = lo;        // (s0[e] has been read: e <= 2 e)
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            ptx::tmem_st32(tmem + kColO + c + lane_base, o);
+                        }
+                        ptx::tmem_wait_st();
+                    }
+                    m_ref = m_new;
+                }
+                sm.mref[hf][r] = m_ref;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm.bar.turn[qd][hf]);
+                // the group's sums move to this reference
+                if (__any_sync(0xffffffffu, m_ref != m_used)) {
+                    const float f = m_used == -INFINITY ? 0.f : ptx::ex2(m_used - m_ref);
+                    la = mul2(la, f);
+                    lb = mul2(lb, f);
+                    m_used = m_ref;
+                }
+                // the row's 64 weights -> 32 packed columns per term (the output MMAs of u - kSub, the
+                // last reader of P there, finished before these scores were written)
+                const float mr = m_ref == -INFINITY ? 0.f : m_ref;
+                auto weights = [&](uint32_t(&s)[32]) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float2 d = sub2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])),
+                                              make_float2(mr, mr));
+                        const float2 pe = make_float2(ptx::ex2(d.x), ptx::ex2(d.y));
+                        if (e & 1) lb = add2(lb, pe); else la = add2(la, pe);
+                        if constexpr (C::kFp16P) {
+                            s[e] = pack_f16(pe.x, pe.y);
+                        } else {
+                            s[2 * e] = __float_as_uint(pe.x);
+                            s[2 * e + 1] = __float_as_uint(pe.y);
+                        }
+                    }
+                };
+                weights(s0);
+                weights(s1);
+                if constexpr (C::kFp16P) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s0[16 + e] = s1[e];
+                    ptx::tmem_st32(sbuf, s0);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < C::kPTerms; ++t) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            w[e] = take_term(s0[2 * e], s0[2 * e + 1]);
+                            w[16 + e] = take_term(s1[2 * e], s1[2 * e + 1]);
+                        }
+                        ptx::tmem_st32(sbuf + 32 * t, w);
+                    }
+                }
+                ptx::tmem_wait_st();
+                ptx::tc_fence_before();
+                // rows of the tile written here (generic-proxy stores) are read next by the output MMAs
+                if (C::kFp16P || drafts_here) ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm.bar.p_full[sb]);
             }
-            // P over the buffer (the output MMAs of u - kSub, the last reader of P there, finished
-            // before these scores were written)
-            ptx::tmem_st32(sbuf, hi);
-            ptx::tmem_st32(sbuf + 32, s0);
-            ptx::tmem_wait_st();
-            ptx::tc_fence_before();
-            if (drafts_here) ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&sm.p_full[sb]);
-        }
 
-        // Epilogue: out = O / l, or the run's state (m, l, O); l is the two groups' shares at the
-        // reference of the last half tile. This warp's 64 output dims.
-        const int last = n_sub - 1, lb2 = last & 1;
-        if (okl && lb2 != hf) okl = wait(&sm.turn[qd][lb2], (last >> 1) & 1);
-        const bool oke = okl && wait(&sm.s_free[last % kSub], (last / kSub) & 1);
-        float l = (la.x + la.y) + (lb.x + lb.y);
-        if (oke && lb2 != hf) {
+            // Epilogue: out = O / l, or the part's state (m, l, O); l is the two groups' shares at the
+            // reference of the last half tile. This warp's 64 output dims.
+            const int last = n_sub - 1, lb2 = last & 1;
+            if (okl && lb2 != hf) okl = wait(&sm.bar.turn[qd][lb2], (last >> 1) & 1);
+            const bool oke = okl && wait(&sm.bar.s_free[last % kSub], (last / kSub) & 1);
+            float l = (la.x + la.y) + (lb.x + lb.y);
             const float m_fin = sm.mref[lb2][r];
-            l = m_used == -INFINITY ? 0.f : l * ptx::ex2(m_used - m_fin);
-        }
-        sm.lsum[hf][r] = l;
-        const bool okp = ptx::bar_and(kBarCompute, 32 * kComputeWarps, oke);
-        if (okp) {
-            ptx::tc_fence_after();
-            const float lt = l + sm.lsum[hf ^ 1][r];
-            const bool whole = runs == 1;
-            const float f = !whole ? 1.f : lt == 0.f ? 0.f : 1.f / lt;
-            float *state = a.part_o + (row_id * a.S + split) * kD + c0;
+            if (oke && lb2 != hf) l = m_used == -INFINITY ? 0.f : l * ptx::ex2(m_used - m_fin);
+            sm.lsum[hf][r] = l;
+            const bool okp = ptx::bar_and(kBarCompute, 32 * kComputeWarps, oke);
+            if (okp) {
+                ptx::tc_fence_after();
+                float lt = l + sm.lsum[hf ^ 1][r];
+                if (C::kFp16P && has_drafts) {
+                    const uint64_t o0 = sm.over[0] | (uint64_t)sm.over[1] << 32;
+                    const uint64_t o1 = sm.over[2] | (uint64_t)sm.over[3] << 32;
+                    if ((anc_lo & o0) | (anc_hi & o1)) lt = NAN;
+                }
+                const float f = !whole ? 1.f : lt == 0.f ? 0.f : 1.f / lt;
+                const bool folded = C::kFold && last >= kFoldSub;
+                float fs = 0.f;                              // of the sum
+                if (folded) fs = sm.fref[r] == -INFINITY ? 0.f : ptx::ex2(sm.fref[r] - m_fin);
+                // a part's state: [32 chunks of 4 dims][128 rows] float4, then [128 rows] {m, l}
+                uint8_t *state = a.states + (size_t)(2 * blockIdx.x + (si > 0)) * kTreeStateBytes;
+                float nf = lt * 0.f;                         // x * 0 is NaN exactly when x is not finite
 #pragma unroll
-            for (int c4 = 0; c4 < 2; ++c4) {
-                uint32_t u[32];
-                ptx::tmem_ld32(tmem + kColO + c0 + c4 * 32 + lane_base, u);
-                ptx::tmem_wait_ld();
-                ptx::reg_fence(u);
-                if (live && (!whole || a.out_dtype == KL_FP32)) {
-                    float4 *o = reinterpret_cast<float4 *>(
-                        whole ? static_cast<float *>(a.out) + row_id * kD + c0 + c4 * 32 : state + c4 * 32);
+                for (int c4 = 0; c4 < 2; ++c4) {
+                    uint32_t u[32];
+                    ptx::tmem_ld32(tmem + kColO + c0 + c4 * 32 + lane_base, u);
+                    ptx::tmem_wait_ld();
+                    ptx::reg_fence(u);
+                    if (folded) {
+                        const float4 *row = reinterpret_cast<const float4 *>(sm.sum) + r * 32;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        o[c] = make_float4(__uint_as_float(u[4 * c]) * f, __uint_as_float(u[4 * c + 1]) * f,
-                                           __uint_as_float(u[4 * c + 2]) * f, __uint_as_float(u[4 * c + 3]) * f);
-                } else if (live) {
-                    uint4 *o = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + row_id * kD + c0 +
-                                                         c4 * 32);
+                        for (int e = 0; e < 8; ++e) {
+                            const float4 y = row[(c0 / 4 + c4 * 8 + e) ^ lane];
+                            u[4 * e] = __float_as_uint(fmaf(y.x, fs, __uint_as_float(u[4 * e])));
+                            u[4 * e + 1] = __float_as_uint(fmaf(y.y, fs, __uint_as_float(u[4 * e + 1])));
+                            u[4 * e + 2] = __float_as_uint(fmaf(y.z, fs, __uint_as_float(u[4 * e + 2])));
+                            u[4 * e + 3] = __float_as_uint(fmaf(y.w, fs, __uint_as_float(u[4 * e + 3])));
+                        }
+                    }
+                    if (live) {
+                        if (C::kFp16P)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t w[4];
+                            for (int e = 0; e < 32; ++e) nf = fmaf(__uint_as_float(u[e]), 0.f, nf);
+                        float4 *o = whole ? reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row_id * kD) +
+                                                c0 / 4 + c4 * 8
+                                          : reinterpret_cast<float4 *>(state) + (c0 / 4 + c4 * 8) * kBM + r;
+                        if (!whole || a.out_dtype == KL_FP32) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = pack2(__uint_as_float(u[8 * c + 2 * e]) * f,
-                                         __uint_as_float(u[8 * c + 2 * e + 1]) * f);
-                        o[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int c = 0; c < 8; ++c)
+                                o[whole ? c : c * kBM] =
+                                    make_float4(__uint_as_float(u[4 * c]) * f, __uint_as_float(u[4 * c + 1]) * f,
+                                                __uint_as_float(u[4 * c + 2]) * f, __uint_as_float(u[4 * c + 3]) * f);
+                        } else {
+                            uint4 *ob = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) +
+                                                                  row_id * kD + c0 + c4 * 32);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    w[e] = pack2(__uint_as_float(u[8 * c + 2 * e]) * f,
+                                                 __uint_as_float(u[8 * c + 2 * e + 1]) * f);
+                                ob[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                        }
                     }
                 }
-            }
-            if (!whole) {
-                if (hf == 0 && live)
-                    reinterpret_cast<float2 *>(a.part_ml)[row_id * a.S + split] =
-                        make_float2(sm.mref[lb2][r], lt);
-                // The last CTA of the block to finish merges the states: out = sum_s w_s O_s / sum_s
-                // w_s l_s with w_s = 2^(m_s - M); a warp per row, 4 dims per lane.
-                ptx::bar_sync(kBarCompute, 32 * kComputeWarps);
-                if (tid == 0)
-                    sm.is_last = arrive_last(a.counters + ((size_t)b * geo.Hkv + g) * a.blocks + blk, runs);
-                ptx::bar_sync(kBarCompute, 32 * kComputeWarps);
-                if (sm.is_last) {
-                    for (int i = warp; i < rows * hp; i += kComputeWarps) {
-                        const int mi = i / hp, mh = i - mi * hp;
-                        if (mh >= hn) continue;
-                        const size_t id = (size_t)(q0 + m0 + mi) * geo.Hq + h + mh;
-                        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + id * a.S;
-                        float M = -INFINITY;
-                        for (int s = lane; s < runs; s += 32) {
-                            const float2 v = __ldcg(ml + s);
-                            if (v.y != 0.f) M = fmaxf(M, v.x);
-                        }
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-                        const float4 *po = reinterpret_cast<const float4 *>(a.part_o + id * a.S * kD) + lane;
-                        float z = 0.f;
-                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                        for (int s = 0; s < runs; ++s) {
-                            const float2 v = __ldcg(ml + s);
-                            const float4 x = __ldcg(po + (size_t)s * (kD / 4));
-                            // (a run in which the row sees nothing has l = 0 and m = -inf)
-                            const float w = v.y == 0.f ? 0.f : ptx::ex2(v.x - M);
-                            z = fmaf(w, v.y, z);
-                            acc.x = fmaf(w, x.x, acc.x);
-                            acc.y = fmaf(w, x.y, acc.y);
-                            acc.z = fmaf(w, x.z, acc.z);
-                            acc.w = fmaf(w, x.w, acc.w);
-                        }
-                        const float inv = z == 0.f ? 0.f : 1.f / z;
-                        if (a.out_dtype == KL_FP32)
-                            reinterpret_cast<float4 *>(static_cast<float *>(a.out) + id * kD)[lane] =
-                                make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-                        else
-                            reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + id * kD)[lane] =
-                                make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-                    }
-                }
+                if (!whole && hf == 0 && live)
+                    reinterpret_cast<float2 *>(state + kBM * kD * 4)[r] = make_float2(m_fin, lt);
+                if (C::kFp16P && __any_sync(0xffffffffu, nf != nf) && lane == 0) raise_flag(a.err, KL_FLAG_RANGE);
             }
         }
+
+        ptx::tc_fence_before();
+        __syncthreads();
+        ptx::tc_fence_after();
+        x += n_tiles;
+        if (x >= x1 || sm.abort) break;
     }
 
-    ptx::tc_fence_before();
-    __syncthreads();
-    if (warp == kMmaWarp) {
-        ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem, kTmemCols);
+    if (warp == kMmaWarp) ptx::tmem_dealloc(tmem, kTmemCols);
+}
+
+// Merge of the parts of the units that lie in several runs: out = sum_s w_s O_s / sum_s w_s l_s with w_s =
+// 2^(m_s - M) and M the largest m_s of a part with l_s > 0. CTA (c, y): the unit that run c enters first
+// inside, dims 8 y .. + 7; thread = row and 4 dims. (One sequence of 131072 tokens, 8 heads, 19 parts
+// each: about 3 us behind the attention.)
+constexpr int kMergeThreads = 2 * kBM;
+
+__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const TreeArgs a) {
+    grid_dep_wait();
+    grid_dep_launch();
+    const int c = blockIdx.x + 1;
+    const TreeMerge t = a.merge[c];
+    const int r = threadIdx.x % kBM, chunk = blockIdx.y * 2 + threadIdx.x / kBM;
+    const int ri = r / a.hp, hh = r - ri * a.hp;
+    if (ri >= t.rows || hh >= t.hn) return;
+    // part i is run c - 1 + i's; its state is the run's first where the run starts inside the unit
+    const int first = c - 1, parts = t.last - first + 1;
+    auto cut = [&](int run) -> int64_t {
+        const int64_t x = run_start(t.total, run, t.runs) - t.unit0;
+        return x >= t.tiles ? t.tiles : x <= 0 ? 0 : x / t.step * t.step;
+    };
+    auto state = [&](int i) {
+        const int run = first + i;
+        return a.states + (size_t)(2 * run + (run_start(t.total, run, t.runs) < t.unit0)) * kTreeStateBytes;
+    };
+    float M = -INFINITY;
+    for (int i = 0; i < parts; ++i) {
+        if (cut(first + i) == cut(first + i + 1)) continue;          // (nothing of the unit in this run)
+        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(state(i) + kBM * kD * 4) + r);
+        if (ml.y != 0.f) M = fmaxf(M, ml.x);
     }
+    float z = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+        if (cut(first + i) == cut(first + i + 1)) continue;
+        const uint8_t *s = state(i);
+        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(s + kBM * kD * 4) + r);
+        const float4 o = __ldcg(reinterpret_cast<const float4 *>(s) + chunk * kBM + r);
+        const float w = ml.y == 0.f ? 0.f : ptx::ex2(ml.x - M);      // (l = 0: the row sees nothing there)
+        z = fmaf(w, ml.y, z);
+        acc.x = fmaf(w, o.x, acc.x);
+        acc.y = fmaf(w, o.y, acc.y);
+        acc.z = fmaf(w, o.z, acc.z);
+        acc.w = fmaf(w, o.w, acc.w);
+    }
+    const float inv = z == 0.f ? 0.f : 1.f / z;
+    const size_t at = ((size_t)(t.row0 + ri) * a.geo.Hq + t.h + hh) * kD + 4 * chunk;
+    if (a.out_dtype == KL_FP32)
+        *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) =
+            make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    else
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + at) =
+            make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
 }
 
 // ------------------------------------------------------------------------ host side ------
@@ -690,19 +946,26 @@ cudaError_t launch_tree_tc(const TreeArgs &a) {
         const cuuint32_t qbox[3] = {64, (cuuint32_t)a.hp, (cuuint32_t)a.rpb};
         if (!encode(&qmap, a.q, 3, qdims, qstrides, qbox)) return cudaErrorInvalidValue;
     }
-    const size_t smem = sizeof(TreeSmem) + 1024;
-    static PerDeviceOnce once;
-    const cudaError_t e = once.run([&] {
-        return cudaFuncSetAttribute(tree_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const bool full = a.out_dtype == KL_FP32;
+    const auto kernel = full ? tree_tc_kernel<Full> : tree_tc_kernel<Half>;
+    const size_t smem = (full ? sizeof(TreeSmem<Full>) : sizeof(TreeSmem<Half>)) + 1024;
+    static PerDeviceOnce once[2];
+    cudaError_t e = once[full].run([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.blocks * a.S, g.Hkv, g.B);
+    cfg.gridDim = dim3((unsigned)a.ctas);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
-    return cudaLaunchKernelEx(&cfg, tree_tc_kernel, vmap, wmap, qmap, a);
+    e = cudaLaunchKernelEx(&cfg, kernel, vmap, wmap, qmap, a);
+    if (e != cudaSuccess || a.ctas == 1 || a.num_splits == 1) return e;
+    cfg.gridDim = dim3((unsigned)a.ctas - 1, kD / 8);
+    cfg.blockDim = dim3(kMergeThreads);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, tree_merge_kernel, a);
 }
 
 }  // namespace kl

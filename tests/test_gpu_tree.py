@@ -144,6 +144,37 @@ def test_a_row_that_is_not_finite_reaches_those_who_see_it(value):
                 assert torch.isnan(got[r]).all(), (b, i)
 
 
+def test_half_precision_outputs_and_values_beyond_it():
+    """bf16 outputs take the values in fp16: a drafted row beyond its range, or not finite, reaches those who
+    see it alone; a committed one raises the flag."""
+    x = tree_inputs((150, 90), (40, 70), 8, 2, kind="random", seed=9)
+    cu = x["cu_q"].tolist()
+    P = 16
+    x["v_cache"][0, 0, 0, 0] = 65280.0
+    want = tree_reference(x)
+    y = dict(x, v_cache=x["v_cache"].clone())
+    bad = {0: 5, 1: 33}
+    for (b, i), value in zip(bad.items(), (70000.0, math.inf)):
+        t = int(x["seq_lens"][b]) - x["drafts"][b] + i
+        y["v_cache"][int(x["block_table"][b, t // P]), :, t % P, 3::40] = value
+    got = run(y, torch.bfloat16, flags=kl.KL_FLAG_RANGE)
+    for b in range(2):
+        for i in range(x["drafts"][b]):
+            j = i
+            while j > bad[b]:
+                j = int(x["parents"][cu[b] + j])
+            r = cu[b] + i
+            if j != bad[b]:
+                d = got[r].double() - want[r]
+                assert float(d.norm() / want[r].norm()) < 4 * REL[torch.bfloat16], (b, i)
+            else:
+                assert torch.isnan(got[r].float()).all(), (b, i)
+    y = dict(x, v_cache=x["v_cache"].clone())
+    y["v_cache"][int(x["block_table"][0, 0]), :, 3, 5] = 70000.0
+    run(y, torch.bfloat16, flags=kl.KL_FLAG_RANGE)
+    check(run(y)[cu[1]:], tree_reference(y)[cu[1]:])
+
+
 def test_rows_past_the_end_and_unused_pages_may_hold_anything():
     x = tree_inputs((150, 33), (17, 33), 8, 2)
     want = tree_reference(x)
@@ -184,6 +215,14 @@ def test_flags():
     check(torch.cat([got[:10], got[15:]]), torch.cat([want[:10], want[15:]]))
 
 
+def test_a_missing_or_small_workspace_is_refused():
+    x = tree_inputs((300,), (5,))
+    for ws in (torch.zeros(1000, dtype=torch.uint8, device="cuda"), torch.zeros(1 << 23, dtype=torch.uint8, device="cuda")[8:]):
+        with pytest.raises(kl.KLError) as e:
+            run(x, ws=ws)
+        assert e.value.status == kl.KL_ERR_WORKSPACE
+
+
 def test_another_stream_and_a_graph():
     x = tree_inputs((1200, 300), (20, 33), 8, 2)
     g, want = to_dev(x), tree_reference(x)
@@ -215,6 +254,18 @@ def test_another_stream_and_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     check(out.cpu(), want)
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lens,drafts", [
+    ((20000, 3, 700, 1, 5000), (5, 3, 64, 1, 33)),       # runs that end inside units of one long sequence
+    ((500,) * 90, (7,) * 90),                             # more units than CTAs
+    ((260, 17, 0, 128, 129, 384) * 70, (1, 2, 0, 3, 4, 5) * 70)])   # more sequences than threads
+def test_runs_of_many_lengths(lens, drafts, out):
+    x = tree_inputs(lens, drafts, 8, 2, seed=len(lens))
+    want = tree_reference(x)
+    for splits in (0, 1, 3):
+        check(run(x, out, splits=splits), want, out)
 
 
 def test_a_long_cache():

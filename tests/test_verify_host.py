@@ -42,9 +42,8 @@ def test_tree_refusals():
     _refused(kl.KL_ERR_UNSUPPORTED, _tree, _shape(), mq=kl.KL_TREE_MAX_DRAFTS + 1)
     _refused(kl.KL_ERR_UNSUPPORTED, _tree, _shape(head_dim=64))
     assert kl.kl_tree_workspace_size(_shape(head_dim=96), 10, 8, 2) == 0
-    assert kl.kl_tree_workspace_size(_shape(), 10, 8, 1) == 0
-    # two runs of 256 tokens: the counters' region and the states
-    assert kl.kl_tree_workspace_size(_shape(), 10, 8, 2) >= 65536 + 10 * 8 * 2 * 130 * 4
+    # the shared front region, then two states of 128 rows for each run of two tiles
+    assert kl.kl_tree_workspace_size(_shape(), 10, 8, 2) >= 65536 + 2 * 128 * 130 * 4
 
 
 def _commit(sh, cu=16, path=16, n=16, mp=4, bt=16, sl=16, new=16, v=16):
@@ -85,9 +84,9 @@ def test_logprob_refusals():
 
 SRC = """
 #include "kl_tree_plan.cuh"
-extern "C" void plan(int B, int Hkv, int G, int max_q, long long tokens, int splits, int fp32, int sms, int *o) {
-    const kl::TreePlan p = kl::plan_tree(B, Hkv, G, max_q, tokens, splits, fp32 != 0, sms);
-    o[0] = p.hp; o[1] = p.rpb; o[2] = p.blocks; o[3] = p.S; o[4] = p.chunk;
+extern "C" void plan(int B, int Hkv, int G, int max_q, long long tokens, int sms, int *o) {
+    const kl::TreePlan p = kl::plan_tree(B, Hkv, G, max_q, tokens, sms);
+    o[0] = p.hp; o[1] = p.rpb; o[2] = p.blocks; o[3] = p.ctas;
 }
 """
 
@@ -100,25 +99,23 @@ def plan(tmp_path_factory):
     subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-O1", "-shared", "-fPIC", "-I", builder.CSRC,
                     str(d / "plan.cpp"), "-o", lib], check=True)
     f = ctypes.CDLL(lib).plan
-    f.argtypes = [ctypes.c_int] * 4 + [ctypes.c_longlong] + [ctypes.c_int] * 3 + [ctypes.POINTER(ctypes.c_int)]
+    f.argtypes = [ctypes.c_int] * 4 + [ctypes.c_longlong, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]
 
-    def call(B, Hkv, G, max_q, tokens, splits=0, fp32=False, sms=152):
-        o = (ctypes.c_int * 5)()
-        f(B, Hkv, G, max_q, tokens, splits, int(fp32), sms, o)
+    def call(B, Hkv, G, max_q, tokens, sms=152):
+        o = (ctypes.c_int * 4)()
+        f(B, Hkv, G, max_q, tokens, sms, o)
         return tuple(o)
     return call
 
 
 @pytest.mark.parametrize("G", [1, 2, 3, 6, 7, 8, 16, 32, 71, 128])
-def test_layouts_cover_all_rows_and_tokens(plan, G):
+def test_layouts_cover_all_rows(plan, G):
     for n in (1, 2, 15, 16, 17, 33, 64, 127, 128):
-        for tokens in (16, 127, 128, 129, 5000, 131072):
-            for splits in (0, 1, 3, 1024):
-                for fp32 in (False, True):
-                    hp, rpb, blocks, S, chunk = plan(3, 2, G, n, tokens, splits, fp32)
-                    assert 1 <= hp <= G and hp * rpb <= 128
-                    assert blocks == -(-G // hp) * -(-n // rpb)
-                    assert chunk % 128 == 0 and chunk * S >= tokens > chunk * (S - 1)
-                    assert not fp32 or chunk <= 4096
-                    if splits == 1 and not fp32:
-                        assert S == 1
+        for B in (0, 1, 3, 300):
+            for tokens in (16, 127, 128, 129, 5000, 131072, 1 << 29):
+                hp, rpb, blocks, ctas = plan(B, 2, G, n, tokens)
+                assert 1 <= hp <= G and hp * rpb <= 128
+                assert blocks == -(-G // hp) * -(-n // rpb)
+                assert blocks <= G * -(-n // 128)
+                tiles = -(-tokens // 128) * max(B, 1) * 2 * blocks
+                assert 1 <= ctas <= 152 and (ctas == 152 or ctas == max(1, tiles // 2))
