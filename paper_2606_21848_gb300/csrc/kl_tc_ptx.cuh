@@ -195,6 +195,17 @@ __device__ __forceinline__ void fence_proxy_async_global() {
     asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
+// ------------------------------------------------------------------ register shares ----
+// All warps of a warpgroup take or give up registers (of those the CTA was launched with).
+template <uint32_t N>
+__device__ __forceinline__ void regs_inc() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <uint32_t N>
+__device__ __forceinline__ void regs_dec() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // ------------------------------------------------------------------ named barriers ----
 // Barrier `id` over `count` threads (whole warps). All of them must reach it.
 __device__ __forceinline__ void bar_sync(uint32_t id, uint32_t count) {
@@ -416,6 +427,16 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *u) {
         "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]),
         "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]),
         "r"(u[29]), "r"(u[30]), "r"(u[31])
+        : "memory");
+}
+
+// Store 16 consecutive 32-bit columns of the thread's TMEM lane (complete with tmem_wait_st()).
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
+        "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
         : "memory");
 }
 

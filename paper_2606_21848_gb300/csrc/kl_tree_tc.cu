@@ -21,18 +21,21 @@
 // feeds both products from the same shared-memory copy, as the K-major B operand of the scores and the
 // MN-major one of the output. Q and P are A operands in tensor memory.
 //
-// Precision. bf16 outputs (Half): the routed query is a pair of bf16 operands (16 significant bits), the
-// weights one fp16 operand (11 bits) against the tile converted to fp16 in place, as in the prefill:
-// three MMAs per tile; cached values of magnitude 65536 or more have no fp16 form (KL_FLAG_RANGE).
+// Precision. bf16 outputs (Half): the tile is converted to fp16 in place (exact for bf16 values of magnitude
+// 2^-14 to 65280), the routed query and the weights are one fp16 operand each (11 bits): two MMAs per
+// tile. A weight is off by |s| 2^-12 / sqrt(3) at rms, against the output's own rounding of 2^-9; with the
+// query as two operands (three MMAs) the tensor cores, at the rate that the power cap leaves them, took
+// 1.24 us per tile where HBM delivers one in 0.73. Values or queries past fp16's range make the outputs
+// that take part in them NaN (KL_FLAG_RANGE).
 // fp32 outputs (Full): query and weights are sums of three bf16 terms (24 bits), and since the tensor
 // core's adds truncate, O moves every 256 tokens to a sum that the softmax warps keep in shared memory.
 //
-// The unit of the pipeline is a half tile of 64 tokens, kSub in flight, as in the prefill: thread = row
-// = TMEM lane; two groups of four softmax warps take alternate half tiles and share each row's
-// reference maximum, which moves only when a half tile's maximum passes it by more than 2^7.
+// The softmax works on half tiles of 64 tokens, thread = row = TMEM lane. A row's reference maximum moves
+// only when a half tile's maximum passes it by more than 2^7.
 //
-// Roles (352 threads): warps 0-7 softmax and epilogue, warp 8 producer (TMA), warp 9 routing and score
-// MMAs (owner of the tensor memory), warp 10 output MMAs. Every wait is bounded (about one second); a
+// Roles: two groups of four softmax warps (and epilogue), then one warp each for the producer (TMA), the routing
+// and score MMAs (owner of the tensor memory) and the output MMAs, and for Half four warps that convert
+// tiles to fp16 ahead of their score MMAs. Every wait is bounded (about one second); a
 // wait that runs out raises KL_FLAG_TIMEOUT and every role leaves, drains its copies and MMAs and
 // frees the tensor memory.
 #include <cudaTypedefs.h>
@@ -49,9 +52,6 @@ constexpr int kD = 128;
 constexpr int kBM = kTreeRows;                    // rows per block
 constexpr int kBN = kTreeTile;                    // cache rows per tile
 constexpr int kBS = 64;                           // cache rows per half tile
-constexpr int kComputeWarps = 8;                  // two per TMEM lane quarter
-constexpr int kProducerWarp = 8, kMmaWarp = 9, kPvWarp = 10;
-constexpr int kThreads = 11 * 32;
 constexpr uint32_t kTileBytes = kBN * kD * 2;     // 32 KiB
 constexpr uint32_t kHalfBytes = kTileBytes / 2;   // one 64-dim half: 128 rows x 128 B
 constexpr uint32_t kTmemCols = 512;
@@ -59,46 +59,67 @@ constexpr float kRescaleLog2 = 7.f;
 constexpr uint64_t kTimeoutNs = kRowsTimeoutNs;
 constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 is __syncthreads)
 
-// Operand forms and the layout that they leave room for. Tensor memory: kSub buffers of kBuf columns (64
-// of scores, then the weights, 32 per term), O (128), the query's terms (64 each); the routed queries
-// first land in columns 0 .. 255, before anything else is there.
+// Operand forms and the layout that they leave room for. Two groups of four softmax warps (thread = row =
+// TMEM lane) take alternate half tiles. Tensor memory: kSub buffers of kBuf columns (64 of scores, then the
+// weights, 32 per term), then
+//   Half: an O of 128 columns for each group, which so keeps its own reference and never waits for the other
+//     (one O for both made each half tile's reference wait for the one before: 1.04 us per tile); the
+//     query, fp16, in shared memory; scores of a whole tile at once (N = 128, since with the query in
+//     shared memory N = 64 is bound by its reads); four warps convert tiles to fp16 ahead of that.
+//   Full: one O, the query's terms (64 columns each).
+// The routed queries first land in columns 0 .. 255, before anything else is there.
 struct Half {
-    static constexpr bool kFp16P = true, kFold = false;
-    static constexpr int kQTerms = 2, kPTerms = 1, kSub = 4, kStages = 5;
-    static constexpr uint32_t kBuf = 64, kColO = 256, kColQ = 384;
+    static constexpr bool kFp16 = true;
+    static constexpr int kQTerms = 1, kPTerms = 1, kSub = 4, kConvWarps = 4, kStages = 5;
+    static constexpr uint32_t kBuf = 64, kColO = 256, kColQ = 0;
 };
 struct Full {
-    static constexpr bool kFp16P = false, kFold = true;
-    static constexpr int kQTerms = 3, kPTerms = 3, kSub = 2, kStages = 3;
+    static constexpr bool kFp16 = false;
+    static constexpr int kQTerms = 3, kPTerms = 3, kSub = 2, kConvWarps = 0, kStages = 3;
     static constexpr uint32_t kBuf = 96, kColO = 192, kColQ = 320;
 };
-constexpr int kFoldSub = 4;           // half tiles between two moves of O to the fp32 sum (Full)
+constexpr int kGroups = 2;
+// Half's registers: of the 128 per thread at launch, the other warps give up 40 and the softmax warps take them
+// (a half tile of scores and weights, 64 registers, spilled at 128).
+constexpr uint32_t kSoftmaxRegs = 168, kOtherRegs = 88;
+static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "");
+template <typename C>
+struct Warps {
+    static constexpr int kCompute = 4 * kGroups;
+    static constexpr int kProducer = kCompute, kMma = kCompute + 1, kPv = kCompute + 2, kConv = kCompute + 4;
+    static constexpr int kThreads = 32 * (C::kConvWarps ? kConv + C::kConvWarps : kPv + 1);
+};
+constexpr int kFoldSub = 4;           // Full: half tiles between two moves of O to the fp32 sum
 
 template <typename C>
 struct __align__(1024) TreeSmem {
-    uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B]
+    uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B];
+                                           // Half: then the routed query, fp16
     // Ring: the W^R matrices, then the cache tiles ([64-dim half][128 rows][128 B], SW128).
     uint8_t tiles[C::kStages][kTileBytes];
-    float sum[C::kFold ? kBM * kD : 4];    // Full: O of the half tiles folded so far, [row][128], its
+    float sum[C::kFp16 ? 4 : kBM * kD];    // Full: O of the half tiles folded so far, [row][128], its
                                            // 16-byte chunks c at c ^ (row % 32)
     // Barriers (set up anew for every segment): one completion per half tile u of its buffer u % kSub
-    // on s_full (its scores), p_full (its weights) and s_free (its output MMAs are done), and per
-    // lane quarter on turn[.][u % 2] (the references after it).
+    // on p_full (its weights) and s_free (its output MMAs are done); on s_full per half tile (Full) or per
+    // tile t on t % 2 (Half; its scores), on v_full[t % kStages] (Half: its rows are fp16; by the tile's
+    // number and not by its ring slot, which W^R may have used before), and per lane quarter on
+    // turn[.][u % 2] (Full: the references after it).
     struct Bars {
         uint64_t full[C::kStages], empty[C::kStages];
-        uint64_t s_full[C::kSub], s_free[C::kSub], p_full[C::kSub];
-        uint64_t turn[4][2];
+        uint64_t s_full[C::kSub], s_free[C::kSub];
+        uint64_t p_full[C::kSub], v_full[C::kStages];
+        uint64_t turn[4][kGroups];
         uint64_t first[4];                 // per lane quarter: the maxima of half tile 1 are in lsum[1]
         uint64_t r_full[2], r_free[2];     // routing results, alternating halves of columns 0 .. 255
         uint64_t qr_ready, drain, drain2;
     } bar;
-    float mref[2][kBM];        // the rows' references after the last half tile of each parity
-    float lsum[2][kBM];        // the two groups' shares of the row sums, for the epilogue
+    float mref[kGroups][kBM];  // the rows' references after the last half tile of each group
+    float lsum[kGroups][kBM];  // the groups' shares of the row sums, for the epilogue
     float fref[kBM];           // Full: the references of `sum`
     int32_t parent[KL_TREE_MAX_DRAFTS];
     unsigned int over[KL_TREE_MAX_DRAFTS / 32];   // Half: drafts with a finite value beyond fp16's range
     TreeSegment seg[2];        // this segment and the next
-    int64_t warp_sum[kThreads / 32];
+    int64_t warp_sum[Warps<C>::kThreads / 32];
     int64_t x0, x1;            // this CTA's run
     uint32_t tmem_base;
     int abort;
@@ -109,8 +130,8 @@ static_assert(sizeof(TreeSmem<Half>) + 1024 <= 227 * 1024 && sizeof(TreeSmem<Ful
 template <typename C>
 __device__ __forceinline__ uint32_t bar_count(int i) {
     using B = typename TreeSmem<C>::Bars;
-    if (i >= (int)(offsetof(B, p_full) / 8) && i < (int)(offsetof(B, turn) / 8)) return kComputeWarps / 2;
-    if (i >= (int)(offsetof(B, r_free) / 8) && i <= (int)(offsetof(B, qr_ready) / 8)) return kComputeWarps;
+    if (i >= (int)(offsetof(B, p_full) / 8) && i < (int)(offsetof(B, turn) / 8)) return 4;
+    if (i >= (int)(offsetof(B, r_free) / 8) && i <= (int)(offsetof(B, qr_ready) / 8)) return Warps<C>::kCompute;
     return 1;
 }
 
@@ -157,7 +178,7 @@ __device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { r
 template <typename C>
 __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = blockIdx.x;
-    const int B = a.geo.B, per = (B + kThreads - 1) / kThreads;
+    const int B = a.geo.B, per = (B + Warps<C>::kThreads - 1) / Warps<C>::kThreads;
     int64_t mine = 0;
     for (int b = tid * per; b < min(B, (tid + 1) * per); ++b) {
         const TreeSeq s = tree_seq(a, b, c == 0);
@@ -177,7 +198,7 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
     __syncthreads();
     int64_t total = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
+    for (int w = 0; w < Warps<C>::kThreads / 32; ++w) {
         if (w < warp) upto += sm.warp_sum[w];
         total += sm.warp_sum[w];
     }
@@ -251,10 +272,12 @@ __device__ __forceinline__ TreeSegment next_segment(const TreeArgs &a, const Tre
 
 // ------------------------------------------------------------------------------- kernel ----
 template <typename C>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Warps<C>::kThreads, 1)
     tree_tc_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap wmap,
                    const __grid_constant__ CUtensorMap qmap, const TreeArgs a) {
     constexpr int kSub = C::kSub, kStages = C::kStages;
+    constexpr int kComputeWarps = Warps<C>::kCompute, kProducerWarp = Warps<C>::kProducer;
+    constexpr int kMmaWarp = Warps<C>::kMma, kPvWarp = Warps<C>::kPv, kConvWarp = Warps<C>::kConv;
     constexpr uint32_t kColO = C::kColO, kColQ = C::kColQ;
     using Smem = TreeSmem<C>;
     extern __shared__ uint8_t smem_raw[];
@@ -280,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     // rows of the query block that its box does not fill
     if (a.w_r) {
-        for (int i = tid; i < (kBM - hp * rpb) * 16; i += kThreads)
+        for (int i = tid; i < (kBM - hp * rpb) * 16; i += Warps<C>::kThreads)
             *reinterpret_cast<uint4 *>(sm.q + (i & 8 ? kHalfBytes : 0) + (hp * rpb + (i >> 4)) * 128 +
                                        (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
         ptx::fence_proxy_async_smem();
@@ -288,16 +311,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int64_t x1 = sm.x1;
     int64_t x = sm.x0;
     const Waiter wait{&sm.abort, a.err};
-    uint32_t tmem = 0;
 
-    for (int si = 0;; ++si) {
+    // One segment's start for all threads: its block, the barriers, the drafts' parents
+    struct Part {
+        TreeSegment sg;
+        TreeBlock blk;
+        int n_sub, ro;         // half tiles; ring positions of W^R matrices
+        bool has_drafts, whole;
+    };
+    auto begin = [&](int si) -> Part {
         TreeSegment sg = sm.seg[si & 1];
         if (sg.n_tiles > x1 - x) sg.n_tiles = (int)(x1 - x);
         // The block: drafts m0 .. m0 + rows - 1, heads h .. h + hn - 1 of the group; row r of the 128 is
         // draft m0 + r / hp with head h + r % hp.
         const TreeBlock blk = tree_block(a, sg);
-        const int m0 = blk.m0, rows = blk.rows, h = blk.h, hn = blk.hn, g = blk.g;
-        const int q0 = sg.q0, n = sg.n, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int hn = blk.hn, q0 = sg.q0, n = sg.n, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
         const int base = L - n;                      // committed tokens
         const int n_sub = min(2 * n_tiles, (L + kBS - 1) / kBS - 2 * tile0);   // half tiles
         const bool has_drafts = (tile0 + n_tiles) * kBN > base;
@@ -322,11 +350,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tc_fence_before();
         __syncthreads();
         ptx::tc_fence_after();
-        if (si == 0) {
-            grid_dep_launch();
-            tmem = sm.tmem_base;
-        }
+        if (si == 0) grid_dep_launch();
+        return Part{sg, blk, n_sub, ro, has_drafts, whole};
+    };
+    // ... and its end; false after the run's last
+    auto end = [&](const Part &k) {
+        ptx::tc_fence_before();
+        __syncthreads();
+        ptx::tc_fence_after();
+        x += k.sg.n_tiles;
+        return x < x1 && !sm.abort;
+    };
 
+    if (warp >= kComputeWarps) {
+        if constexpr (C::kFp16) ptx::regs_dec<kOtherRegs>();
+        for (int si = 0;; ++si) {
+        const Part k = begin(si);
+        const uint32_t tmem = sm.tmem_base;
+        const TreeSegment &sg = k.sg;
+        const int m0 = k.blk.m0, h = k.blk.h, g = k.blk.g;
+        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
         if (warp == kProducerWarp) {
             // -------------------------------------------------------------- producer ----
             const int P = geo.P;
@@ -390,9 +434,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             // K-major SW128 operands step 32 B per 16 columns inside a 64-column half and jump a
             // half (kHalfBytes) every 4 steps; MN-major SW128 operands step 16 rows = 2 KiB; TMEM
             // A operands step 8 columns (16 packed 16-bit values).
-            constexpr uint32_t idesc_qk = ptx::idesc_bf16(128, kBS, false, false);
+            constexpr uint32_t idesc_qk =
+                C::kFp16 ? idesc_f16(128, kBN, false, false) : ptx::idesc_bf16(128, kBS, false, false);
             constexpr uint32_t idesc_route = ptx::idesc_bf16(128, 128, false, true);
-            constexpr uint32_t idesc_pv = C::kFp16P ? idesc_f16(128, 128, false, true) : idesc_route;
+            constexpr uint32_t idesc_pv = C::kFp16 ? idesc_f16(128, 128, false, true) : idesc_route;
             const uint64_t q_desc = ptx::smem_desc(ptx::smem_addr(sm.q), 16, 1024, ptx::kSwizzle128B);
             const uint64_t k_desc = ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), 16, 1024, ptx::kSwizzle128B);
             const uint64_t mn_desc =
@@ -422,30 +467,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // (the loop by one lane: warp-wide waits between two half tiles leave the tensor cores idle)
                 if (ok && ptx::elect_one()) {
                     ptx::tc_fence_after();
-                    for (int u = 0; u < n_sub; ++u) {
-                        const int r = (u >> 1) + ro, s = r % kStages, sb = u % kSub;
-                        if (!wait.one(&sm.bar.full[s], (r / kStages) & 1)) break;
-                        if (u >= kSub && !wait.one(&sm.bar.s_free[sb], (u / kSub - 1) & 1)) break;
-                        ptx::tc_fence_after();
-                        const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+                    if constexpr (C::kFp16) {
+                        for (int t = 0; t < n_tiles; ++t) {
+                            if (!wait.one(&sm.bar.v_full[t % kStages], (t / kStages) & 1)) break;
+                            // the output MMAs of tile t - 2 have read these buffers' weights
+                            if (t > 1 && !(wait.one(&sm.bar.s_free[(2 * t) % kSub], ((t - 2) >> 1) & 1) &&
+                                           wait.one(&sm.bar.s_free[(2 * t + 1) % kSub], ((t - 2) >> 1) & 1)))
+                                break;
+                            ptx::tc_fence_after();
+                            const uint64_t b0 = k_desc + ((((t + ro) % kStages) * kTileBytes) >> 4);
 #pragma unroll
-                        for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
-                            ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
-                                             idesc_qk, kk > 0);
-                        ptx::mma_commit(&sm.bar.s_full[sb]);
+                            for (int kk = 0; kk < kD / 16; ++kk)
+                                ptx::mma_bf16(tmem + (t & 1) * 2 * C::kBuf, q_desc + kstep(kk), b0 + kstep(kk),
+                                              idesc_qk, kk > 0);
+                            ptx::mma_commit(&sm.bar.s_full[t & 1]);
+                        }
+                    } else {
+                        for (int u = 0; u < n_sub; ++u) {
+                            const int r = (u >> 1) + ro, s = r % kStages, sb = u % kSub;
+                            if (!wait.one(&sm.bar.full[s], (r / kStages) & 1)) break;
+                            if (u >= kSub && !wait.one(&sm.bar.s_free[sb], (u / kSub - 1) & 1)) break;
+                            ptx::tc_fence_after();
+                            const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+#pragma unroll
+                            for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
+                                ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
+                                                 idesc_qk, kk > 0);
+                            ptx::mma_commit(&sm.bar.s_full[sb]);
+                        }
                     }
                 }
             } else if (ptx::elect_one()) {
-                // O += P . V; at a fold O starts over (its old value has been read by then)
+                // O += P . V (Half: the group's); at a fold O starts over (its old value has been read by then)
                 for (int u = 0; u < n_sub; ++u) {
                     const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
                     if (!wait.one(&sm.bar.p_full[sb], (u / kSub) & 1)) break;
                     ptx::tc_fence_after();
                     const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
-                    const bool more = C::kFold ? u % kFoldSub != 0 : u > 0;
+                    const bool more = C::kFp16 ? u >= kGroups : u % kFoldSub != 0;
+                    const uint32_t o = tmem + kColO + (C::kFp16 ? (u & 1) * kD : 0);
 #pragma unroll
                     for (int kk = 0; kk < C::kPTerms * kBS / 16; ++kk)
-                        ptx::mma_bf16_ts(tmem + kColO, tmem + sb * C::kBuf + kk * 8,
+                        ptx::mma_bf16_ts(o, tmem + sb * C::kBuf + kk * 8,
                                          b0 + (((kk & 3) * 2048) >> 4), idesc_pv, (more || kk > 0) ? 1u : 0u);
                     ptx::mma_commit(&sm.bar.s_free[sb]);
                     if ((u & 1) || u == n_sub - 1) ptx::mma_commit(&sm.bar.empty[s]);
@@ -459,175 +522,231 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t t0 = ptx::globaltimer();
             while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer() - t0 < kTimeoutNs) {
             }
-        } else {
+        } else if (C::kFp16 && warp >= kConvWarp) {
+            // ----------------------------------------------------------- tiles to fp16 ----
+            // Thread = (row, 64 dims) of both half tiles, in place, ahead of the score MMAs. The lanes start at
+            // different 16-byte chunks so that a warp's accesses spread over all banks.
+            const int r = (warp - kConvWarp) * 32 + lane;
+            for (int t = 0; t < n_tiles; ++t) {
+                const int ring = t + ro, st = ring % kStages;
+                if (!wait(&sm.bar.full[st], (ring / kStages) & 1)) break;
+                const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes + (r & 63) * 128;
+                const int t0 = (tile0 + t) * kBN;
+                uint32_t v[2][32];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        ld_shared_v4(v_s + j * kBS * 128 + ((c + lane) & 7) * 16, v[j] + 4 * c);
+                if (t0 + kBN > base) {
+                    // Rows that not every draft sees must not reach the others through 0 * NaN: a row past the
+                    // sequence's end, or a drafted one without a finite fp16 form, becomes zeros; a draft
+                    // that sees such a row gets NaN by its bit in `over`.
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int vt = t0 + j * kBS + (r & 63);
+                        bool over = false;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) over |= past_fp16(v[j][e]);
+                        if (over && vt >= base && vt < L)
+                            atomicOr(&sm.over[(vt - base) >> 5], 1u << ((vt - base) & 31));
+                        if (vt >= L || (over && vt >= base))
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[j][e] = 0u;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+#pragma unroll
+                        for (int e = 4 * c; e < 4 * c + 4; ++e)
+                            v[j][e] = pack_f16(__uint_as_float(v[j][e] << 16),
+                                               __uint_as_float(v[j][e] & 0xffff0000u));
+                        st_shared_v4(v_s + j * kBS * 128 + ((c + lane) & 7) * 16, v[j][4 * c], v[j][4 * c + 1],
+                                     v[j][4 * c + 2], v[j][4 * c + 3]);
+                    }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm.bar.v_full[t % kStages]);
+            }
+        }
+        if (!end(k)) break;
+        }
+    } else {
+        if constexpr (C::kFp16) ptx::regs_inc<kSoftmaxRegs>();
+        for (int si = 0;; ++si) {
+        const Part k = begin(si);
+        const uint32_t tmem = sm.tmem_base;
+        const bool has_drafts = k.has_drafts, whole = k.whole;
+        const TreeSegment &sg = k.sg;
+        const int m0 = k.blk.m0, rows = k.blk.rows, h = k.blk.h, hn = k.blk.hn;
+        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
             // ----------------------------------------------------- softmax, epilogue ----
             if (tid == 0) sm.seg[(si + 1) & 1] = next_segment(a, sg, x1 - x - n_tiles);
-            const int qd = warp & 3, hf = warp >> 2;     // lane quarter; group, and half of the columns
+            constexpr int kCols = kD / kGroups;             // columns of the query and of O per group
+            const int qd = warp & 3, grp = warp >> 2;    // lane quarter, group
             const int r = qd * 32 + lane;                // row = TMEM lane
             const int ri = r / hp, hh = r - ri * hp;     // draft and head within the block
             const bool live = ri < rows && hh < hn;
-            const int c0 = hf * 64;
+            const int c0 = grp * kCols;
+            const uint32_t own_o = tmem + kColO + (C::kFp16 ? grp * kD : 0);
             const uint32_t lane_base = (uint32_t)(qd * 32) << 16;
             const float sl2 = geo.scale * kLog2e;
-            const size_t row_id = (size_t)(q0 + m0 + ri) * geo.Hq + h + hh;   // of q and out
+            auto row_id = [&] { return (size_t)(q0 + m0 + ri) * geo.Hq + h + hh; };   // of q and out
             bool ok = true;
 
-            // Routed query row, this warp's 64 columns, times scale * log2 e, as bf16 terms
-            {
-                uint32_t q[64];
-                if (ro == 0) {
-                    // the composed query, as it is
-                    const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row_id * kD + c0);
+            // Routed query row, this group's columns, times scale * log2 e, as operand terms
+            uint32_t q[kCols];
+            if (ro == 0) {
+                // the composed query, as it is
+                const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row_id() * kD + c0);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                for (int c = 0; c < kCols / 8; ++c) {
+                    const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            q[8 * c + 2 * e] = w[e] << 16;
-                            q[8 * c + 2 * e + 1] = w[e] & 0xffff0000u;
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 64; ++e) q[e] = 0u;
-                    for (int i = 0; ok && i < ro; ++i) {
-                        ok = wait(&sm.bar.r_full[i & 1], (i >> 1) & 1);
-                        if (!ok) break;
-                        ptx::tc_fence_after();
-                        const bool mine = ro == 1 || hh == i;
-                        const uint32_t rc = tmem + (i & 1) * 128 + c0 + lane_base;
-#pragma unroll
-                        for (int c = 0; c < 64; c += 32) {
-                            uint32_t u[32];
-                            ptx::tmem_ld32(rc + c, u);
-                            ptx::tmem_wait_ld();
-                            ptx::reg_fence(u);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (mine) q[c + e] = u[e];
-                        }
-                        ptx::tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive(&sm.bar.r_free[i & 1]);
+                    for (int e = 0; e < 4; ++e) {
+                        q[8 * c + 2 * e] = w[e] << 16;
+                        q[8 * c + 2 * e + 1] = w[e] & 0xffff0000u;
                     }
                 }
-                if (ok) {
+            } else {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * sl2);
+                for (int e = 0; e < kCols; ++e) q[e] = 0u;
+                for (int i = 0; ok && i < ro; ++i) {
+                    ok = wait(&sm.bar.r_full[i & 1], (i >> 1) & 1);
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    const bool mine = ro == 1 || hh == i;
 #pragma unroll
-                    for (int t = 0; t < C::kQTerms; ++t) {
-                        uint32_t w[32];
+                    for (int c = 0; c < kCols; c += 32) {
+                        uint32_t u[32];
+                        ptx::tmem_ld32(tmem + (i & 1) * 128 + c0 + c + lane_base, u);
+                        ptx::tmem_wait_ld();
+                        ptx::reg_fence(u);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) w[e] = take_term(q[2 * e], q[2 * e + 1]);
-                        ptx::tmem_st32(tmem + kColQ + 64 * t + c0 / 2 + lane_base, w);
+                        for (int e = 0; e < 32; ++e)
+                            if (mine) q[c + e] = u[e];
                     }
-                    ptx::tmem_wait_st();
                     ptx::tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&sm.bar.qr_ready);
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.r_free[i & 1]);
                 }
+            }
+            if (ok) {
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * sl2);
+                if constexpr (C::kFp16) {
+                    // (the routing MMAs, the readers of the query block, are done)
+                    const uint32_t row = ptx::smem_addr(sm.q) + grp * kHalfBytes + r * 128;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = pack_f16(__uint_as_float(q[8 * c + 2 * e]), __uint_as_float(q[8 * c + 2 * e + 1]));
+                        st_shared_v4(row + ((c ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
+                    }
+                    ptx::fence_proxy_async_smem();
+                }
+#pragma unroll
+                for (int t = 0; t < (C::kFp16 ? 0 : C::kQTerms); ++t)
+#pragma unroll
+                    for (int c = 0; c < kCols / 2; c += 16) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            uint32_t &x0 = q[2 * (c + e)], &x1 = q[2 * (c + e) + 1];
+                            w[e] = take_term(x0, x1);
+                        }
+                        ptx::tmem_st16(tmem + kColQ + 64 * t + c0 / 2 + c + lane_base, w);
+                    }
+            }
+            if (ok) {
+                ptx::tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm.bar.qr_ready);
             }
 
-            // the drafts that this row's draft sees: itself and its ancestors
-            uint64_t anc_lo = 0, anc_hi = 0;
-            if (has_drafts) {
+            // the drafts that this row's draft sees: itself and its ancestors (walked where they are needed,
+            // in up to three half tiles of a unit)
+            auto ancestors = [&](uint64_t &lo, uint64_t &hi) {
+                lo = hi = 0;
                 for (int j = m0 + min(ri, rows - 1); j >= 0; j = sm.parent[j]) {
-                    if (j < 64) anc_lo |= 1ull << j;
-                    else anc_hi |= 1ull << (j - 64);
+                    if (j < 64) lo |= 1ull << j;
+                    else hi |= 1ull << (j - 64);
                 }
-            }
+            };
 
             float m_used = -INFINITY;  // the reference of this thread's share of the row sum
             float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
             float m_sum = -INFINITY;   // Full: the reference of sm.sum (group 0)
             bool okl = ok;
-            for (int u = hf; okl && u < n_sub; u += 2) {
+            for (int u = grp; okl && u < n_sub; u += kGroups) {
                 const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
                 const uint32_t sbuf = tmem + (uint32_t)sb * C::kBuf + lane_base;   // S, then P
-                const int ring = (u >> 1) + ro, st = ring % kStages;
                 const bool drafts_here = t0 + kBS > base;
-                // This thread's half (64 dims) of a cache row of the half tile. Half: converted to fp16
-                // while the scores are on their way. Rows that not every draft sees must not reach the
-                // others through 0 * NaN: a row past the sequence's end, or a drafted one that is not
-                // finite in the output MMAs' operand, becomes zeros for them (the score MMAs have read it by
-                // then: a draft that sees a NaN or infinity has a NaN score; one that sees a finite value
-                // beyond fp16's range gets NaN by its bit in `over`). The lanes start at different 16-byte
-                // chunks so that a warp's accesses spread over all banks.
-                const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes +
-                                     (hf * kBS + (r & 63)) * 128;
-                const int vt = t0 + (r & 63);
-                uint32_t vr[C::kFp16P ? 32 : 1];
-                bool zero = vt >= L;
-                if (C::kFp16P || drafts_here) {
-                    okl = wait(&sm.bar.full[st], (ring / kStages) & 1);
-                    if (!okl) break;
-                }
-                if constexpr (C::kFp16P) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) ld_shared_v4(v_s + ((c + lane) & 7) * 16, vr + 4 * c);
-                    if (drafts_here && vt >= base) {
-                        bool over = false;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            zero |= not_finite(vr[e]);
-                            over |= past_fp16(vr[e]);
-                        }
-                        if (over && !zero) atomicOr(&sm.over[(vt - base) >> 5], 1u << ((vt - base) & 31));
-                        zero |= over;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float x = __uint_as_float(vr[e] << 16), y = __uint_as_float(vr[e] & 0xffff0000u);
-                        vr[e] = zero ? 0u : pack_f16(x, y);
-                    }
-                } else if (drafts_here && vt >= base) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t v[4];
-                        ld_shared_v4(v_s + ((c + lane) & 7) * 16, v);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) zero |= not_finite(v[e]);
-                    }
-                }
-                okl = wait(&sm.bar.s_full[sb], (u / kSub) & 1);
+                okl = C::kFp16 ? wait(&sm.bar.s_full[(u >> 1) & 1], (u >> 2) & 1) : wait(&sm.bar.s_full[sb], (u / kSub) & 1);
                 if (!okl) break;
                 ptx::tc_fence_after();
+                if constexpr (!C::kFp16) {
+                    // Rows that not every draft sees must not reach the others through 0 * NaN: a row past the
+                    // sequence's end, or a drafted one that is not finite, becomes zeros for the output MMAs
+                    // (the score MMAs have read it: a draft that sees it has a NaN score).
+                    const int ring = (u >> 1) + ro, vt = t0 + (r & 63);
+                    if (drafts_here) {
+                        okl = wait(&sm.bar.full[ring % kStages], (ring / kStages) & 1);
+                        if (!okl) break;
+                    }
+                    if (drafts_here && vt >= base) {
+                        const uint32_t v_s = ptx::smem_addr(sm.tiles[ring % kStages]) + (r >> 6) * kHalfBytes +
+                                             ((u & 1) * kBS + (r & 63)) * 128;   // thread = (cache row, 64 dims)
+                        bool zero = vt >= L;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t v[4];
+                            ld_shared_v4(v_s + ((c + lane) & 7) * 16, v);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) zero |= not_finite(v[e]);
+                        }
+                        if (zero)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) st_shared_v4(v_s + c * 16, 0u, 0u, 0u, 0u);
+                    }
+                }
                 uint32_t s0[32], s1[32];
                 ptx::tmem_ld32(sbuf, s0);
                 ptx::tmem_ld32(sbuf + 32, s1);
-                if constexpr (C::kFp16P) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        st_shared_v4(v_s + ((c + lane) & 7) * 16, vr[4 * c], vr[4 * c + 1], vr[4 * c + 2],
-                                     vr[4 * c + 3]);
-                } else if (zero) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) st_shared_v4(v_s + c * 16, 0u, 0u, 0u, 0u);
-                }
                 ptx::tmem_wait_ld();
                 ptx::reg_fence(s0);
                 ptx::reg_fence(s1);
                 if (drafts_here) {
-                    const uint64_t vis = window64(anc_lo, anc_hi, t0 - base);
-                    const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
+                    uint64_t lo, hi;
+                    ancestors(lo, hi);
+                    const uint64_t see = window64(lo, hi, t0 - base);
+                    const uint32_t v0 = (uint32_t)see, v1 = (uint32_t)(see >> 32);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        if (!(v0 & (1u << c))) s0[c] = 0xff800000u;
-                        if (!(v1 & (1u << c))) s1[c] = 0xff800000u;
+                    for (int e = 0; e < 32; ++e) {
+                        if (!(v0 & (1u << e))) s0[e] = 0xff800000u;
+                        if (!(v1 & (1u << e))) s1[e] = 0xff800000u;
                     }
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    mx[0] = max3(mx[0], __uint_as_float(s0[c]), __uint_as_float(s0[c + 1]));
-                    mx[1] = max3(mx[1], __uint_as_float(s0[c + 2]), __uint_as_float(s0[c + 3]));
-                    mx[2] = max3(mx[2], __uint_as_float(s1[c]), __uint_as_float(s1[c + 1]));
-                    mx[3] = max3(mx[3], __uint_as_float(s1[c + 2]), __uint_as_float(s1[c + 3]));
+                for (int e = 0; e < 32; e += 4) {
+                    mx[0] = max3(mx[0], __uint_as_float(s0[e]), __uint_as_float(s0[e + 1]));
+                    mx[1] = max3(mx[1], __uint_as_float(s0[e + 2]), __uint_as_float(s0[e + 3]));
+                    mx[2] = max3(mx[2], __uint_as_float(s1[e]), __uint_as_float(s1[e + 1]));
+                    mx[3] = max3(mx[3], __uint_as_float(s1[e + 2]), __uint_as_float(s1[e + 3]));
                 }
                 float mt = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
                 float m_ref = -INFINITY;
-                if (u == 0) {
+                if constexpr (C::kFp16) {
+                    m_ref = m_used;                      // the group's own
+                } else if (u == 0) {
                     // the row's first reference is the maximum of its first two half tiles
                     if (n_sub > 1) {
                         okl = wait(&sm.bar.first[qd], 0);
@@ -640,16 +759,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                         __syncwarp();
                         if (lane == 0) ptx::mbar_arrive(&sm.bar.first[qd]);
                     }
-                    okl = wait(&sm.bar.turn[qd][hf ^ 1], ((u - 1) >> 1) & 1);
+                    okl = wait(&sm.bar.turn[qd][(u - 1) % kGroups], ((u - 1) / kGroups) & 1);
                     if (!okl) break;
-                    m_ref = sm.mref[hf ^ 1][r];
+                    m_ref = sm.mref[(u - 1) % kGroups][r];
                 }
                 const float m_new = fmaxf(m_ref, mt);
                 const bool moves = __any_sync(0xffffffffu, m_new > m_ref + kRescaleLog2);
-                const bool fold = C::kFold && u > 0 && u % kFoldSub == 0;
-                if (u > 0 && (moves || fold)) {
-                    // O holds half tiles .. u - 1 once the output MMAs of u - 1 are done
-                    okl = wait(&sm.bar.s_free[(u - 1) % kSub], ((u - 1) / kSub) & 1);
+                const bool fold = !C::kFp16 && u > 0 && u % kFoldSub == 0;
+                const int before = C::kFp16 ? u - kGroups : u - 1;   // the last half tile that O holds
+                if (before >= 0 && (moves || fold)) {
+                    okl = wait(&sm.bar.s_free[before % kSub], (before / kSub) & 1);
                     if (!okl) break;
                     ptx::tc_fence_after();
                 }
@@ -681,26 +800,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 // a new reference when the maximum grew by more than 2^7 (or is the first finite)
                 if (moves) {
-                    if (u > 0 && !fold) {
+                    if (before >= 0 && !fold) {
                         const float f =
                             (m_new == -INFINITY || m_ref == -INFINITY) ? 0.f : ptx::ex2(m_ref - m_new);
 #pragma unroll
                         for (int c = 0; c < 128; c += 32) {
                             uint32_t o[32];
-                            ptx::tmem_ld32(tmem + kColO + c + lane_base, o);
+                            ptx::tmem_ld32(own_o + c + lane_base, o);
                             ptx::tmem_wait_ld();
                             ptx::reg_fence(o);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            ptx::tmem_st32(tmem + kColO + c + lane_base, o);
+                            ptx::tmem_st32(own_o + c + lane_base, o);
                         }
                         ptx::tmem_wait_st();
                     }
                     m_ref = m_new;
                 }
-                sm.mref[hf][r] = m_ref;
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sm.bar.turn[qd][hf]);
+                if constexpr (!C::kFp16) {
+                    sm.mref[grp][r] = m_ref;
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.turn[qd][grp]);
+                }
                 // the group's sums move to this reference
                 if (__any_sync(0xffffffffu, m_ref != m_used)) {
                     const float f = m_used == -INFINITY ? 0.f : ptx::ex2(m_used - m_ref);
@@ -718,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                               make_float2(mr, mr));
                         const float2 pe = make_float2(ptx::ex2(d.x), ptx::ex2(d.y));
                         if (e & 1) lb = add2(lb, pe); else la = add2(la, pe);
-                        if constexpr (C::kFp16P) {
+                        if constexpr (C::kFp16) {
                             s[e] = pack_f16(pe.x, pe.y);
                         } else {
                             s[2 * e] = __float_as_uint(pe.x);
@@ -728,10 +849,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 };
                 weights(s0);
                 weights(s1);
-                if constexpr (C::kFp16P) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s0[16 + e] = s1[e];
-                    ptx::tmem_st32(sbuf, s0);
+                if constexpr (C::kFp16) {
+                    ptx::tmem_st16(sbuf, s0);
+                    ptx::tmem_st16(sbuf + 16, s1);
                 } else {
 #pragma unroll
                     for (int t = 0; t < C::kPTerms; ++t) {
@@ -746,43 +866,75 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 ptx::tmem_wait_st();
                 ptx::tc_fence_before();
-                // rows of the tile written here (generic-proxy stores) are read next by the output MMAs
-                if (C::kFp16P || drafts_here) ptx::fence_proxy_async_smem();
+                // rows zeroed here (generic-proxy stores) are read next by the output MMAs
+                if (!C::kFp16 && drafts_here) ptx::fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&sm.bar.p_full[sb]);
             }
 
-            // Epilogue: out = O / l, or the part's state (m, l, O); l is the two groups' shares at the
-            // reference of the last half tile. This warp's 64 output dims.
-            const int last = n_sub - 1, lb2 = last & 1;
-            if (okl && lb2 != hf) okl = wait(&sm.bar.turn[qd][lb2], (last >> 1) & 1);
-            const bool oke = okl && wait(&sm.bar.s_free[last % kSub], (last / kSub) & 1);
+            // Epilogue: out = O / l, or the part's state (m, l, O). Full: l is the groups' shares at the
+            // reference of the last half tile; Half: the groups' states are joined as parts are. This
+            // group's output dims.
+            const int last = n_sub - 1, lg = last % kGroups;
+            if (!C::kFp16 && okl && lg != grp) okl = wait(&sm.bar.turn[qd][lg], (last / kGroups) & 1);
+            bool oke = okl && wait(&sm.bar.s_free[last % kSub], (last / kSub) & 1);
+            if (C::kFp16 && oke && last > 0) oke = wait(&sm.bar.s_free[(last - 1) % kSub], ((last - 1) / kSub) & 1);
             float l = (la.x + la.y) + (lb.x + lb.y);
-            const float m_fin = sm.mref[lb2][r];
-            if (oke && lb2 != hf) l = m_used == -INFINITY ? 0.f : l * ptx::ex2(m_used - m_fin);
-            sm.lsum[hf][r] = l;
+            float m_fin = 0.f;
+            if constexpr (C::kFp16) {
+                sm.mref[grp][r] = m_used;
+            } else {
+                m_fin = sm.mref[lg][r];
+                if (oke && lg != grp) l = m_used == -INFINITY ? 0.f : l * ptx::ex2(m_used - m_fin);
+            }
+            sm.lsum[grp][r] = l;
             const bool okp = ptx::bar_and(kBarCompute, 32 * kComputeWarps, oke);
             if (okp) {
                 ptx::tc_fence_after();
-                float lt = l + sm.lsum[hf ^ 1][r];
-                if (C::kFp16P && has_drafts) {
+                float w0 = 1.f, w1 = 1.f;                    // of the groups' O
+                if constexpr (C::kFp16) {
+                    const float m0 = sm.mref[0][r], m1 = sm.mref[1][r];
+                    m_fin = fmaxf(m0, m1);
+                    // (a group that saw nothing has m = -inf, l = 0 and O = 0, or no O at all)
+                    w0 = m0 == -INFINITY ? 0.f : ptx::ex2(m0 - m_fin);
+                    w1 = m1 == -INFINITY ? 0.f : ptx::ex2(m1 - m_fin);
+                }
+                float lt = w0 * sm.lsum[0][r] + w1 * sm.lsum[1][r];
+                if (C::kFp16 && has_drafts) {
                     const uint64_t o0 = sm.over[0] | (uint64_t)sm.over[1] << 32;
                     const uint64_t o1 = sm.over[2] | (uint64_t)sm.over[3] << 32;
-                    if ((anc_lo & o0) | (anc_hi & o1)) lt = NAN;
+                    if (o0 | o1) {
+                        uint64_t lo, hi;
+                        ancestors(lo, hi);
+                        if ((lo & o0) | (hi & o1)) lt = NAN;
+                    }
                 }
                 const float f = !whole ? 1.f : lt == 0.f ? 0.f : 1.f / lt;
-                const bool folded = C::kFold && last >= kFoldSub;
+                const bool folded = !C::kFp16 && last >= kFoldSub;
                 float fs = 0.f;                              // of the sum
                 if (folded) fs = sm.fref[r] == -INFINITY ? 0.f : ptx::ex2(sm.fref[r] - m_fin);
                 // a part's state: [32 chunks of 4 dims][128 rows] float4, then [128 rows] {m, l}
                 uint8_t *state = a.states + (size_t)(2 * blockIdx.x + (si > 0)) * kTreeStateBytes;
-                float nf = lt * 0.f;                         // x * 0 is NaN exactly when x is not finite
-#pragma unroll
-                for (int c4 = 0; c4 < 2; ++c4) {
+                float nf = live ? lt * 0.f : 0.f;            // x * 0 is NaN exactly when x is not finite
+#pragma unroll 1
+                for (int c4 = 0; c4 < kCols / 32; ++c4) {
                     uint32_t u[32];
                     ptx::tmem_ld32(tmem + kColO + c0 + c4 * 32 + lane_base, u);
                     ptx::tmem_wait_ld();
                     ptx::reg_fence(u);
+                    if constexpr (C::kFp16) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * w0);
+                        if (n_sub > 1) {
+                            uint32_t v[32];
+                            ptx::tmem_ld32(tmem + kColO + kD + c0 + c4 * 32 + lane_base, v);
+                            ptx::tmem_wait_ld();
+                            ptx::reg_fence(v);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                u[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), w1, __uint_as_float(u[e])));
+                        }
+                    }
                     if (folded) {
                         const float4 *row = reinterpret_cast<const float4 *>(sm.sum) + r * 32;
 #pragma unroll
@@ -795,10 +947,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     if (live) {
-                        if (C::kFp16P)
+                        if (C::kFp16)
 #pragma unroll
                             for (int e = 0; e < 32; ++e) nf = fmaf(__uint_as_float(u[e]), 0.f, nf);
-                        float4 *o = whole ? reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row_id * kD) +
+                        float4 *o = whole ? reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row_id() * kD) +
                                                 c0 / 4 + c4 * 8
                                           : reinterpret_cast<float4 *>(state) + (c0 / 4 + c4 * 8) * kBM + r;
                         if (!whole || a.out_dtype == KL_FP32) {
@@ -809,7 +961,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                                 __uint_as_float(u[4 * c + 2]) * f, __uint_as_float(u[4 * c + 3]) * f);
                         } else {
                             uint4 *ob = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) +
-                                                                  row_id * kD + c0 + c4 * 32);
+                                                                  row_id() * kD + c0 + c4 * 32);
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 uint32_t w[4];
@@ -822,20 +974,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                 }
-                if (!whole && hf == 0 && live)
+                if (!whole && grp == 0 && live)
                     reinterpret_cast<float2 *>(state + kBM * kD * 4)[r] = make_float2(m_fin, lt);
-                if (C::kFp16P && __any_sync(0xffffffffu, nf != nf) && lane == 0) raise_flag(a.err, KL_FLAG_RANGE);
+                if (C::kFp16 && __any_sync(0xffffffffu, nf != nf) && lane == 0) raise_flag(a.err, KL_FLAG_RANGE);
             }
+        if (!end(k)) break;
         }
-
-        ptx::tc_fence_before();
-        __syncthreads();
-        ptx::tc_fence_after();
-        x += n_tiles;
-        if (x >= x1 || sm.abort) break;
     }
 
-    if (warp == kMmaWarp) ptx::tmem_dealloc(tmem, kTmemCols);
+    if (warp == kMmaWarp) ptx::tmem_dealloc(sm.tmem_base, kTmemCols);
 }
 
 // Merge of the parts of the units that lie in several runs: out = sum_s w_s O_s / sum_s w_s l_s with w_s =
@@ -956,7 +1103,7 @@ cudaError_t launch_tree_tc(const TreeArgs &a) {
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.ctas);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(full ? Warps<Full>::kThreads : Warps<Half>::kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
