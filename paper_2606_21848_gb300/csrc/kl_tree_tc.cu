@@ -63,15 +63,14 @@ constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 i
 // TMEM lane) take alternate half tiles. Tensor memory: kSub buffers of kBuf columns (64 of scores, then the
 // weights, 32 per term), then
 //   Half: an O of 128 columns for each group, which so keeps its own reference and never waits for the other
-//     (one O for both made each half tile's reference wait for the one before: 1.04 us per tile); the
-//     query, fp16, in shared memory; scores of a whole tile at once (N = 128, since with the query in
-//     shared memory N = 64 is bound by its reads); four warps convert tiles to fp16 ahead of that.
+//     (one O for both made each half tile's reference wait for the one before: 1.04 us per tile, 1.00 this
+//     way), and the query (64 columns); four warps convert tiles to fp16 ahead of the score MMAs.
 //   Full: one O, the query's terms (64 columns each).
 // The routed queries first land in columns 0 .. 255, before anything else is there.
 struct Half {
     static constexpr bool kFp16 = true;
-    static constexpr int kQTerms = 1, kPTerms = 1, kSub = 4, kConvWarps = 4, kStages = 5;
-    static constexpr uint32_t kBuf = 64, kColO = 256, kColQ = 0;
+    static constexpr int kQTerms = 1, kPTerms = 1, kSub = 3, kConvWarps = 4, kStages = 5;
+    static constexpr uint32_t kBuf = 64, kColO = 192, kColQ = 448;
 };
 struct Full {
     static constexpr bool kFp16 = false;
@@ -93,17 +92,16 @@ constexpr int kFoldSub = 4;           // Full: half tiles between two moves of O
 
 template <typename C>
 struct __align__(1024) TreeSmem {
-    uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B];
-                                           // Half: then the routed query, fp16
+    uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B]
     // Ring: the W^R matrices, then the cache tiles ([64-dim half][128 rows][128 B], SW128).
     uint8_t tiles[C::kStages][kTileBytes];
     float sum[C::kFp16 ? 4 : kBM * kD];    // Full: O of the half tiles folded so far, [row][128], its
                                            // 16-byte chunks c at c ^ (row % 32)
     // Barriers (set up anew for every segment): one completion per half tile u of its buffer u % kSub
-    // on p_full (its weights) and s_free (its output MMAs are done); on s_full per half tile (Full) or per
-    // tile t on t % 2 (Half; its scores), on v_full[t % kStages] (Half: its rows are fp16; by the tile's
-    // number and not by its ring slot, which W^R may have used before), and per lane quarter on
-    // turn[.][u % 2] (Full: the references after it).
+    // on s_full (its scores), p_full (its weights) and s_free (its output MMAs are done), on
+    // v_full[t % kStages] per tile t (Half: its rows are fp16; by the tile's number and not by its ring
+    // slot, which W^R may have used before), and per lane quarter on turn[.][u % 2] (Full: the references
+    // after it).
     struct Bars {
         uint64_t full[C::kStages], empty[C::kStages];
         uint64_t s_full[C::kSub], s_free[C::kSub];
@@ -126,12 +124,14 @@ struct __align__(1024) TreeSmem {
 };
 static_assert(sizeof(TreeSmem<Half>) + 1024 <= 227 * 1024 && sizeof(TreeSmem<Full>) + 1024 <= 227 * 1024, "");
 
-// Arrivals that complete a phase of barrier i (in the order of Bars).
+// Arrivals that complete a phase of barrier i (in the order of Bars) when `quarters` of the four lane quarters
+// hold rows (the softmax warps of the others rest).
 template <typename C>
-__device__ __forceinline__ uint32_t bar_count(int i) {
+__device__ __forceinline__ uint32_t bar_count(int i, int quarters) {
     using B = typename TreeSmem<C>::Bars;
-    if (i >= (int)(offsetof(B, p_full) / 8) && i < (int)(offsetof(B, turn) / 8)) return 4;
-    if (i >= (int)(offsetof(B, r_free) / 8) && i <= (int)(offsetof(B, qr_ready) / 8)) return Warps<C>::kCompute;
+    if (i >= (int)(offsetof(B, p_full) / 8) && i < (int)(offsetof(B, v_full) / 8)) return quarters;
+    if (i >= (int)(offsetof(B, v_full) / 8) && i < (int)(offsetof(B, turn) / 8)) return 4;
+    if (i >= (int)(offsetof(B, r_free) / 8) && i <= (int)(offsetof(B, qr_ready) / 8)) return kGroups * quarters;
     return 1;
 }
 
@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         uint64_t *const bars = reinterpret_cast<uint64_t *>(&sm.bar);
         if (tid < (int)(sizeof(sm.bar) / 8)) {
             if (si > 0) ptx::mbar_inval(bars + tid);
-            ptx::mbar_init(bars + tid, bar_count<C>(tid));
+            ptx::mbar_init(bars + tid, bar_count<C>(tid, (blk.rows * hp + 31) >> 5));
             ptx::fence_mbar_init();
         }
         if (tid < KL_TREE_MAX_DRAFTS / 32) sm.over[tid] = 0;
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             // half (kHalfBytes) every 4 steps; MN-major SW128 operands step 16 rows = 2 KiB; TMEM
             // A operands step 8 columns (16 packed 16-bit values).
             constexpr uint32_t idesc_qk =
-                C::kFp16 ? idesc_f16(128, kBN, false, false) : ptx::idesc_bf16(128, kBS, false, false);
+                C::kFp16 ? idesc_f16(128, kBS, false, false) : ptx::idesc_bf16(128, kBS, false, false);
             constexpr uint32_t idesc_route = ptx::idesc_bf16(128, 128, false, true);
             constexpr uint32_t idesc_pv = C::kFp16 ? idesc_f16(128, 128, false, true) : idesc_route;
             const uint64_t q_desc = ptx::smem_desc(ptx::smem_addr(sm.q), 16, 1024, ptx::kSwizzle128B);
@@ -467,34 +467,20 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 // (the loop by one lane: warp-wide waits between two half tiles leave the tensor cores idle)
                 if (ok && ptx::elect_one()) {
                     ptx::tc_fence_after();
-                    if constexpr (C::kFp16) {
-                        for (int t = 0; t < n_tiles; ++t) {
-                            if (!wait.one(&sm.bar.v_full[t % kStages], (t / kStages) & 1)) break;
-                            // the output MMAs of tile t - 2 have read these buffers' weights
-                            if (t > 1 && !(wait.one(&sm.bar.s_free[(2 * t) % kSub], ((t - 2) >> 1) & 1) &&
-                                           wait.one(&sm.bar.s_free[(2 * t + 1) % kSub], ((t - 2) >> 1) & 1)))
-                                break;
-                            ptx::tc_fence_after();
-                            const uint64_t b0 = k_desc + ((((t + ro) % kStages) * kTileBytes) >> 4);
+                    for (int u = 0; u < n_sub; ++u) {
+                        const int t = u >> 1, r = t + ro, s = r % kStages, sb = u % kSub;
+                        if (C::kFp16 ? !wait.one(&sm.bar.v_full[t % kStages], (t / kStages) & 1)
+                                     : !wait.one(&sm.bar.full[s], (r / kStages) & 1))
+                            break;
+                        // the output MMAs of half tile u - kSub have read this buffer's weights
+                        if (u >= kSub && !wait.one(&sm.bar.s_free[sb], (u / kSub - 1) & 1)) break;
+                        ptx::tc_fence_after();
+                        const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
 #pragma unroll
-                            for (int kk = 0; kk < kD / 16; ++kk)
-                                ptx::mma_bf16(tmem + (t & 1) * 2 * C::kBuf, q_desc + kstep(kk), b0 + kstep(kk),
-                                              idesc_qk, kk > 0);
-                            ptx::mma_commit(&sm.bar.s_full[t & 1]);
-                        }
-                    } else {
-                        for (int u = 0; u < n_sub; ++u) {
-                            const int r = (u >> 1) + ro, s = r % kStages, sb = u % kSub;
-                            if (!wait.one(&sm.bar.full[s], (r / kStages) & 1)) break;
-                            if (u >= kSub && !wait.one(&sm.bar.s_free[sb], (u / kSub - 1) & 1)) break;
-                            ptx::tc_fence_after();
-                            const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
-#pragma unroll
-                            for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
-                                ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
-                                                 idesc_qk, kk > 0);
-                            ptx::mma_commit(&sm.bar.s_full[sb]);
-                        }
+                        for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
+                            ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
+                                             idesc_qk, kk > 0);
+                        ptx::mma_commit(&sm.bar.s_full[sb]);
                     }
                 }
             } else if (ptx::elect_one()) {
@@ -587,6 +573,12 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             if (tid == 0) sm.seg[(si + 1) & 1] = next_segment(a, sg, x1 - x - n_tiles);
             constexpr int kCols = kD / kGroups;             // columns of the query and of O per group
             const int qd = warp & 3, grp = warp >> 2;    // lane quarter, group
+            const int quarters = (rows * hp + 31) >> 5;  // with rows of the block
+            if (qd >= quarters) {
+                (void)ptx::bar_and(kBarCompute, 32 * kComputeWarps, true);
+                if (!end(k)) break;
+                continue;
+            }
             const int r = qd * 32 + lane;                // row = TMEM lane
             const int ri = r / hp, hh = r - ri * hp;     // draft and head within the block
             const bool live = ri < rows && hh < hn;
@@ -638,28 +630,15 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             if (ok) {
 #pragma unroll
                 for (int e = 0; e < kCols; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * sl2);
-                if constexpr (C::kFp16) {
-                    // (the routing MMAs, the readers of the query block, are done)
-                    const uint32_t row = ptx::smem_addr(sm.q) + grp * kHalfBytes + r * 128;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = pack_f16(__uint_as_float(q[8 * c + 2 * e]), __uint_as_float(q[8 * c + 2 * e + 1]));
-                        st_shared_v4(row + ((c ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
-                    }
-                    ptx::fence_proxy_async_smem();
-                }
-#pragma unroll
-                for (int t = 0; t < (C::kFp16 ? 0 : C::kQTerms); ++t)
+                for (int t = 0; t < C::kQTerms; ++t)
 #pragma unroll
                     for (int c = 0; c < kCols / 2; c += 16) {
                         uint32_t w[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             uint32_t &x0 = q[2 * (c + e)], &x1 = q[2 * (c + e) + 1];
-                            w[e] = take_term(x0, x1);
+                            w[e] = C::kFp16 ? pack_f16(__uint_as_float(x0), __uint_as_float(x1)) : take_term(x0, x1);
                         }
                         ptx::tmem_st16(tmem + kColQ + 64 * t + c0 / 2 + c + lane_base, w);
                     }
@@ -689,21 +668,25 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
                 const uint32_t sbuf = tmem + (uint32_t)sb * C::kBuf + lane_base;   // S, then P
                 const bool drafts_here = t0 + kBS > base;
-                okl = C::kFp16 ? wait(&sm.bar.s_full[(u >> 1) & 1], (u >> 2) & 1) : wait(&sm.bar.s_full[sb], (u / kSub) & 1);
+                okl = wait(&sm.bar.s_full[sb], (u / kSub) & 1);
                 if (!okl) break;
                 ptx::tc_fence_after();
                 if constexpr (!C::kFp16) {
                     // Rows that not every draft sees must not reach the others through 0 * NaN: a row past the
                     // sequence's end, or a drafted one that is not finite, becomes zeros for the output MMAs
                     // (the score MMAs have read it: a draft that sees it has a NaN score).
-                    const int ring = (u >> 1) + ro, vt = t0 + (r & 63);
+                    const int ring = (u >> 1) + ro;
                     if (drafts_here) {
                         okl = wait(&sm.bar.full[ring % kStages], (ring / kStages) & 1);
                         if (!okl) break;
                     }
-                    if (drafts_here && vt >= base) {
-                        const uint32_t v_s = ptx::smem_addr(sm.tiles[ring % kStages]) + (r >> 6) * kHalfBytes +
-                                             ((u & 1) * kBS + (r & 63)) * 128;   // thread = (cache row, 64 dims)
+                    // thread = (cache row, 64 dims)
+#pragma unroll 1
+                    for (int i = r; drafts_here && i < kBM; i += 32 * quarters) {
+                        const int vt = t0 + (i & 63);
+                        if (vt < base) continue;
+                        const uint32_t v_s = ptx::smem_addr(sm.tiles[ring % kStages]) + (i >> 6) * kHalfBytes +
+                                             ((u & 1) * kBS + (i & 63)) * 128;
                         bool zero = vt >= L;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
