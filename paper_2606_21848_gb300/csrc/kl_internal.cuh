@@ -101,12 +101,19 @@ struct PrefillArgs {
     cudaStream_t stream;
 };
 
+// How all units' tiles are shared out among the runs: `each` to a run, one more to the first `extra`.
+struct TreeShare {
+    int64_t each;
+    int extra, runs;
+};
+
 // A unit that lies in several runs, for the merge of its parts (written by the first run that starts inside
 // it; rows 0: none).
 struct TreeMerge {
-    int64_t unit0, total;     // its first tile among all units' tiles, and their number
+    int64_t unit0;            // its first tile among all units' tiles
+    TreeShare share;
     int tiles, step;          // its tiles, and what cuts fall on multiples of
-    int runs, last;           // runs of the call, and the last that holds some of the unit
+    int last;                 // the last run that holds some of the unit
     int row0, rows, h, hn;    // its drafts (rows of q and out) and heads
 };
 

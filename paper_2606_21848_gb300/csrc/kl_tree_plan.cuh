@@ -15,9 +15,9 @@ struct TreePlan {
 
 constexpr int kTreeRows = 128;      // rows of a block
 constexpr int kTreeTile = 128;      // cache rows of a tile
-// Cuts inside a unit fall on multiples of this many tiles, and a run has at least as many: a part costs a
-// start and a state.
-constexpr int kTreeCut = 2;
+// A part costs a start, a state and the merge: units of up to kTreeRun tiles are not cut, and there are no more
+// runs than units or shares of kTreeRun tiles. Cuts fall on multiples of kTreeCut tiles.
+constexpr int kTreeRun = 8, kTreeCut = 2;
 // A part's state: O [32][128 rows] float4 and {m, l} [128 rows]. Every run has up to two parts.
 constexpr size_t kTreeStateBytes = kTreeRows * 128 * sizeof(float) + kTreeRows * 2 * sizeof(float);
 
@@ -34,8 +34,9 @@ inline TreePlan plan_tree(int B, int Hkv, int G, int max_q, int64_t max_tokens, 
         if (blocks_of(hp) < blocks_of(p.hp)) p.hp = hp;
     p.rpb = kTreeRows / p.hp;
     p.blocks = (int)blocks_of(p.hp);
-    const int64_t tiles = (max_tokens + kTreeTile - 1) / kTreeTile * (B > 0 ? B : 1) * Hkv * p.blocks;
-    const int64_t most = tiles / kTreeCut;
+    const int64_t units = (int64_t)(B > 0 ? B : 1) * Hkv * p.blocks;
+    const int64_t shared = (max_tokens + kTreeTile - 1) / kTreeTile * units / kTreeRun;
+    const int64_t most = shared > units ? shared : units;
     p.ctas = (int)(most < 1 ? 1 : most < sms ? most : sms);
     return p;
 }

@@ -109,7 +109,7 @@ struct __align__(1024) TreeSmem {
         uint64_t turn[4][kGroups];
         uint64_t first[4];                 // per lane quarter: the maxima of half tile 1 are in lsum[1]
         uint64_t r_full[2], r_free[2];     // routing results, alternating halves of columns 0 .. 255
-        uint64_t qr_ready, drain, drain2;
+        uint64_t qr_ready, par_ready, drain, drain2;
     } bar;
     float mref[kGroups][kBM];  // the rows' references after the last half tile of each group
     float lsum[kGroups][kBM];  // the groups' shares of the row sums, for the epilogue
@@ -117,7 +117,8 @@ struct __align__(1024) TreeSmem {
     int32_t parent[KL_TREE_MAX_DRAFTS];
     unsigned int over[KL_TREE_MAX_DRAFTS / 32];   // Half: drafts with a finite value beyond fp16's range
     TreeSegment seg[2];        // this segment and the next
-    int64_t warp_sum[Warps<C>::kThreads / 32];
+    int64_t warp_tiles[Warps<C>::kThreads / 32];
+    int warp_units[Warps<C>::kThreads / 32];
     int64_t x0, x1;            // this CTA's run
     uint32_t tmem_base;
     int abort;
@@ -167,22 +168,35 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int b, bool repor
 
 // Cuts inside a unit of `tiles` tiles fall on multiples of this.
 __device__ __forceinline__ int cut_step(const TreeArgs &a, int tiles) {
-    return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : kTreeCut;
+    return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : tiles <= kTreeRun ? tiles : kTreeCut;
 }
 
-// The start of run c of `runs` when `total` tiles are shared out, before it moves down to a cut.
-__device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { return total * c / runs; }
+// The start of run c when all units' tiles are shared out (`each` to a run, one more to the first `extra`),
+// before it moves down to a cut.
+__device__ __forceinline__ int64_t run_start(const TreeShare &s, int c) {
+    return s.each * c + min(c, s.extra);
+}
+// The run whose share holds tile x.
+__device__ __forceinline__ int run_of(const TreeShare &s, int64_t x) {
+    const int64_t first = (s.each + 1) * s.extra;
+    return x < first ? (int)(x / (s.each + 1)) : s.extra + (int)((x - first) / s.each);
+}
 
 // Finds this CTA's run: sm.x0, sm.x1 and the first segment; writes the CTA's entry for the merge. All
 // threads; ends behind a barrier. False if there is nothing to do.
 template <typename C>
 __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
+    constexpr int kThreads = Warps<C>::kThreads;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = blockIdx.x;
-    const int B = a.geo.B, per = (B + Warps<C>::kThreads - 1) / Warps<C>::kThreads;
+    const int B = a.geo.B, per = (B + kThreads - 1) / kThreads;
+    const int b0 = tid * per, b1 = min(B, b0 + per);
     int64_t mine = 0;
-    for (int b = tid * per; b < min(B, (tid + 1) * per); ++b) {
-        const TreeSeq s = tree_seq(a, b, c == 0);
-        mine += (int64_t)s.tiles * s.units;
+    int units = 0;
+    TreeSeq only = TreeSeq{0, 0, 0, 0, 0};           // (the sequence of a thread that has one)
+    for (int b = b0; b < b1; ++b) {
+        only = tree_seq(a, b, c == 0);
+        mine += (int64_t)only.tiles * only.units;
+        units += only.units;
     }
     int64_t upto = mine;                             // inclusive prefix
 #pragma unroll
@@ -190,35 +204,43 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += x;
     }
-    if (lane == 31) sm.warp_sum[warp] = upto;
+    units = __reduce_add_sync(0xffffffffu, units);
+    if (lane == 31) {
+        sm.warp_tiles[warp] = upto;
+        sm.warp_units[warp] = units;
+    }
     if (tid == 0) {
         sm.seg[0].n_tiles = 0;
         a.merge[c].rows = 0;
     }
     __syncthreads();
     int64_t total = 0;
+    units = 0;
 #pragma unroll
-    for (int w = 0; w < Warps<C>::kThreads / 32; ++w) {
-        if (w < warp) upto += sm.warp_sum[w];
-        total += sm.warp_sum[w];
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) upto += sm.warp_tiles[w];
+        total += sm.warp_tiles[w];
+        units += sm.warp_units[w];
     }
-    const int64_t most = total / kTreeCut;
-    const int runs = (int)(most < 1 ? 1 : most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x);
-    if (total == 0 || c >= runs) return false;
+    // as many runs as there are CTAs, while they have kTreeRun tiles or a unit each
+    const int64_t most = max((int64_t)units, total / kTreeRun);
+    const int runs = (int)(most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x);
+    if (c >= runs) return false;
+    const TreeShare share{total / runs, (int)(total % runs), runs};
     // the threads whose sequences hold the run's two ends move them down to a cut
     for (int end = 0; end < 2; ++end) {
-        int64_t x = run_start(total, c + end, runs);
+        const int64_t x = run_start(share, c + end);
         if (x == total) {
             if (tid == 0) sm.x1 = total;
             continue;
         }
         if (x < upto - mine || x >= upto) continue;
         int64_t start = upto - mine;
-        for (int b = tid * per; b < min(B, (tid + 1) * per); ++b) {
-            const TreeSeq s = tree_seq(a, b, false);
+        for (int b = b0; b < b1; ++b) {
+            const TreeSeq s = per == 1 ? only : tree_seq(a, b, false);
             const int64_t all = (int64_t)s.tiles * s.units;
             if (x < start + all) {
-                const int unit = (int)((x - start) / s.tiles);
+                const int unit = all <= INT32_MAX ? (int)(x - start) / s.tiles : (int)((x - start) / s.tiles);
                 const int64_t unit0 = start + (int64_t)unit * s.tiles;
                 const int step = cut_step(a, s.tiles), tile0 = (int)(x - unit0) / step * step;
                 if (end == 1) {
@@ -227,11 +249,10 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
                     sm.x0 = unit0 + tile0;
                     sm.seg[0] = TreeSegment{b, unit, tile0, s.tiles - tile0, s.q0, s.n, s.L, s.tiles, s.units};
                     // the first run that starts inside the unit announces its parts
-                    if (tile0 > 0 && run_start(total, c - 1, runs) < unit0 + step) {
+                    if (tile0 > 0 && run_start(share, c - 1) < unit0 + step) {
                         const TreeBlock k = tree_block(a, sm.seg[0]);
-                        a.merge[c] = TreeMerge{unit0, total, s.tiles, step, runs,
-                                               (int)(((unit0 + s.tiles) * runs - 1) / total), s.q0 + k.m0, k.rows,
-                                               k.h, k.hn};
+                        a.merge[c] = TreeMerge{unit0, share, s.tiles, step, run_of(share, unit0 + s.tiles - 1),
+                                               s.q0 + k.m0, k.rows, k.h, k.hn};
                     }
                 }
                 break;
@@ -240,9 +261,7 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         }
     }
     __syncthreads();
-    const int64_t left = sm.x1 - sm.x0;
-    if (left <= 0) return false;
-    return true;
+    return sm.x1 > sm.x0;
 }
 
 // The segment after `s` (which ends at x of the run): the next unit's start, or none (n_tiles 0).
@@ -286,9 +305,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int hp = a.hp, rpb = a.rpb;
 
-    grid_dep_wait();
-    const bool any = find_run(sm, a);
-    if (!any) return;
+    // (set up while the kernel ahead ends: nothing here touches global memory)
     if (tid == 0) sm.abort = 0;
     if (warp == kMmaWarp) {
         ptx::tmem_alloc(&sm.tmem_base, kTmemCols);
@@ -308,6 +325,14 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                                        (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
         ptx::fence_proxy_async_smem();
     }
+    grid_dep_wait();
+    ptx::tc_fence_before();
+    const bool any = find_run(sm, a);
+    ptx::tc_fence_after();
+    if (!any) {
+        if (warp == kMmaWarp) ptx::tmem_dealloc(sm.tmem_base, kTmemCols);
+        return;
+    }
     const int64_t x1 = sm.x1;
     int64_t x = sm.x0;
     const Waiter wait{&sm.abort, a.err};
@@ -325,7 +350,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         // The block: drafts m0 .. m0 + rows - 1, heads h .. h + hn - 1 of the group; row r of the 128 is
         // draft m0 + r / hp with head h + r % hp.
         const TreeBlock blk = tree_block(a, sg);
-        const int hn = blk.hn, q0 = sg.q0, n = sg.n, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int hn = blk.hn, n = sg.n, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
         const int base = L - n;                      // committed tokens
         const int n_sub = min(2 * n_tiles, (L + kBS - 1) / kBS - 2 * tile0);   // half tiles
         const bool has_drafts = (tile0 + n_tiles) * kBN > base;
@@ -340,13 +365,6 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             ptx::fence_mbar_init();
         }
         if (tid < KL_TREE_MAX_DRAFTS / 32) sm.over[tid] = 0;
-        // (a parent that is not an earlier draft or -1 counts as -1)
-        if (has_drafts && tid < n) {
-            const int p = a.parents[q0 + tid];
-            const bool fine = p >= -1 && p < tid;
-            if (!fine) raise_flag(a.err, KL_FLAG_BAD_TREE);
-            sm.parent[tid] = fine ? p : -1;
-        }
         ptx::tc_fence_before();
         __syncthreads();
         ptx::tc_fence_after();
@@ -380,6 +398,13 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             const int32_t *bt = a.block_table + (size_t)sg.b * geo.max_pages;
             int issued = 0;
             bool bad = false, ok = true;
+            // the drafts' parents, on their way while the first copies are issued
+            constexpr int kPer = KL_TREE_MAX_DRAFTS / 32;
+            int32_t parent[kPer];
+            if (k.has_drafts)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    parent[i] = i * 32 + lane < sg.n ? a.parents[q0 + i * 32 + lane] : -1;
             // W^R matrices (B operand of the routing MMAs); the first brings the query block along
             for (int r = 0; r < ro; ++r) {
                 const int s = r % kStages;
@@ -396,6 +421,20 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 }
                 __syncwarp();
                 issued = r + 1;
+            }
+            if (k.has_drafts) {
+                // (one that is not an earlier draft or -1 counts as -1)
+                bool wrong = false;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int j = i * 32 + lane;
+                    const bool fine = parent[i] >= -1 && parent[i] < j;
+                    wrong |= !fine;
+                    sm.parent[j] = fine ? parent[i] : -1;
+                }
+                if (wrong) raise_flag(a.err, KL_FLAG_BAD_TREE);
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm.bar.par_ready);
             }
             for (int i = 0; ok && i < n_tiles; ++i) {
                 const int r = i + ro, s = r % kStages;
@@ -708,6 +747,8 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 ptx::reg_fence(s1);
                 if (drafts_here) {
                     uint64_t lo, hi;
+                    okl = wait(&sm.bar.par_ready, 0);
+                    if (!okl) break;
                     ancestors(lo, hi);
                     const uint64_t see = window64(lo, hi, t0 - base);
                     const uint32_t v0 = (uint32_t)see, v1 = (uint32_t)(see >> 32);
@@ -888,6 +929,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     const uint64_t o1 = sm.over[2] | (uint64_t)sm.over[3] << 32;
                     if (o0 | o1) {
                         uint64_t lo, hi;
+                        (void)wait(&sm.bar.par_ready, 0);
                         ancestors(lo, hi);
                         if ((lo & o0) | (hi & o1)) lt = NAN;
                     }
@@ -970,48 +1012,71 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
 
 // Merge of the parts of the units that lie in several runs: out = sum_s w_s O_s / sum_s w_s l_s with w_s =
 // 2^(m_s - M) and M the largest m_s of a part with l_s > 0. CTA (c, y): the unit that run c enters first
-// inside, dims 8 y .. + 7; thread = row and 4 dims. (One sequence of 131072 tokens, 8 heads, 19 parts
-// each: about 3 us behind the attention.)
-constexpr int kMergeThreads = 2 * kBM;
+// inside, dims 8 y .. + 7; thread = row and 4 dims, kMergeAhead parts in flight against a running M.
+constexpr int kMergeThreads = 2 * kBM, kMergeAhead = 8;
+constexpr int kMaxRuns = 512;                        // (SMs: one run each)
 
 __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const TreeArgs a) {
+    __shared__ const uint8_t *part[kMaxRuns];
+    __shared__ int parts;
     grid_dep_wait();
     grid_dep_launch();
-    const int c = blockIdx.x + 1;
+    const int c = blockIdx.x + 1, tid = threadIdx.x;
     const TreeMerge t = a.merge[c];
-    const int r = threadIdx.x % kBM, chunk = blockIdx.y * 2 + threadIdx.x / kBM;
+    if (t.rows == 0) return;
+    if (tid < 32) {
+        // The runs from c - 1 on that hold some of the unit; a run's first state where it starts inside it.
+        auto cut = [&](int run) {
+            const int64_t x = run_start(t.share, run) - t.unit0;
+            return x >= t.tiles ? t.tiles : x <= 0 ? 0 : (int)x / t.step * t.step;
+        };
+        int n = 0;
+        for (int r0 = c - 1; r0 <= t.last; r0 += 32) {
+            const int run = r0 + tid;
+            const bool some = run <= t.last && cut(run) < cut(run + 1);
+            const unsigned all = __ballot_sync(0xffffffffu, some);
+            if (some)
+                part[n + __popc(all & ((1u << tid) - 1))] =
+                    a.states + (size_t)(2 * run + (run_start(t.share, run) < t.unit0)) * kTreeStateBytes;
+            n += __popc(all);
+        }
+        if (tid == 0) parts = n;
+    }
+    __syncthreads();
+    const int r = tid % kBM, chunk = blockIdx.y * 2 + tid / kBM;
     const int ri = r / a.hp, hh = r - ri * a.hp;
     if (ri >= t.rows || hh >= t.hn) return;
-    // part i is run c - 1 + i's; its state is the run's first where the run starts inside the unit
-    const int first = c - 1, parts = t.last - first + 1;
-    auto cut = [&](int run) -> int64_t {
-        const int64_t x = run_start(t.total, run, t.runs) - t.unit0;
-        return x >= t.tiles ? t.tiles : x <= 0 ? 0 : x / t.step * t.step;
-    };
-    auto state = [&](int i) {
-        const int run = first + i;
-        return a.states + (size_t)(2 * run + (run_start(t.total, run, t.runs) < t.unit0)) * kTreeStateBytes;
-    };
-    float M = -INFINITY;
-    for (int i = 0; i < parts; ++i) {
-        if (cut(first + i) == cut(first + i + 1)) continue;          // (nothing of the unit in this run)
-        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(state(i) + kBM * kD * 4) + r);
-        if (ml.y != 0.f) M = fmaxf(M, ml.x);
-    }
-    float z = 0.f;
+    float M = -INFINITY, z = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
-        if (cut(first + i) == cut(first + i + 1)) continue;
-        const uint8_t *s = state(i);
-        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(s + kBM * kD * 4) + r);
-        const float4 o = __ldcg(reinterpret_cast<const float4 *>(s) + chunk * kBM + r);
-        const float w = ml.y == 0.f ? 0.f : ptx::ex2(ml.x - M);      // (l = 0: the row sees nothing there)
-        z = fmaf(w, ml.y, z);
-        acc.x = fmaf(w, o.x, acc.x);
-        acc.y = fmaf(w, o.y, acc.y);
-        acc.z = fmaf(w, o.z, acc.z);
-        acc.w = fmaf(w, o.w, acc.w);
+    for (int i = 0; i < parts; i += kMergeAhead) {
+        float2 ml[kMergeAhead];
+        float4 o[kMergeAhead];
+        float top = M;
+#pragma unroll
+        for (int e = 0; e < kMergeAhead; ++e) {
+            ml[e] = make_float2(-INFINITY, 0.f);
+            o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i + e < parts) {
+                ml[e] = __ldcg(reinterpret_cast<const float2 *>(part[i + e] + kBM * kD * 4) + r);
+                o[e] = __ldcg(reinterpret_cast<const float4 *>(part[i + e]) + chunk * kBM + r);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kMergeAhead; ++e)
+            if (ml[e].y != 0.f) top = fmaxf(top, ml[e].x);           // (l = 0: the row sees nothing there)
+        const float f = M == -INFINITY ? 0.f : ptx::ex2(M - top);
+        M = top;
+        z *= f;
+        acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+#pragma unroll
+        for (int e = 0; e < kMergeAhead; ++e) {
+            const float w = ml[e].y == 0.f ? 0.f : ptx::ex2(ml[e].x - M);
+            z = fmaf(w, ml[e].y, z);
+            acc.x = fmaf(w, o[e].x, acc.x);
+            acc.y = fmaf(w, o[e].y, acc.y);
+            acc.z = fmaf(w, o[e].z, acc.z);
+            acc.w = fmaf(w, o[e].w, acc.w);
+        }
     }
     const float inv = z == 0.f ? 0.f : 1.f / z;
     const size_t at = ((size_t)(t.row0 + ri) * a.geo.Hq + t.h + hh) * kD + 4 * chunk;
@@ -1091,7 +1156,10 @@ cudaError_t launch_tree_tc(const TreeArgs &a) {
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
     e = cudaLaunchKernelEx(&cfg, kernel, vmap, wmap, qmap, a);
-    if (e != cudaSuccess || a.ctas == 1 || a.num_splits == 1) return e;
+    // (units of up to kTreeRun tiles are not cut)
+    const int64_t most_tiles = ((int64_t)g.max_pages * g.P + kBN - 1) / kBN;
+    if (e != cudaSuccess || a.ctas == 1 || a.num_splits == 1 || (a.num_splits == 0 && most_tiles <= kTreeRun))
+        return e;
     cfg.gridDim = dim3((unsigned)a.ctas - 1, kD / 8);
     cfg.blockDim = dim3(kMergeThreads);
     cfg.dynamicSmemBytes = 0;

@@ -117,5 +117,5 @@ def test_layouts_cover_all_rows(plan, G):
                 assert 1 <= hp <= G and hp * rpb <= 128
                 assert blocks == -(-G // hp) * -(-n // rpb)
                 assert blocks <= G * -(-n // 128)
-                tiles = -(-tokens // 128) * max(B, 1) * 2 * blocks
-                assert 1 <= ctas <= 152 and (ctas == 152 or ctas == max(1, tiles // 2))
+                units = max(B, 1) * 2 * blocks
+                assert ctas == min(152, max(units, -(-tokens // 128) * units // 8))
