@@ -101,7 +101,7 @@ struct PrefillArgs {
     cudaStream_t stream;
 };
 
-// How all units' tiles are shared out among the runs: `each` to a run, one more to the first `extra`.
+// How the line of all units is shared out among the runs: `each` to a run, one more to the first `extra`.
 struct TreeShare {
     int64_t each;
     int extra, runs;
@@ -110,7 +110,7 @@ struct TreeShare {
 // A unit that lies in several runs, for the merge of its parts (written by the first run that starts inside
 // it; rows 0: none).
 struct TreeMerge {
-    int64_t unit0;            // its first tile among all units' tiles
+    int64_t unit0;            // its start on the line of all units
     TreeShare share;
     int tiles, step;          // its tiles, and what cuts fall on multiples of
     int last;                 // the last run that holds some of the unit
@@ -140,9 +140,10 @@ struct TreeArgs {
     cudaStream_t stream;
 };
 
-// A segment: the part of a unit (sequence b, its block `unit`) that lies in a run.
+// A segment, the part of a unit (sequence b, its block `unit`) that lies in a run: from tile0 on.
 struct TreeSegment {
-    int b, unit, tile0, n_tiles;
+    int64_t unit0;                // the unit's start on the line of all units
+    int b, unit, tile0;
     int q0, n, L, tiles, units;   // of the sequence: drafts, length, tiles per unit, units
 };
 

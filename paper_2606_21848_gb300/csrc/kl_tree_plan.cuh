@@ -18,6 +18,8 @@ constexpr int kTreeTile = 128;      // cache rows of a tile
 // A part costs a start, a state and the merge: units of up to kTreeRun tiles are not cut, and there are no more
 // runs than units or shares of kTreeRun tiles. Cuts fall on multiples of kTreeCut tiles.
 constexpr int kTreeRun = 8, kTreeCut = 2;
+// What starting a segment takes, in tiles (about 5 us), in the runs' shares.
+constexpr int kTreeStart = 5;
 // A part's state: O [32][128 rows] float4 and {m, l} [128 rows]. Every run has up to two parts.
 constexpr size_t kTreeStateBytes = kTreeRows * 128 * sizeof(float) + kTreeRows * 2 * sizeof(float);
 
@@ -35,7 +37,7 @@ inline TreePlan plan_tree(int B, int Hkv, int G, int max_q, int64_t max_tokens, 
     p.rpb = kTreeRows / p.hp;
     p.blocks = (int)blocks_of(p.hp);
     const int64_t units = (int64_t)(B > 0 ? B : 1) * Hkv * p.blocks;
-    const int64_t shared = (max_tokens + kTreeTile - 1) / kTreeTile * units / kTreeRun;
+    const int64_t shared = ((max_tokens + kTreeTile - 1) / kTreeTile + kTreeStart) * units / (kTreeRun + kTreeStart);
     const int64_t most = shared > units ? shared : units;
     p.ctas = (int)(most < 1 ? 1 : most < sms ? most : sms);
     return p;

@@ -119,7 +119,7 @@ struct __align__(1024) TreeSmem {
     TreeSegment seg[2];        // this segment and the next
     int64_t warp_tiles[Warps<C>::kThreads / 32];
     int warp_units[Warps<C>::kThreads / 32];
-    int64_t x0, x1;            // this CTA's run
+    int64_t x0, x1;            // this CTA's run, moved down to cuts
     uint32_t tmem_base;
     int abort;
 };
@@ -144,6 +144,10 @@ __device__ __forceinline__ uint64_t window64(uint64_t lo, uint64_t hi, int off) 
 }
 
 // ---------------------------------------------------------------------- runs and segments ----
+//
+// All units lie end to end on one line, each as kTreeStart (what starting a segment takes, in tiles) and its
+// tiles; the runs are equal shares of it. A run's start moves down to a cut: the unit's start, or a multiple
+// of the unit's step among its tiles.
 
 // Sequence b as the units see it: its drafts, length, tiles per unit and units (0 where it has none).
 struct TreeSeq {
@@ -171,15 +175,23 @@ __device__ __forceinline__ int cut_step(const TreeArgs &a, int tiles) {
     return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : tiles <= kTreeRun ? tiles : kTreeCut;
 }
 
-// The start of run c when all units' tiles are shared out (`each` to a run, one more to the first `extra`),
-// before it moves down to a cut.
+// Quotients of what mostly fits 32 bits (the 64-bit division takes most of a microsecond).
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+    return (x | y) <= INT32_MAX ? (int)x / (int)y : x / y;
+}
+
+// The start of run c of the line that `s` shares out, and the run whose share holds x.
 __device__ __forceinline__ int64_t run_start(const TreeShare &s, int c) {
     return s.each * c + min(c, s.extra);
 }
-// The run whose share holds tile x.
 __device__ __forceinline__ int run_of(const TreeShare &s, int64_t x) {
     const int64_t first = (s.each + 1) * s.extra;
-    return x < first ? (int)(x / (s.each + 1)) : s.extra + (int)((x - first) / s.each);
+    return x < first ? (int)quotient(x, s.each + 1) : s.extra + (int)quotient(x - first, s.each);
+}
+
+// The tile of a unit (`off` past its start on the line) that a run's start moves down to.
+__device__ __forceinline__ int cut_tile(int64_t off, int tiles, int step) {
+    return off <= kTreeStart ? 0 : off >= kTreeStart + tiles ? tiles : ((int)off - kTreeStart) / step * step;
 }
 
 // Finds this CTA's run: sm.x0, sm.x1 and the first segment; writes the CTA's entry for the merge. All
@@ -195,7 +207,7 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
     TreeSeq only = TreeSeq{0, 0, 0, 0, 0};           // (the sequence of a thread that has one)
     for (int b = b0; b < b1; ++b) {
         only = tree_seq(a, b, c == 0);
-        mine += (int64_t)only.tiles * only.units;
+        mine += (int64_t)(only.tiles + kTreeStart) * only.units;
         units += only.units;
     }
     int64_t upto = mine;                             // inclusive prefix
@@ -209,10 +221,7 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         sm.warp_tiles[warp] = upto;
         sm.warp_units[warp] = units;
     }
-    if (tid == 0) {
-        sm.seg[0].n_tiles = 0;
-        a.merge[c].rows = 0;
-    }
+    if (tid == 0) a.merge[c].rows = 0;
     __syncthreads();
     int64_t total = 0;
     units = 0;
@@ -223,10 +232,11 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         units += sm.warp_units[w];
     }
     // as many runs as there are CTAs, while they have kTreeRun tiles or a unit each
-    const int64_t most = max((int64_t)units, total / kTreeRun);
+    const int64_t most = max((int64_t)units, total / (kTreeRun + kTreeStart));
     const int runs = (int)(most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x);
     if (c >= runs) return false;
-    const TreeShare share{total / runs, (int)(total % runs), runs};
+    const int64_t each = quotient(total, runs);
+    const TreeShare share{each, (int)(total - each * runs), runs};
     // the threads whose sequences hold the run's two ends move them down to a cut
     for (int end = 0; end < 2; ++end) {
         const int64_t x = run_start(share, c + end);
@@ -238,21 +248,24 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         int64_t start = upto - mine;
         for (int b = b0; b < b1; ++b) {
             const TreeSeq s = per == 1 ? only : tree_seq(a, b, false);
-            const int64_t all = (int64_t)s.tiles * s.units;
+            const int len = s.tiles + kTreeStart;
+            const int64_t all = (int64_t)len * s.units;
             if (x < start + all) {
-                const int unit = all <= INT32_MAX ? (int)(x - start) / s.tiles : (int)((x - start) / s.tiles);
-                const int64_t unit0 = start + (int64_t)unit * s.tiles;
-                const int step = cut_step(a, s.tiles), tile0 = (int)(x - unit0) / step * step;
+                const int unit = (int)quotient(x - start, len);
+                const int64_t unit0 = start + (int64_t)unit * len;
+                const int step = cut_step(a, s.tiles), tile0 = cut_tile(x - unit0, s.tiles, step);
+                const int64_t at = tile0 ? unit0 + kTreeStart + tile0 : unit0;
                 if (end == 1) {
-                    sm.x1 = unit0 + tile0;
+                    sm.x1 = at;
                 } else {
-                    sm.x0 = unit0 + tile0;
-                    sm.seg[0] = TreeSegment{b, unit, tile0, s.tiles - tile0, s.q0, s.n, s.L, s.tiles, s.units};
+                    sm.x0 = at;
+                    sm.seg[0] = TreeSegment{unit0, b, unit, tile0, s.q0, s.n, s.L, s.tiles, s.units};
                     // the first run that starts inside the unit announces its parts
-                    if (tile0 > 0 && run_start(share, c - 1) < unit0 + step) {
+                    if (tile0 > 0 && cut_tile(run_start(share, c - 1) - unit0, s.tiles, step) == 0) {
                         const TreeBlock k = tree_block(a, sm.seg[0]);
-                        a.merge[c] = TreeMerge{unit0, share, s.tiles, step, run_of(share, unit0 + s.tiles - 1),
-                                               s.q0 + k.m0, k.rows, k.h, k.hn};
+                        a.merge[c] = TreeMerge{unit0, share, s.tiles, step,
+                                               run_of(share, unit0 + kTreeStart + s.tiles - 1), s.q0 + k.m0, k.rows,
+                                               k.h, k.hn};
                     }
                 }
                 break;
@@ -264,28 +277,24 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
     return sm.x1 > sm.x0;
 }
 
-// The segment after `s` (which ends at x of the run): the next unit's start, or none (n_tiles 0).
-__device__ __forceinline__ TreeSegment next_segment(const TreeArgs &a, const TreeSegment &s, int64_t left) {
+// The segment after `s` in a run that goes on behind s's unit: the next unit.
+__device__ __forceinline__ TreeSegment next_segment(const TreeArgs &a, const TreeSegment &s) {
     TreeSegment t = s;
+    t.unit0 = s.unit0 + kTreeStart + s.tiles;
     t.tile0 = 0;
-    if (left <= 0) {
-        t.n_tiles = 0;
-        return t;
-    }
     if (++t.unit == s.units) {
         t.unit = 0;
         TreeSeq q;
         do {
             ++t.b;
             q = tree_seq(a, t.b, false);
-        } while (q.units == 0);                      // (tiles are left, so a sequence follows)
+        } while (q.units == 0);                      // (the line goes on, so a sequence follows)
         t.q0 = q.q0;
         t.n = q.n;
         t.L = q.L;
         t.tiles = q.tiles;
         t.units = q.units;
     }
-    t.n_tiles = (int)(left < t.tiles ? left : t.tiles);
     return t;
 }
 
@@ -334,23 +343,24 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         return;
     }
     const int64_t x1 = sm.x1;
-    int64_t x = sm.x0;
     const Waiter wait{&sm.abort, a.err};
 
     // One segment's start for all threads: its block, the barriers, the drafts' parents
     struct Part {
         TreeSegment sg;
         TreeBlock blk;
-        int n_sub, ro;         // half tiles; ring positions of W^R matrices
-        bool has_drafts, whole;
+        int n_tiles, n_sub;    // tiles, half tiles
+        int ro;                // ring positions of W^R matrices
+        bool has_drafts, whole, more;
     };
     auto begin = [&](int si) -> Part {
-        TreeSegment sg = sm.seg[si & 1];
-        if (sg.n_tiles > x1 - x) sg.n_tiles = (int)(x1 - x);
+        const TreeSegment sg = sm.seg[si & 1];
+        const bool more = x1 > sg.unit0 + kTreeStart + sg.tiles;     // the run goes on behind the unit
+        const int n_tiles = (int)min((int64_t)sg.tiles, x1 - sg.unit0 - kTreeStart) - sg.tile0;
         // The block: drafts m0 .. m0 + rows - 1, heads h .. h + hn - 1 of the group; row r of the 128 is
         // draft m0 + r / hp with head h + r % hp.
         const TreeBlock blk = tree_block(a, sg);
-        const int hn = blk.hn, n = sg.n, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int hn = blk.hn, n = sg.n, L = sg.L, tile0 = sg.tile0;
         const int base = L - n;                      // committed tokens
         const int n_sub = min(2 * n_tiles, (L + kBS - 1) / kBS - 2 * tile0);   // half tiles
         const bool has_drafts = (tile0 + n_tiles) * kBN > base;
@@ -369,15 +379,14 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         __syncthreads();
         ptx::tc_fence_after();
         if (si == 0) grid_dep_launch();
-        return Part{sg, blk, n_sub, ro, has_drafts, whole};
+        return Part{sg, blk, n_tiles, n_sub, ro, has_drafts, whole, more};
     };
     // ... and its end; false after the run's last
     auto end = [&](const Part &k) {
         ptx::tc_fence_before();
         __syncthreads();
         ptx::tc_fence_after();
-        x += k.sg.n_tiles;
-        return x < x1 && !sm.abort;
+        return k.more && !sm.abort;
     };
 
     if (warp >= kComputeWarps) {
@@ -387,7 +396,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         const uint32_t tmem = sm.tmem_base;
         const TreeSegment &sg = k.sg;
         const int m0 = k.blk.m0, h = k.blk.h, g = k.blk.g;
-        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = k.n_tiles;
         const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
         if (warp == kProducerWarp) {
             // -------------------------------------------------------------- producer ----
@@ -606,10 +615,10 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         const bool has_drafts = k.has_drafts, whole = k.whole;
         const TreeSegment &sg = k.sg;
         const int m0 = k.blk.m0, rows = k.blk.rows, h = k.blk.h, hn = k.blk.hn;
-        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = sg.n_tiles;
+        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = k.n_tiles;
         const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
             // ----------------------------------------------------- softmax, epilogue ----
-            if (tid == 0) sm.seg[(si + 1) & 1] = next_segment(a, sg, x1 - x - n_tiles);
+            if (tid == 0 && k.more) sm.seg[(si + 1) & 1] = next_segment(a, sg);
             constexpr int kCols = kD / kGroups;             // columns of the query and of O per group
             const int qd = warp & 3, grp = warp >> 2;    // lane quarter, group
             const int quarters = (rows * hp + 31) >> 5;  // with rows of the block
@@ -1026,10 +1035,7 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const TreeArg
     if (t.rows == 0) return;
     if (tid < 32) {
         // The runs from c - 1 on that hold some of the unit; a run's first state where it starts inside it.
-        auto cut = [&](int run) {
-            const int64_t x = run_start(t.share, run) - t.unit0;
-            return x >= t.tiles ? t.tiles : x <= 0 ? 0 : (int)x / t.step * t.step;
-        };
+        auto cut = [&](int run) { return cut_tile(run_start(t.share, run) - t.unit0, t.tiles, t.step); };
         int n = 0;
         for (int r0 = c - 1; r0 <= t.last; r0 += 32) {
             const int run = r0 + tid;
