@@ -366,17 +366,30 @@ SharedLayout shared_layout(size_t counters, size_t state_bytes, size_t extra_byt
 }
 
 // Geometry and layout of a tree-attention call, and the workspace behind the shared front region: the
-// runs' entries for the merge, then their states (none of which a decode's counters ever share).
+// runs' entries for the merge, then their states (none of which a decode's counters ever share). `wide`: on
+// the wide decode's kernel, with its split plan, counters in the front region and split states.
 kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t num_splits,
-                         Geometry *g, TreePlan *p, SharedLayout *w) {
-    const kl_status st = resolve(shape, -1, g);
+                         bool wide, Geometry *g, TreePlan *p, SharedLayout *w) {
+    const kl_status st = resolve(shape, wide ? num_splits : -1, g);
     if (st != KL_OK) return st;
     if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits) return KL_ERR_INVALID_ARG;
     if (max_q_len > KL_TREE_MAX_DRAFTS) return KL_ERR_UNSUPPORTED;
+    if (wide) {
+        const size_t rows = (size_t)g->B * g->Hq * max_q_len * g->S;
+        *w = shared_layout((size_t)g->B * g->Hkv, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
+        return KL_OK;
+    }
     *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P,
                    device_sm_count());
     *w = shared_layout(0, p->ctas * sizeof(TreeMerge), p->ctas * 2 * kTreeStateBytes);
     return KL_OK;
+}
+
+// Whether a call can run on the wide decode's kernel: few rows per value head, one W^R each; and outputs whose
+// rounding hides the pair operands' error (3e-6).
+bool tree_wide(const kl_shape *s, int32_t max_q_len, bool fp32) {
+    return !fp32 && s && s->num_kv_heads > 0 && !s->wr_per_query_head && max_q_len > 0 &&
+           (int64_t)(s->num_q_heads / s->num_kv_heads) * max_q_len <= kTreeWideRows;
 }
 
 }  // namespace
@@ -387,8 +400,11 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
                               int32_t num_splits) {
     Geometry g;
     TreePlan p;
-    SharedLayout w;
-    return plan_tree_call(shape, total_q, max_q_len, num_splits, &g, &p, &w) == KL_OK ? w.total : 0;
+    SharedLayout w, ww{0, 0, 0};
+    if (plan_tree_call(shape, total_q, max_q_len, num_splits, false, &g, &p, &w) != KL_OK) return 0;
+    if (tree_wide(shape, max_q_len, false))
+        (void)plan_tree_call(shape, total_q, max_q_len, num_splits, true, &g, &p, &ww);
+    return w.total > ww.total ? w.total : ww.total;
 }
 
 kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
@@ -400,7 +416,8 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     Geometry g;
     TreePlan p;
     SharedLayout w;
-    const kl_status st = plan_tree_call(shape, total_q, max_q_len, num_splits, &g, &p, &w);
+    const bool wide = tree_wide(shape, max_q_len, out_dtype == KL_FP32);
+    const kl_status st = plan_tree_call(shape, total_q, max_q_len, num_splits, wide, &g, &p, &w);
     if (st != KL_OK) return st;
     if (!prefill_tc_supported(g)) return KL_ERR_UNSUPPORTED;
     if (g.B == 0 || total_q == 0 || max_q_len == 0) return KL_OK;
@@ -410,6 +427,28 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
         return KL_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < w.total || !aligned(workspace, 256)) return KL_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
+    if (wide) {
+        DecodeArgs d{};
+        d.geo = g;
+        d.q = static_cast<const uint16_t *>(q);
+        d.w_r = static_cast<const uint16_t *>(w_r);
+        d.v_cache = static_cast<const uint16_t *>(v_cache);
+        d.block_table = block_table;
+        d.seq_lens = seq_lens;
+        d.tree.cu_q = cu_q_lens;
+        d.tree.parents = parents;
+        d.tree.total_q = total_q;
+        d.tree.max_q = max_q_len;
+        d.counters = reinterpret_cast<unsigned int *>(ws);
+        d.part_o = reinterpret_cast<float *>(ws + w.states);
+        d.part_ml = reinterpret_cast<float *>(ws + w.extra);
+        d.out = out;
+        d.direct_out = g.S == 1;
+        d.out_dtype = out_dtype;
+        d.err = err;
+        d.stream = reinterpret_cast<cudaStream_t>(stream);
+        return from_cuda(launch_tree_wide(d));
+    }
     TreeArgs a;
     a.geo = g;
     a.total_q = total_q;

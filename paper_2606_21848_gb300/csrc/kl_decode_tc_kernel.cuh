@@ -260,13 +260,13 @@ __device__ __forceinline__ uint32_t qr_offset(int n, int k) {
            ((kk & 7) << 1);
 }
 
-// Merge of the n_u split states of (b, g) by the compute warps of the CTA that finished last
-// (t = the thread's index among them)
+// Merge of the n_u split states of (b, g), rows row0 .. row0 + G - 1 of the states, into rows out_row(h) of the
+// output, by the compute warps of the CTA that finished last (t = the thread's index among them)
 // (kl_combine's formula). Up to eight splits: direct loads. More: the cache ring is idle by
 // now; the {m, l} table and the normalized weights go to its front, and TMA bulk copies bring
 // the state rows through the rest, folded by thread (head, 4 dims) from shared memory.
-template <int kComputeWarps, int D, typename SmemT, typename WaitT>
-__device__ void merge_states(SmemT &sm, const DecodeArgs &a, int b, int qh0, int G, int n_u,
+template <int kComputeWarps, int D, typename SmemT, typename RowT, typename WaitT>
+__device__ void merge_states(SmemT &sm, const DecodeArgs &a, size_t row0, const RowT &out_row, int G, int n_u,
                              int t, int warp, int lane, const WaitT &wait) {
     constexpr int kComputeThreads = kComputeWarps * 32;
     const Geometry &geo = a.geo;
@@ -277,7 +277,7 @@ __device__ void merge_states(SmemT &sm, const DecodeArgs &a, int b, int qh0, int
         // (one round trip) and folds them; no staging.
         const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
         for (int h = warp; h < G; h += kComputeWarps) {
-            const size_t bh = (size_t)b * geo.Hq + qh0 + h;
+            const size_t bh = row0 + h;
             const float4 *po = reinterpret_cast<const float4 *>(a.part_o + bh * geo.S * D) + lane;
             float2 v[8];
             float4 r[8];
@@ -307,7 +307,7 @@ __device__ void merge_states(SmemT &sm, const DecodeArgs &a, int b, int qh0, int
             }
             const float inv = z > 0.f ? 1.f / z : 0.f;
             acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-            const size_t oi = bh * D + 4 * lane;
+            const size_t oi = out_row(h) * D + 4 * lane;
             if (!lane_live) continue;
             if (a.out_dtype == KL_FP32) {
                 *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + oi) = acc;
@@ -336,14 +336,14 @@ __device__ void merge_states(SmemT &sm, const DecodeArgs &a, int b, int qh0, int
             ptx::mbar_arrive_expect_tx(&sm.merge_full, (uint32_t)(G * nrow * D * sizeof(float)));
             for (int h = 0; h < G; ++h)
                 ptx::bulk_load(rows + (size_t)h * cap * D,
-                               a.part_o + (((size_t)b * geo.Hq + qh0 + h) * geo.S + c0) * D,
+                               a.part_o + ((row0 + h) * geo.S + c0) * D,
                                (uint32_t)(nrow * D * sizeof(float)), &sm.merge_full);
         }
     };
     issue_rows(0, min(cap, n_u));
     for (int i = t; i < G * n_u; i += kComputeThreads) {
         const int h = i / n_u, j = i - h * n_u;
-        tab[i] = __ldcg(ml + ((size_t)b * geo.Hq + qh0 + h) * geo.S + j);
+        tab[i] = __ldcg(ml + (row0 + h) * geo.S + j);
     }
     ptx::bar_sync(kBarCompute, kComputeThreads);
     for (int h = warp; h < G; h += kComputeWarps) {
@@ -406,7 +406,7 @@ __device__ void merge_states(SmemT &sm, const DecodeArgs &a, int b, int qh0, int
     for (int pass = 0; pass < 2; ++pass) {
         const int h = warp + pass * kComputeWarps;
         if (h >= G || !lane_live) continue;
-        const size_t oi = ((size_t)b * geo.Hq + qh0 + h) * D + 4 * lane;
+        const size_t oi = out_row(h) * D + 4 * lane;
         if (a.out_dtype == KL_FP32) {
             *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + oi) = acc[pass];
         } else {
@@ -1241,7 +1241,9 @@ __global__ void __launch_bounds__(Roles<KH>::kThreads, 2)
                             a.counters + ((size_t)b * geo.Hkv + g) * geo.nhb + hb, n_cta_u) ? 1 : 0;
                     ptx::bar_sync(kBarCompute, kComputeThreads);
                     if (sm.is_last)
-                        merge_states<kComputeWarps, D>(sm, a, b, qh0, G, n_cta_u, tid, warp, lane, wait);
+                        merge_states<kComputeWarps, D>(
+                            sm, a, (size_t)b * geo.Hq + qh0,
+                            [&](int h) { return (size_t)b * geo.Hq + qh0 + h; }, G, n_cta_u, tid, warp, lane, wait);
                 }
             }
         }

@@ -77,6 +77,11 @@ struct DecodeArgs {
     // every role then sleeps in grid_dep_wait until that kernel has finished (the compute warps
     // before reading q_routed; a CTA with an empty run before it ends).
     bool pdl = false;
+    // The wide decode's tree form (kl_tree_attention): sequence b's drafts are rows cu_q[b] .. of q and out.
+    struct {
+        const int32_t *cu_q = nullptr, *parents = nullptr;
+        int total_q = 0, max_q = 1;
+    } tree;
 };
 
 // Arguments of a chunked-prefill launch (kl_prefill_attention). Sequence b's query rows are
@@ -281,6 +286,10 @@ cudaError_t launch_append_chunk(const Geometry &g, int total_q, int max_q, const
 // Attention of a tree of drafted tokens (the geometry of the prefill), and the move of the accepted
 // path's rows.
 cudaError_t launch_tree_tc(const TreeArgs &a);
+// The same by the wide decode's kernel, for up to kTreeWideRows rows per value head, bf16 outputs and one W^R
+// per value head (or none): a.geo with its splits, a.tree.
+constexpr int kTreeWideRows = 32;
+cudaError_t launch_tree_wide(const DecodeArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
                                const int32_t *path_lens, int max_path, const int32_t *block_table,
                                const int32_t *seq_lens, int32_t *new_lens, uint16_t *v_cache,

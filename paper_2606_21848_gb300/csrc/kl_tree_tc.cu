@@ -97,15 +97,17 @@ struct __align__(1024) TreeSmem {
     uint8_t tiles[C::kStages][kTileBytes];
     float sum[C::kFp16 ? 4 : kBM * kD];    // Full: O of the half tiles folded so far, [row][128], its
                                            // 16-byte chunks c at c ^ (row % 32)
-    // Barriers (set up anew for every segment): one completion per half tile u of its buffer u % kSub
-    // on s_full (its scores), p_full (its weights) and s_free (its output MMAs are done), on
-    // v_full[t % kStages] per tile t (Half: its rows are fp16; by the tile's number and not by its ring
-    // slot, which W^R may have used before), and per lane quarter on turn[.][u % 2] (Full: the references
-    // after it).
+    // Barriers (set up anew for every segment): one completion per ring position r of its slot r % kStages on
+    // empty, and on w_full where it holds a W^R; per tile t on full[t % kStages] (the copy) and v_full[t %
+    // kStages] (Half: its rows are fp16) -- by the tile's number and not by its slot, so that a warp which
+    // waits for tiles alone never meets W^R's phases; per half tile u on s_full[u % 4] (its scores),
+    // p_full[u % 4] (its weights) and s_free[u % 4] (its output MMAs are done; of its buffer u % kSub: but
+    // barriers by u % 4, so that a group meets every phase of those it waits for), and per lane quarter on
+    // turn[.][u % 2] (Full: the references after it).
     struct Bars {
-        uint64_t full[C::kStages], empty[C::kStages];
-        uint64_t s_full[C::kSub], s_free[C::kSub];
-        uint64_t p_full[C::kSub], v_full[C::kStages];
+        uint64_t w_full[C::kStages], full[C::kStages], empty[C::kStages];
+        uint64_t s_full[4], s_free[4];
+        uint64_t p_full[4], v_full[C::kStages];
         uint64_t turn[4][kGroups];
         uint64_t first[4];                 // per lane quarter: the maxima of half tile 1 are in lsum[1]
         uint64_t r_full[2], r_free[2];     // routing results, alternating halves of columns 0 .. 255
@@ -420,12 +422,12 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 if (r >= kStages && !(ok = wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1))) break;
                 if (lane == 0) {
                     const int wrow = (geo.wr_per_qh ? h + r : g) * kD;
-                    ptx::mbar_arrive_expect_tx(&sm.bar.full[s], kTileBytes + (r == 0 ? hp * rpb * kD * 2 : 0));
-                    ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.bar.full[s], 0, wrow);
-                    ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.bar.full[s], 64, wrow);
+                    ptx::mbar_arrive_expect_tx(&sm.bar.w_full[s], kTileBytes + (r == 0 ? hp * rpb * kD * 2 : 0));
+                    ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.bar.w_full[s], 0, wrow);
+                    ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.bar.w_full[s], 64, wrow);
                     if (r == 0) {
-                        ptx::tma_load_3d(sm.q, &qmap, &sm.bar.full[s], 0, h, q0 + m0);
-                        ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.bar.full[s], 64, h, q0 + m0);
+                        ptx::tma_load_3d(sm.q, &qmap, &sm.bar.w_full[s], 0, h, q0 + m0);
+                        ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.bar.w_full[s], 64, h, q0 + m0);
                     }
                 }
                 __syncwarp();
@@ -447,6 +449,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             }
             for (int i = 0; ok && i < n_tiles; ++i) {
                 const int r = i + ro, s = r % kStages;
+                uint64_t *const full = &sm.bar.full[i % kStages];
                 const int pg = (tile0 + i) * ppt + lane;      // page index within the sequence
                 const bool exists = lane < ppt && pg < seq_pages;
                 const int page = exists ? bt[pg] : -1;
@@ -456,11 +459,11 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 const unsigned mask = __ballot_sync(0xffffffffu, in_range);
                 ptx::for_pages(
                     (page * geo.Hkv + g) * P, mask,
-                    [&] { ptx::mbar_arrive_expect_tx(&sm.bar.full[s], __popc(mask) * page_bytes * 2u); },
+                    [&] { ptx::mbar_arrive_expect_tx(full, __popc(mask) * page_bytes * 2u); },
                     [&](int p, int row) {
                         uint8_t *dst = sm.tiles[s] + p * page_bytes;
-                        ptx::tma_load_2d(dst, &vmap, &sm.bar.full[s], 0, row);
-                        ptx::tma_load_2d(dst + kHalfBytes, &vmap, &sm.bar.full[s], 64, row);
+                        ptx::tma_load_2d(dst, &vmap, full, 0, row);
+                        ptx::tma_load_2d(dst + kHalfBytes, &vmap, full, 64, row);
                     });
                 issued = r + 1;
             }
@@ -471,9 +474,11 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             if (sm.abort) {
                 // copies still in flight land before the CTA's shared memory goes away
                 for (int i = max(0, issued - kStages); i < issued; ++i) {
+                    const int t = i - ro;
+                    uint64_t *const full = t < 0 ? &sm.bar.w_full[i % kStages] : &sm.bar.full[t % kStages];
+                    const uint32_t parity = ((t < 0 ? i : t) / kStages) & 1;
                     const uint64_t t0 = ptx::globaltimer();
-                    while (!ptx::mbar_try_wait(&sm.bar.full[i % kStages], (i / kStages) & 1) &&
-                           ptx::globaltimer() - t0 < kTimeoutNs) {
+                    while (!ptx::mbar_try_wait(full, parity) && ptx::globaltimer() - t0 < kTimeoutNs) {
                     }
                 }
             }
@@ -497,7 +502,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 bool ok = true;
                 for (int r = 0; ok && r < ro; ++r) {
                     const int s = r % kStages;
-                    ok = wait(&sm.bar.full[s], (r / kStages) & 1) &&
+                    ok = wait(&sm.bar.w_full[s], (r / kStages) & 1) &&
                          (r < 2 || wait(&sm.bar.r_free[r & 1], ((r >> 1) - 1) & 1));
                     if (!ok) break;
                     ptx::tc_fence_after();
@@ -516,26 +521,26 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 if (ok && ptx::elect_one()) {
                     ptx::tc_fence_after();
                     for (int u = 0; u < n_sub; ++u) {
-                        const int t = u >> 1, r = t + ro, s = r % kStages, sb = u % kSub;
-                        if (C::kFp16 ? !wait.one(&sm.bar.v_full[t % kStages], (t / kStages) & 1)
-                                     : !wait.one(&sm.bar.full[s], (r / kStages) & 1))
+                        const int t = u >> 1, s = (t + ro) % kStages, sb = u % kSub;
+                        if (!wait.one(C::kFp16 ? &sm.bar.v_full[t % kStages] : &sm.bar.full[t % kStages],
+                                      (t / kStages) & 1))
                             break;
                         // the output MMAs of half tile u - kSub have read this buffer's weights
-                        if (u >= kSub && !wait.one(&sm.bar.s_free[sb], (u / kSub - 1) & 1)) break;
+                        if (u >= kSub && !wait.one(&sm.bar.s_free[(u - kSub) & 3], ((u - kSub) >> 2) & 1)) break;
                         ptx::tc_fence_after();
                         const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
 #pragma unroll
                         for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
                             ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
                                              idesc_qk, kk > 0);
-                        ptx::mma_commit(&sm.bar.s_full[sb]);
+                        ptx::mma_commit(&sm.bar.s_full[u & 3]);
                     }
                 }
             } else if (ptx::elect_one()) {
                 // O += P . V (Half: the group's); at a fold O starts over (its old value has been read by then)
                 for (int u = 0; u < n_sub; ++u) {
                     const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
-                    if (!wait.one(&sm.bar.p_full[sb], (u / kSub) & 1)) break;
+                    if (!wait.one(&sm.bar.p_full[u & 3], (u >> 2) & 1)) break;
                     ptx::tc_fence_after();
                     const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
                     const bool more = C::kFp16 ? u >= kGroups : u % kFoldSub != 0;
@@ -544,7 +549,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     for (int kk = 0; kk < C::kPTerms * kBS / 16; ++kk)
                         ptx::mma_bf16_ts(o, tmem + sb * C::kBuf + kk * 8,
                                          b0 + (((kk & 3) * 2048) >> 4), idesc_pv, (more || kk > 0) ? 1u : 0u);
-                    ptx::mma_commit(&sm.bar.s_free[sb]);
+                    ptx::mma_commit(&sm.bar.s_free[u & 3]);
                     if ((u & 1) || u == n_sub - 1) ptx::mma_commit(&sm.bar.empty[s]);
                 }
             }
@@ -562,8 +567,8 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             // different 16-byte chunks so that a warp's accesses spread over all banks.
             const int r = (warp - kConvWarp) * 32 + lane;
             for (int t = 0; t < n_tiles; ++t) {
-                const int ring = t + ro, st = ring % kStages;
-                if (!wait(&sm.bar.full[st], (ring / kStages) & 1)) break;
+                const int st = (t + ro) % kStages;
+                if (!wait(&sm.bar.full[t % kStages], (t / kStages) & 1)) break;
                 const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes + (r & 63) * 128;
                 const int t0 = (tile0 + t) * kBN;
                 uint32_t v[2][32];
@@ -615,7 +620,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         const bool has_drafts = k.has_drafts, whole = k.whole;
         const TreeSegment &sg = k.sg;
         const int m0 = k.blk.m0, rows = k.blk.rows, h = k.blk.h, hn = k.blk.hn;
-        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = k.n_tiles;
+        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0;
         const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
             // ----------------------------------------------------- softmax, epilogue ----
             if (tid == 0 && k.more) sm.seg[(si + 1) & 1] = next_segment(a, sg);
@@ -716,7 +721,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
                 const uint32_t sbuf = tmem + (uint32_t)sb * C::kBuf + lane_base;   // S, then P
                 const bool drafts_here = t0 + kBS > base;
-                okl = wait(&sm.bar.s_full[sb], (u / kSub) & 1);
+                okl = wait(&sm.bar.s_full[u & 3], (u >> 2) & 1);
                 if (!okl) break;
                 ptx::tc_fence_after();
                 if constexpr (!C::kFp16) {
@@ -725,7 +730,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     // (the score MMAs have read it: a draft that sees it has a NaN score).
                     const int ring = (u >> 1) + ro;
                     if (drafts_here) {
-                        okl = wait(&sm.bar.full[ring % kStages], (ring / kStages) & 1);
+                        okl = wait(&sm.bar.full[(u >> 1) % kStages], ((u >> 1) / kStages) & 1);
                         if (!okl) break;
                     }
                     // thread = (cache row, 64 dims)
@@ -801,7 +806,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 const bool fold = !C::kFp16 && u > 0 && u % kFoldSub == 0;
                 const int before = C::kFp16 ? u - kGroups : u - 1;   // the last half tile that O holds
                 if (before >= 0 && (moves || fold)) {
-                    okl = wait(&sm.bar.s_free[before % kSub], (before / kSub) & 1);
+                    okl = wait(&sm.bar.s_free[before & 3], (before >> 2) & 1);
                     if (!okl) break;
                     ptx::tc_fence_after();
                 }
@@ -902,7 +907,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 // rows zeroed here (generic-proxy stores) are read next by the output MMAs
                 if (!C::kFp16 && drafts_here) ptx::fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sm.bar.p_full[sb]);
+                if (lane == 0) ptx::mbar_arrive(&sm.bar.p_full[u & 3]);
             }
 
             // Epilogue: out = O / l, or the part's state (m, l, O). Full: l is the groups' shares at the
@@ -910,8 +915,9 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             // group's output dims.
             const int last = n_sub - 1, lg = last % kGroups;
             if (!C::kFp16 && okl && lg != grp) okl = wait(&sm.bar.turn[qd][lg], (last / kGroups) & 1);
-            bool oke = okl && wait(&sm.bar.s_free[last % kSub], (last / kSub) & 1);
-            if (C::kFp16 && oke && last > 0) oke = wait(&sm.bar.s_free[(last - 1) % kSub], ((last - 1) / kSub) & 1);
+            // (all of the last commits land before the barriers are set up anew)
+            bool oke = okl;
+            for (int u = last; oke && u >= 0 && u > last - 3; --u) oke = wait(&sm.bar.s_free[u & 3], (u >> 2) & 1);
             float l = (la.x + la.y) + (lb.x + lb.y);
             float m_fin = 0.f;
             if constexpr (C::kFp16) {

@@ -1,0 +1,39 @@
+// Attention of a tree of drafted tokens with few rows per value head (drafts x heads of a group <= 32) on the
+// wide decode's kernel (kl_decode_wide_kernel.cuh, kTree): there a tile costs what its 16 or 32 rows cost,
+// where a block of kl_tree_tc.cu costs 128 rows, and the splits merge inside.
+#include "kl_decode_wide_kernel.cuh"
+
+namespace kl {
+
+cudaError_t launch_tree_wide(const DecodeArgs &a) {
+    DecodeArgs la = a;
+    Geometry &g = la.geo;
+    const int rows = g.G * a.tree.max_q;
+    const int64_t sms = device_sm_count(), units = (int64_t)g.B * g.Hkv;
+    const bool w32 = rows > 16, two_per_sm = !w32 && units > sms;     // (as the decode's blocks of heads)
+    g.nhb = 1;
+    g.qbox = rows;
+    g.spc = splits_per_cta(g.S, units, two_per_sm ? 2 * sms : sms);
+    CUtensorMap vmap, wmap, qmap;
+    if (!make_map(&vmap, a.v_cache, kD, (uint64_t)g.num_pages * g.Hkv * g.P, (uint32_t)g.P))
+        return cudaErrorInvalidValue;
+    wmap = qmap = vmap;
+    if (a.w_r) {
+        if (!make_map(&wmap, a.w_r, kD, (uint64_t)g.Hkv * kD, (uint32_t)kD)) return cudaErrorInvalidValue;
+        // q as [total_q][Hq][128], one box = max_q consecutive drafts of a group's heads (64 dims); rows past
+        // total_q read as zeros
+        auto fn = encode_fn();
+        const cuuint64_t dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)a.tree.total_q};
+        const cuuint64_t strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)a.tree.max_q}, estr[3] = {1, 1, 1};
+        if (!fn || fn(&qmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t *>(a.q), dims, strides, box,
+                      estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    if (w32) return launch_kernel_wide<32, 2, false, true>(la, vmap, wmap, qmap);
+    return two_per_sm ? launch_kernel_wide<16, 1, false, true>(la, vmap, wmap, qmap)
+                      : launch_kernel_wide<16, 2, false, true>(la, vmap, wmap, qmap);
+}
+
+}  // namespace kl

@@ -62,14 +62,18 @@ def test_tree_shapes(kind, out):
 @pytest.mark.parametrize("per_q", [False, True])
 def test_head_layouts(Hq, Hkv, per_q):
     x = tree_inputs((200, 40), (9, 16), Hq, Hkv, wr_per_query_head=per_q, seed=Hq)
-    check(run(x), tree_reference(x))
+    want = tree_reference(x)
+    check(run(x), want)
+    check(run(x, torch.bfloat16), want, torch.bfloat16)
 
 
 @pytest.mark.parametrize("n", [1, 2, 21, 22, 32, 33, 63, 64, 65, 127, 128])
 @pytest.mark.parametrize("committed", [0, 1, 63, 64, 65, 127, 128, 200, 1000])
 def test_lengths_around_tiles(n, committed):
     x = tree_inputs((committed + n, committed + 1), (n, 1), 6, 1, seed=n + committed)
-    check(run(x), tree_reference(x))
+    want = tree_reference(x)
+    check(run(x), want)
+    check(run(x, torch.bfloat16), want, torch.bfloat16)
 
 
 @pytest.mark.parametrize("P", [16, 32, 64, 128])
@@ -77,6 +81,72 @@ def test_lengths_around_tiles(n, committed):
 def test_pages_and_splits(P, splits):
     x = tree_inputs((1500, 3, 131, 700, 129), (20, 3, 5, 0, 1), 8, 2, P=P, seed=P)
     check(run(x, splits=splits), tree_reference(x))
+
+
+# Few rows per value head (drafts x heads of a group up to 32) with bf16 outputs: CTAs of 16 and of 32 rows, one
+# and two to an SM.
+@pytest.mark.parametrize("Hq,Hkv,n", [(1, 1, 1), (1, 1, 17), (1, 1, 32), (4, 1, 4), (8, 2, 8), (6, 1, 5), (16, 1, 2),
+                                      (32, 1, 1), (5, 1, 3), (40, 8, 6)])
+@pytest.mark.parametrize("committed", [0, 1, 127, 128, 300])
+@pytest.mark.parametrize("splits", [0, 1, 3])
+def test_few_rows(Hq, Hkv, n, committed, splits):
+    x = tree_inputs((committed + n, committed + max(1, n // 2), 900, 0), (n, max(1, n // 2), min(n, 2), 0), Hq, Hkv,
+                    seed=n + committed)
+    check(run(x, torch.bfloat16, splits=splits), tree_reference(x), torch.bfloat16)
+
+
+@pytest.mark.parametrize("n", [2, 4, 8])
+def test_few_rows_of_many_sequences(n):
+    lens = tuple(60 + 37 * (i % 11) for i in range(90))
+    x = tree_inputs(lens, tuple(1 + i % n for i in range(90)), 8, 2, seed=n)
+    check(run(x, torch.bfloat16), tree_reference(x), torch.bfloat16)
+    check(run(x, torch.bfloat16, composed=True), tree_reference(x, composed=True), torch.bfloat16)
+
+
+def test_few_rows_of_a_long_cache():
+    x = tree_inputs((30000, 5000), (8, 3), 8, 2, P=32, seed=78)
+    want = tree_reference(x)
+    for splits in (0, 1, 40):
+        check(run(x, torch.bfloat16, splits=splits), want, torch.bfloat16)
+
+
+@pytest.mark.parametrize("splits", [0, 4])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_few_rows_and_a_row_that_is_not_finite(value, splits):
+    x = tree_inputs((530, 140), (8, 7), 8, 2, seed=11)
+    want = tree_reference(x)
+    P, cu, bad = 16, x["cu_q"].tolist(), {0: 2, 1: 0}
+    for b, i in bad.items():
+        t = int(x["seq_lens"][b]) - x["drafts"][b] + i
+        x["v_cache"][int(x["block_table"][b, t // P]), :, t % P, 5] = value
+        L = int(x["seq_lens"][b])
+        x["v_cache"][int(x["block_table"][b, L // P]), :, L % P:] = math.nan      # behind the end
+    got = run(x, torch.bfloat16, splits=splits)
+    for b in range(2):
+        for i in range(x["drafts"][b]):
+            j = i
+            while j > bad[b]:
+                j = int(x["parents"][cu[b] + j])
+            r = cu[b] + i
+            if j != bad[b]:
+                d = got[r].double() - want[r]
+                assert float(d.norm() / want[r].norm()) < 4 * REL[torch.bfloat16], (b, i)
+            elif math.isnan(value):
+                assert torch.isnan(got[r].float()).all(), (b, i)
+
+
+def test_few_rows_flags():
+    x = tree_inputs((100, 50, 80), (5, 5, 8))
+    want = tree_reference(x)
+    y = dict(x, parents=x["parents"].clone())
+    y["parents"][7] = 2                           # sequence 1, draft 2: itself
+    got = run(y, torch.bfloat16, flags=kl.KL_FLAG_BAD_TREE)
+    check(got[:5], want[:5])
+    y = dict(x, seq_lens=x["seq_lens"].clone())
+    y["seq_lens"][1] = 4                          # fewer rows than drafts
+    got = run(y, torch.bfloat16, flags=kl.KL_FLAG_BAD_LENGTH)
+    check(got[10:], want[10:])
+    assert torch.isnan(got[5:10].float()).all()
 
 
 def test_no_drafts_anywhere_but_one():
@@ -106,6 +176,17 @@ def test_a_larger_bound_and_a_shared_workspace():
     want = tree_reference(x)
     for max_q, splits in ((128, 5), (40, 0), (64, 3)):
         check(run(x, max_q=max_q, splits=splits, ws=ws), want)
+
+
+def test_bf16_outputs_of_large_scores():
+    """One fp16 operand each for query and weights (more than 32 rows) or bf16 pairs (fewer): against scores of tens
+    of units, whose weights the fp16 query moves by up to |s| 2^-12."""
+    for drafts in ((30, 64), (8, 5)):
+        x = tree_inputs((900, 333), drafts, 8, 2)
+        x["q"] = (x["q"].float() * 6).to(torch.bfloat16)
+        want = tree_reference(x)
+        d = run(x, torch.bfloat16).double() - want
+        assert float(d.norm() / want.norm()) < (60 * 2.0 ** -12 if drafts[0] > 8 else REL[torch.bfloat16])
 
 
 def test_large_scores_and_outliers():
