@@ -28,10 +28,10 @@
 // 1.24 us per tile where HBM delivers one in 0.73. Values or queries past fp16's range make the outputs
 // that take part in them NaN (KL_FLAG_RANGE).
 // fp32 outputs (Full): query and weights are sums of three bf16 terms (24 bits), and since the tensor
-// core's adds truncate, O moves every 256 tokens to a sum that the softmax warps keep in shared memory.
+// core's adds truncate, O moves every 128 tokens to a sum that the softmax warps keep in shared memory.
 //
 // The softmax works on half tiles of 64 tokens, thread = row = TMEM lane. A row's reference maximum moves
-// only when a half tile's maximum passes it by more than 2^7.
+// only when a half tile's maximum passes it by more than 2^14.
 //
 // Roles: two groups of four softmax warps (and epilogue), then one warp each for the producer (TMA), the routing
 // and score MMAs (owner of the tensor memory) and the output MMAs, and for Half four warps that convert
@@ -55,7 +55,9 @@ constexpr int kBS = 64;                           // cache rows per half tile
 constexpr uint32_t kTileBytes = kBN * kD * 2;     // 32 KiB
 constexpr uint32_t kHalfBytes = kTileBytes / 2;   // one 64-dim half: 128 rows x 128 B
 constexpr uint32_t kTmemCols = 512;
-constexpr float kRescaleLog2 = 7.f;
+// A reference moves when a weight would pass 2^14 (fp16 ends at 2^16; a stale reference costs no precision that
+// bf16 outputs show, and three bf16 terms have fp32's range).
+constexpr float kRescaleLog2 = 14.f;
 constexpr uint64_t kTimeoutNs = kRowsTimeoutNs;
 constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 is __syncthreads)
 
@@ -88,7 +90,7 @@ struct Warps {
     static constexpr int kProducer = kCompute, kMma = kCompute + 1, kPv = kCompute + 2, kConv = kCompute + 4;
     static constexpr int kThreads = 32 * (C::kConvWarps ? kConv + C::kConvWarps : kPv + 1);
 };
-constexpr int kFoldSub = 4;           // Full: half tiles between two moves of O to the fp32 sum
+constexpr int kFoldSub = 2;           // Full: half tiles between two moves of O to the fp32 sum
 
 template <typename C>
 struct __align__(1024) TreeSmem {
@@ -529,10 +531,13 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                         if (u >= kSub && !wait.one(&sm.bar.s_free[(u - kSub) & 3], ((u - kSub) >> 2) & 1)) break;
                         ptx::tc_fence_after();
                         const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+                        // (the small terms first: the tensor core's adds truncate the sum)
 #pragma unroll
-                        for (int kk = 0; kk < C::kQTerms * kD / 16; ++kk)
-                            ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + kk * 8, b0 + kstep(kk & 7),
-                                             idesc_qk, kk > 0);
+                        for (int i = C::kQTerms - 1; i >= 0; --i)
+#pragma unroll
+                            for (int kk = 0; kk < kD / 16; ++kk)
+                                ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + 64 * i + kk * 8,
+                                                 b0 + kstep(kk), idesc_qk, i < C::kQTerms - 1 || kk > 0);
                         ptx::mma_commit(&sm.bar.s_full[u & 3]);
                     }
                 }
@@ -836,7 +841,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     m_sum = m_ref;
                     sm.fref[r] = m_ref;
                 }
-                // a new reference when the maximum grew by more than 2^7 (or is the first finite)
+                // a new reference when the maximum grew by more than 2^14 (or is the first finite)
                 if (moves) {
                     if (before >= 0 && !fold) {
                         const float f =
