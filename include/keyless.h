@@ -56,9 +56,10 @@ typedef enum kl_status {
 #define KL_FLAG_BAD_POSITION 0x2 /* append position outside [0, max_pages_per_seq * P) */
 #define KL_FLAG_BAD_LENGTH 0x4   /* seq_len outside [0, max_pages_per_seq * P] */
 #define KL_FLAG_TIMEOUT 0x8      /* a bounded pipeline wait gave up (output invalid) */
-#define KL_FLAG_RANGE 0x10       /* a non-finite output of kl_prefill_attention (a cached value
-                                    beyond its fp16 range, or a non-finite input); a NaN or +inf
-                                    logit in kl_token_logprobs */
+#define KL_FLAG_RANGE 0x10       /* a non-finite output of kl_prefill_attention, or of kl_tree_attention
+                                    where it computes in fp16 (a cached value or routed query beyond
+                                    fp16's range, or a non-finite input); a NaN or +inf logit in
+                                    kl_token_logprobs */
 #define KL_FLAG_BAD_TREE 0x20    /* a parent, or an accepted path, that is not in its sequence's tree */
 #define KL_FLAG_BAD_TOKEN 0x40   /* a token id outside [-1, vocab) */
 
@@ -267,7 +268,7 @@ kl_status kl_prefill_attention(const kl_shape *shape, const void *q, const void 
 /* Most drafted tokens per sequence. */
 #define KL_TREE_MAX_DRAFTS 128
 
-/* Bytes of device workspace kl_tree_attention needs (0 when it needs none, or on an invalid shape).
+/* Bytes of device workspace kl_tree_attention needs for either type of output (0 on an invalid shape).
  * The contract of kl_decode_workspace_size: zero-filled before its first use, then shared by any
  * sequence of calls and shapes, decodes included. */
 size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len,
@@ -283,14 +284,21 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
  * over these tokens. n_b = 1 is the decode step; parents[r] = i - 1 is the causal chunk.
  * q, out: [total_q][Hq][D] (q bf16, out of out_dtype); cu_q_lens: [B + 1] int32 on the device,
  * non-decreasing from 0; parents: [total_q] int32; max_q_len: a host-side bound on every n_b, at most
- * KL_TREE_MAX_DRAFTS; w_r (NULL: q is the composed query), v_cache, block_table, seq_lens, num_splits as
- * in kl_decode_attention. Workspace: kl_tree_workspace_size bytes of the same arguments, 256-byte
- * aligned. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3 (KL_ERR_UNSUPPORTED
+ * KL_TREE_MAX_DRAFTS; w_r (NULL: q is the composed query), v_cache, block_table, seq_lens as in
+ * kl_decode_attention; num_splits: the parts that a sequence is cut into at most (0: chosen from the
+ * lengths and the GPU). Workspace: kl_tree_workspace_size bytes of the same arguments, 256-byte aligned.
+ * One launch, or two where sequences may be cut. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3 (KL_ERR_UNSUPPORTED
  * otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <=
  * max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine: nothing is
  * written); a parent outside [-1, i) raises KL_FLAG_BAD_TREE and counts as -1; a bad page id leaves the
  * affected outputs unspecified. A drafted row that is not finite reaches the drafts that see it
- * alone. fp32 accumulation; the routed query and the softmax weights carry about 16 significant bits.
+ * alone.
+ * Precision: scores, softmax and sums in fp32. The operands of the products depend on the form:
+ *   fp32 outputs: the routed query and the weights carry 24 significant bits (error about 1e-6);
+ *   bf16 outputs with (Hq / Hkv) * max_q_len <= 32 and one W^R per value head or none: 16 bits;
+ *   other bf16 outputs: fp16, 11 bits, cached values of magnitude 2^-14 to 65280 exactly. There a routed
+ *   query times scale * log2 e, or a cached value, beyond 65504 makes the outputs that it takes part in
+ *   NaN (a drafted row: those of the drafts that see it), and a non-finite output raises KL_FLAG_RANGE.
  */
 kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
                             const int32_t *block_table, const int32_t *seq_lens,
@@ -330,8 +338,8 @@ size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_t
  *   top_logprobs[r][0 ..] = their log probabilities
  * logits: [num_rows][row_stride] of logits_dtype, the first `vocab` of each row, row_stride >= vocab
  * elements, aligned to their own size alone; tokens: [num_rows][tokens_per_row] int32; outputs fp32 and
- * int32, dense; num_top <= min(vocab, KL_LOGPROBS_MAX_TOP), vocab <= 2^30; num_top 0: none (top_* are then not written),
- * tokens_per_row may be 0. A token id outside [-1, vocab) raises KL_FLAG_BAD_TOKEN and gets NaN. Logits of
+ * int32, dense; vocab <= 2^30; num_top <= min(vocab, KL_LOGPROBS_MAX_TOP), 0: none (top_* are then not
+ * written); tokens_per_row may be 0. A token id outside [-1, vocab) raises KL_FLAG_BAD_TOKEN and gets NaN. Logits of
  * -inf have probability 0; a row of -inf alone gives log probabilities of -inf and entropy 0. A NaN
  * or +inf logit makes the row's log probabilities and entropy NaN and raises KL_FLAG_RANGE; NaN is never
  * among the largest (an id of -1 stands where no logit is left). fp32 sums. One launch; the workspace

@@ -15,8 +15,14 @@
 //
 // Selection: keys (value, lowest index first) above the smallest of the `top` best so far go to a list of
 // candidates in shared memory, which is ranked by counting and cut to `top` after the row's first chunk,
-// when it fills up and at the row's end. The first chunk's bound comes from the threads' maxima: with `top` of them known to be >= t, so are `top` logits; t is the larger of (the smallest, over the
-// 8 warps, of the ceil(top / 8)-th largest maximum) and (the largest over the warps of the top-th).
+// when it fills up and at the row's end. The first chunk's bound comes from the threads' maxima: with
+// `top` of them known to be >= t, so are `top` logits; t is the larger of (the smallest, over the 8 warps,
+// of the ceil(top / 8)-th largest maximum) and (the largest over the warps of the top-th).
+//
+// Measured: 2048 rows of 151936 bf16 logits, no alternatives, 100 us (6200 GB/s, 0.91 of a copy's); 512 rows of
+// 128256 with the 8 largest 39.6 us (3300 GB/s: 1.1 runs per row, whose selections' steps, some 4 us a row, do
+// not overlap within a CTA); 96 rows of 50257 fp32 logits with the 20 largest 16.4 us, and one row of 32000 7.9 us
+// (latency: first copy 1, first selection 2, further chunks 3, ranking 1.3, the join of a row's parts 4).
 #include <float.h>
 #include <math.h>
 
@@ -209,8 +215,8 @@ __device__ __noinline__ void wait_slow(uint64_t *bar, uint32_t phase, int32_t *e
         }
 }
 
-// Runs of chunks: `each` per CTA, one more for the first `extra`. (The quotients mostly fit 32 bits; a 64-bit
-// division takes 0.2 us.)
+// Runs of chunks: `each` per CTA, one more for the first `extra`. (The quotients mostly fit 32 bits, whose
+// division is much shorter.)
 struct LogprobRuns {
     int64_t each;
     int extra;

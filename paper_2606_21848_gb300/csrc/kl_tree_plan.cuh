@@ -20,6 +20,7 @@ constexpr int kTreeTile = 128;      // cache rows of a tile
 constexpr int kTreeRun = 8, kTreeCut = 2;
 // What starting a segment takes, in tiles (about 5 us), in the runs' shares.
 constexpr int kTreeStart = 5;
+constexpr int kTreeMaxRuns = 512;   // (one per SM; the merge lists a unit's parts in shared memory)
 // A part's state: O [32][128 rows] float4 and {m, l} [128 rows]. Every run has up to two parts.
 constexpr size_t kTreeStateBytes = kTreeRows * 128 * sizeof(float) + kTreeRows * 2 * sizeof(float);
 
@@ -39,7 +40,8 @@ inline TreePlan plan_tree(int B, int Hkv, int G, int max_q, int64_t max_tokens, 
     const int64_t units = (int64_t)(B > 0 ? B : 1) * Hkv * p.blocks;
     const int64_t shared = ((max_tokens + kTreeTile - 1) / kTreeTile + kTreeStart) * units / (kTreeRun + kTreeStart);
     const int64_t most = shared > units ? shared : units;
-    p.ctas = (int)(most < 1 ? 1 : most < sms ? most : sms);
+    const int64_t top = sms < kTreeMaxRuns ? sms : kTreeMaxRuns;
+    p.ctas = (int)(most < 1 ? 1 : most < top ? most : top);
     return p;
 }
 

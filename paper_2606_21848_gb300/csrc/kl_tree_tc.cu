@@ -22,13 +22,21 @@
 // MN-major one of the output. Q and P are A operands in tensor memory.
 //
 // Precision. bf16 outputs (Half): the tile is converted to fp16 in place (exact for bf16 values of magnitude
-// 2^-14 to 65280), the routed query and the weights are one fp16 operand each (11 bits): two MMAs per
-// tile. A weight is off by |s| 2^-12 / sqrt(3) at rms, against the output's own rounding of 2^-9; with the
-// query as two operands (three MMAs) the tensor cores, at the rate that the power cap leaves them, took
-// 1.24 us per tile where HBM delivers one in 0.73. Values or queries past fp16's range make the outputs
-// that take part in them NaN (KL_FLAG_RANGE).
+// 2^-14 to 65280), the routed query and the weights are one fp16 operand each (11 bits), so that each
+// product takes one term. A weight is off by |s| 2^-12 / sqrt(3) at rms, against the output's own rounding
+// of 2^-9; with the query as two terms a tile took 1.24 us (19 sequences of 32768 tokens, 32 / 8 heads, 32
+// drafts; HBM delivers a tile to every SM in 0.73 us, and this form takes 1.0). Values or queries past fp16's
+// range make the outputs that take part in them NaN (KL_FLAG_RANGE).
 // fp32 outputs (Full): query and weights are sums of three bf16 terms (24 bits), and since the tensor
 // core's adds truncate, O moves every 128 tokens to a sum that the softmax warps keep in shared memory.
+//
+// What bounds it. Half, on long caches: nothing alone. Of the 253 us of the sizes above (4700 GB/s of cache,
+// 1.1 PFLOP/s) removing the conversion, the exponentials, or one of the two products saved 18 to 35 us each, and
+// removing all of them 52. 64 sequences of 512 to 32768 tokens, up to 24 drafts: 494 us (323 at HBM's rate);
+// one of 131072 tokens, 32 drafts: 71 us (40). Short caches are bound by latency: starting a segment takes
+// 5 us, of them the routing and the first scores 3.5, and units of several parts 3 to 5 us for the merge.
+// Full: six score and six output products per tile; 12 sequences of 3001 to 6007 tokens, 12 / 2 heads, 61 to
+// 64 drafts, W^R per query head: 93 us.
 //
 // The softmax works on half tiles of 64 tokens, thread = row = TMEM lane. A row's reference maximum moves
 // only when a half tile's maximum passes it by more than 2^14.
@@ -116,7 +124,8 @@ struct __align__(1024) TreeSmem {
         uint64_t qr_ready, par_ready, drain, drain2;
     } bar;
     float mref[kGroups][kBM];  // the rows' references after the last half tile of each group
-    float lsum[kGroups][kBM];  // the groups' shares of the row sums, for the epilogue
+    float lsum[kGroups][kBM];  // the groups' shares of the row sums, for the epilogue; Full: before it,
+                               // lsum[1] holds half tile 1's maxima for the first reference
     float fref[kBM];           // Full: the references of `sum`
     int32_t parent[KL_TREE_MAX_DRAFTS];
     unsigned int over[KL_TREE_MAX_DRAFTS / 32];   // Half: drafts with a finite value beyond fp16's range
@@ -179,7 +188,7 @@ __device__ __forceinline__ int cut_step(const TreeArgs &a, int tiles) {
     return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : tiles <= kTreeRun ? tiles : kTreeCut;
 }
 
-// Quotients of what mostly fits 32 bits (the 64-bit division takes most of a microsecond).
+// Quotients of what mostly fits 32 bits (the 64-bit division is a long sequence of instructions).
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
     return (x | y) <= INT32_MAX ? (int)x / (int)y : x / y;
 }
@@ -396,237 +405,237 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
     if (warp >= kComputeWarps) {
         if constexpr (C::kFp16) ptx::regs_dec<kOtherRegs>();
         for (int si = 0;; ++si) {
-        const Part k = begin(si);
-        const uint32_t tmem = sm.tmem_base;
-        const TreeSegment &sg = k.sg;
-        const int m0 = k.blk.m0, h = k.blk.h, g = k.blk.g;
-        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = k.n_tiles;
-        const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
-        if (warp == kProducerWarp) {
-            // -------------------------------------------------------------- producer ----
-            const int P = geo.P;
-            const int ppt = kBN / P;                          // pages per tile (<= 8)
-            const int seq_pages = (L + P - 1) / P;
-            const uint32_t page_bytes = (uint32_t)P * 128u;   // one half of one page
-            const int32_t *bt = a.block_table + (size_t)sg.b * geo.max_pages;
-            int issued = 0;
-            bool bad = false, ok = true;
-            // the drafts' parents, on their way while the first copies are issued
-            constexpr int kPer = KL_TREE_MAX_DRAFTS / 32;
-            int32_t parent[kPer];
-            if (k.has_drafts)
+            const Part k = begin(si);
+            const uint32_t tmem = sm.tmem_base;
+            const TreeSegment &sg = k.sg;
+            const int m0 = k.blk.m0, h = k.blk.h, g = k.blk.g;
+            const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0, n_tiles = k.n_tiles;
+            const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
+            if (warp == kProducerWarp) {
+                // -------------------------------------------------------------- producer ----
+                const int P = geo.P;
+                const int ppt = kBN / P;                          // pages per tile (<= 8)
+                const int seq_pages = (L + P - 1) / P;
+                const uint32_t page_bytes = (uint32_t)P * 128u;   // one half of one page
+                const int32_t *bt = a.block_table + (size_t)sg.b * geo.max_pages;
+                int issued = 0;
+                bool bad = false, ok = true;
+                // the drafts' parents, on their way while the first copies are issued
+                constexpr int kPer = KL_TREE_MAX_DRAFTS / 32;
+                int32_t parent[kPer];
+                if (k.has_drafts)
 #pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    parent[i] = i * 32 + lane < sg.n ? a.parents[q0 + i * 32 + lane] : -1;
-            // W^R matrices (B operand of the routing MMAs); the first brings the query block along
-            for (int r = 0; r < ro; ++r) {
-                const int s = r % kStages;
-                if (r >= kStages && !(ok = wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1))) break;
-                if (lane == 0) {
-                    const int wrow = (geo.wr_per_qh ? h + r : g) * kD;
-                    ptx::mbar_arrive_expect_tx(&sm.bar.w_full[s], kTileBytes + (r == 0 ? hp * rpb * kD * 2 : 0));
-                    ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.bar.w_full[s], 0, wrow);
-                    ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.bar.w_full[s], 64, wrow);
-                    if (r == 0) {
-                        ptx::tma_load_3d(sm.q, &qmap, &sm.bar.w_full[s], 0, h, q0 + m0);
-                        ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.bar.w_full[s], 64, h, q0 + m0);
-                    }
-                }
-                __syncwarp();
-                issued = r + 1;
-            }
-            if (k.has_drafts) {
-                // (one that is not an earlier draft or -1 counts as -1)
-                bool wrong = false;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int j = i * 32 + lane;
-                    const bool fine = parent[i] >= -1 && parent[i] < j;
-                    wrong |= !fine;
-                    sm.parent[j] = fine ? parent[i] : -1;
-                }
-                if (wrong) raise_flag(a.err, KL_FLAG_BAD_TREE);
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sm.bar.par_ready);
-            }
-            for (int i = 0; ok && i < n_tiles; ++i) {
-                const int r = i + ro, s = r % kStages;
-                uint64_t *const full = &sm.bar.full[i % kStages];
-                const int pg = (tile0 + i) * ppt + lane;      // page index within the sequence
-                const bool exists = lane < ppt && pg < seq_pages;
-                const int page = exists ? bt[pg] : -1;
-                if (r >= kStages && !wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1)) break;
-                const bool in_range = exists && page >= 0 && page < geo.num_pages;
-                if (exists && !in_range) bad = true;
-                const unsigned mask = __ballot_sync(0xffffffffu, in_range);
-                ptx::for_pages(
-                    (page * geo.Hkv + g) * P, mask,
-                    [&] { ptx::mbar_arrive_expect_tx(full, __popc(mask) * page_bytes * 2u); },
-                    [&](int p, int row) {
-                        uint8_t *dst = sm.tiles[s] + p * page_bytes;
-                        ptx::tma_load_2d(dst, &vmap, full, 0, row);
-                        ptx::tma_load_2d(dst + kHalfBytes, &vmap, full, 64, row);
-                    });
-                issued = r + 1;
-            }
-            // the last commit of every slot lands before the barriers are set up anew
-            for (int i = max(0, ro + n_tiles - kStages); ok && i < ro + n_tiles; ++i)
-                ok = wait(&sm.bar.empty[i % kStages], (i / kStages) & 1);
-            if (__any_sync(0xffffffffu, bad) && lane == 0) raise_flag(a.err, KL_FLAG_BAD_PAGE);
-            if (sm.abort) {
-                // copies still in flight land before the CTA's shared memory goes away
-                for (int i = max(0, issued - kStages); i < issued; ++i) {
-                    const int t = i - ro;
-                    uint64_t *const full = t < 0 ? &sm.bar.w_full[i % kStages] : &sm.bar.full[t % kStages];
-                    const uint32_t parity = ((t < 0 ? i : t) / kStages) & 1;
-                    const uint64_t t0 = ptx::globaltimer();
-                    while (!ptx::mbar_try_wait(full, parity) && ptx::globaltimer() - t0 < kTimeoutNs) {
-                    }
-                }
-            }
-        } else if (warp == kMmaWarp || warp == kPvWarp) {
-            // ------------------------------------------------------------ MMA issuers ----
-            // K-major SW128 operands step 32 B per 16 columns inside a 64-column half and jump a
-            // half (kHalfBytes) every 4 steps; MN-major SW128 operands step 16 rows = 2 KiB; TMEM
-            // A operands step 8 columns (16 packed 16-bit values).
-            constexpr uint32_t idesc_qk =
-                C::kFp16 ? idesc_f16(128, kBS, false, false) : ptx::idesc_bf16(128, kBS, false, false);
-            constexpr uint32_t idesc_route = ptx::idesc_bf16(128, 128, false, true);
-            constexpr uint32_t idesc_pv = C::kFp16 ? idesc_f16(128, 128, false, true) : idesc_route;
-            const uint64_t q_desc = ptx::smem_desc(ptx::smem_addr(sm.q), 16, 1024, ptx::kSwizzle128B);
-            const uint64_t k_desc = ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), 16, 1024, ptx::kSwizzle128B);
-            const uint64_t mn_desc =
-                ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), kHalfBytes, 1024, ptx::kSwizzle128B);
-            auto kstep = [](int kk) -> uint32_t { return ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4; };
-            if (warp == kMmaWarp) {
-                // Q_r = Q . W^R for all 128 rows, once per matrix, into alternating halves of columns
-                // 0 .. 255 (a row keeps the result of its head's matrix), then the scores
-                bool ok = true;
-                for (int r = 0; ok && r < ro; ++r) {
+                    for (int i = 0; i < kPer; ++i)
+                        parent[i] = i * 32 + lane < sg.n ? a.parents[q0 + i * 32 + lane] : -1;
+                // W^R matrices (B operand of the routing MMAs); the first brings the query block along
+                for (int r = 0; r < ro; ++r) {
                     const int s = r % kStages;
-                    ok = wait(&sm.bar.w_full[s], (r / kStages) & 1) &&
-                         (r < 2 || wait(&sm.bar.r_free[r & 1], ((r >> 1) - 1) & 1));
-                    if (!ok) break;
-                    ptx::tc_fence_after();
-                    if (ptx::elect_one()) {
-#pragma unroll
-                        for (int kk = 0; kk < kD / 16; ++kk)
-                            ptx::mma_bf16(tmem + (r & 1) * 128, q_desc + kstep(kk),
-                                          mn_desc + ((s * kTileBytes + kk * 2048) >> 4), idesc_route, kk > 0);
-                        ptx::mma_commit(&sm.bar.empty[s]);
-                        ptx::mma_commit(&sm.bar.r_full[r & 1]);
+                    if (r >= kStages && !(ok = wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1))) break;
+                    if (lane == 0) {
+                        const int wrow = (geo.wr_per_qh ? h + r : g) * kD;
+                        ptx::mbar_arrive_expect_tx(&sm.bar.w_full[s], kTileBytes + (r == 0 ? hp * rpb * kD * 2 : 0));
+                        ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.bar.w_full[s], 0, wrow);
+                        ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.bar.w_full[s], 64, wrow);
+                        if (r == 0) {
+                            ptx::tma_load_3d(sm.q, &qmap, &sm.bar.w_full[s], 0, h, q0 + m0);
+                            ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.bar.w_full[s], 64, h, q0 + m0);
+                        }
                     }
                     __syncwarp();
+                    issued = r + 1;
                 }
-                ok = ok && wait(&sm.bar.qr_ready, 0);
-                // (the loop by one lane: warp-wide waits between two half tiles leave the tensor cores idle)
-                if (ok && ptx::elect_one()) {
-                    ptx::tc_fence_after();
-                    for (int u = 0; u < n_sub; ++u) {
-                        const int t = u >> 1, s = (t + ro) % kStages, sb = u % kSub;
-                        if (!wait.one(C::kFp16 ? &sm.bar.v_full[t % kStages] : &sm.bar.full[t % kStages],
-                                      (t / kStages) & 1))
-                            break;
-                        // the output MMAs of half tile u - kSub have read this buffer's weights
-                        if (u >= kSub && !wait.one(&sm.bar.s_free[(u - kSub) & 3], ((u - kSub) >> 2) & 1)) break;
-                        ptx::tc_fence_after();
-                        const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
-                        // (the small terms first: the tensor core's adds truncate the sum)
+                if (k.has_drafts) {
+                    // (one that is not an earlier draft or -1 counts as -1)
+                    bool wrong = false;
 #pragma unroll
-                        for (int i = C::kQTerms - 1; i >= 0; --i)
+                    for (int i = 0; i < kPer; ++i) {
+                        const int j = i * 32 + lane;
+                        const bool fine = parent[i] >= -1 && parent[i] < j;
+                        wrong |= !fine;
+                        sm.parent[j] = fine ? parent[i] : -1;
+                    }
+                    if (wrong) raise_flag(a.err, KL_FLAG_BAD_TREE);
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.par_ready);
+                }
+                for (int i = 0; ok && i < n_tiles; ++i) {
+                    const int r = i + ro, s = r % kStages;
+                    uint64_t *const full = &sm.bar.full[i % kStages];
+                    const int pg = (tile0 + i) * ppt + lane;      // page index within the sequence
+                    const bool exists = lane < ppt && pg < seq_pages;
+                    const int page = exists ? bt[pg] : -1;
+                    if (r >= kStages && !wait(&sm.bar.empty[s], ((r / kStages) & 1) ^ 1)) break;
+                    const bool in_range = exists && page >= 0 && page < geo.num_pages;
+                    if (exists && !in_range) bad = true;
+                    const unsigned mask = __ballot_sync(0xffffffffu, in_range);
+                    ptx::for_pages(
+                        (page * geo.Hkv + g) * P, mask,
+                        [&] { ptx::mbar_arrive_expect_tx(full, __popc(mask) * page_bytes * 2u); },
+                        [&](int p, int row) {
+                            uint8_t *dst = sm.tiles[s] + p * page_bytes;
+                            ptx::tma_load_2d(dst, &vmap, full, 0, row);
+                            ptx::tma_load_2d(dst + kHalfBytes, &vmap, full, 64, row);
+                        });
+                    issued = r + 1;
+                }
+                // the last commit of every slot lands before the barriers are set up anew
+                for (int i = max(0, ro + n_tiles - kStages); ok && i < ro + n_tiles; ++i)
+                    ok = wait(&sm.bar.empty[i % kStages], (i / kStages) & 1);
+                if (__any_sync(0xffffffffu, bad) && lane == 0) raise_flag(a.err, KL_FLAG_BAD_PAGE);
+                if (sm.abort) {
+                    // copies still in flight land before the CTA's shared memory goes away
+                    for (int i = max(0, issued - kStages); i < issued; ++i) {
+                        const int t = i - ro;
+                        uint64_t *const full = t < 0 ? &sm.bar.w_full[i % kStages] : &sm.bar.full[t % kStages];
+                        const uint32_t parity = ((t < 0 ? i : t) / kStages) & 1;
+                        const uint64_t t0 = ptx::globaltimer();
+                        while (!ptx::mbar_try_wait(full, parity) && ptx::globaltimer() - t0 < kTimeoutNs) {
+                        }
+                    }
+                }
+            } else if (warp == kMmaWarp || warp == kPvWarp) {
+                // ------------------------------------------------------------ MMA issuers ----
+                // K-major SW128 operands step 32 B per 16 columns inside a 64-column half and jump a
+                // half (kHalfBytes) every 4 steps; MN-major SW128 operands step 16 rows = 2 KiB; TMEM
+                // A operands step 8 columns (16 packed 16-bit values).
+                constexpr uint32_t idesc_qk =
+                    C::kFp16 ? idesc_f16(128, kBS, false, false) : ptx::idesc_bf16(128, kBS, false, false);
+                constexpr uint32_t idesc_route = ptx::idesc_bf16(128, 128, false, true);
+                constexpr uint32_t idesc_pv = C::kFp16 ? idesc_f16(128, 128, false, true) : idesc_route;
+                const uint64_t q_desc = ptx::smem_desc(ptx::smem_addr(sm.q), 16, 1024, ptx::kSwizzle128B);
+                const uint64_t k_desc = ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), 16, 1024, ptx::kSwizzle128B);
+                const uint64_t mn_desc =
+                    ptx::smem_desc(ptx::smem_addr(sm.tiles[0]), kHalfBytes, 1024, ptx::kSwizzle128B);
+                auto kstep = [](int kk) -> uint32_t { return ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4; };
+                if (warp == kMmaWarp) {
+                    // Q_r = Q . W^R for all 128 rows, once per matrix, into alternating halves of columns
+                    // 0 .. 255 (a row keeps the result of its head's matrix), then the scores
+                    bool ok = true;
+                    for (int r = 0; ok && r < ro; ++r) {
+                        const int s = r % kStages;
+                        ok = wait(&sm.bar.w_full[s], (r / kStages) & 1) &&
+                             (r < 2 || wait(&sm.bar.r_free[r & 1], ((r >> 1) - 1) & 1));
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one()) {
 #pragma unroll
                             for (int kk = 0; kk < kD / 16; ++kk)
-                                ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + 64 * i + kk * 8,
-                                                 b0 + kstep(kk), idesc_qk, i < C::kQTerms - 1 || kk > 0);
-                        ptx::mma_commit(&sm.bar.s_full[u & 3]);
+                                ptx::mma_bf16(tmem + (r & 1) * 128, q_desc + kstep(kk),
+                                              mn_desc + ((s * kTileBytes + kk * 2048) >> 4), idesc_route, kk > 0);
+                            ptx::mma_commit(&sm.bar.empty[s]);
+                            ptx::mma_commit(&sm.bar.r_full[r & 1]);
+                        }
+                        __syncwarp();
+                    }
+                    ok = ok && wait(&sm.bar.qr_ready, 0);
+                    // (the loop by one lane: warp-wide waits between two half tiles leave the tensor cores idle)
+                    if (ok && ptx::elect_one()) {
+                        ptx::tc_fence_after();
+                        for (int u = 0; u < n_sub; ++u) {
+                            const int t = u >> 1, s = (t + ro) % kStages, sb = u % kSub;
+                            if (!wait.one(C::kFp16 ? &sm.bar.v_full[t % kStages] : &sm.bar.full[t % kStages],
+                                          (t / kStages) & 1))
+                                break;
+                            // the output MMAs of half tile u - kSub have read this buffer's weights
+                            if (u >= kSub && !wait.one(&sm.bar.s_free[(u - kSub) & 3], ((u - kSub) >> 2) & 1)) break;
+                            ptx::tc_fence_after();
+                            const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+                            // (the small terms first: the tensor core's adds truncate the sum)
+#pragma unroll
+                            for (int i = C::kQTerms - 1; i >= 0; --i)
+#pragma unroll
+                                for (int kk = 0; kk < kD / 16; ++kk)
+                                    ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + 64 * i + kk * 8,
+                                                     b0 + kstep(kk), idesc_qk, i < C::kQTerms - 1 || kk > 0);
+                            ptx::mma_commit(&sm.bar.s_full[u & 3]);
+                        }
+                    }
+                } else if (ptx::elect_one()) {
+                    // O += P . V (Half: the group's); at a fold O starts over (its old value has been read by then)
+                    for (int u = 0; u < n_sub; ++u) {
+                        const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
+                        if (!wait.one(&sm.bar.p_full[u & 3], (u >> 2) & 1)) break;
+                        ptx::tc_fence_after();
+                        const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
+                        const bool more = C::kFp16 ? u >= kGroups : u % kFoldSub != 0;
+                        const uint32_t o = tmem + kColO + (C::kFp16 ? (u & 1) * kD : 0);
+#pragma unroll
+                        for (int kk = 0; kk < C::kPTerms * kBS / 16; ++kk)
+                            ptx::mma_bf16_ts(o, tmem + sb * C::kBuf + kk * 8,
+                                             b0 + (((kk & 3) * 2048) >> 4), idesc_pv, (more || kk > 0) ? 1u : 0u);
+                        ptx::mma_commit(&sm.bar.s_free[u & 3]);
+                        if ((u & 1) || u == n_sub - 1) ptx::mma_commit(&sm.bar.empty[s]);
                     }
                 }
-            } else if (ptx::elect_one()) {
-                // O += P . V (Half: the group's); at a fold O starts over (its old value has been read by then)
-                for (int u = 0; u < n_sub; ++u) {
-                    const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
-                    if (!wait.one(&sm.bar.p_full[u & 3], (u >> 2) & 1)) break;
-                    ptx::tc_fence_after();
-                    const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
-                    const bool more = C::kFp16 ? u >= kGroups : u % kFoldSub != 0;
-                    const uint32_t o = tmem + kColO + (C::kFp16 ? (u & 1) * kD : 0);
-#pragma unroll
-                    for (int kk = 0; kk < C::kPTerms * kBS / 16; ++kk)
-                        ptx::mma_bf16_ts(o, tmem + sb * C::kBuf + kk * 8,
-                                         b0 + (((kk & 3) * 2048) >> 4), idesc_pv, (more || kk > 0) ? 1u : 0u);
-                    ptx::mma_commit(&sm.bar.s_free[u & 3]);
-                    if ((u & 1) || u == n_sub - 1) ptx::mma_commit(&sm.bar.empty[s]);
-                }
-            }
-            __syncwarp();
-            // every MMA this warp issued completes before the segment ends
-            uint64_t *drain = warp == kMmaWarp ? &sm.bar.drain : &sm.bar.drain2;
-            if (ptx::elect_one()) ptx::mma_commit(drain);
-            __syncwarp();
-            const uint64_t t0 = ptx::globaltimer();
-            while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer() - t0 < kTimeoutNs) {
-            }
-        } else if (C::kFp16 && warp >= kConvWarp) {
-            // ----------------------------------------------------------- tiles to fp16 ----
-            // Thread = (row, 64 dims) of both half tiles, in place, ahead of the score MMAs. The lanes start at
-            // different 16-byte chunks so that a warp's accesses spread over all banks.
-            const int r = (warp - kConvWarp) * 32 + lane;
-            for (int t = 0; t < n_tiles; ++t) {
-                const int st = (t + ro) % kStages;
-                if (!wait(&sm.bar.full[t % kStages], (t / kStages) & 1)) break;
-                const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes + (r & 63) * 128;
-                const int t0 = (tile0 + t) * kBN;
-                uint32_t v[2][32];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        ld_shared_v4(v_s + j * kBS * 128 + ((c + lane) & 7) * 16, v[j] + 4 * c);
-                if (t0 + kBN > base) {
-                    // Rows that not every draft sees must not reach the others through 0 * NaN: a row past the
-                    // sequence's end, or a drafted one without a finite fp16 form, becomes zeros; a draft
-                    // that sees such a row gets NaN by its bit in `over`.
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int vt = t0 + j * kBS + (r & 63);
-                        bool over = false;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) over |= past_fp16(v[j][e]);
-                        if (over && vt >= base && vt < L)
-                            atomicOr(&sm.over[(vt - base) >> 5], 1u << ((vt - base) & 31));
-                        if (vt >= L || (over && vt >= base))
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[j][e] = 0u;
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-#pragma unroll
-                        for (int e = 4 * c; e < 4 * c + 4; ++e)
-                            v[j][e] = pack_f16(__uint_as_float(v[j][e] << 16),
-                                               __uint_as_float(v[j][e] & 0xffff0000u));
-                        st_shared_v4(v_s + j * kBS * 128 + ((c + lane) & 7) * 16, v[j][4 * c], v[j][4 * c + 1],
-                                     v[j][4 * c + 2], v[j][4 * c + 3]);
-                    }
-                ptx::fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sm.bar.v_full[t % kStages]);
+                // every MMA this warp issued completes before the segment ends
+                uint64_t *drain = warp == kMmaWarp ? &sm.bar.drain : &sm.bar.drain2;
+                if (ptx::elect_one()) ptx::mma_commit(drain);
+                __syncwarp();
+                const uint64_t t0 = ptx::globaltimer();
+                while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer() - t0 < kTimeoutNs) {
+                }
+            } else if (C::kFp16 && warp >= kConvWarp) {
+                // ----------------------------------------------------------- tiles to fp16 ----
+                // Thread = (row, 64 dims) of both half tiles, in place, ahead of the score MMAs. The lanes start at
+                // different 16-byte chunks so that a warp's accesses spread over all banks.
+                const int r = (warp - kConvWarp) * 32 + lane;
+                for (int t = 0; t < n_tiles; ++t) {
+                    const int st = (t + ro) % kStages;
+                    if (!wait(&sm.bar.full[t % kStages], (t / kStages) & 1)) break;
+                    const uint32_t v_s = ptx::smem_addr(sm.tiles[st]) + (r >> 6) * kHalfBytes + (r & 63) * 128;
+                    const int t0 = (tile0 + t) * kBN;
+                    uint32_t v[2][32];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            ld_shared_v4(v_s + j * kBS * 128 + ((c + lane) & 7) * 16, v[j] + 4 * c);
+                    if (t0 + kBN > base) {
+                        // Rows that not every draft sees must not reach the others through 0 * NaN: a row past the
+                        // sequence's end, or a drafted one without a finite fp16 form, becomes zeros; a draft
+                        // that sees such a row gets NaN by its bit in `over`.
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int vt = t0 + j * kBS + (r & 63);
+                            bool over = false;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) over |= past_fp16(v[j][e]);
+                            if (over && vt >= base && vt < L)
+                                atomicOr(&sm.over[(vt - base) >> 5], 1u << ((vt - base) & 31));
+                            if (vt >= L || (over && vt >= base))
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) v[j][e] = 0u;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+#pragma unroll
+                            for (int e = 4 * c; e < 4 * c + 4; ++e)
+                                v[j][e] = pack_f16(__uint_as_float(v[j][e] << 16),
+                                                   __uint_as_float(v[j][e] & 0xffff0000u));
+                            st_shared_v4(v_s + j * kBS * 128 + ((c + lane) & 7) * 16, v[j][4 * c], v[j][4 * c + 1],
+                                         v[j][4 * c + 2], v[j][4 * c + 3]);
+                        }
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.v_full[t % kStages]);
+                }
             }
-        }
-        if (!end(k)) break;
+            if (!end(k)) break;
         }
     } else {
         if constexpr (C::kFp16) ptx::regs_inc<kSoftmaxRegs>();
         for (int si = 0;; ++si) {
-        const Part k = begin(si);
-        const uint32_t tmem = sm.tmem_base;
-        const bool has_drafts = k.has_drafts, whole = k.whole;
-        const TreeSegment &sg = k.sg;
-        const int m0 = k.blk.m0, rows = k.blk.rows, h = k.blk.h, hn = k.blk.hn;
-        const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0;
-        const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
+            const Part k = begin(si);
+            const uint32_t tmem = sm.tmem_base;
+            const bool has_drafts = k.has_drafts, whole = k.whole;
+            const TreeSegment &sg = k.sg;
+            const int m0 = k.blk.m0, rows = k.blk.rows, h = k.blk.h, hn = k.blk.hn;
+            const int q0 = sg.q0, L = sg.L, tile0 = sg.tile0;
+            const int base = L - sg.n, n_sub = k.n_sub, ro = k.ro;
             // ----------------------------------------------------- softmax, epilogue ----
             if (tid == 0 && k.more) sm.seg[(si + 1) & 1] = next_segment(a, sg);
             constexpr int kCols = kD / kGroups;             // columns of the query and of O per group
@@ -1023,7 +1032,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     reinterpret_cast<float2 *>(state + kBM * kD * 4)[r] = make_float2(m_fin, lt);
                 if (C::kFp16 && __any_sync(0xffffffffu, nf != nf) && lane == 0) raise_flag(a.err, KL_FLAG_RANGE);
             }
-        if (!end(k)) break;
+            if (!end(k)) break;
         }
     }
 
@@ -1034,10 +1043,9 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
 // 2^(m_s - M) and M the largest m_s of a part with l_s > 0. CTA (c, y): the unit that run c enters first
 // inside, dims 8 y .. + 7; thread = row and 4 dims, kMergeAhead parts in flight against a running M.
 constexpr int kMergeThreads = 2 * kBM, kMergeAhead = 8;
-constexpr int kMaxRuns = 512;                        // (SMs: one run each)
 
 __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const TreeArgs a) {
-    __shared__ const uint8_t *part[kMaxRuns];
+    __shared__ const uint8_t *part[kTreeMaxRuns];
     __shared__ int parts;
     grid_dep_wait();
     grid_dep_launch();

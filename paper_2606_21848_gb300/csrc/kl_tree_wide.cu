@@ -1,6 +1,9 @@
 // Attention of a tree of drafted tokens with few rows per value head (drafts x heads of a group <= 32) on the
 // wide decode's kernel (kl_decode_wide_kernel.cuh, kTree): there a tile costs what its 16 or 32 rows cost,
 // where a block of kl_tree_tc.cu costs 128 rows, and the splits merge inside.
+// Measured, 32 / 8 heads: 4 drafts on 700 tokens 9.7 us (12.2 in kl_tree_tc.cu; latency); 8 sequences of 4096
+// tokens, 8 drafts 26 us (34; HBM 10, the rest the start-up and the splits' merge); 64 of 8192, 4 drafts 172 us
+// (6250 GB/s), 8 drafts 224 us (the tile chain of 32 rows); one of 131072, 8 drafts 60 us (HBM 40).
 #include "kl_decode_wide_kernel.cuh"
 
 namespace kl {
