@@ -79,12 +79,12 @@ constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 i
 // The routed queries first land in columns 0 .. 255, before anything else is there.
 struct Half {
     static constexpr bool kFp16 = true;
-    static constexpr int kQTerms = 1, kPTerms = 1, kSub = 3, kConvWarps = 4, kStages = 5;
+    static constexpr int kQTerms = 1, kPTerms = 1, kSub = 3, kStages = 5;
     static constexpr uint32_t kBuf = 64, kColO = 192, kColQ = 448;
 };
 struct Full {
     static constexpr bool kFp16 = false;
-    static constexpr int kQTerms = 3, kPTerms = 3, kSub = 2, kConvWarps = 0, kStages = 3;
+    static constexpr int kQTerms = 3, kPTerms = 3, kSub = 2, kStages = 3;
     static constexpr uint32_t kBuf = 96, kColO = 192, kColQ = 320;
 };
 constexpr int kGroups = 2;
@@ -95,8 +95,8 @@ static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "");
 template <typename C>
 struct Warps {
     static constexpr int kCompute = 4 * kGroups;
-    static constexpr int kProducer = kCompute, kMma = kCompute + 1, kPv = kCompute + 2, kConv = kCompute + 4;
-    static constexpr int kThreads = 32 * (C::kConvWarps ? kConv + C::kConvWarps : kPv + 1);
+    static constexpr int kProducer = kCompute, kMma = kCompute + 1, kPv = kCompute + 2, kHelp = kCompute + 4;
+    static constexpr int kThreads = 32 * (kHelp + 4);
 };
 constexpr int kFoldSub = 2;           // Full: half tiles between two moves of O to the fp32 sum
 
@@ -117,13 +117,13 @@ struct __align__(1024) TreeSmem {
     struct Bars {
         uint64_t w_full[C::kStages], full[C::kStages], empty[C::kStages];
         uint64_t s_full[4], s_free[4];
-        uint64_t p_full[4], v_full[C::kStages];
+        uint64_t p_full[4], o_free, sum_full, v_full[C::kStages];
         uint64_t turn[4][kGroups];
         uint64_t first[4];                 // per lane quarter: the maxima of half tile 1 are in lsum[1]
         uint64_t r_full[2], r_free[2];     // routing results, alternating halves of columns 0 .. 255
         uint64_t qr_ready, par_ready, drain, drain2;
     } bar;
-    float mref[kGroups][kBM];  // the rows' references after the last half tile of each group
+    float mref[4][kBM];        // the rows' references: Full after half tile u at u % 4, Half each group's last
     float lsum[kGroups][kBM];  // the groups' shares of the row sums, for the epilogue; Full: before it,
                                // lsum[1] holds half tile 1's maxima for the first reference
     float fref[kBM];           // Full: the references of `sum`
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                    const __grid_constant__ CUtensorMap qmap, const TreeArgs a) {
     constexpr int kSub = C::kSub, kStages = C::kStages;
     constexpr int kComputeWarps = Warps<C>::kCompute, kProducerWarp = Warps<C>::kProducer;
-    constexpr int kMmaWarp = Warps<C>::kMma, kPvWarp = Warps<C>::kPv, kConvWarp = Warps<C>::kConv;
+    constexpr int kMmaWarp = Warps<C>::kMma, kPvWarp = Warps<C>::kPv, kHelpWarp = Warps<C>::kHelp;
     constexpr uint32_t kColO = C::kColO, kColQ = C::kColQ;
     using Smem = TreeSmem<C>;
     extern __shared__ uint8_t smem_raw[];
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
     };
 
     if (warp >= kComputeWarps) {
-        if constexpr (C::kFp16) ptx::regs_dec<kOtherRegs>();
+        ptx::regs_dec<kOtherRegs>();
         for (int si = 0;; ++si) {
             const Part k = begin(si);
             const uint32_t tmem = sm.tmem_base;
@@ -555,6 +555,8 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     for (int u = 0; u < n_sub; ++u) {
                         const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
                         if (!wait.one(&sm.bar.p_full[u & 3], (u >> 2) & 1)) break;
+                        if (!C::kFp16 && u && u % kFoldSub == 0 && !wait.one(&sm.bar.o_free, (u / kFoldSub - 1) & 1))
+                            break;
                         ptx::tc_fence_after();
                         const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
                         const bool more = C::kFp16 ? u >= kGroups : u % kFoldSub != 0;
@@ -575,11 +577,11 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 const uint64_t t0 = ptx::globaltimer();
                 while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer() - t0 < kTimeoutNs) {
                 }
-            } else if (C::kFp16 && warp >= kConvWarp) {
+            } else if (C::kFp16 && warp >= kHelpWarp) {
                 // ----------------------------------------------------------- tiles to fp16 ----
                 // Thread = (row, 64 dims) of both half tiles, in place, ahead of the score MMAs. The lanes start at
                 // different 16-byte chunks so that a warp's accesses spread over all banks.
-                const int r = (warp - kConvWarp) * 32 + lane;
+                const int r = (warp - kHelpWarp) * 32 + lane;
                 for (int t = 0; t < n_tiles; ++t) {
                     const int st = (t + ro) % kStages;
                     if (!wait(&sm.bar.full[t % kStages], (t / kStages) & 1)) break;
@@ -623,11 +625,57 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(&sm.bar.v_full[t % kStages]);
                 }
+            } else if (!C::kFp16 && warp >= kHelpWarp) {
+                // ------------------------------------------------------------- O to the sum ----
+                // Every kFoldSub half tiles O, at its reference, joins the fp32 sum and the output MMAs start
+                // over as soon as it has been read (thread = row = TMEM lane).
+                const int qd = warp & 3, r = qd * 32 + lane;
+                const uint32_t lane_base = (uint32_t)(qd * 32) << 16;
+                float4 *const row = reinterpret_cast<float4 *>(sm.sum) + r * 32;
+                float m_sum = -INFINITY;                     // the sum's reference
+                bool okf = qd < (k.blk.rows * hp + 31) >> 5; // (a quarter without rows rests)
+                for (int u = kFoldSub; okf && u < n_sub; u += kFoldSub) {
+                    okf = wait(&sm.bar.s_free[(u - 1) & 3], ((u - 1) >> 2) & 1) &&
+                          wait(&sm.bar.turn[qd][(u - 1) % kGroups], ((u - 1) / kGroups) & 1);
+                    if (!okf) break;
+                    ptx::tc_fence_after();
+                    const float m = sm.mref[(u - 1) & 3][r];
+                    const float f = m_sum == -INFINITY ? 0.f : ptx::ex2(m_sum - m);
+                    const bool had = u > kFoldSub;
+                    m_sum = m;
+#pragma unroll
+                    for (int c = 0; c < kD; c += 32) {
+                        uint32_t o[32];
+                        ptx::tmem_ld32(tmem + kColO + c + lane_base, o);
+                        ptx::tmem_wait_ld();
+                        ptx::reg_fence(o);
+                        if (c == kD - 32) {
+                            ptx::tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(&sm.bar.o_free);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float4 &w = row[(c / 4 + e) ^ lane];
+                            float4 y = had ? w : make_float4(0.f, 0.f, 0.f, 0.f);
+                            y.x = fmaf(y.x, f, __uint_as_float(o[4 * e]));
+                            y.y = fmaf(y.y, f, __uint_as_float(o[4 * e + 1]));
+                            y.z = fmaf(y.z, f, __uint_as_float(o[4 * e + 2]));
+                            y.w = fmaf(y.w, f, __uint_as_float(o[4 * e + 3]));
+                            w = y;
+                        }
+                    }
+                }
+                if (okf && n_sub > kFoldSub) {
+                    sm.fref[r] = m_sum;
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.sum_full);
+                }
             }
             if (!end(k)) break;
         }
     } else {
-        if constexpr (C::kFp16) ptx::regs_inc<kSoftmaxRegs>();
+        ptx::regs_inc<kSoftmaxRegs>();
         for (int si = 0;; ++si) {
             const Part k = begin(si);
             const uint32_t tmem = sm.tmem_base;
@@ -729,7 +777,6 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
 
             float m_used = -INFINITY;  // the reference of this thread's share of the row sum
             float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
-            float m_sum = -INFINITY;   // Full: the reference of sm.sum (group 0)
             bool okl = ok;
             for (int u = grp; okl && u < n_sub; u += kGroups) {
                 const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
@@ -813,46 +860,18 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     }
                     okl = wait(&sm.bar.turn[qd][(u - 1) % kGroups], ((u - 1) / kGroups) & 1);
                     if (!okl) break;
-                    m_ref = sm.mref[(u - 1) % kGroups][r];
+                    m_ref = sm.mref[(u - 1) & 3][r];
                 }
                 const float m_new = fmaxf(m_ref, mt);
                 const bool moves = __any_sync(0xffffffffu, m_new > m_ref + kRescaleLog2);
-                const bool fold = !C::kFp16 && u > 0 && u % kFoldSub == 0;
-                const int before = C::kFp16 ? u - kGroups : u - 1;   // the last half tile that O holds
-                if (before >= 0 && (moves || fold)) {
-                    okl = wait(&sm.bar.s_free[before & 3], (before >> 2) & 1);
-                    if (!okl) break;
-                    ptx::tc_fence_after();
-                }
-                if (fold) {
-                    // O, at reference m_ref, joins the sum; the output MMAs of u start over
-                    const float f = m_sum == -INFINITY ? 0.f : ptx::ex2(m_sum - m_ref);
-                    const bool had = u > kFoldSub;
-                    float4 *row = reinterpret_cast<float4 *>(sm.sum) + r * 32;
-#pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
-                        uint32_t o[32];
-                        ptx::tmem_ld32(tmem + kColO + c + lane_base, o);
-                        ptx::tmem_wait_ld();
-                        ptx::reg_fence(o);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float4 &w = row[(c / 4 + e) ^ lane];
-                            float4 y = had ? w : make_float4(0.f, 0.f, 0.f, 0.f);
-                            y.x = fmaf(y.x, f, __uint_as_float(o[4 * e]));
-                            y.y = fmaf(y.y, f, __uint_as_float(o[4 * e + 1]));
-                            y.z = fmaf(y.z, f, __uint_as_float(o[4 * e + 2]));
-                            y.w = fmaf(y.w, f, __uint_as_float(o[4 * e + 3]));
-                            w = y;
-                        }
-                    }
-                    ptx::tc_fence_before();
-                    m_sum = m_ref;
-                    sm.fref[r] = m_ref;
-                }
+                // the last half tile that O holds (Full: O starts over at even half tiles)
+                const int before = C::kFp16 ? u - kGroups : u % kFoldSub ? u - 1 : -1;
                 // a new reference when the maximum grew by more than 2^14 (or is the first finite)
                 if (moves) {
-                    if (before >= 0 && !fold) {
+                    if (before >= 0) {
+                        okl = wait(&sm.bar.s_free[before & 3], (before >> 2) & 1);
+                        if (!okl) break;
+                        ptx::tc_fence_after();
                         const float f =
                             (m_new == -INFINITY || m_ref == -INFINITY) ? 0.f : ptx::ex2(m_ref - m_new);
 #pragma unroll
@@ -870,7 +889,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     m_ref = m_new;
                 }
                 if constexpr (!C::kFp16) {
-                    sm.mref[grp][r] = m_ref;
+                    sm.mref[u & 3][r] = m_ref;
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(&sm.bar.turn[qd][grp]);
                 }
@@ -931,13 +950,14 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             if (!C::kFp16 && okl && lg != grp) okl = wait(&sm.bar.turn[qd][lg], (last / kGroups) & 1);
             // (all of the last commits land before the barriers are set up anew)
             bool oke = okl;
+            if (!C::kFp16 && oke && last >= kFoldSub) oke = wait(&sm.bar.sum_full, 0);
             for (int u = last; oke && u >= 0 && u > last - 3; --u) oke = wait(&sm.bar.s_free[u & 3], (u >> 2) & 1);
             float l = (la.x + la.y) + (lb.x + lb.y);
             float m_fin = 0.f;
             if constexpr (C::kFp16) {
                 sm.mref[grp][r] = m_used;
             } else {
-                m_fin = sm.mref[lg][r];
+                m_fin = sm.mref[last & 3][r];
                 if (oke && lg != grp) l = m_used == -INFINITY ? 0.f : l * ptx::ex2(m_used - m_fin);
             }
             sm.lsum[grp][r] = l;
