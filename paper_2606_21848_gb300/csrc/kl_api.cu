@@ -369,7 +369,7 @@ SharedLayout shared_layout(size_t counters, size_t state_bytes, size_t extra_byt
 // runs' entries for the merge, then their states (none of which a decode's counters ever share). `wide`: on
 // the wide decode's kernel, with its split plan, counters in the front region and split states.
 kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t num_splits,
-                         bool wide, Geometry *g, TreePlan *p, SharedLayout *w) {
+                         bool wide, bool fp32, Geometry *g, TreePlan *p, SharedLayout *w) {
     const kl_status st = resolve(shape, wide ? num_splits : -1, g);
     if (st != KL_OK) return st;
     if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits) return KL_ERR_INVALID_ARG;
@@ -380,7 +380,7 @@ kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_l
         return KL_OK;
     }
     *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P,
-                   device_sm_count());
+                   device_sm_count(), fp32);
     *w = shared_layout(0, p->ctas * sizeof(TreeMerge), p->ctas * 2 * kTreeStateBytes);
     return KL_OK;
 }
@@ -400,11 +400,13 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
                               int32_t num_splits) {
     Geometry g;
     TreePlan p;
-    SharedLayout w, ww{0, 0, 0};
-    if (plan_tree_call(shape, total_q, max_q_len, num_splits, false, &g, &p, &w) != KL_OK) return 0;
-    if (tree_wide(shape, max_q_len, false))
-        (void)plan_tree_call(shape, total_q, max_q_len, num_splits, true, &g, &p, &ww);
-    return w.total > ww.total ? w.total : ww.total;
+    SharedLayout w;
+    if (plan_tree_call(shape, total_q, max_q_len, num_splits, false, true, &g, &p, &w) != KL_OK) return 0;
+    size_t most = w.total;
+    const bool wide = tree_wide(shape, max_q_len, false);
+    if (plan_tree_call(shape, total_q, max_q_len, num_splits, wide, false, &g, &p, &w) == KL_OK && w.total > most)
+        most = w.total;
+    return most;
 }
 
 kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
@@ -417,7 +419,7 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     TreePlan p;
     SharedLayout w;
     const bool wide = tree_wide(shape, max_q_len, out_dtype == KL_FP32);
-    const kl_status st = plan_tree_call(shape, total_q, max_q_len, num_splits, wide, &g, &p, &w);
+    const kl_status st = plan_tree_call(shape, total_q, max_q_len, num_splits, wide, out_dtype == KL_FP32, &g, &p, &w);
     if (st != KL_OK) return st;
     if (!prefill_tc_supported(g)) return KL_ERR_UNSUPPORTED;
     if (g.B == 0 || total_q == 0 || max_q_len == 0) return KL_OK;
@@ -456,6 +458,9 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     a.hp = p.hp;
     a.rpb = p.rpb;
     a.ctas = p.ctas;
+    a.start = p.start;
+    a.run = p.run;
+    a.whole = p.whole;
     a.num_splits = num_splits;
     a.q = static_cast<const uint16_t *>(q);
     a.w_r = static_cast<const uint16_t *>(w_r);

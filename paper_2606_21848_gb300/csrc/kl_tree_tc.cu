@@ -158,7 +158,7 @@ __device__ __forceinline__ uint64_t window64(uint64_t lo, uint64_t hi, int off) 
 
 // ---------------------------------------------------------------------- runs and segments ----
 //
-// All units lie end to end on one line, each as kTreeStart (what starting a segment takes, in tiles) and its
+// All units lie end to end on one line, each as a.start (what starting a segment takes, in tiles) and its
 // tiles; the runs are equal shares of it. A run's start moves down to a cut: the unit's start, or a multiple
 // of the unit's step among its tiles.
 
@@ -185,7 +185,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int b, bool repor
 
 // Cuts inside a unit of `tiles` tiles fall on multiples of this.
 __device__ __forceinline__ int cut_step(const TreeArgs &a, int tiles) {
-    return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : tiles <= kTreeRun ? tiles : kTreeCut;
+    return a.num_splits > 0 ? (tiles + a.num_splits - 1) / a.num_splits : tiles <= a.whole ? tiles : kTreeCut;
 }
 
 // Quotients of what mostly fits 32 bits (the 64-bit division is a long sequence of instructions).
@@ -203,8 +203,8 @@ __device__ __forceinline__ int run_of(const TreeShare &s, int64_t x) {
 }
 
 // The tile of a unit (`off` past its start on the line) that a run's start moves down to.
-__device__ __forceinline__ int cut_tile(int64_t off, int tiles, int step) {
-    return off <= kTreeStart ? 0 : off >= kTreeStart + tiles ? tiles : ((int)off - kTreeStart) / step * step;
+__device__ __forceinline__ int cut_tile(int start, int64_t off, int tiles, int step) {
+    return off <= start ? 0 : off >= start + tiles ? tiles : ((int)off - start) / step * step;
 }
 
 // Finds this CTA's run: sm.x0, sm.x1 and the first segment; writes the CTA's entry for the merge. All
@@ -220,7 +220,7 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
     TreeSeq only = TreeSeq{0, 0, 0, 0, 0};           // (the sequence of a thread that has one)
     for (int b = b0; b < b1; ++b) {
         only = tree_seq(a, b, c == 0);
-        mine += (int64_t)(only.tiles + kTreeStart) * only.units;
+        mine += (int64_t)(only.tiles + a.start) * only.units;
         units += only.units;
     }
     int64_t upto = mine;                             // inclusive prefix
@@ -244,8 +244,8 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         total += sm.warp_tiles[w];
         units += sm.warp_units[w];
     }
-    // as many runs as there are CTAs, while they have kTreeRun tiles or a unit each
-    const int64_t most = max((int64_t)units, total / (kTreeRun + kTreeStart));
+    // as many runs as there are CTAs, while they have a.run tiles or a unit each
+    const int64_t most = max((int64_t)units, total / (a.run + a.start));
     const int runs = (int)(most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x);
     if (c >= runs) return false;
     const int64_t each = quotient(total, runs);
@@ -261,23 +261,23 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
         int64_t start = upto - mine;
         for (int b = b0; b < b1; ++b) {
             const TreeSeq s = per == 1 ? only : tree_seq(a, b, false);
-            const int len = s.tiles + kTreeStart;
+            const int len = s.tiles + a.start;
             const int64_t all = (int64_t)len * s.units;
             if (x < start + all) {
                 const int unit = (int)quotient(x - start, len);
                 const int64_t unit0 = start + (int64_t)unit * len;
-                const int step = cut_step(a, s.tiles), tile0 = cut_tile(x - unit0, s.tiles, step);
-                const int64_t at = tile0 ? unit0 + kTreeStart + tile0 : unit0;
+                const int step = cut_step(a, s.tiles), tile0 = cut_tile(a.start, x - unit0, s.tiles, step);
+                const int64_t at = tile0 ? unit0 + a.start + tile0 : unit0;
                 if (end == 1) {
                     sm.x1 = at;
                 } else {
                     sm.x0 = at;
                     sm.seg[0] = TreeSegment{unit0, b, unit, tile0, s.q0, s.n, s.L, s.tiles, s.units};
                     // the first run that starts inside the unit announces its parts
-                    if (tile0 > 0 && cut_tile(run_start(share, c - 1) - unit0, s.tiles, step) == 0) {
+                    if (tile0 > 0 && cut_tile(a.start, run_start(share, c - 1) - unit0, s.tiles, step) == 0) {
                         const TreeBlock k = tree_block(a, sm.seg[0]);
                         a.merge[c] = TreeMerge{unit0, share, s.tiles, step,
-                                               run_of(share, unit0 + kTreeStart + s.tiles - 1), s.q0 + k.m0, k.rows,
+                                               run_of(share, unit0 + a.start + s.tiles - 1), s.q0 + k.m0, k.rows,
                                                k.h, k.hn};
                     }
                 }
@@ -293,7 +293,7 @@ __device__ bool find_run(TreeSmem<C> &sm, const TreeArgs &a) {
 // The segment after `s` in a run that goes on behind s's unit: the next unit.
 __device__ __forceinline__ TreeSegment next_segment(const TreeArgs &a, const TreeSegment &s) {
     TreeSegment t = s;
-    t.unit0 = s.unit0 + kTreeStart + s.tiles;
+    t.unit0 = s.unit0 + a.start + s.tiles;
     t.tile0 = 0;
     if (++t.unit == s.units) {
         t.unit = 0;
@@ -368,8 +368,8 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
     };
     auto begin = [&](int si) -> Part {
         const TreeSegment sg = sm.seg[si & 1];
-        const bool more = x1 > sg.unit0 + kTreeStart + sg.tiles;     // the run goes on behind the unit
-        const int n_tiles = (int)min((int64_t)sg.tiles, x1 - sg.unit0 - kTreeStart) - sg.tile0;
+        const bool more = x1 > sg.unit0 + a.start + sg.tiles;     // the run goes on behind the unit
+        const int n_tiles = (int)min((int64_t)sg.tiles, x1 - sg.unit0 - a.start) - sg.tile0;
         // The block: drafts m0 .. m0 + rows - 1, heads h .. h + hn - 1 of the group; row r of the 128 is
         // draft m0 + r / hp with head h + r % hp.
         const TreeBlock blk = tree_block(a, sg);
@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const TreeArg
     if (t.rows == 0) return;
     if (tid < 32) {
         // The runs from c - 1 on that hold some of the unit; a run's first state where it starts inside it.
-        auto cut = [&](int run) { return cut_tile(run_start(t.share, run) - t.unit0, t.tiles, t.step); };
+        auto cut = [&](int run) { return cut_tile(a.start, run_start(t.share, run) - t.unit0, t.tiles, t.step); };
         int n = 0;
         for (int r0 = c - 1; r0 <= t.last; r0 += 32) {
             const int run = r0 + tid;
@@ -1201,9 +1201,9 @@ cudaError_t launch_tree_tc(const TreeArgs &a) {
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
     e = cudaLaunchKernelEx(&cfg, kernel, vmap, wmap, qmap, a);
-    // (units of up to kTreeRun tiles are not cut)
+    // (units of up to a.whole tiles are not cut)
     const int64_t most_tiles = ((int64_t)g.max_pages * g.P + kBN - 1) / kBN;
-    if (e != cudaSuccess || a.ctas == 1 || a.num_splits == 1 || (a.num_splits == 0 && most_tiles <= kTreeRun))
+    if (e != cudaSuccess || a.ctas == 1 || a.num_splits == 1 || (a.num_splits == 0 && most_tiles <= a.whole))
         return e;
     cfg.gridDim = dim3((unsigned)a.ctas - 1, kD / 8);
     cfg.blockDim = dim3(kMergeThreads);

@@ -118,4 +118,4 @@ def test_layouts_cover_all_rows(plan, G):
                 assert blocks == -(-G // hp) * -(-n // rpb)
                 assert blocks <= G * -(-n // 128)
                 units = max(B, 1) * 2 * blocks
-                assert ctas == min(152, max(units, (-(-tokens // 128) + 5) * units // 13))
+                assert ctas == min(152, max(units, (-(-tokens // 128) + 5) * units // 7))
