@@ -88,9 +88,9 @@ struct Full {
     static constexpr uint32_t kBuf = 96, kColO = 192, kColQ = 320;
 };
 constexpr int kGroups = 2;
-// Half's registers: of the 128 per thread at launch, the other warps give up 40 and the softmax warps take them
+// Half's registers: of the 128 per thread at launch, the other warps give up 32 and the softmax warps take them
 // (a half tile of scores and weights, 64 registers, spilled at 128).
-constexpr uint32_t kSoftmaxRegs = 168, kOtherRegs = 88;
+constexpr uint32_t kSoftmaxRegs = 160, kOtherRegs = 96;
 static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "");
 template <typename C>
 struct Warps {
