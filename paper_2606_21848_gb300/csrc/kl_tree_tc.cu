@@ -776,7 +776,9 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             };
 
             float m_used = -INFINITY;  // the reference of this thread's share of the row sum
-            float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
+            // The sum of this thread's half tiles' sums, and (Full) what its roundings lost: one number for all
+            // weights loses the small ones (fp32 error of 64615 tokens with outliers in two parts 1e-5, 7e-7 so).
+            float l_sum = 0.f, l_err = 0.f;
             bool okl = ok;
             for (int u = grp; okl && u < n_sub; u += kGroups) {
                 const int t0 = tile0 * kBN + u * kBS, sb = u % kSub;
@@ -896,13 +898,14 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 // the group's sums move to this reference
                 if (__any_sync(0xffffffffu, m_ref != m_used)) {
                     const float f = m_used == -INFINITY ? 0.f : ptx::ex2(m_used - m_ref);
-                    la = mul2(la, f);
-                    lb = mul2(lb, f);
+                    l_sum *= f;
+                    l_err *= f;
                     m_used = m_ref;
                 }
                 // the row's 64 weights -> 32 packed columns per term (the output MMAs of u - kSub, the
                 // last reader of P there, finished before these scores were written)
                 const float mr = m_ref == -INFINITY ? 0.f : m_ref;
+                float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
                 auto weights = [&](uint32_t(&s)[32]) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -920,6 +923,9 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 };
                 weights(s0);
                 weights(s1);
+                const float x = (la.x + la.y) + (lb.x + lb.y), t = l_sum + x, y = t - l_sum;
+                if constexpr (!C::kFp16) l_err += (l_sum - (t - y)) + (x - y);
+                l_sum = t;
                 if constexpr (C::kFp16) {
                     ptx::tmem_st16(sbuf, s0);
                     ptx::tmem_st16(sbuf + 16, s1);
@@ -952,7 +958,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             bool oke = okl;
             if (!C::kFp16 && oke && last >= kFoldSub) oke = wait(&sm.bar.sum_full, 0);
             for (int u = last; oke && u >= 0 && u > last - 3; --u) oke = wait(&sm.bar.s_free[u & 3], (u >> 2) & 1);
-            float l = (la.x + la.y) + (lb.x + lb.y);
+            float l = l_sum + l_err;
             float m_fin = 0.f;
             if constexpr (C::kFp16) {
                 sm.mref[grp][r] = m_used;

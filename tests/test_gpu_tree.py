@@ -355,3 +355,17 @@ def test_a_long_cache():
         check(run(x, splits=splits), tree_reference(x))
     check(run(x, torch.bfloat16), tree_reference(x), torch.bfloat16)
     assert np.isfinite(run(x).numpy()).all()
+
+
+@pytest.mark.parametrize("splits", [1, 2])
+def test_fp32_sums_of_a_long_cache_with_outliers(splits):
+    # A few tokens of large scores hold most of the weight, so that each of the others is small against the sum.
+    # Scores reach about 32 in units of log2: a score product adds eight K steps, each of which truncates on
+    # average half of 2^-19 there, so a weight may be off by 8 x 2^-20 x ln 2; the sums add their own few 2^-24.
+    x = tree_inputs((64615,), (2,), Hq=4, Hkv=4, P=32, kind="chain", seed=9)
+    v = x["v_cache"]
+    big = torch.rand(v.shape, generator=torch.Generator().manual_seed(77)) < 0.01
+    x["v_cache"] = torch.where(big, v / v.float().std() * 20, v / v.float().std()).to(torch.bfloat16)
+    want = tree_reference(x, composed=True)
+    d = run(x, torch.float32, splits=splits, composed=True).double() - want
+    assert float(d.norm()) <= (8 * 2.0 ** -20 * math.log(2) + 2.0 ** -22) * float(want.norm())
