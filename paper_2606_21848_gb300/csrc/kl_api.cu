@@ -385,11 +385,10 @@ kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_l
     return KL_OK;
 }
 
-// Whether a call can run on the wide decode's kernel: few rows per value head, one W^R each; and outputs whose
-// rounding hides the pair operands' error (3e-6).
+// Whether a call can run on the wide decode's kernel: few rows per value head, one W^R each.
 bool tree_wide(const kl_shape *s, int32_t max_q_len, bool fp32) {
-    return !fp32 && s && s->num_kv_heads > 0 && !s->wr_per_query_head && max_q_len > 0 &&
-           (int64_t)(s->num_q_heads / s->num_kv_heads) * max_q_len <= kTreeWideRows;
+    return s && s->num_kv_heads > 0 && !s->wr_per_query_head && max_q_len > 0 &&
+           (int64_t)(s->num_q_heads / s->num_kv_heads) * max_q_len <= (fp32 ? kTreeWideRowsFp32 : kTreeWideRows);
 }
 
 }  // namespace
@@ -400,12 +399,13 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
                               int32_t num_splits) {
     Geometry g;
     TreePlan p;
-    SharedLayout w;
-    if (plan_tree_call(shape, total_q, max_q_len, num_splits, false, true, &g, &p, &w) != KL_OK) return 0;
-    size_t most = w.total;
-    const bool wide = tree_wide(shape, max_q_len, false);
-    if (plan_tree_call(shape, total_q, max_q_len, num_splits, wide, false, &g, &p, &w) == KL_OK && w.total > most)
-        most = w.total;
+    size_t most = 0;
+    for (int fp32 = 0; fp32 < 2; ++fp32) {
+        SharedLayout w;
+        const bool wide = tree_wide(shape, max_q_len, fp32);
+        if (plan_tree_call(shape, total_q, max_q_len, num_splits, wide, fp32, &g, &p, &w) != KL_OK) return 0;
+        if (w.total > most) most = w.total;
+    }
     return most;
 }
 

@@ -58,11 +58,11 @@ constexpr int kWideMaxRuns = 256;                    // states merged per (b, g,
 // sequences of 1000 to 60000 tokens with outliers took 231 instead of 180 us.)
 constexpr float kWideLazy = 1024.f;
 
-// Warp roles and sizes for NH heads per CTA and NG softmax groups: NG = 2, one CTA per SM; NG = 1,
-// two CTAs per SM.
-template <int NH, int NG>
+// Warp roles and sizes for NH heads per CTA, operands of T bf16 terms and NG softmax groups: NG = 2, one CTA
+// per SM; NG = 1, two CTAs per SM.
+template <int NH, int NG, int T = 2>
 struct Wide {
-    static constexpr int kStages = NG == 1 ? 3 : NH == 32 ? 5 : 6;
+    static constexpr int kStages = NG == 1 ? 3 : NH * T > 32 ? 5 : 6;
     static constexpr int kWarps = 8 * NG;                // compute warps
     static constexpr int kProducer = kWarps, kMma = kWarps + 1, kPv = kWarps + 2;
     static constexpr int kThreads = (kWarps + 3) * 32;
@@ -70,13 +70,13 @@ struct Wide {
     static constexpr uint32_t kTmemCols = 512 / kCtas;
 };
 
-template <int NH, int NG>
+template <int NH, int NG, int T = 2>
 struct __align__(1024) WideSmem {
-    static constexpr int kStages = Wide<NH, NG>::kStages;
+    static constexpr int kStages = Wide<NH, NG, T>::kStages;
     uint8_t tiles[kStages][kTileBytes];              // as Smem<false>::tiles
-    uint8_t qr[2 * 2 * NH * 128];                    // routed query [half][hi | lo rows][128 B]
-    uint8_t p[NG][kTile * 2 * NH * 2];               // per group: [16 groups of 8 tokens]
-                                                     // [2 NH / 8 blocks][8 tokens][16 B]
+    uint8_t qr[2 * T * NH * 128];                    // routed query [half][hi | lo rows][128 B]
+    uint8_t p[NG][kTile * T * NH * 2];               // per group: [16 groups of 8 tokens]
+                                                     // [T NH / 8 blocks][8 tokens][16 B]
     float red[NG][4][NH];                            // per group and lane quarter: maxima
     float lred[NG][4][NH];                           // ... row sums
     float mref[NG][NH];                              // per group: the heads' references (in
@@ -90,7 +90,8 @@ struct __align__(1024) WideSmem {
 };
 // (228 KB per SM, of which each CTA takes 1 KB for the system)
 static_assert(sizeof(WideSmem<16, 1>) <= 228 * 1024 / 2 - 1024, "two CTAs per SM");
-static_assert(sizeof(WideSmem<32, 2>) <= 227 * 1024 && sizeof(WideSmem<16, 2>) <= 227 * 1024, "one");
+static_assert(sizeof(WideSmem<32, 2>) <= 227 * 1024 && sizeof(WideSmem<16, 2>) <= 227 * 1024 &&
+                  sizeof(WideSmem<16, 2, 3>) <= 227 * 1024, "one");
 
 // 8 consecutive columns at `a` and at `b` of the thread's TMEM lane, one wait.
 __device__ __forceinline__ void tmem_ld_cols8(uint32_t a, uint32_t b, float (&x)[8], float (&y)[8]) {
@@ -169,18 +170,18 @@ __device__ __forceinline__ float warp_max_redux(float f) {
     return __int_as_float(k >= 0 ? k : k ^ 0x7FFFFFFF);
 }
 
-template <int NH, int NG, bool kExact, bool kTree>
-__global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
+template <int NH, int NG, bool kExact, bool kTree, int T>
+__global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kCtas)
     decode_wide_kernel(const __grid_constant__ CUtensorMap vmap,
                        const __grid_constant__ CUtensorMap wmap,
                        const __grid_constant__ CUtensorMap qmap, const DecodeArgs a) {
-    using S = WideSmem<NH, NG>;
-    using W = Wide<NH, NG>;
+    using S = WideSmem<NH, NG, T>;
+    using W = Wide<NH, NG, T>;
     constexpr int NS = W::kStages, kWideWarps = W::kWarps, kWideComputeThreads = 32 * W::kWarps;
     constexpr int kWideProducer = W::kProducer, kWideMma = W::kMma, kWidePv = W::kPv;
     constexpr uint32_t kWideTmemCols = W::kTmemCols;
     constexpr int KH = NH / 2;                           // heads per compute warp
-    constexpr int N = 2 * NH;                            // MMA columns: hi | lo
+    constexpr int N = T * NH;                            // MMA columns: hi | lo (| lowest)
     constexpr uint32_t kQHalf = N * 128;                 // one 64-dim half of the query operand
     constexpr uint32_t kGroupBytes = N / 8 * 128;        // P: one group of 8 tokens
     // TMEM columns: two S buffers and the O of a tile of each group, N each; then each group's summed
@@ -522,14 +523,16 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
             const float sl2 = geo.scale * kLog2e;
 #pragma unroll
             for (int e = 0; e < KR; ++e) {
-                const float v = acc[e] * sl2;
-                const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-                const __nv_bfloat16 lo = __float2bfloat16_rn(v - __bfloat162float(hi));
+                float v = acc[e] * sl2;
                 const int n = h1 + e, k = t;
                 uint8_t *row = sm.qr + (k >> 6) * kQHalf + (n & 7) * 128 +
                                ((((k & 63) >> 3) ^ (n & 7)) << 4) + ((k & 7) << 1);
-                *reinterpret_cast<__nv_bfloat16 *>(row + (n >> 3) * 1024) = hi;
-                *reinterpret_cast<__nv_bfloat16 *>(row + ((NH + n) >> 3) * 1024) = lo;
+#pragma unroll
+                for (int i = 0; i < T; ++i) {
+                    const __nv_bfloat16 term = __float2bfloat16_rn(v);
+                    *reinterpret_cast<__nv_bfloat16 *>(row + ((i * NH + n) >> 3) * 1024) = term;
+                    v -= __bfloat162float(term);
+                }
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
@@ -545,14 +548,25 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
         // One barrier per tile for the group: it counts the threads with a weight past the slack
         // or a failed wait. Only then a second one exchanges the tile maxima (or lets the whole
         // group leave together).
-        // summed O of heads h .. h + 7 += the tile's O, hi and lo (thread = output dim t)
+        // the sum of the terms of 8 columns
+        auto ld_terms = [&](uint32_t at, float (&x)[8]) {
+            float lo[8];
+            tmem_ld_cols8(at, at + NH, x, lo);
+            if constexpr (T == 3) {
+                float lowest[8];
+                tmem_ld_col8(at + 2 * NH, lowest);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) lo[e] += lowest[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += lo[e];
+        };
+        // summed O of heads h .. h + 7 += the tile's O, all terms (thread = output dim t)
         auto fold = [&](int h, bool add) {
             float oh[8], ol[8];
             const uint32_t oc = tmem + kColO + grp * N + h + lane_base;
             const uint32_t fc = tmem + kColF + grp * NH + h + lane_base;
-            tmem_ld_cols8(oc, oc + NH, oh, ol);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) oh[e] += ol[e];
+            ld_terms(oc, oh);
             if (add) {
                 tmem_ld_col8(fc, ol);
 #pragma unroll
@@ -610,6 +624,11 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                 for (int c = 0; c < KH; c += 8) {
                     float hi[8], lo[8], m[8];
                     tmem_ld_cols8(sc + c, sc + NH + c, hi, lo);
+                    if constexpr (T == 3) {
+                        tmem_ld_col8(sc + 2 * NH + c, m);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) lo[e] += m[e];
+                    }
                     *reinterpret_cast<float4 *>(m) = *reinterpret_cast<const float4 *>(mref + c);
                     *reinterpret_cast<float4 *>(m + 4) = *reinterpret_cast<const float4 *>(mref + c + 4);
 #pragma unroll
@@ -638,11 +657,11 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                 if (ready) {
 #pragma unroll
                     for (int c = 0; c < KH; c += 8) {
-                        float hi[8], lo[8];
-                        tmem_ld_cols8(sc + c, sc + NH + c, hi, lo);
+                        float s[8];
+                        ld_terms(sc + c, s);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            p[c + e] = past || (kTree && (hidden >> (c + e) & 1)) ? -INFINITY : hi[e] + lo[e];
+                            p[c + e] = past || (kTree && (hidden >> (c + e) & 1)) ? -INFINITY : s[e];
                             const float wm = warp_max_redux(p[c + e]);
                             if (lane == e) sm.red[grp][qd][h0 + c + e] = wm;
                         }
@@ -681,6 +700,12 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                         }
                         tmem_st_cols8(oc, oh);
                         tmem_st_cols8(oc + NH, ol);
+                        if constexpr (T == 3) {
+                            tmem_ld_col8(oc + 2 * NH, oh);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) oh[e] *= alpha[e];
+                            tmem_st_cols8(oc + 2 * NH, oh);
+                        }
                         if (k > 1) {
                             const uint32_t fc = tmem + kColF + grp * NH + h0 + c + lane_base;
                             tmem_ld_col8(fc, oh);
@@ -706,7 +731,7 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
             if (lane == 0) ptx::mbar_arrive(&sm.s_empty[sb]);
             // P^T row of token t, this warp's heads, hi and lo (formed before the wait: the MMAs that
             // read the weight buffer are still running)
-            uint32_t ph[KH / 2], pl[KH / 2];
+            uint32_t ph[KH / 2], pl[KH / 2], pm[T == 3 ? KH / 2 : 1];
 #pragma unroll
             for (int e = 0; e < KH / 2; ++e) {
                 const F2 pe = f2(p[2 * e], p[2 * e + 1]);
@@ -718,6 +743,11 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                 const F2 r = sub2(pe, f2(__uint_as_float(ph[e] << 16), __uint_as_float(ph[e] & 0xffff0000u)));
                 const __nv_bfloat162 l2 = __floats2bfloat162_rn(r.x, r.y);
                 pl[e] = *reinterpret_cast<const uint32_t *>(&l2);
+                if constexpr (T == 3) {
+                    const F2 rm = sub2(r, f2(__uint_as_float(pl[e] << 16), __uint_as_float(pl[e] & 0xffff0000u)));
+                    const __nv_bfloat162 m2 = __floats2bfloat162_rn(rm.x, rm.y);
+                    pm[e] = *reinterpret_cast<const uint32_t *>(&m2);
+                }
             }
             if (!freed) carried = wait(&sm.o_full[grp], (k - 1) & 1);
             if (carried) {
@@ -736,6 +766,9 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                         make_uint4(ph[4 * c], ph[4 * c + 1], ph[4 * c + 2], ph[4 * c + 3]);
                     *reinterpret_cast<uint4 *>(row + (NH / 8 + c) * 128) =
                         make_uint4(pl[4 * c], pl[4 * c + 1], pl[4 * c + 2], pl[4 * c + 3]);
+                    if constexpr (T == 3)
+                        *reinterpret_cast<uint4 *>(row + (2 * NH / 8 + c) * 128) =
+                            make_uint4(pm[4 * c], pm[4 * c + 1], pm[4 * c + 2], pm[4 * c + 3]);
                 }
                 // rows past the end inside the last 16-token MMA step must be finite: zero them
                 // (each of the lane quarter's two warps one 64-dim half)
@@ -798,9 +831,7 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                 const uint32_t fc = tmem + kColF + gi * NH + h1 + lane_base;
                 if constexpr (KR == 8) {
                     float lo[8];
-                    tmem_ld_cols8(oc, oc + NH, o, lo);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] += lo[e];
+                    ld_terms(oc, o);
                     if (n > 1) {
                         tmem_ld_col8(fc, lo);
 #pragma unroll
@@ -809,7 +840,9 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
                 } else {
 #pragma unroll
                     for (int e = 0; e < KR; ++e) {
-                        o[e] = ptx::tmem_ld1(oc + e) + ptx::tmem_ld1(oc + NH + e);
+                        o[e] = ptx::tmem_ld1(oc + NH + e);
+                        if constexpr (T == 3) o[e] += ptx::tmem_ld1(oc + 2 * NH + e);
+                        o[e] += ptx::tmem_ld1(oc + e);
                         if (n > 1) o[e] += ptx::tmem_ld1(fc + e);
                     }
                 }
@@ -883,24 +916,24 @@ __global__ void __launch_bounds__(Wide<NH, NG>::kThreads, Wide<NH, NG>::kCtas)
     }
 }
 
-template <int NH, int NG, bool kExact, bool kTree>
+template <int NH, int NG, bool kExact, bool kTree, int T = 2>
 cudaError_t launch_kernel_wide(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
                                const CUtensorMap &qmap) {
     const Geometry &g = la.geo;
-    const size_t smem = sizeof(WideSmem<NH, NG>);
+    const size_t smem = sizeof(WideSmem<NH, NG, T>);
     static PerDeviceOnce once;
     const cudaError_t e = once.run([&] {
-        return cudaFuncSetAttribute(decode_wide_kernel<NH, NG, kExact, kTree>,
+        return cudaFuncSetAttribute(decode_wide_kernel<NH, NG, kExact, kTree, T>,
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((g.S + g.spc - 1) / g.spc * g.nhb, g.Hkv, g.B);
-    cfg.blockDim = dim3(Wide<NH, NG>::kThreads);
+    cfg.blockDim = dim3(Wide<NH, NG, T>::kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = la.stream;
     const OverlapAttr overlap(cfg);
-    return cudaLaunchKernelEx(&cfg, decode_wide_kernel<NH, NG, kExact, kTree>, vmap, wmap, qmap, la);
+    return cudaLaunchKernelEx(&cfg, decode_wide_kernel<NH, NG, kExact, kTree, T>, vmap, wmap, qmap, la);
 }
 
 // Consecutive splits per CTA: the fewest that fit one wave of `slots` CTAs (when the units alone do not fill

@@ -13,7 +13,8 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
     Geometry &g = la.geo;
     const int rows = g.G * a.tree.max_q;
     const int64_t sms = device_sm_count(), units = (int64_t)g.B * g.Hkv;
-    const bool w32 = rows > 16, two_per_sm = !w32 && units > sms;     // (as the decode's blocks of heads)
+    // (as the decode's blocks of heads; three terms leave no room for two CTAs)
+    const bool fp32 = a.out_dtype == KL_FP32, w32 = rows > 16, two_per_sm = !w32 && !fp32 && units > sms;
     g.nhb = 1;
     g.qbox = rows;
     g.spc = splits_per_cta(g.S, units, two_per_sm ? 2 * sms : sms);
@@ -34,6 +35,7 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     }
+    if (fp32) return launch_kernel_wide<16, 2, false, true, 3>(la, vmap, wmap, qmap);
     if (w32) return launch_kernel_wide<32, 2, false, true>(la, vmap, wmap, qmap);
     return two_per_sm ? launch_kernel_wide<16, 1, false, true>(la, vmap, wmap, qmap)
                       : launch_kernel_wide<16, 2, false, true>(la, vmap, wmap, qmap);
