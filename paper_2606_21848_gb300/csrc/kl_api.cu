@@ -376,7 +376,7 @@ kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_l
     if (max_q_len > KL_TREE_MAX_DRAFTS) return KL_ERR_UNSUPPORTED;
     if (wide) {
         const size_t rows = (size_t)g->B * g->Hq * max_q_len * g->S;
-        *w = shared_layout((size_t)g->B * g->Hkv, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
+        *w = shared_layout((size_t)g->B * g->Hkv * 2, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
         return KL_OK;
     }
     *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P,

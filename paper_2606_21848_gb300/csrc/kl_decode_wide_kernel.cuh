@@ -38,7 +38,7 @@
 // Each wait is bounded as in kl_decode_tc_kernel.cuh.
 //
 // kTree: the verification step's rows (kl_tree_attention with at most 32 rows per value head): the "heads" of
-// a CTA are the (draft, head) rows of one sequence and value head, row n = draft n / G with head n % G, and
+// a CTA are a block of the (draft, head) rows of one sequence and value head, row n = draft n / G with head n % G, and
 // a tile that holds drafts gives weight 0 to the rows that do not see a token. One W^R per value head or
 // the composed query.
 #pragma once
@@ -201,13 +201,15 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     int G = min(NH, geo.G - NH * hb);                    // query heads (rows) of this CTA
-    const int qh0 = g * geo.G + NH * hb;                 // its first query head
+    const int qh0 = g * geo.G + (kTree ? 0 : NH * hb);   // its first query head
+    const int row0 = kTree ? NH * hb : 0;                // kTree: its first row
     // rows of q and out, and of the split states
     auto out_row = [&](int h) -> size_t {
-        if constexpr (kTree) return (size_t)(drafts0 + h / geo.G) * geo.Hq + qh0 + h % geo.G;
+        if constexpr (kTree) return (size_t)(drafts0 + (row0 + h) / geo.G) * geo.Hq + qh0 + (row0 + h) % geo.G;
         return (size_t)b * geo.Hq + qh0 + h;
     };
-    const size_t state0 = kTree ? ((size_t)b * geo.Hkv + g) * geo.G * a.tree.max_q : (size_t)b * geo.Hq + qh0;
+    const size_t state0 =
+        kTree ? ((size_t)b * geo.Hkv + g) * geo.G * a.tree.max_q + row0 : (size_t)b * geo.Hq + qh0;
     const bool route = a.w_r != nullptr;                 // else q is the composed query
     const bool route_pq = route && geo.wr_per_qh;
     const int ro = !route ? 0 : route_pq ? G : 1;        // ring positions of W^R matrices
@@ -251,9 +253,9 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         drafts0 = a.tree.cu_q[b];
         const int end = a.tree.cu_q[b + 1];
         drafts = end - drafts0;
-        G = drafts * geo.G;
+        G = min(NH, drafts * geo.G - row0);
         if (drafts0 < 0 || drafts < 0 || end > a.tree.total_q || drafts > a.tree.max_q || L_raw < drafts) L_raw = -1;
-        else if (drafts == 0) L_raw = min(L_raw, 0);     // (no rows: an empty run)
+        else if (G <= 0) L_raw = min(L_raw, 0);          // (no rows: an empty run)
     }
     const int pos_raw = a.v_new ? a.positions[b] : -1;
     const int t_begin = split0 * geo.chunk;
@@ -420,7 +422,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             ptx::tc_fence_after();
             if (ptx::elect_one()) {
                 const uint64_t w0 = w_desc + ((s * kTileBytes) >> 4);
-                const uint64_t q0 = q_desc + (route_pq ? ((r >> 4) * 2048) >> 4 : 0);
+                const uint64_t q0 = q_desc + ((route_pq ? (r >> 4) * 2048 : row0 * 128) >> 4);
                 const uint32_t dst = route_pq ? tmem + 16 * r : tmem + kColO;
                 const uint32_t idesc_r = route_pq ? ptx::idesc_bf16(128, 16, true, false)
                                                   : ptx::idesc_bf16(128, NH, true, false);
@@ -600,7 +602,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             uint32_t m = 0;
 #pragma unroll
             for (int e = 0; e < KH; ++e) {
-                const uint32_t sees = __shfl_sync(0xffffffffu, line, min((h0 + e) / geo.G, 31));
+                const uint32_t sees = __shfl_sync(0xffffffffu, line, min((row0 + h0 + e) / geo.G, 31));
                 if (d >= 0 && (d > 31 || !(sees >> d & 1))) m |= 1u << e;
             }
             return m;

@@ -289,7 +289,7 @@ cudaError_t launch_append_chunk(const Geometry &g, int total_q, int max_q, const
 cudaError_t launch_tree_tc(const TreeArgs &a);
 // The same by the wide decode's kernel, for up to kTreeWideRows (bf16 outputs) or kTreeWideRowsFp32 rows per
 // value head and one W^R per value head (or none): a.geo with its splits, a.tree.
-constexpr int kTreeWideRows = 32, kTreeWideRowsFp32 = 16;
+constexpr int kTreeWideRows = 32, kTreeWideRowsFp32 = 32;
 cudaError_t launch_tree_wide(const DecodeArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
                                const int32_t *path_lens, int max_path, const int32_t *block_table,

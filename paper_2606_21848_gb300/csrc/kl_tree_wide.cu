@@ -15,9 +15,9 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
     const int64_t sms = device_sm_count(), units = (int64_t)g.B * g.Hkv;
     // (as the decode's blocks of heads; three terms leave no room for two CTAs)
     const bool fp32 = a.out_dtype == KL_FP32, w32 = rows > 16, two_per_sm = !w32 && !fp32 && units > sms;
-    g.nhb = 1;
+    g.nhb = fp32 && w32 ? 2 : 1;         // (32 rows of three terms leave no tensor memory)
     g.qbox = rows;
-    g.spc = splits_per_cta(g.S, units, two_per_sm ? 2 * sms : sms);
+    g.spc = splits_per_cta(g.S, units * g.nhb, two_per_sm ? 2 * sms : sms);
     CUtensorMap vmap, wmap, qmap;
     if (!make_map(&vmap, a.v_cache, kD, (uint64_t)g.num_pages * g.Hkv * g.P, (uint32_t)g.P))
         return cudaErrorInvalidValue;
