@@ -40,7 +40,8 @@
 // kTree: the verification step's rows (kl_tree_attention with at most 32 rows per value head): the "heads" of
 // a CTA are a block of the (draft, head) rows of one sequence and value head, row n = draft n / G with head n % G, and
 // a tile that holds drafts gives weight 0 to the rows that do not see a token. One W^R per value head or
-// the composed query.
+// the composed query. T = 3 (kTree, fp32 outputs): query and weights of three bf16 terms, N = 3 NH columns; the
+// terms' products meet in fp32, rounded to nearest.
 #pragma once
 
 #include "kl_decode_tc_kernel.cuh"

@@ -129,7 +129,7 @@ struct TreeArgs {
     int total_q;              // rows of q and out
     int max_q;                // host bound on n_b
     int hp, rpb, ctas;        // layout (plan_tree)
-    int start, run, whole;
+    int start, run, whole;    // ... in tiles
     int num_splits;           // most parts of a unit; 0: no such limit
     const uint16_t *q;        // [total_q][Hq][D] bf16
     const uint16_t *w_r;      // [Hw][D][D] bf16, or nullptr: q is the composed query

@@ -28,22 +28,24 @@
 // drafts; HBM delivers a tile to every SM in 0.73 us, and this form takes 1.0). Values or queries past fp16's
 // range make the outputs that take part in them NaN (KL_FLAG_RANGE).
 // fp32 outputs (Full): query and weights are sums of three bf16 terms (24 bits), and since the tensor
-// core's adds truncate, O moves every 128 tokens to a sum that the softmax warps keep in shared memory.
+// core's adds truncate, O moves every 128 tokens to a sum in shared memory.
 //
-// What bounds it. Half, on long caches: nothing alone. Of the 253 us of the sizes above (4700 GB/s of cache,
-// 1.1 PFLOP/s) removing the conversion, the exponentials, or one of the two products saved 18 to 35 us each, and
-// removing all of them 52. 64 sequences of 512 to 32768 tokens, up to 24 drafts: 494 us (323 at HBM's rate);
-// one of 131072 tokens, 32 drafts: 71 us (40). Short caches are bound by latency: starting a segment takes
-// 5 us, of them the routing and the first scores 3.5, and units of several parts 3 to 5 us for the merge.
-// Full: six score and six output products per tile; 12 sequences of 3001 to 6007 tokens, 12 / 2 heads, 61 to
-// 64 drafts, W^R per query head: 93 us.
+// What bounds it. Half, on long caches: nothing alone. Of the 253 us of the sizes above (5100 GB/s of cache,
+// 1.3 PFLOP/s) removing the conversion, the exponentials, or one of the two products saved 18 to 35 us each, and
+// removing all of them 52. 64 sequences of 512 to 32768 tokens, up to 24 drafts: 493 us (323 at HBM's rate);
+// one of 131072 tokens, 32 drafts: 72 us (40); 64 of 8192, 16 drafts, 64 / 8 heads: 246 us (163). Short caches
+// are bound by latency: starting a segment takes 5 us, of them the routing and the first scores 3.5, and units
+// of several parts 3 to 5 us for the merge.
+// Full: three score and three output products per tile (2.0 us at the peak rate); a tile takes 2.7 us. 12
+// sequences of 3001 to 6007 tokens, 12 / 2 heads, 61 to 64 drafts, W^R per query head: 74 us.
 //
 // The softmax works on half tiles of 64 tokens, thread = row = TMEM lane. A row's reference maximum moves
 // only when a half tile's maximum passes it by more than 2^14.
 //
 // Roles: two groups of four softmax warps (and epilogue), then one warp each for the producer (TMA), the routing
-// and score MMAs (owner of the tensor memory) and the output MMAs, and for Half four warps that convert
-// tiles to fp16 ahead of their score MMAs. Every wait is bounded (about one second); a
+// and score MMAs (owner of the tensor memory) and the output MMAs, and four helpers, which for Half convert
+// tiles to fp16 ahead of their score MMAs and for Full move O to the sum (by the softmax warps, between a half
+// tile's maximum and its weights, a tile took 5 us). Every wait is bounded (about one second); a
 // wait that runs out raises KL_FLAG_TIMEOUT and every role leaves, drains its copies and MMAs and
 // frees the tensor memory.
 #include <cudaTypedefs.h>
@@ -88,8 +90,8 @@ struct Full {
     static constexpr uint32_t kBuf = 96, kColO = 192, kColQ = 320;
 };
 constexpr int kGroups = 2;
-// Half's registers: of the 128 per thread at launch, the other warps give up 32 and the softmax warps take them
-// (a half tile of scores and weights, 64 registers, spilled at 128).
+// Registers: of the 128 per thread at launch, the other warps give up 32 and the softmax warps take them
+// (a half tile of scores and weights, 64 registers, spilled at 128. 168 / 88: 1 to 3 % slower).
 constexpr uint32_t kSoftmaxRegs = 160, kOtherRegs = 96;
 static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "");
 template <typename C>
