@@ -295,7 +295,7 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
  * alone.
  * Precision: scores, softmax and sums in fp32. The operands of the products depend on the form:
  *   fp32 outputs: the routed query and the weights carry 24 significant bits (error about 1e-6);
- *   bf16 outputs with (Hq / Hkv) * max_q_len <= 32 and one W^R per value head or none: 16 bits;
+ *   bf16 outputs with R = (Hq / Hkv) * max_q_len <= 16, or R <= 32 on some sizes: 16 bits;
  *   other bf16 outputs: fp16, 11 bits, cached values of magnitude 2^-14 to 65280 exactly. There a routed
  *   query times scale * log2 e, or a cached value, beyond 65504 makes the outputs that it takes part in
  *   NaN (a drafted row: those of the drafts that see it), and a non-finite output raises KL_FLAG_RANGE.

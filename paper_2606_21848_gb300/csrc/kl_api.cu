@@ -369,14 +369,15 @@ SharedLayout shared_layout(size_t counters, size_t state_bytes, size_t extra_byt
 // runs' entries for the merge, then their states (none of which a decode's counters ever share). `wide`: on
 // the wide decode's kernel, with its split plan, counters in the front region and split states.
 kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t num_splits,
-                         bool wide, bool fp32, Geometry *g, TreePlan *p, SharedLayout *w) {
+                         int wide, bool fp32, Geometry *g, TreePlan *p, SharedLayout *w) {
     const kl_status st = resolve(shape, wide ? num_splits : -1, g);
     if (st != KL_OK) return st;
     if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits) return KL_ERR_INVALID_ARG;
     if (max_q_len > KL_TREE_MAX_DRAFTS) return KL_ERR_UNSUPPORTED;
     if (wide) {
         const size_t rows = (size_t)g->B * g->Hq * max_q_len * g->S;
-        *w = shared_layout((size_t)g->B * g->Hkv * 2, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
+        g->nhb = wide;
+        *w = shared_layout((size_t)g->B * g->Hkv * wide, rows * g->D * sizeof(float), rows * 2 * sizeof(float));
         return KL_OK;
     }
     *p = plan_tree(g->B, g->Hkv, g->G, max_q_len > 0 ? max_q_len : 1, (int64_t)g->max_pages * g->P,
@@ -385,10 +386,13 @@ kl_status plan_tree_call(const kl_shape *shape, int32_t total_q, int32_t max_q_l
     return KL_OK;
 }
 
-// Whether a call can run on the wide decode's kernel: few rows per value head, one W^R each.
-bool tree_wide(const kl_shape *s, int32_t max_q_len, bool fp32) {
-    return s && s->num_kv_heads > 0 && !s->wr_per_query_head && max_q_len > 0 &&
-           (int64_t)(s->num_q_heads / s->num_kv_heads) * max_q_len <= (fp32 ? kTreeWideRowsFp32 : kTreeWideRows);
+// The blocks of rows on the wide decode's kernel; 0: not there.
+int tree_wide(const kl_shape *s, int32_t max_q_len, bool fp32) {
+    if (!s || s->num_kv_heads <= 0 || max_q_len <= 0) return 0;
+    return tree_wide_blocks((int64_t)s->num_seqs * s->num_kv_heads,
+                            ((int64_t)s->max_pages_per_seq * s->page_size + kTreeTile - 1) / kTreeTile,
+                            (int64_t)(s->num_q_heads / s->num_kv_heads) * max_q_len, fp32, s->wr_per_query_head != 0,
+                            device_sm_count());
 }
 
 }  // namespace
@@ -402,7 +406,7 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
     size_t most = 0;
     for (int fp32 = 0; fp32 < 2; ++fp32) {
         SharedLayout w;
-        const bool wide = tree_wide(shape, max_q_len, fp32);
+        const int wide = tree_wide(shape, max_q_len, fp32);
         if (plan_tree_call(shape, total_q, max_q_len, num_splits, wide, fp32, &g, &p, &w) != KL_OK) return 0;
         if (w.total > most) most = w.total;
     }
@@ -418,7 +422,7 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     Geometry g;
     TreePlan p;
     SharedLayout w;
-    const bool wide = tree_wide(shape, max_q_len, out_dtype == KL_FP32);
+    const int wide = tree_wide(shape, max_q_len, out_dtype == KL_FP32);
     const kl_status st = plan_tree_call(shape, total_q, max_q_len, num_splits, wide, out_dtype == KL_FP32, &g, &p, &w);
     if (st != KL_OK) return st;
     if (!prefill_tc_supported(g)) return KL_ERR_UNSUPPORTED;

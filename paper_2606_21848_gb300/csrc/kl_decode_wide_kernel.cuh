@@ -39,8 +39,7 @@
 //
 // kTree: the verification step's rows (kl_tree_attention with at most 32 rows per value head): the "heads" of
 // a CTA are a block of the (draft, head) rows of one sequence and value head, row n = draft n / G with head n % G, and
-// a tile that holds drafts gives weight 0 to the rows that do not see a token. One W^R per value head or
-// the composed query. T = 3 (kTree, fp32 outputs): query and weights of three bf16 terms, N = 3 NH columns; the
+// a tile that holds drafts gives weight 0 to the rows that do not see a token. W^R per query head: NH = 16. T = 3 (kTree, fp32 outputs): query and weights of three bf16 terms, N = 3 NH columns; the
 // terms' products meet in fp32, rounded to nearest.
 #pragma once
 
@@ -213,7 +212,9 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         kTree ? ((size_t)b * geo.Hkv + g) * geo.G * a.tree.max_q + row0 : (size_t)b * geo.Hq + qh0;
     const bool route = a.w_r != nullptr;                 // else q is the composed query
     const bool route_pq = route && geo.wr_per_qh;
-    const int ro = !route ? 0 : route_pq ? G : 1;        // ring positions of W^R matrices
+    // ring positions of W^R matrices (kTree, per query head: that of head (row0 + r) % G at position r; row n
+    // of the CTA takes position n % G's result)
+    const int ro = !route ? 0 : !route_pq ? 1 : kTree ? min(geo.G, NH) : G;
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) {
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
     auto issue_route = [&](int r) {
         const int s = r % NS;
         if (lane == 0) {
-            const int wrow = (route_pq ? qh0 + r : g) * kD;
+            const int wrow = (!route_pq ? g : qh0 + (kTree ? (row0 + r) % geo.G : r)) * kD;
             ptx::mbar_arrive_expect_tx(&sm.full[s],
                                        kTileBytes + (r == 0 ? 2u * (uint32_t)geo.qbox * 128u : 0u));
             ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.full[s], 0, wrow);
@@ -423,7 +424,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             ptx::tc_fence_after();
             if (ptx::elect_one()) {
                 const uint64_t w0 = w_desc + ((s * kTileBytes) >> 4);
-                const uint64_t q0 = q_desc + ((route_pq ? (r >> 4) * 2048 : row0 * 128) >> 4);
+                const uint64_t q0 = q_desc + ((kTree ? row0 * 128 : route_pq ? (r >> 4) * 2048 : 0) >> 4);
                 const uint32_t dst = route_pq ? tmem + 16 * r : tmem + kColO;
                 const uint32_t idesc_r = route_pq ? ptx::idesc_bf16(128, 16, true, false)
                                                   : ptx::idesc_bf16(128, NH, true, false);
@@ -516,7 +517,9 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 if (h < G) {
                     if (route)
                         acc[e] = ptx::tmem_ld1(tmem + lane_base +
-                                               (route_pq ? 16 * h + (h & 15) : kColO + h));
+                                               (!route_pq ? kColO + h
+                                                : kTree   ? 16 * (h % geo.G) + h
+                                                          : 16 * h + (h & 15)));
                     else
                         acc[e] = __uint_as_float((uint32_t)a.q[out_row(h) * kD + t] << 16);
                 }

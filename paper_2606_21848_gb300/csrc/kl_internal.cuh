@@ -287,9 +287,7 @@ cudaError_t launch_append_chunk(const Geometry &g, int total_q, int max_q, const
 // Attention of a tree of drafted tokens (the geometry of the prefill), and the move of the accepted
 // path's rows.
 cudaError_t launch_tree_tc(const TreeArgs &a);
-// The same by the wide decode's kernel, for up to kTreeWideRows (bf16 outputs) or kTreeWideRowsFp32 rows per
-// value head and one W^R per value head (or none): a.geo with its splits, a.tree.
-constexpr int kTreeWideRows = 32, kTreeWideRowsFp32 = 32;
+// The same by the wide decode's kernel (tree_wide_blocks): a.geo with its splits and blocks (nhb), a.tree.
 cudaError_t launch_tree_wide(const DecodeArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
                                const int32_t *path_lens, int max_path, const int32_t *block_table,

@@ -53,4 +53,23 @@ inline TreePlan plan_tree(int B, int Hkv, int G, int max_q, int64_t max_tokens, 
     return p;
 }
 
+// How a call with `rows` rows per value head (drafts x heads of a group) over `units` (sequence, value head) pairs
+// of up to `tiles` tiles runs: in blocks of 128 rows (0, kl_tree_tc.cu), or on the wide decode's kernel in one
+// block of 16 or 32 rows (1) or two of 16 (2). `per_qh`: W^R per query head.
+// - Two blocks of 16: three terms, or the routing by a W^R per query head, leave no tensor memory for 32 rows. Else
+//   a tile takes a block of 32 0.87 us and one of 16 0.62, but the block of 32 starts 4 us later, so while
+//   every CTA has an SM and few tiles. (bf16, 8 drafts of 32 / 8 heads: one sequence of 300 tokens in two blocks
+//   9.3 us, in one 13.0; of 16384 18.9 and 24.4; of 131072 75.6 and 60.5; 8 of 4096 24.5 and 26.8; 16 of 4096
+//   65 and 35. W^R per query head, in two blocks and in 128 rows: 8 of 4096 25.8 and 36.1, one of 131072 77 and 68,
+//   64 of 1000 92 and 61; fp32 8 of 4096 26.5 and 59.)
+// - Blocks of 128 rows for many short units, whose starts a persistent CTA pays without a launch wave's rest (8
+//   drafts of 32 / 8 heads in 128 rows and in one block: 64 of 500 tokens 43 and 58 us, of 1000 57 and 69, of 2000
+//   88 and 91, 32 of 1000 31 and 35.5, of 4096 80 and 69).
+inline int tree_wide_blocks(int64_t units, int64_t tiles, int64_t rows, bool fp32, bool per_qh, int64_t sms) {
+    if (rows > 32) return 0;
+    if (rows <= 16) return 1;
+    if (fp32 || (2 * units <= sms && units * tiles <= 16 * sms)) return 2;
+    return per_qh || (units > sms && tiles <= 16) ? 0 : 1;
+}
+
 }  // namespace kl

@@ -15,18 +15,9 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
     Geometry &g = la.geo;
     const int rows = g.G * a.tree.max_q;
     const int64_t sms = device_sm_count(), units = (int64_t)g.B * g.Hkv;
-    const bool fp32 = a.out_dtype == KL_FP32;
-    // More than 16 rows: one block of 32, or two of 16. Three terms leave no tensor memory for 32. With two terms a
-    // tile takes a block of 32 0.87 us and one of 16 0.62, but the block of 32 starts 4 us later: two blocks
-    // while every CTA has an SM and few tiles. (One sequence of 300 tokens, 8 drafts of 32 / 8 heads: 9.3 us in two
-    // blocks, 13.0 in one; of 16384 18.9 and 24.4; of 131072 75.6 and 60.5; 8 of 4096 24.5 and 26.8; 16 of 4096
-    // 65 and 35; 8 of 16384, 6 drafts, 71 and 58.)
-    const int64_t tiles = ((int64_t)g.max_pages * g.P + 127) / 128;
-    const bool blocks = rows > 16 && (fp32 || (2 * units <= sms && units * tiles <= 16 * sms));
-    const bool w32 = rows > 16 && !blocks;
+    const bool fp32 = a.out_dtype == KL_FP32, w32 = rows > 16 && g.nhb == 1;
     // (two CTAs per SM as the decode's blocks of heads; three terms leave no room for that)
     const bool two_per_sm = rows <= 16 && !fp32 && units > sms;
-    g.nhb = blocks ? 2 : 1;
     g.qbox = rows;
     g.spc = splits_per_cta(g.S, units * g.nhb, two_per_sm ? 2 * sms : sms);
     CUtensorMap vmap, wmap, qmap;
@@ -34,7 +25,8 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
         return cudaErrorInvalidValue;
     wmap = qmap = vmap;
     if (a.w_r) {
-        if (!make_map(&wmap, a.w_r, kD, (uint64_t)g.Hkv * kD, (uint32_t)kD)) return cudaErrorInvalidValue;
+        const uint64_t hw = g.wr_per_qh ? g.Hq : g.Hkv;
+        if (!make_map(&wmap, a.w_r, kD, hw * kD, (uint32_t)kD)) return cudaErrorInvalidValue;
         // q as [total_q][Hq][128], one box = max_q consecutive drafts of a group's heads (64 dims); rows past
         // total_q read as zeros
         auto fn = encode_fn();

@@ -369,3 +369,24 @@ def test_fp32_sums_of_a_long_cache_with_outliers(splits):
     want = tree_reference(x, composed=True)
     d = run(x, torch.float32, splits=splits, composed=True).double() - want
     assert float(d.norm()) <= (8 * 2.0 ** -20 * math.log(2) + 2.0 ** -22) * float(want.norm())
+
+
+@pytest.mark.parametrize("Hq,Hkv,n", [(1, 1, 7), (4, 1, 4), (8, 2, 8), (6, 1, 5), (16, 1, 2), (20, 1, 1), (32, 1, 1),
+                                      (11, 1, 2), (40, 8, 6), (15, 3, 3)])
+@pytest.mark.parametrize("per_q", [False, True])
+@pytest.mark.parametrize("splits", [0, 3])
+def test_few_rows_of_either_type(Hq, Hkv, n, per_q, splits):
+    # blocks of 16 rows that hold a part of a group's heads, or the same head of several drafts
+    x = tree_inputs((500 + n, n, 131, 1), (n, max(1, n // 2), min(n, 2), 0), Hq, Hkv, wr_per_query_head=per_q,
+                    seed=Hq + n)
+    want = tree_reference(x)
+    check(run(x, splits=splits), want)
+    check(run(x, torch.bfloat16, splits=splits), want, torch.bfloat16)
+
+
+def test_few_rows_of_many_sequences_and_w_r_per_query_head():
+    lens = tuple(60 + 37 * (i % 11) for i in range(90))
+    x = tree_inputs(lens, tuple(1 + i % 4 for i in range(90)), 8, 2, wr_per_query_head=True, seed=4)
+    want = tree_reference(x)
+    check(run(x), want)
+    check(run(x, torch.bfloat16), want, torch.bfloat16)
