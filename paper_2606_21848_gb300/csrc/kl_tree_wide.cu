@@ -19,7 +19,11 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
     // (two CTAs per SM as the decode's blocks of heads; three terms leave no room for that)
     const bool two_per_sm = rows <= 16 && !fp32 && units > sms;
     g.qbox = rows;
-    g.spc = splits_per_cta(g.S, units * g.nhb, two_per_sm ? 2 * sms : sms);
+    const int64_t slots = two_per_sm ? 2 * sms : sms, ctas = units * g.nhb;
+    g.spc = splits_per_cta(g.S, ctas, slots);
+    // (and no more than four waves of CTAs, each of which pays a start: a split count of the caller's may ask for
+    // any number of short runs)
+    while (g.spc < g.S && (g.S + g.spc - 1) / g.spc * ctas > 4 * slots) ++g.spc;
     CUtensorMap vmap, wmap, qmap;
     if (!make_map(&vmap, a.v_cache, kD, (uint64_t)g.num_pages * g.Hkv * g.P, (uint32_t)g.P))
         return cudaErrorInvalidValue;
