@@ -62,7 +62,7 @@ constexpr float kWideLazy = 1024.f;
 // per SM; NG = 1, two CTAs per SM.
 template <int NH, int NG, int T = 2>
 struct Wide {
-    static constexpr int kStages = NG == 1 ? 3 : NH * T > 32 ? 5 : 6;
+    static constexpr int kStages = NG == 1 ? 5 - T : NH * T > 32 ? 5 : 6;
     static constexpr int kWarps = 8 * NG;                // compute warps
     static constexpr int kProducer = kWarps, kMma = kWarps + 1, kPv = kWarps + 2;
     static constexpr int kThreads = (kWarps + 3) * 32;
@@ -89,7 +89,8 @@ struct __align__(1024) WideSmem {
     int abort;
 };
 // (228 KB per SM, of which each CTA takes 1 KB for the system)
-static_assert(sizeof(WideSmem<16, 1>) <= 228 * 1024 / 2 - 1024, "two CTAs per SM");
+static_assert(sizeof(WideSmem<16, 1>) <= 228 * 1024 / 2 - 1024 && sizeof(WideSmem<16, 1, 3>) <= 228 * 1024 / 2 - 1024,
+              "two CTAs per SM");
 static_assert(sizeof(WideSmem<32, 2>) <= 227 * 1024 && sizeof(WideSmem<16, 2>) <= 227 * 1024 &&
                   sizeof(WideSmem<16, 2, 3>) <= 227 * 1024, "one");
 

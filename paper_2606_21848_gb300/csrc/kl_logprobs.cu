@@ -16,8 +16,9 @@
 // Selection: keys (value, lowest index first) above the smallest of the `top` best so far go to a list of
 // candidates in shared memory, which is ranked by counting and cut to `top` after the row's first chunk,
 // when it fills up and at the row's end. The first chunk's bound comes from the threads' maxima: with
-// `top` of them known to be >= t, so are `top` logits; t is the larger of (the smallest, over the 8 warps,
-// of the ceil(top / 8)-th largest maximum) and (the largest over the warps of the top-th).
+// `top` of them known to be >= t, so are `top` logits; t is the larger of (the smallest, over the w warps
+// with a vector for every thread, of the ceil(top / w)-th largest maximum) and (the largest over all warps of the
+// top-th).
 //
 // Measured: 2048 rows of 151936 bf16 logits, no alternatives, 100 us (6200 GB/s, 0.91 of a copy's); 512 rows of
 // 128256 with the 8 largest 39.6 us (3300 GB/s: 1.1 runs per row, whose selections' steps, some 4 us a row, do
@@ -501,6 +502,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
         if (top > 0) {
             float bound = from;
             if (first) {
+                const int full = min(kLpWarps, max(1, nv >> 5));     // warps without an idle thread
                 // the bound: the threads' maxima sorted over the lanes (descending)
                 float s = tmax;
 #pragma unroll
@@ -511,13 +513,14 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
                         const bool larger = ((lane & j) == 0) == ((lane & g) == 0);
                         s = larger ? fmaxf(s, o) : fminf(s, o);
                     }
-                if (lane == (top + kLpWarps - 1) / kLpWarps - 1) sm.wnth[warp] = s;
+                const int nth = (top + full - 1) / full;
+                if (lane == nth - 1) sm.wnth[warp] = s;
                 if (lane == top - 1) sm.wtop[warp] = s;
                 __syncthreads();
                 float lowest = sm.wnth[0], best = sm.wtop[0];
 #pragma unroll
                 for (int w = 1; w < kLpWarps; ++w) {
-                    lowest = fminf(lowest, sm.wnth[w]);
+                    if (w < full) lowest = fminf(lowest, sm.wnth[w]);
                     best = fmaxf(best, sm.wtop[w]);
                 }
                 bound = fmaxf(-FLT_MAX, fmaxf(best, lowest));
@@ -655,13 +658,13 @@ int chunk_vectors(int64_t vecs, int chunks) {
     return (int)((each + kLpThreads - 1) / kLpThreads * kLpThreads);
 }
 
-// Chunks of a row of `vecs` 16-byte vectors: of kLpChunk vectors, or smaller (kLpMinChunk) while the rows
-// leave CTAs idle.
+// Chunks of a row of `vecs` 16-byte vectors: of kLpChunk vectors, or smaller (kLpMinChunk) while every CTA still
+// has one chunk at most (427 rows of 5428 bf16 logits, 8 alternatives: a chunk each 7.7 us, two 10.4).
 int chunks_of(int64_t rows, int64_t vecs) {
     const int64_t ctas = (int64_t)kLpCtas * device_sm_count();
     int64_t n = (vecs + kLpChunk - 1) / kLpChunk;
     if (rows * n < ctas) {
-        const int64_t want = (ctas + rows - 1) / rows, most = (vecs + kLpMinChunk - 1) / kLpMinChunk;
+        const int64_t want = ctas / rows, most = (vecs + kLpMinChunk - 1) / kLpMinChunk;
         n = max(n, min(want, most));
     }
     if (n < 1) return 1;

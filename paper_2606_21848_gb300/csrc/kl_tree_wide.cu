@@ -16,8 +16,11 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
     const int rows = g.G * a.tree.max_q;
     const int64_t sms = device_sm_count(), units = (int64_t)g.B * g.Hkv;
     const bool fp32 = a.out_dtype == KL_FP32, w32 = rows > 16 && g.nhb == 1;
-    // (two CTAs per SM as the decode's blocks of heads; three terms leave no room for that)
-    const bool two_per_sm = rows <= 16 && !fp32 && units > sms;
+    // Two CTAs per SM as the decode's blocks of heads. With three terms these have rings of two tiles, which
+    // suits short caches alone (fp32, 32 / 8 heads, two and one per SM: 64 sequences of 1000 tokens, 4 drafts 43.6
+    // and 51.5 us, 16 of 4096, 8 drafts 54 and 70, 64 of 8192 208 and 196, of 64 / 8 heads 370 and 297).
+    const int64_t tiles = ((int64_t)g.max_pages * g.P + 127) / 128;
+    const bool two_per_sm = !w32 && units * g.nhb > sms && (!fp32 || tiles <= 32);
     g.qbox = rows;
     const int64_t slots = two_per_sm ? 2 * sms : sms, ctas = units * g.nhb;
     g.spc = splits_per_cta(g.S, ctas, slots);
@@ -42,7 +45,9 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     }
-    if (fp32) return launch_kernel_wide<16, 2, false, true, 3>(la, vmap, wmap, qmap);
+    if (fp32)
+        return two_per_sm ? launch_kernel_wide<16, 1, false, true, 3>(la, vmap, wmap, qmap)
+                          : launch_kernel_wide<16, 2, false, true, 3>(la, vmap, wmap, qmap);
     if (w32) return launch_kernel_wide<32, 2, false, true>(la, vmap, wmap, qmap);
     return two_per_sm ? launch_kernel_wide<16, 1, false, true>(la, vmap, wmap, qmap)
                       : launch_kernel_wide<16, 2, false, true>(la, vmap, wmap, qmap);
