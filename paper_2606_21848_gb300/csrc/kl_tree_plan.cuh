@@ -27,6 +27,12 @@ constexpr int kTreeCut = 2, kTreeRun = 2;
 constexpr int kTreeStart = 5, kTreeWhole = 8;
 constexpr int kTreeStartFp32 = 2, kTreeWholeFp32 = 4;
 constexpr int kTreeMaxRuns = 512;   // (one per SM; the merge lists a unit's parts in shared memory)
+// The pipeline of a segment: softmax groups (half tile u is group u % kTreeGroups'), buffers of scores with bf16
+// and with fp32 outputs, and with fp32 outputs the half tiles between two moves of O to its sum and the barriers
+// on which the references are announced (half tile u's on u % kTreeTurns, phase u / kTreeTurns). A wait by parity
+// holds only while its barrier is in that phase or the next one: with a barrier per group the softmax could
+// pass two half tiles, and with them two phases, before the warps that move O came to wait for the first.
+constexpr int kTreeGroups = 2, kTreeSub = 3, kTreeSubFp32 = 2, kTreeFold = 2, kTreeTurns = 4;
 // A part's state: O [32][128 rows] float4 and {m, l} [128 rows]. Every run has up to two parts.
 constexpr size_t kTreeStateBytes = kTreeRows * 128 * sizeof(float) + kTreeRows * 2 * sizeof(float);
 

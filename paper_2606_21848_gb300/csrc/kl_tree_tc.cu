@@ -81,15 +81,15 @@ constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 i
 // The routed queries first land in columns 0 .. 255, before anything else is there.
 struct Half {
     static constexpr bool kFp16 = true;
-    static constexpr int kQTerms = 1, kPTerms = 1, kSub = 3, kStages = 5;
+    static constexpr int kQTerms = 1, kPTerms = 1, kSub = kTreeSub, kStages = 5;
     static constexpr uint32_t kBuf = 64, kColO = 192, kColQ = 448;
 };
 struct Full {
     static constexpr bool kFp16 = false;
-    static constexpr int kQTerms = 3, kPTerms = 3, kSub = 2, kStages = 3;
+    static constexpr int kQTerms = 3, kPTerms = 3, kSub = kTreeSubFp32, kStages = 3;
     static constexpr uint32_t kBuf = 96, kColO = 192, kColQ = 320;
 };
-constexpr int kGroups = 2;
+constexpr int kGroups = kTreeGroups;
 // Registers: of the 128 per thread at launch, the other warps give up 32 and the softmax warps take them
 // (a half tile of scores and weights, 64 registers, spilled at 128. 168 / 88: 1 to 3 % slower).
 constexpr uint32_t kSoftmaxRegs = 160, kOtherRegs = 96;
@@ -100,7 +100,7 @@ struct Warps {
     static constexpr int kProducer = kCompute, kMma = kCompute + 1, kPv = kCompute + 2, kHelp = kCompute + 4;
     static constexpr int kThreads = 32 * (kHelp + 4);
 };
-constexpr int kFoldSub = 2;           // Full: half tiles between two moves of O to the fp32 sum
+constexpr int kFoldSub = kTreeFold;   // Full: half tiles between two moves of O to the fp32 sum
 
 template <typename C>
 struct __align__(1024) TreeSmem {
@@ -115,12 +115,12 @@ struct __align__(1024) TreeSmem {
     // waits for tiles alone never meets W^R's phases; per half tile u on s_full[u % 4] (its scores),
     // p_full[u % 4] (its weights) and s_free[u % 4] (its output MMAs are done; of its buffer u % kSub: but
     // barriers by u % 4, so that a group meets every phase of those it waits for), and per lane quarter on
-    // turn[.][u % 2] (Full: the references after it).
+    // turn[.][u % kTreeTurns] (Full: the references after it).
     struct Bars {
         uint64_t w_full[C::kStages], full[C::kStages], empty[C::kStages];
         uint64_t s_full[4], s_free[4];
         uint64_t p_full[4], o_free, sum_full, v_full[C::kStages];
-        uint64_t turn[4][kGroups];
+        uint64_t turn[4][kTreeTurns];
         uint64_t first[4];                 // per lane quarter: the maxima of half tile 1 are in lsum[1]
         uint64_t r_full[2], r_free[2];     // routing results, alternating halves of columns 0 .. 255
         uint64_t qr_ready, par_ready, drain, drain2;
@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 bool okf = qd < (k.blk.rows * hp + 31) >> 5; // (a quarter without rows rests)
                 for (int u = kFoldSub; okf && u < n_sub; u += kFoldSub) {
                     okf = wait(&sm.bar.s_free[(u - 1) & 3], ((u - 1) >> 2) & 1) &&
-                          wait(&sm.bar.turn[qd][(u - 1) % kGroups], ((u - 1) / kGroups) & 1);
+                          wait(&sm.bar.turn[qd][(u - 1) % kTreeTurns], ((u - 1) / kTreeTurns) & 1);
                     if (!okf) break;
                     ptx::tc_fence_after();
                     const float m = sm.mref[(u - 1) & 3][r];
@@ -862,7 +862,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                         __syncwarp();
                         if (lane == 0) ptx::mbar_arrive(&sm.bar.first[qd]);
                     }
-                    okl = wait(&sm.bar.turn[qd][(u - 1) % kGroups], ((u - 1) / kGroups) & 1);
+                    okl = wait(&sm.bar.turn[qd][(u - 1) % kTreeTurns], ((u - 1) / kTreeTurns) & 1);
                     if (!okl) break;
                     m_ref = sm.mref[(u - 1) & 3][r];
                 }
@@ -895,7 +895,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 if constexpr (!C::kFp16) {
                     sm.mref[u & 3][r] = m_ref;
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&sm.bar.turn[qd][grp]);
+                    if (lane == 0) ptx::mbar_arrive(&sm.bar.turn[qd][u % kTreeTurns]);
                 }
                 // the group's sums move to this reference
                 if (__any_sync(0xffffffffu, m_ref != m_used)) {
@@ -955,7 +955,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
             // reference of the last half tile; Half: the groups' states are joined as parts are. This
             // group's output dims.
             const int last = n_sub - 1, lg = last % kGroups;
-            if (!C::kFp16 && okl && lg != grp) okl = wait(&sm.bar.turn[qd][lg], (last / kGroups) & 1);
+            if (!C::kFp16 && okl && lg != grp) okl = wait(&sm.bar.turn[qd][last % kTreeTurns], (last / kTreeTurns) & 1);
             // (all of the last commits land before the barriers are set up anew)
             bool oke = okl;
             if (!C::kFp16 && oke && last >= kFoldSub) oke = wait(&sm.bar.sum_full, 0);
