@@ -516,7 +516,13 @@ extern "C" {
 
 size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top) {
     if (num_rows < 0 || vocab <= 0 || vocab > (1 << 30) || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
-    return logprobs_layout(num_rows, logprob_chunks(num_rows, vocab, KL_FP32), num_top).total;
+    // (neither type always has the more chunks: a chunk's size is rounded up once their number is chosen)
+    size_t most = 0;
+    for (const kl_dtype t : {KL_BF16, KL_FP32}) {
+        const size_t n = logprobs_layout(num_rows, logprob_chunks(num_rows, vocab, t), num_top).total;
+        if (n > most) most = n;
+    }
+    return most;
 }
 
 kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride, const void *logits,
