@@ -503,9 +503,10 @@ kl_status kl_tree_commit(const kl_shape *shape, const int32_t *cu_q_lens, const 
 
 namespace {
 
-SharedLayout logprobs_layout(int32_t rows, int chunks, int32_t top) {
-    const size_t slots = (size_t)rows * chunks;
-    SharedLayout w = shared_layout((size_t)rows, slots * sizeof(float4), slots * top * sizeof(uint64_t));
+// A counter for each CTA, which every number of rows leaves inside the front region, and two parts.
+SharedLayout logprobs_layout(int chunks, int32_t top) {
+    const size_t ctas = logprob_ctas();
+    SharedLayout w = shared_layout(ctas, 2 * ctas * sizeof(float4), 2 * ctas * top * sizeof(uint64_t));
     if (chunks <= 1) w.total = 0;
     return w;
 }
@@ -517,12 +518,8 @@ extern "C" {
 size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top) {
     if (num_rows < 0 || vocab <= 0 || vocab > (1 << 30) || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
     // (neither type always has the more chunks: a chunk's size is rounded up once their number is chosen)
-    size_t most = 0;
-    for (const kl_dtype t : {KL_BF16, KL_FP32}) {
-        const size_t n = logprobs_layout(num_rows, logprob_chunks(num_rows, vocab, t), num_top).total;
-        if (n > most) most = n;
-    }
-    return most;
+    const int c16 = logprob_chunks(num_rows, vocab, KL_BF16), c32 = logprob_chunks(num_rows, vocab, KL_FP32);
+    return logprobs_layout(c16 > c32 ? c16 : c32, num_top).total;
 }
 
 kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride, const void *logits,
@@ -540,7 +537,7 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     if (!logits || (tokens_per_row > 0 && (!tokens || !logprobs)) || (num_top > 0 && (!top_logprobs || !top_ids)))
         return KL_ERR_INVALID_ARG;
     if (!aligned(logits, logits_dtype == KL_FP32 ? 4 : 2)) return KL_ERR_INVALID_ARG;
-    const SharedLayout w = logprobs_layout(num_rows, chunks, num_top);
+    const SharedLayout w = logprobs_layout(chunks, num_top);
     if (w.total > 0 && (!workspace || workspace_bytes < w.total || !aligned(workspace, 256)))
         return KL_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
@@ -554,7 +551,7 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     a.tokens = tokens;
     a.per_row = tokens_per_row;
     a.top = num_top;
-    a.chunks = a.slots = chunks;
+    a.chunks = chunks;
     a.logprobs = logprobs;
     a.entropy = entropy;
     a.top_logprobs = top_logprobs;

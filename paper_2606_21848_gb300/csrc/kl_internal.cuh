@@ -181,14 +181,14 @@ struct LogprobArgs {
     int per_row;
     int top;                  // largest logits wanted
     int chunks;               // pieces of a row (logprob_chunks)
-    int slots;                // of a row in part and part_top: at least its chunks
     float *logprobs;          // [T][per_row]
     float *entropy;           // [T] or nullptr
     float *top_logprobs;      // [T][top]
     int32_t *top_ids;         // [T][top]
-    unsigned int *counters;   // [T] arrivals (zero between calls); chunks > 1
-    float4 *part;             // [T][slots] {maximum, sum, weighted sum, -}
-    uint64_t *part_top;       // [T][slots][top] keys, largest first
+    // chunks > 1, for up to logprob_ctas() CTAs:
+    unsigned int *counters;   // [CTA] arrivals of the row that starts there and goes on (zero between calls)
+    float4 *part;             // [CTA][2] {maximum, sum, weighted sum, -}: of a row begun earlier, of that one
+    uint64_t *part_top;       // [CTA][2][top] keys, largest first
     int32_t *err;
     cudaStream_t stream;
 };
@@ -294,8 +294,9 @@ cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int
                                const int32_t *seq_lens, int32_t *new_lens, uint16_t *v_cache,
                                int32_t *err, cudaStream_t stream);
 
-// Log probabilities, entropy and largest logits of rows of logits; the pieces of a row.
+// Log probabilities, entropy and largest logits of rows of logits; the pieces of a row; most CTAs of a launch.
 int logprob_chunks(int rows, int vocab, kl_dtype dtype);
+int logprob_ctas();
 cudaError_t launch_logprobs(const LogprobArgs &a);
 
 // FP8 value cache (E4M3 codes [num_pages][Hkv][P][D] with fp32 row scales [num_pages][Hkv][P]):

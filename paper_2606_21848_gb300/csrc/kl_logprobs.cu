@@ -236,19 +236,24 @@ struct LogprobRuns {
     }
 };
 
-// The parts of a row, joined by the CTA that arrived last: the sums to every thread, the keys to the list.
-__device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int row, int parts, float c, float &m,
+// Where the part of a row in CTA c's run lies, of a row that starts in CTA c0's: every run has at most one row
+// that began in an earlier one (its first) and one that goes on in the next (its last).
+__device__ __forceinline__ size_t part_slot(int c, int c0) { return 2 * (size_t)c + (c == c0); }
+
+// The parts of a row that starts in CTA c0's run, joined by the CTA that arrived last: the sums to every
+// thread, the keys to the list.
+__device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int c0, int parts, float c, float &m,
                            float &s1, float &s2) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, top = a.top;
-    const float4 *part = a.part + (size_t)row * a.slots;
-    const uint64_t *keys = a.part_top + (size_t)row * a.slots * top;
+    auto part = [&](int i) { return a.part + part_slot(c0 + i, c0); };
+    auto keys = [&](int i) { return a.part_top + part_slot(c0 + i, c0) * top; };
     // every part's last key is a bound; the largest of them leaves few
     float M = -INFINITY;
     uint64_t least = 0;
     for (int i = tid; i < parts; i += kLpThreads) {
-        M = fmaxf(M, __ldcg(part + i).x);
+        M = fmaxf(M, __ldcg(part(i)).x);
         if (top > 0) {
-            const uint64_t x = __ldcg(keys + (size_t)i * top + top - 1);
+            const uint64_t x = __ldcg(keys(i) + top - 1);
             if (x > least) least = x;
         }
     }
@@ -263,7 +268,7 @@ __device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int row, int p
     M = block_max(sm, M, warp, lane);
     float a1 = 0.f, a2 = 0.f;
     for (int i = tid; i < parts; i += kLpThreads) {
-        const float4 q = __ldcg(part + i);
+        const float4 q = __ldcg(part(i));
         float p1 = q.y, p2 = q.z;
         move_state(q.x, M, c, p1, p2);
         a1 += p1;
@@ -276,7 +281,7 @@ __device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int row, int p
         for (int w = 0; w < kLpWarps; ++w)
             if (sm.wkey[w] > least) least = sm.wkey[w];
         for (int i = tid; i < parts * top; i += kLpThreads) {
-            const uint64_t x = __ldcg(keys + i);
+            const uint64_t x = __ldcg(keys(i / top) + i % top);
             if (x != 0 && x >= least) {
                 const int at = atomicAdd(&sm.wcount[0], 1);
                 if (at < kLpCap) sm.cand[at] = x;
@@ -294,7 +299,7 @@ __device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int row, int p
             take_keys(sm, top, tid, [&](uint64_t prev) {
                 uint64_t best = 0;
                 for (int i = tid; i < parts * top; i += kLpThreads) {
-                    const uint64_t x = __ldcg(keys + i);
+                    const uint64_t x = __ldcg(keys(i / top) + i % top);
                     if (x < prev && x > best) best = x;
                 }
                 return best;
@@ -635,16 +640,16 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
         const int c0 = runs.of(row0);
         const int parts = runs.of(row0 + a.chunks - 1) - c0 + 1;
         if (parts > 1) {
-            const size_t at = (size_t)row * a.slots + (blockIdx.x - c0);
+            const size_t at = part_slot(blockIdx.x, c0);
             if (warp == 0) {
                 if (lane == 0) a.part[at] = make_float4(m, s1, s2, 0.f);
                 if (lane < top) a.part_top[at * top + lane] = sm.list[lane];
                 __syncwarp();
-                if (lane == 0) sm.is_last = arrive_last(a.counters + row, parts);
+                if (lane == 0) sm.is_last = arrive_last(a.counters + c0, parts);
             }
             __syncthreads();
             if (!sm.is_last) continue;
-            join_parts(sm, a, row, parts, c, m, s1, s2);
+            join_parts(sm, a, c0, parts, c, m, s1, s2);
         }
         finish_row<T>(sm, a, r.p, row, c, m, s1, s2, token, given);
         __syncthreads();
@@ -661,7 +666,7 @@ int chunk_vectors(int64_t vecs, int chunks) {
 // Chunks of a row of `vecs` 16-byte vectors: of kLpChunk vectors, or smaller (kLpMinChunk) while every CTA still
 // has one chunk at most (427 rows of 5428 bf16 logits, 8 alternatives: a chunk each 7.7 us, two 10.4).
 int chunks_of(int64_t rows, int64_t vecs) {
-    const int64_t ctas = (int64_t)kLpCtas * device_sm_count();
+    const int64_t ctas = logprob_ctas();
     int64_t n = (vecs + kLpChunk - 1) / kLpChunk;
     if (rows * n < ctas) {
         const int64_t want = ctas / rows, most = (vecs + kLpMinChunk - 1) / kLpMinChunk;
@@ -674,13 +679,15 @@ int chunks_of(int64_t rows, int64_t vecs) {
 
 }  // namespace
 
+int logprob_ctas() { return kLpCtas * device_sm_count(); }
+
 int logprob_chunks(int rows, int vocab, kl_dtype dtype) {
     return chunks_of(rows, vocab / (dtype == KL_FP32 ? 4 : 8));
 }
 
 cudaError_t launch_logprobs(const LogprobArgs &a) {
     const int per_chunk = chunk_vectors(a.vocab / (a.dtype == KL_FP32 ? 4 : 8), a.chunks);
-    const int64_t total = (int64_t)a.rows * a.chunks, ctas = (int64_t)kLpCtas * device_sm_count();
+    const int64_t total = (int64_t)a.rows * a.chunks, ctas = logprob_ctas();
     const auto kernel = a.dtype == KL_FP32 ? logprobs_kernel<float> : logprobs_kernel<uint16_t>;
     static PerDeviceOnce once[2];
     const cudaError_t e = once[a.dtype == KL_FP32].run([&] {
