@@ -516,7 +516,7 @@ SharedLayout logprobs_layout(int chunks, int32_t top) {
 extern "C" {
 
 size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top) {
-    if (num_rows < 0 || vocab <= 0 || vocab > (1 << 30) || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
+    if (num_rows <= 0 || vocab <= 0 || vocab > (1 << 30) || num_top < 0 || num_top > KL_LOGPROBS_MAX_TOP) return 0;
     // (neither type always has the more chunks: a chunk's size is rounded up once their number is chosen)
     const int c16 = logprob_chunks(num_rows, vocab, KL_BF16), c32 = logprob_chunks(num_rows, vocab, KL_FP32);
     return logprobs_layout(c16 > c32 ? c16 : c32, num_top).total;
