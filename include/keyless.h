@@ -330,7 +330,8 @@ kl_status kl_tree_commit(const kl_shape *shape, const int32_t *cu_q_lens, const 
 size_t kl_logprobs_workspace_size(int32_t num_rows, int32_t vocab, int32_t num_top);
 
 /*
- * Log probabilities under x = scale * logits (scale <= 0 selects 1; 1 / temperature otherwise). For row
+ * Log probabilities under x = scale * logits (scale <= 0 selects 1; 1 / temperature otherwise; one
+ * whose product with log2 e is not finite in fp32 -- from 2.36e38 on -- is KL_ERR_INVALID_ARG). For row
  * r, with z = sum_j exp(x_j):
  *   logprobs[r][k]      = x_t - log z,  t = tokens[r][k]   (-1: no token, 0 is written)
  *   entropy[r]          = -sum_j p_j log p_j, p = exp(x) / z           (in nats; NULL: not wanted)

@@ -530,7 +530,7 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     if (logits_dtype != KL_BF16 && logits_dtype != KL_FP32) return KL_ERR_INVALID_ARG;
     if (num_rows < 0 || vocab <= 0 || row_stride < vocab || tokens_per_row < 0 || num_top < 0 || num_top > vocab)
         return KL_ERR_INVALID_ARG;
-    if (!(scale == scale) || scale > 3e38f) return KL_ERR_INVALID_ARG;     // NaN, infinity
+    if (!(scale == scale) || isinf(scale > 0.f ? scale * kLog2e : 0.f)) return KL_ERR_INVALID_ARG;
     if (num_top > KL_LOGPROBS_MAX_TOP || vocab > (1 << 30)) return KL_ERR_UNSUPPORTED;
     if (num_rows == 0) return KL_OK;
     const int chunks = logprob_chunks(num_rows, vocab, logits_dtype);
