@@ -548,6 +548,8 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     a.logits = logits;
     a.dtype = logits_dtype;
     a.scale = scale > 0.f ? scale : 1.f;
+    const float c = a.scale * kLog2e;
+    a.c_error = c > 0.f ? (float)(a.scale * 1.4426950408889634 / c - 1.0) : 0.f;
     a.tokens = tokens;
     a.per_row = tokens_per_row;
     a.top = num_top;

@@ -177,6 +177,7 @@ struct LogprobArgs {
     const void *logits;       // [T][stride], the first V of each row
     kl_dtype dtype;
     float scale;
+    float c_error;            // (scale log2 e - c) / c of c, its value in fp32
     const int32_t *tokens;    // [T][per_row]
     int per_row;
     int top;                  // largest logits wanted

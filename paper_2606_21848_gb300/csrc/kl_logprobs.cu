@@ -10,8 +10,10 @@
 // threads do. A thread keeps its own state over the chunks of a row, in fp32: its largest logit m, and
 // with y = (x - m) scale log2 e (the difference first, so that rows of huge or lowest values neither
 // overflow nor cancel) s1 = sum 2^y and s2 = sum y 2^y. States join as softmax states do: with d =
-// (m - M) scale log2 e, s1' = 2^d s1, s2' = 2^d s2 + d s1'; at last log z = log2(s1) ln 2 above scale * M
-// and H = (log2 s1 - s2 / s1) ln 2. A row that lies in several CTAs' runs is joined by the last of them.
+// (m - M) scale log2 e, s1' = 2^d s1, s2' = 2^d s2 + d s1'; at last log z = log(s1) above scale * M and
+// H = log(s1) - s2 / s1 ln 2. (The rounding of scale log2 e to fp32 moves every y by the same part, which
+// s2 takes out of s1 again; log probabilities are within a few units of 2^-24 of 1 and of their size.) A row
+// that lies in several CTAs' runs is joined by the last of them.
 //
 // Selection: keys (value, lowest index first) above the smallest of the `top` best so far go to a list of
 // candidates in shared memory, which is ranked by counting and cut to `top` after the row's first chunk,
@@ -52,7 +54,7 @@ struct __align__(16) LogprobSmem {
     uint64_t list[KL_LOGPROBS_MAX_TOP];                  // keys, largest first
     uint64_t wkey[kLpWarps];
     float wmax[kLpWarps], wnth[kLpWarps], wtop[kLpWarps];
-    float s1[kLpWarps], s2[kLpWarps];
+    float s1[kLpWarps], e1[kLpWarps], s2[kLpWarps];
     int wcount[kLpWarps];
     int added[3];                                        // candidates of a chunk, by chunk number % 3
     int is_last;
@@ -117,25 +119,39 @@ __device__ __forceinline__ float lp_load(const void *row, int idx) {
     else return bf16lo((uint32_t)static_cast<const uint16_t *>(row)[idx]);
 }
 
-// Sum over each warp of s1 and s2, to the warps' slots (block_sums() after the next barrier).
+// s + x, with what the rounding lost added to e (exactly that while s and x are finite).
+__device__ __forceinline__ float sum_of(float s, float x, float &e) {
+    const float t = s + x, y = t - s;
+    e += (s - (t - y)) + (x - y);
+    return t;
+}
+
+// Sum over each warp of s1 and s2, to the warps' slots (block_sums() after the next barrier). Of s1, in which one
+// logit often holds most, the roundings are kept: the other 12 adds would each take half a unit of it.
 __device__ __forceinline__ void warp_sums(LogprobSmem &sm, float s1, float s2, int warp, int lane) {
+    float e = 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        e += __shfl_xor_sync(0xffffffffu, e, o);
+        s1 = sum_of(s1, __shfl_xor_sync(0xffffffffu, s1, o), e);
         s2 += __shfl_xor_sync(0xffffffffu, s2, o);
     }
     if (lane == 0) {
         sm.s1[warp] = s1;
+        sm.e1[warp] = e;
         sm.s2[warp] = s2;
     }
 }
 __device__ __forceinline__ void block_sums(const LogprobSmem &sm, float &s1, float &s2) {
+    float e = 0.f;
     s1 = s2 = 0.f;
 #pragma unroll
     for (int w = 0; w < kLpWarps; ++w) {
-        s1 += sm.s1[w];
+        s1 = sum_of(s1, sm.s1[w], e);
+        e += sm.e1[w];
         s2 += sm.s2[w];
     }
+    s1 += e;
 }
 
 // The keys cand[0 .. n - 1] (all different), ranked: the largest `top` of them to list. n <= kLpCap.
@@ -312,12 +328,12 @@ __device__ void join_parts(LogprobSmem &sm, const LogprobArgs &a, int c0, int pa
 // The results of a row. One of -inf alone has no distribution: log probabilities of -inf, entropy 0. A NaN
 // or +inf logit makes the sums, and with them everything but the ids, NaN.
 template <typename T>
-__device__ void finish_row(LogprobSmem &sm, const LogprobArgs &a, const char *rp, int row, float c, float m,
-                           float s1, float s2, int token, float given) {
+__device__ void finish_row(LogprobSmem &sm, const LogprobArgs &a, const char *rp, int row, float m, float s1,
+                           float s2, int token, float given) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, top = a.top;
     const bool none = s1 == 0.f;
-    const float lz = log2f(s1);
-    auto logprob = [&](float x) { return none ? -INFINITY : ((x - m) * c - lz) * kLn2; };
+    const float lz = logf(fmaf(a.c_error * kLn2, s2, s1));       // (to first order: dz / dc = ln 2 s2 / c)
+    auto logprob = [&](float x) { return none ? -INFINITY : fmaf(x - m, a.scale, -lz); };
     for (int i = tid; i < a.per_row; i += kLpThreads) {
         const bool here = i < kLpThreads;                // (the thread's first)
         const int id = here ? token : a.tokens[(size_t)row * a.per_row + i];
@@ -330,7 +346,7 @@ __device__ void finish_row(LogprobSmem &sm, const LogprobArgs &a, const char *rp
         }
         a.logprobs[(size_t)row * a.per_row + i] = lp;
     }
-    if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : (lz - s2 / s1) * kLn2;
+    if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : fmaf(s2 / s1, -kLn2, lz);
     if (tid == 0 && s1 != s1) raise_flag(a.err, KL_FLAG_RANGE);
     if (top > 0 && sm.list[top - 1] == 0) {
         // fewer than `top` logits above -inf: the first of the others, in order
@@ -551,11 +567,10 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
             }
         }
 
-        // the sums, at the thread's reference
-        // (moved when a weight would pass 2^16: m need not be the largest logit itself)
-        const bool moves = (tmax - m) * c > 16.f;
-        if (__any_sync(0xffffffffu, moves)) {
-            const float to = moves ? tmax : m;
+        // the sums, at the thread's largest logit (a reference that stays behind leaves log2 s1 and the largest
+        // x - m large, and their difference with those numbers' roundings)
+        if (__any_sync(0xffffffffu, tmax > m)) {
+            const float to = fmaxf(tmax, m);
             move_state(m, to, c, s1, s2);
             m = to;
         }
@@ -570,18 +585,18 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
                     float2 y = lp_mul2(lp_add2(x, neg_m), cc);
                     const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
                     if constexpr (decltype(clamp)::value) y = make_float2(fmaxf(y.x, -1e30f), fmaxf(y.y, -1e30f));
-                    a1 = lp_add2(a1, p);
                     a2 = lp_fma2(p, y, a2);
+                    return p;
                 };
+                // (a vector's own sum first: fewer roundings of the whole)
                 auto vec = [&](const uint4 &x) {
                     if constexpr (VEC == 4) {
-                        pair(make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
-                        pair(make_float2(__uint_as_float(x.z), __uint_as_float(x.w)));
+                        const float2 p = pair(make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
+                        a1 = lp_add2(a1, lp_add2(p, pair(make_float2(__uint_as_float(x.z), __uint_as_float(x.w)))));
                     } else {
-                        pair(lp_unpack<T>(x.x));
-                        pair(lp_unpack<T>(x.y));
-                        pair(lp_unpack<T>(x.z));
-                        pair(lp_unpack<T>(x.w));
+                        const float2 p = lp_add2(pair(lp_unpack<T>(x.x)), pair(lp_unpack<T>(x.y)));
+                        const float2 q = lp_add2(pair(lp_unpack<T>(x.z)), pair(lp_unpack<T>(x.w)));
+                        a1 = lp_add2(a1, lp_add2(p, q));
                     }
                 };
                 if (mine == kLpVecs && !decltype(clamp)::value) {
@@ -606,7 +621,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
 
         // ------------------------------------------------------- the row, or its part in this run ----
         if (extra_at >= 0) {
-            if ((extra - m) * c > 16.f) {
+            if (extra > m) {
                 move_state(m, extra, c, s1, s2);
                 m = extra;
             }
@@ -651,7 +666,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
             if (!sm.is_last) continue;
             join_parts(sm, a, c0, parts, c, m, s1, s2);
         }
-        finish_row<T>(sm, a, r.p, row, c, m, s1, s2, token, given);
+        finish_row<T>(sm, a, r.p, row, m, s1, s2, token, given);
         __syncthreads();
     }
 }
