@@ -561,6 +561,7 @@ kl_status kl_token_logprobs(int32_t num_rows, int32_t vocab, int64_t row_stride,
     a.counters = w.total ? reinterpret_cast<unsigned int *>(ws) : nullptr;
     a.part = w.total ? reinterpret_cast<float4 *>(ws + w.states) : nullptr;
     a.part_top = w.total ? reinterpret_cast<uint64_t *>(ws + w.extra) : nullptr;
+    a.wait_ns = current_wait_ns();
     a.err = err;
     a.stream = reinterpret_cast<cudaStream_t>(stream);
     return from_cuda(launch_logprobs(a));

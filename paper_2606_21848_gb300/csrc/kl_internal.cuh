@@ -190,6 +190,7 @@ struct LogprobArgs {
     unsigned int *counters;   // [CTA] arrivals of the row that starts there and goes on (zero between calls)
     float4 *part;             // [CTA][2] {maximum, sum, weighted sum, -}: of a row begun earlier, of that one
     uint64_t *part_top;       // [CTA][2][top] keys, largest first
+    uint64_t wait_ns;         // bound of the waits for copies (kl_set_wait_timeout_ns)
     int32_t *err;
     cudaStream_t stream;
 };

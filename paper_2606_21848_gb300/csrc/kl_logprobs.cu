@@ -27,6 +27,7 @@
 // not overlap within a CTA); 96 rows of 50257 fp32 logits with the 20 largest 16.4 us, and one row of 32000 7.9 us
 // (latency: first copy 1, first selection 2, further chunks 3, ranking 1.3, the join of a row's parts 4).
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
@@ -58,6 +59,7 @@ struct __align__(16) LogprobSmem {
     int wcount[kLpWarps];
     int added[3];                                        // candidates of a chunk, by chunk number % 3
     int is_last;
+    int lost;                                            // 1 + the number of a chunk that did not land in time
 };
 static_assert(sizeof(LogprobSmem) * kLpCtas <= (228 - kLpCtas) * 1024, "CTAs per SM");
 
@@ -222,12 +224,15 @@ struct LogprobRow {
     }
 };
 
-// A copy that has not landed at the first look: bounded (about one second).
-__device__ __noinline__ void wait_slow(uint64_t *bar, uint32_t phase, int32_t *err) {
+// The copy of chunk k that has not landed at the first look, up to `limit` ns (short ones by the poll that does
+// not suspend the thread); else sm.lost becomes k + 1.
+__device__ __noinline__ void wait_slow(LogprobSmem &sm, int k, uint64_t limit) {
+    uint64_t *bar = &sm.full[k % kLpStages];
+    const uint32_t phase = (k / kLpStages) & 1;
     const uint64_t t0 = ptx::globaltimer();
-    while (!ptx::mbar_try_wait(bar, phase))
-        if (ptx::globaltimer() - t0 > kDefaultWaitNs) {
-            raise_flag(err, KL_FLAG_TIMEOUT);
+    while (!(limit < kExactWaitNs ? ptx::mbar_test_wait(bar, phase) : ptx::mbar_try_wait(bar, phase)))
+        if (ptx::globaltimer() - t0 > limit) {
+            sm.lost = k + 1;
             return;
         }
 }
@@ -394,6 +399,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
         ptx::fence_mbar_init();
     }
     if (tid < 3) sm.added[tid] = 0;
+    if (tid == 3) sm.lost = INT_MAX;
     __syncthreads();
     grid_dep_wait();
     grid_dep_launch();
@@ -466,8 +472,6 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
         if (tid == 0) sm.added[k % 3] = 0;
         __syncthreads();
     };
-    int slot = 0;                                        // of chunk k, and the phase of its copy
-    uint32_t phase = 0;
 
     for (int k = 0; k < steps; ++k, ++ch) {
         if (ch == a.chunks) {
@@ -491,11 +495,15 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
         }
         // Everyone has read the last chunk's slot, and its candidates are complete.
         __syncthreads();
+        // (the CTA leaves as a whole: a thread that is ahead may lose chunk k, but none before it)
+        if (*(volatile int *)&sm.lost <= k) break;
         if (tid == 0 && k > 0 && k - 1 + kLpStages < steps) fetch(k - 1 + kLpStages);
         if (top > 0 && !first) settle(k - 1, false);
         // the chunk: vector i of the thread is i * 256 + tid
+        const int slot = k % kLpStages;
         const int q0 = ch * per_chunk, nv = min(per_chunk, r.vecs - q0);
-        if (!ptx::mbar_try_wait(&sm.full[slot], phase)) wait_slow(&sm.full[slot], phase, a.err);
+        if (a.wait_ns < kExactWaitNs || !ptx::mbar_try_wait(&sm.full[slot], (k / kLpStages) & 1))
+            wait_slow(sm, k, a.wait_ns);
         // (read from shared memory once for the maximum and once for the sums: 64 logits held in between
         // spilled)
         const uint4 *const data = reinterpret_cast<const uint4 *>(sm.ring[slot]) + tid;
@@ -613,10 +621,6 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
             if (__any_sync(0xffffffffu, s2 != s2 && s1 == s1)) sums(std::true_type{});
         }
         if (first) given = token >= 0 && token < a.vocab ? lp_load<T>(r.p, token) : 0.f;
-        if (++slot == kLpStages) {
-            slot = 0;
-            phase ^= 1;
-        }
         if (!last) continue;
 
         // ------------------------------------------------------- the row, or its part in this run ----
@@ -668,6 +672,13 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtas) logprobs_kernel(const Log
         }
         finish_row<T>(sm, a, r.p, row, m, s1, s2, token, given);
         __syncthreads();
+    }
+    // Copies still in flight land before the CTA's shared memory goes away: the lost chunk's and those behind it.
+    __syncthreads();
+    if (tid == 0 && sm.lost != INT_MAX) {
+        raise_flag(a.err, KL_FLAG_TIMEOUT);
+        const int k = sm.lost - 1;
+        for (int i = k; i < steps && i < k + kLpStages; ++i) wait_slow(sm, i, kDefaultWaitNs);
     }
 }
 
