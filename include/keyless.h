@@ -287,8 +287,8 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
  * KL_TREE_MAX_DRAFTS; w_r (NULL: q is the composed query), v_cache, block_table, seq_lens as in
  * kl_decode_attention; num_splits: the parts that a sequence is cut into at most (0: chosen from the
  * lengths and the GPU). Workspace: kl_tree_workspace_size bytes of the same arguments, 256-byte aligned.
- * One launch, or two where sequences may be cut. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3 (KL_ERR_UNSUPPORTED
- * otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <=
+ * One launch, or two where sequences may be cut. head_dim 128, page size 16, 32, 64 or 128, compute
+ * capability 10.3 (KL_ERR_UNSUPPORTED otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <=
  * max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine: nothing is
  * written); a parent outside [-1, i) raises KL_FLAG_BAD_TREE and counts as -1; a bad page id leaves the
  * affected outputs unspecified. A drafted row that is not finite reaches the drafts that see it
@@ -296,9 +296,11 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
  * Precision: scores, softmax and sums in fp32. The operands of the products depend on the form:
  *   fp32 outputs: the routed query and the weights carry 24 significant bits (error about 1e-6);
  *   bf16 outputs with R = (Hq / Hkv) * max_q_len <= 16, or R <= 32 on some sizes: 16 bits;
- *   other bf16 outputs: fp16, 11 bits, cached values of magnitude 2^-14 to 65280 exactly. There a routed
- *   query times scale * log2 e, or a cached value, beyond 65504 makes the outputs that it takes part in
- *   NaN (a drafted row: those of the drafts that see it), and a non-finite output raises KL_FLAG_RANGE.
+ *   other bf16 outputs: fp16; the routed query times scale * log2 e 22 bits (and within 2^-25), the weights
+ *   11, cached values of magnitude 2^-14 to 65280 exactly and smaller ones within 2^-25 (take fp32 outputs
+ *   where values are smaller than that allows). There a routed query times scale * log2 e, or a cached
+ *   value, beyond 65504 makes the outputs that it takes part in NaN (a drafted row: those of the drafts
+ *   that see it), and a non-finite output raises KL_FLAG_RANGE.
  */
 kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
                             const int32_t *block_table, const int32_t *seq_lens,

@@ -113,6 +113,16 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return d;
 }
 
+// The leading fp16 term of two fp32 values, packed; the values become what is left.
+__device__ __forceinline__ uint32_t take_term_f16(uint32_t &x0, uint32_t &x1) {
+    const float a = __uint_as_float(x0), b = __uint_as_float(x1);
+    const uint32_t t = pack_f16(a, b);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&t));
+    x0 = __float_as_uint(a - f.x);
+    x1 = __float_as_uint(b - f.y);
+    return t;
+}
+
 __device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t *v) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])

@@ -22,18 +22,17 @@
 // MN-major one of the output. Q and P are A operands in tensor memory.
 //
 // Precision. bf16 outputs (Half): the tile is converted to fp16 in place (exact for bf16 values of magnitude
-// 2^-14 to 65280), the routed query and the weights are one fp16 operand each (11 bits), so that each
-// product takes one term. A weight is off by |s| 2^-12 / sqrt(3) at rms, against the output's own rounding
-// of 2^-9; with the query as two terms a tile took 1.24 us (19 sequences of 32768 tokens, 32 / 8 heads, 32
-// drafts; HBM delivers a tile to every SM in 0.73 us, and this form takes 1.0). Values or queries past fp16's
-// range make the outputs that take part in them NaN (KL_FLAG_RANGE).
+// 2^-14 to 65280, within 2^-25 below), the routed query is a sum of two fp16 operands (22 bits), the weights
+// are one (11 bits: an output is off by 2^-12 of a weight's share, against its own rounding of 2^-8). With one
+// operand for the query a score s was off by |s| 2^-12, which moves the weights of tokens with scores of
+// hundreds by a tenth; a tile then took 1.0 us, with two 1.2 (64 sequences of 8192 tokens, 64 / 8 heads, 16 drafts
+// 268 and 322 us, 512 to 32768 tokens, up to 24 drafts 501 and 598, one of 131072, 32 drafts 72 and 86). Values or
+// queries past fp16's range make the outputs that take part in them NaN (KL_FLAG_RANGE).
 // fp32 outputs (Full): query and weights are sums of three bf16 terms (24 bits), and since the tensor
 // core's adds truncate, O moves every 128 tokens to a sum in shared memory.
 //
-// What bounds it. Half, on long caches: nothing alone. Of the 253 us of the sizes above (5100 GB/s of cache,
-// 1.3 PFLOP/s) removing the conversion, the exponentials, or one of the two products saved 18 to 35 us each, and
-// removing all of them 52. 64 sequences of 512 to 32768 tokens, up to 24 drafts: 493 us (323 at HBM's rate);
-// one of 131072 tokens, 32 drafts: 72 us (40); 64 of 8192, 16 drafts, 64 / 8 heads: 246 us (163). Short caches
+// What bounds it. Half, on long caches: nothing alone; a tile's three products take 1.0 us at the peak rate, HBM
+// delivers a tile to every SM in 0.73. (The sizes above take 323, 40 and 163 us at HBM's rate.) Short caches
 // are bound by latency: starting a segment takes 5 us, of them the routing and the first scores 3.5, and units
 // of several parts 3 to 5 us for the merge.
 // Full: three score and three output products per tile (2.0 us at the peak rate); a tile takes 2.7 us. 12
@@ -74,9 +73,10 @@ constexpr uint32_t kBarCompute = 1;   // named barrier of the compute warps (0 i
 // Operand forms and the layout that they leave room for. Two groups of four softmax warps (thread = row =
 // TMEM lane) take alternate half tiles. Tensor memory: kSub buffers of kBuf columns (64 of scores, then the
 // weights, 32 per term), then
-//   Half: an O of 128 columns for each group, which so keeps its own reference and never waits for the other
-//     (one O for both made each half tile's reference wait for the one before: 1.04 us per tile, 1.00 this
-//     way), and the query (64 columns); four warps convert tiles to fp16 ahead of the score MMAs.
+//   Half: an O of 128 columns for each group, which so keeps its own reference and never waits for the other,
+//     and the query's first term (64 columns). The second is in shared memory in the query block's place (with
+//     both here and two buffers of scores 64 sequences of 8192 tokens took 350 us, this way 322). Four warps
+//     convert tiles to fp16 ahead of the score MMAs.
 //   Full: one O, the query's terms (64 columns each).
 // The routed queries first land in columns 0 .. 255, before anything else is there.
 struct Half {
@@ -104,7 +104,8 @@ constexpr int kFoldSub = kTreeFold;   // Full: half tiles between two moves of O
 
 template <typename C>
 struct __align__(1024) TreeSmem {
-    uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B]
+    uint8_t q[kBM * kD * 2];               // query block, K-major SW128: [64-dim half][128 rows][128 B]; Half: then
+                                           // the routed query's second term
     // Ring: the W^R matrices, then the cache tiles ([64-dim half][128 rows][128 B], SW128).
     uint8_t tiles[C::kStages][kTileBytes];
     float sum[C::kFp16 ? 4 : kBM * kD];    // Full: O of the half tiles folded so far, [row][128], its
@@ -543,12 +544,18 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                             ptx::tc_fence_after();
                             const uint64_t b0 = k_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
                             // (the small terms first: the tensor core's adds truncate the sum)
+                            if constexpr (C::kFp16)
+#pragma unroll
+                                for (int kk = 0; kk < kD / 16; ++kk)
+                                    ptx::mma_bf16(tmem + sb * C::kBuf, q_desc + kstep(kk), b0 + kstep(kk), idesc_qk,
+                                                  kk > 0);
 #pragma unroll
                             for (int i = C::kQTerms - 1; i >= 0; --i)
 #pragma unroll
                                 for (int kk = 0; kk < kD / 16; ++kk)
                                     ptx::mma_bf16_ts(tmem + sb * C::kBuf, tmem + kColQ + 64 * i + kk * 8,
-                                                     b0 + kstep(kk), idesc_qk, i < C::kQTerms - 1 || kk > 0);
+                                                     b0 + kstep(kk), idesc_qk,
+                                                     C::kFp16 || i < C::kQTerms - 1 || kk > 0);
                             ptx::mma_commit(&sm.bar.s_full[u & 3]);
                         }
                     }
@@ -755,10 +762,23 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             uint32_t &x0 = q[2 * (c + e)], &x1 = q[2 * (c + e) + 1];
-                            w[e] = C::kFp16 ? pack_f16(__uint_as_float(x0), __uint_as_float(x1)) : take_term(x0, x1);
+                            w[e] = C::kFp16 ? take_term_f16(x0, x1) : take_term(x0, x1);
                         }
                         ptx::tmem_st16(tmem + kColQ + 64 * t + c0 / 2 + c + lane_base, w);
                     }
+                if constexpr (C::kFp16) {
+                    // what is left, as a second fp16 term, takes the query block's place (which the routing has read)
+                    const uint32_t row = ptx::smem_addr(sm.q) + grp * kHalfBytes + r * 128;
+#pragma unroll
+                    for (int c = 0; c < kCols / 8; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = pack_f16(__uint_as_float(q[8 * c + 2 * e]), __uint_as_float(q[8 * c + 2 * e + 1]));
+                        st_shared_v4(row + ((c ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
+                    }
+                    ptx::fence_proxy_async_smem();
+                }
             }
             if (ok) {
                 ptx::tmem_wait_st();

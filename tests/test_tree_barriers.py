@@ -103,3 +103,39 @@ def test_a_barrier_per_group_would_be_missed(sizes):
     """The graph shows the fault of announcing on a barrier per group: the moves of O may come too late."""
     bad = fp32(12, sizes["kTreeGroups"], sizes["kTreeSubFp32"], sizes["kTreeFold"], sizes["kTreeGroups"]).faults()
     assert bad and all(step[0] == "F" and why == "late" for step, _, _, why in bad)
+
+
+def bf16(n, groups, sub):
+    """A segment of n half tiles with bf16 outputs: S scores, R behind a wait that a reference which moves adds, P
+    weights, V output products, E the epilogues. Each group has its own reference and O."""
+    g = Graph()
+    for u in range(n):
+        g.step(("S", u), [("S", u - 1)], [(("s_free", (u - sub) % 4), (u - sub) // 4)] if u >= sub else [],
+               (("s_full", u % 4), u // 4))
+        seen = [(("s_full", u % 4), u // 4)]
+        g.step(("R", u), [("P", u - groups)],
+               seen + ([(("s_free", (u - groups) % 4), (u - groups) // 4)] if u >= groups else []))
+        g.step(("P", u), [("P", u - groups)], seen, (("p_full", u % 4), u // 4))
+        g.step(("V", u), [("V", u - 1)], [(("p_full", u % 4), u // 4)], (("s_free", u % 4), u // 4))
+    last = n - 1
+    for grp in range(groups):
+        mine = [u for u in range(n) if u % groups == grp]
+        g.step(("E", grp), [("P", mine[-1])] if mine else [],
+               [(("s_free", u % 4), u // 4) for u in range(last, max(last - 3, -1), -1)])
+    return g
+
+
+def test_bf16_outputs(sizes):
+    for n in range(1, 24):
+        # (R is on P's way where it is waited for, so what follows from P follows from it)
+        faults = bf16(n, sizes["kTreeGroups"], sizes["kTreeSub"]).faults()
+        assert [f for f in faults if f[0][0] != "R" or f[3] != "late"] == []
+
+
+def test_all_scores_and_output_products_are_waited_for(sizes):
+    """What ends a segment sees every completion on the barriers of scores and weights, which are then set up anew."""
+    for n in range(1, 24):
+        g = bf16(n, sizes["kTreeGroups"], sizes["kTreeSub"])
+        g.resolve()
+        waited = g.ancestors([("E", e) for e in range(sizes["kTreeGroups"])])
+        assert {("V", u) for u in range(n)} | {("S", u) for u in range(n)} <= waited
