@@ -522,8 +522,8 @@ int32_t kl_decode_kernel_available(const kl_shape *shape, int32_t kernel, int32_
  * undefined, and a workspace it used must be zero-filled again before the next call. This sets
  * that limit, in nanoseconds, for every decode launched afterwards by kl_decode_attention(_ex),
  * kl_decode_step, kl_standard_decode, kl_decode_attention_noalloc, the latent decodes and the FP8
- * decodes, and for the waits of kl_token_logprobs for its copies (of which the CTA leaves at the first that
- * runs out), process-wide; 0 restores the default. Returns the limit in force before the call. A
+ * decodes, and in the same way for kl_tree_attention and for the waits of kl_token_logprobs for its copies,
+ * process-wide; 0 restores the default. Returns the limit in force before the call. A
  * small value makes the waits run out on purpose: this is how the timeout path is tested. The
  * paper has no counterpart.
  */

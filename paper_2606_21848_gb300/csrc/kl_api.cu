@@ -452,6 +452,7 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
         d.direct_out = g.S == 1;
         d.out_dtype = out_dtype;
         d.err = err;
+        d.wait_ns = current_wait_ns();
         d.stream = reinterpret_cast<cudaStream_t>(stream);
         return from_cuda(launch_tree_wide(d));
     }
@@ -478,6 +479,7 @@ kl_status kl_tree_attention(const kl_shape *shape, const void *q, const void *w_
     a.out = out;
     a.out_dtype = out_dtype;
     a.err = err;
+    a.wait_ns = current_wait_ns();
     a.stream = reinterpret_cast<cudaStream_t>(stream);
     return from_cuda(launch_tree_tc(a));
 }

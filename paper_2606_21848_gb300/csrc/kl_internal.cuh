@@ -142,6 +142,7 @@ struct TreeArgs {
     uint8_t *states;          // [ctas][2] states of kTreeStateBytes
     void *out;                // [total_q][Hq][D]
     kl_dtype out_dtype;
+    uint64_t wait_ns;         // bound of the pipeline's waits (kl_set_wait_timeout_ns)
     int32_t *err;
     cudaStream_t stream;
 };

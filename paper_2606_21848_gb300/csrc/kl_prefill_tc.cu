@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // made batches of short sequences slower, 16 x 16 heads of 100 to 3000 tokens 203 -> 230 us.)
 
     const uint32_t tmem = sm.tmem_base;
-    const Waiter wait{&sm.abort, a.err};
+    const Waiter<> wait{&sm.abort, a.err};
 
     const int qd = warp & 3, hf = warp >> 2;     // softmax warps: lane quarter and group
     const int r = qd * 32 + lane;                // query row = TMEM lane

@@ -12,16 +12,22 @@ constexpr uint64_t kRowsTimeoutNs = 1000000000ull;   // bound of every wait (abo
 
 // Bounded wait. Warp-collective (every lane calls it in uniform control flow and gets the same
 // answer), or by one lane alone (one(): the MMA issuers, whose successful waits must cost little).
-// False when the CTA is aborting or the wait ran out (about 1 s).
+// False when the CTA is aborting or the wait ran out (`limit` ns; kExact, for short limits, polls without
+// suspending the thread, as in kl_decode_tc_kernel.cuh).
+template <bool kExact = false>
 struct Waiter {
     volatile int *abort;
     int32_t *err;
+    uint64_t limit = kRowsTimeoutNs;
+    __device__ bool poll(uint64_t *bar, uint32_t parity) const {
+        return kExact ? ptx::mbar_test_wait(bar, parity) : ptx::mbar_try_wait(bar, parity);
+    }
     __device__ bool slow(uint64_t *bar, uint32_t parity) const {
         const uint64_t t0 = ptx::globaltimer();
         while (true) {
-            if (ptx::mbar_try_wait(bar, parity)) return true;
+            if (poll(bar, parity)) return true;
             if (*abort) return false;
-            if (ptx::globaltimer() - t0 > kRowsTimeoutNs) {
+            if (ptx::globaltimer() - t0 > limit) {
                 *abort = 1;
                 raise_flag(err, KL_FLAG_TIMEOUT);
                 return false;
@@ -29,7 +35,7 @@ struct Waiter {
         }
     }
     __device__ bool one(uint64_t *bar, uint32_t parity) const {
-        return ptx::mbar_try_wait(bar, parity) || slow(bar, parity);
+        return poll(bar, parity) || slow(bar, parity);
     }
     __device__ bool operator()(uint64_t *bar, uint32_t parity) const {
         return __all_sync(0xffffffffu, one(bar, parity));

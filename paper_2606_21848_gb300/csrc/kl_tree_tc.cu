@@ -44,7 +44,7 @@
 // Roles: two groups of four softmax warps (and epilogue), then one warp each for the producer (TMA), the routing
 // and score MMAs (owner of the tensor memory) and the output MMAs, and four helpers, which for Half convert
 // tiles to fp16 ahead of their score MMAs and for Full move O to the sum (by the softmax warps, between a half
-// tile's maximum and its weights, a tile took 5 us). Every wait is bounded (about one second); a
+// tile's maximum and its weights, a tile took 5 us). Every wait is bounded (kl_set_wait_timeout_ns); a
 // wait that runs out raises KL_FLAG_TIMEOUT and every role leaves, drains its copies and MMAs and
 // frees the tensor memory.
 #include <cudaTypedefs.h>
@@ -315,7 +315,8 @@ __device__ __forceinline__ TreeSegment next_segment(const TreeArgs &a, const Tre
 }
 
 // ------------------------------------------------------------------------------- kernel ----
-template <typename C>
+// kExact: a limit of the waits below kExactWaitNs.
+template <typename C, bool kExact>
 __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
     tree_tc_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap wmap,
                    const __grid_constant__ CUtensorMap qmap, const TreeArgs a) {
@@ -359,7 +360,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
         return;
     }
     const int64_t x1 = sm.x1;
-    const Waiter wait{&sm.abort, a.err};
+    const Waiter<kExact> wait{&sm.abort, a.err, a.wait_ns};
 
     // One segment's start for all threads: its block, the barriers, the drafts' parents
     struct Part {
@@ -1215,10 +1216,12 @@ cudaError_t launch_tree_tc(const TreeArgs &a) {
         if (!encode(&qmap, a.q, 3, qdims, qstrides, qbox)) return cudaErrorInvalidValue;
     }
     const bool full = a.out_dtype == KL_FP32;
-    const auto kernel = full ? tree_tc_kernel<Full> : tree_tc_kernel<Half>;
+    const bool exact = a.wait_ns < kExactWaitNs;
+    const auto kernel = full ? exact ? tree_tc_kernel<Full, true> : tree_tc_kernel<Full, false>
+                             : exact ? tree_tc_kernel<Half, true> : tree_tc_kernel<Half, false>;
     const size_t smem = (full ? sizeof(TreeSmem<Full>) : sizeof(TreeSmem<Half>)) + 1024;
-    static PerDeviceOnce once[2];
-    cudaError_t e = once[full].run([&] {
+    static PerDeviceOnce once[4];
+    cudaError_t e = once[2 * full + exact].run([&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     if (e != cudaSuccess) return e;

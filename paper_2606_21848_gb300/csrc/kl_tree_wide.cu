@@ -9,6 +9,16 @@
 #include "kl_decode_wide_kernel.cuh"
 
 namespace kl {
+namespace {
+
+template <int NH, int NG, int T>
+cudaError_t launch_tree(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
+                        const CUtensorMap &qmap) {
+    return la.wait_ns < kExactWaitNs ? launch_kernel_wide<NH, NG, true, true, T>(la, vmap, wmap, qmap)
+                                     : launch_kernel_wide<NH, NG, false, true, T>(la, vmap, wmap, qmap);
+}
+
+}  // namespace
 
 cudaError_t launch_tree_wide(const DecodeArgs &a) {
     DecodeArgs la = a;
@@ -56,11 +66,9 @@ cudaError_t launch_tree_wide(const DecodeArgs &a) {
             return cudaErrorInvalidValue;
     }
     if (fp32)
-        return two_per_sm ? launch_kernel_wide<16, 1, false, true, 3>(la, vmap, wmap, qmap)
-                          : launch_kernel_wide<16, 2, false, true, 3>(la, vmap, wmap, qmap);
-    if (w32) return launch_kernel_wide<32, 2, false, true>(la, vmap, wmap, qmap);
-    return two_per_sm ? launch_kernel_wide<16, 1, false, true>(la, vmap, wmap, qmap)
-                      : launch_kernel_wide<16, 2, false, true>(la, vmap, wmap, qmap);
+        return two_per_sm ? launch_tree<16, 1, 3>(la, vmap, wmap, qmap) : launch_tree<16, 2, 3>(la, vmap, wmap, qmap);
+    if (w32) return launch_tree<32, 2, 2>(la, vmap, wmap, qmap);
+    return two_per_sm ? launch_tree<16, 1, 2>(la, vmap, wmap, qmap) : launch_tree<16, 2, 2>(la, vmap, wmap, qmap);
 }
 
 }  // namespace kl
