@@ -291,8 +291,8 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
  * capability 10.3 (KL_ERR_UNSUPPORTED otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <=
  * max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine: nothing is
  * written); a parent outside [-1, i) raises KL_FLAG_BAD_TREE and counts as -1; a bad page id leaves the
- * affected outputs unspecified. A drafted row that is not finite reaches the drafts that see it
- * alone.
+ * affected outputs unspecified. A drafted row that is not finite makes the outputs of the drafts that see it
+ * NaN, and reaches no others.
  * Precision: scores, softmax and sums in fp32. The operands of the products depend on the form:
  *   fp32 outputs: the routed query and the weights carry 24 significant bits (error about 1e-6);
  *   bf16 outputs with R = (Hq / Hkv) * max_q_len <= 16, or R <= 32 on some sizes: 16 bits;

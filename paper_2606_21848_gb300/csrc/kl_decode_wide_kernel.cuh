@@ -621,6 +621,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             const bool past = t >= nvalid;               // a token past the end: weight 0
             const bool drafts_here = kTree && t_begin + i * kTile + nvalid > base;
             const uint32_t hidden = drafts_here ? blind(t_begin + i * kTile) : 0;
+            bool bad = false;                            // kTree: the thread's token is a draft that is not finite
             bool ready = carried && wait(&sm.s_full[sb], (k >> 1) & 1);
             // the weights against the current references, 8 heads at a time
             float p[KH];
@@ -648,6 +649,21 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                     }
                 }
                 if (drafts_here) {
+                    // A drafted row that is not finite, which not every row sees, becomes zeros for the output
+                    // MMAs, and those who see it get NaN (their scores may be -inf). Both warps of the lane quarter
+                    // look at all of it, ahead of the group's barrier; each then clears a half.
+                    if (wait(&sm.full[(i + ro) % NS], ((i + ro) / NS) & 1) && !past &&
+                        t_begin + i * kTile + t >= base) {
+                        const uint4 *row = reinterpret_cast<const uint4 *>(sm.tiles[(i + ro) % NS] + t * 128);
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) {
+                            const uint4 x = row[(c >> 3) * (kHalfBytes / 16) + ((c + lane) & 7)];
+                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+                        }
+                    }
                     pmax = 0.f;
 #pragma unroll
                     for (int e = 0; e < KH; ++e) {
@@ -736,6 +752,10 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&sm.s_empty[sb]);
+            if (kTree && bad)
+#pragma unroll
+                for (int e = 0; e < KH; ++e)
+                    if (!(hidden >> e & 1)) p[e] = NAN;
             // P^T row of token t, this warp's heads, hi and lo (formed before the wait: the MMAs that
             // read the weight buffer are still running)
             uint32_t ph[KH / 2], pl[KH / 2], pm[T == 3 ? KH / 2 : 1];
@@ -779,27 +799,10 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 }
                 // rows past the end inside the last 16-token MMA step must be finite: zero them
                 // (each of the lane quarter's two warps one 64-dim half)
-                // (kTree: so are drafted rows that are not finite, which not every row sees: a row that does
-                // has a NaN score)
                 if (nvalid < kTile || drafts_here) {
                     const int st = (i + ro) % NS;
                     carried = wait(&sm.full[st], ((i + ro) / NS) & 1);
-                    if (drafts_here && carried && !past && t_begin + i * kTile + t >= base) {
-                        uint4 *z = reinterpret_cast<uint4 *>(sm.tiles[st] + hs * kHalfBytes + t * 128);
-                        bool bad = false;
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            const uint4 x = z[c];
-                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-                        }
-                        if (bad)
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) z[c] = make_uint4(0, 0, 0, 0);
-                    }
-                    if (carried && past && t < ((nvalid + 15) & ~15)) {
+                    if (carried && (bad || (past && t < ((nvalid + 15) & ~15)))) {
                         uint4 *z = reinterpret_cast<uint4 *>(sm.tiles[st] + hs * kHalfBytes + t * 128);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) z[c] = make_uint4(0, 0, 0, 0);

@@ -131,7 +131,7 @@ struct __align__(1024) TreeSmem {
                                // lsum[1] holds half tile 1's maxima for the first reference
     float fref[kBM];           // Full: the references of `sum`
     int32_t parent[KL_TREE_MAX_DRAFTS];
-    unsigned int over[KL_TREE_MAX_DRAFTS / 32];   // Half: drafts with a finite value beyond fp16's range
+    unsigned int over[KL_TREE_MAX_DRAFTS / 32];   // drafts that are not finite (Half: as fp16)
     TreeSegment seg[2];        // this segment and the next
     int64_t warp_tiles[Warps<C>::kThreads / 32];
     int warp_units[Warps<C>::kThreads / 32];
@@ -812,8 +812,8 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                 ptx::tc_fence_after();
                 if constexpr (!C::kFp16) {
                     // Rows that not every draft sees must not reach the others through 0 * NaN: a row past the
-                    // sequence's end, or a drafted one that is not finite, becomes zeros for the output MMAs
-                    // (the score MMAs have read it: a draft that sees it has a NaN score).
+                    // sequence's end, or a drafted one that is not finite, becomes zeros for the output MMAs; a
+                    // draft that sees such a row gets NaN by its bit in `over` (its score may be -inf).
                     const int ring = (u >> 1) + ro;
                     if (drafts_here) {
                         okl = wait(&sm.bar.full[(u >> 1) % kStages], ((u >> 1) / kStages) & 1);
@@ -826,15 +826,16 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                         if (vt < base) continue;
                         const uint32_t v_s = ptx::smem_addr(sm.tiles[ring % kStages]) + (i >> 6) * kHalfBytes +
                                              ((u & 1) * kBS + (i & 63)) * 128;
-                        bool zero = vt >= L;
+                        bool bad = false;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
                             uint32_t v[4];
                             ld_shared_v4(v_s + ((c + lane) & 7) * 16, v);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) zero |= not_finite(v[e]);
+                            for (int e = 0; e < 4; ++e) bad |= not_finite(v[e]);
                         }
-                        if (zero)
+                        if (bad && vt < L) atomicOr(&sm.over[(vt - base) >> 5], 1u << ((vt - base) & 31));
+                        if (bad || vt >= L)
 #pragma unroll
                             for (int c = 0; c < 8; ++c) st_shared_v4(v_s + c * 16, 0u, 0u, 0u, 0u);
                     }
@@ -1002,7 +1003,7 @@ __global__ void __launch_bounds__(Warps<C>::kThreads, 1)
                     w1 = m1 == -INFINITY ? 0.f : ptx::ex2(m1 - m_fin);
                 }
                 float lt = w0 * sm.lsum[0][r] + w1 * sm.lsum[1][r];
-                if (C::kFp16 && has_drafts) {
+                if (has_drafts) {
                     const uint64_t o0 = sm.over[0] | (uint64_t)sm.over[1] << 32;
                     const uint64_t o1 = sm.over[2] | (uint64_t)sm.over[3] << 32;
                     if (o0 | o1) {
