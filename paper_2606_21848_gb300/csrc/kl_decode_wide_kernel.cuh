@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         drafts = end - drafts0;
         G = min(NH, drafts * geo.G - row0);
         if (drafts0 < 0 || drafts < 0 || end > a.tree.total_q || drafts > a.tree.max_q || L_raw < drafts) L_raw = -1;
-        else if (G <= 0) L_raw = min(L_raw, 0);          // (no rows: an empty run)
+        else if (G <= 0 && L_raw <= geo.max_pages * geo.P) L_raw = 0;    // (no rows: an empty run)
     }
     const int pos_raw = a.v_new ? a.positions[b] : -1;
     const int t_begin = split0 * geo.chunk;
