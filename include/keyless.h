@@ -133,8 +133,9 @@ kl_status kl_append_v(const kl_shape *shape, const void *v_new, const int32_t *b
  * of them (larger shapes extend it), where no split state is ever written, so the workspace
  * serves any sequence of calls and shapes -- batch sizes and split counts that change from
  * call to call included -- except after a call that raised KL_FLAG_TIMEOUT, which may leave
- * counters behind, or a switch from a shape with more than 16384 counters: zero the workspace
- * again then. Calls that share a workspace must not overlap on the GPU.
+ * counters behind, or a switch to or from a shape with more than 16384 counters, part of which lie
+ * where other calls keep states: zero the workspace again then. (kl_tree_attention and
+ * kl_token_logprobs never use more.) Calls that share a workspace must not overlap on the GPU.
  */
 size_t kl_decode_workspace_size(const kl_shape *shape, int32_t num_splits);
 
@@ -288,8 +289,8 @@ size_t kl_tree_workspace_size(const kl_shape *shape, int32_t total_q, int32_t ma
  * kl_decode_attention; num_splits: the parts that a sequence is cut into at most (0: chosen from the
  * lengths and the GPU). Workspace: kl_tree_workspace_size bytes of the same arguments, 256-byte aligned.
  * One launch, or two where sequences may be cut. head_dim 128, page size 16, 32, 64 or 128, compute
- * capability 10.3 (KL_ERR_UNSUPPORTED otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <=
- * max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine: nothing is
+ * capability 10.3 (KL_ERR_UNSUPPORTED otherwise). A length that breaks 0 <= n_b <= min(max_q_len,
+ * seq_lens[b]) or seq_lens[b] <= max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine: nothing is
  * written); a parent outside [-1, i) raises KL_FLAG_BAD_TREE and counts as -1; a bad page id leaves the
  * affected outputs unspecified. A drafted row that is not finite makes the outputs of the drafts that see it
  * NaN, and reaches no others.

@@ -38,9 +38,10 @@
 // Each wait is bounded as in kl_decode_tc_kernel.cuh.
 //
 // kTree: the verification step's rows (kl_tree_attention with at most 32 rows per value head): the "heads" of
-// a CTA are a block of the (draft, head) rows of one sequence and value head, row n = draft n / G with head n % G, and
-// a tile that holds drafts gives weight 0 to the rows that do not see a token. W^R per query head: NH = 16. T = 3 (kTree, fp32 outputs): query and weights of three bf16 terms, N = 3 NH columns; the
-// terms' products meet in fp32, rounded to nearest.
+// a CTA are a block of the (draft, head) rows of one sequence and value head, row n = draft n / G with head
+// n % G, and a tile that holds drafts gives weight 0 to the rows that do not see a token. W^R per query head:
+// NH = 16. T = 3 (kTree, fp32 outputs): query and weights of three bf16 terms, N = 3 NH columns; the terms'
+// products meet in fp32, rounded to nearest.
 #pragma once
 
 #include "kl_decode_tc_kernel.cuh"
@@ -621,7 +622,24 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             const bool past = t >= nvalid;               // a token past the end: weight 0
             const bool drafts_here = kTree && t_begin + i * kTile + nvalid > base;
             const uint32_t hidden = drafts_here ? blind(t_begin + i * kTile) : 0;
-            bool bad = false;                            // kTree: the thread's token is a draft that is not finite
+            // A drafted row that is not finite, which not every row sees, becomes zeros for the output MMAs, and
+            // those who see it get NaN (their scores may be -inf). Both warps of the lane quarter look at all of
+            // it while the scores are on their way; behind the group's barrier each clears a half.
+            bool bad = false;
+            if (drafts_here && carried && wait(&sm.full[(i + ro) % NS], ((i + ro) / NS) & 1) && !past &&
+                t_begin + i * kTile + t >= base) {
+                // (an exponent of all ones, plus one, sets the bit above it; a short loop, since its instructions
+                // are fetched for this tile alone)
+                const uint4 *row = reinterpret_cast<const uint4 *>(sm.tiles[(i + ro) % NS] + t * 128);
+                uint32_t all = 0;
+#pragma unroll 4
+                for (int c = 0; c < 16; ++c) {
+                    const uint4 x = row[(c >> 3) * (kHalfBytes / 16) + ((c + lane) & 7)];
+                    all |= ((x.x & 0x7f807f80u) + 0x800080u) | ((x.y & 0x7f807f80u) + 0x800080u) |
+                           ((x.z & 0x7f807f80u) + 0x800080u) | ((x.w & 0x7f807f80u) + 0x800080u);
+                }
+                bad = (all & 0x80008000u) != 0;
+            }
             bool ready = carried && wait(&sm.s_full[sb], (k >> 1) & 1);
             // the weights against the current references, 8 heads at a time
             float p[KH];
@@ -649,21 +667,6 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                     }
                 }
                 if (drafts_here) {
-                    // A drafted row that is not finite, which not every row sees, becomes zeros for the output
-                    // MMAs, and those who see it get NaN (their scores may be -inf). Both warps of the lane quarter
-                    // look at all of it, ahead of the group's barrier; each then clears a half.
-                    if (wait(&sm.full[(i + ro) % NS], ((i + ro) / NS) & 1) && !past &&
-                        t_begin + i * kTile + t >= base) {
-                        const uint4 *row = reinterpret_cast<const uint4 *>(sm.tiles[(i + ro) % NS] + t * 128);
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) {
-                            const uint4 x = row[(c >> 3) * (kHalfBytes / 16) + ((c + lane) & 7)];
-                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-                        }
-                    }
                     pmax = 0.f;
 #pragma unroll
                     for (int e = 0; e < KH; ++e) {
@@ -752,7 +755,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&sm.s_empty[sb]);
-            if (kTree && bad)
+            if (drafts_here && bad)
 #pragma unroll
                 for (int e = 0; e < KH; ++e)
                     if (!(hidden >> e & 1)) p[e] = NAN;
@@ -802,7 +805,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 if (nvalid < kTile || drafts_here) {
                     const int st = (i + ro) % NS;
                     carried = wait(&sm.full[st], ((i + ro) / NS) & 1);
-                    if (carried && (bad || (past && t < ((nvalid + 15) & ~15)))) {
+                    if (carried && ((drafts_here && bad) || (past && t < ((nvalid + 15) & ~15)))) {
                         uint4 *z = reinterpret_cast<uint4 *>(sm.tiles[st] + hs * kHalfBytes + t * 128);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) z[c] = make_uint4(0, 0, 0, 0);
