@@ -22,9 +22,9 @@
 // with a vector for every thread, of the ceil(top / w)-th largest maximum) and (the largest over all warps of the
 // top-th).
 //
-// Measured: 2048 rows of 151936 bf16 logits, no alternatives, 100 us (6200 GB/s, 0.91 of a copy's); 512 rows of
-// 128256 with the 8 largest 39.6 us (3300 GB/s: 1.1 runs per row, whose selections' steps, some 4 us a row, do
-// not overlap within a CTA); 96 rows of 50257 fp32 logits with the 20 largest 16.4 us, and one row of 32000 7.9 us
+// Measured: 2048 rows of 151936 bf16 logits, no alternatives, 102 us (6100 GB/s, 0.90 of a copy's); 512 rows of
+// 128256 with the 8 largest 40 us (3300 GB/s: 1.1 runs per row, whose selections' steps, some 4 us a row, do
+// not overlap within a CTA); 96 rows of 50257 fp32 logits with the 20 largest 18 us, and one row of 32000 8.3 us
 // (latency: first copy 1, first selection 2, further chunks 3, ranking 1.3, the join of a row's parts 4).
 #include <float.h>
 #include <limits.h>

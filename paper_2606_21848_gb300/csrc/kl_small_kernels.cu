@@ -39,8 +39,8 @@ __global__ void __launch_bounds__(128) append_kernel(int Hkv, int D, int P, int 
 // row L - n + j. One CTA per sequence (which may also replace its own length), thread = 16-byte chunk of a
 // (head, row). A path increases, so path[j] >= j: a row is written only after the rows that the same
 // thread read in this batch and in all later ones have a higher position. kMoves loads are in flight.
-// 8 sequences of 4096 tokens, 8 heads, paths of up to 8: 8.4 us a call; 256 sequences, paths of up to 32: 10.4 us
-// (8 MB at most; the chain length -> path -> page -> row -> store of dependent accesses).
+// 8 sequences of 4096 tokens, 8 heads, paths of up to 8: 8 us a call; 256 sequences, paths of up to 32: 9.3 to
+// 11.5 us, by the host (8 MB at most; the chain length -> path -> page -> row -> store of dependent accesses).
 constexpr int kMoves = 8;
 
 __global__ void __launch_bounds__(256) tree_commit_kernel(int Hkv, int D, int P, int num_pages, int max_pages,

@@ -18,10 +18,10 @@ struct TreePlan {
 
 constexpr int kTreeRows = 128;      // rows of a block
 constexpr int kTreeTile = 128;      // cache rows of a tile
-// A part costs a start (about 5 us), a state and the merge (3 to 5 us). A tile takes 1 us with bf16 outputs, 2.7
-// with fp32 outputs. Cuts fall on multiples of kTreeCut tiles. (32 / 8 heads, bf16: one sequence of 4096 tokens,
-// 16 drafts, with runs of 8 tiles and more 23.9 us, of 2 19.4; 4 of 1000 tokens in one part each 16.2, cut 20.5.
-// fp32: one of 4096 tokens, 16 drafts, with runs of 8 tiles 42.9 us, of 4 33.3, of 2 25.8; one of 700, 4
+// A part costs a start (about 5 us), a state and the merge (3 to 5 us). A tile takes 1.2 us with bf16 outputs, 2.7
+// with fp32 outputs. Cuts fall on multiples of kTreeCut tiles. (32 / 8 heads, bf16, at 1 us per tile: one sequence
+// of 4096 tokens, 16 drafts, with runs of 8 tiles and more 23.9 us, of 2 19.4; 4 of 1000 tokens in one part each
+// 16.2, cut 20.5. fp32: one of 4096 tokens, 16 drafts, with runs of 8 tiles 42.9 us, of 4 33.3, of 2 25.8; one of 700, 4
 // drafts, in one part 24.3, cut 22.8; 64 of 1000 114 and 117.)
 constexpr int kTreeCut = 2, kTreeRun = 2;
 constexpr int kTreeStart = 5, kTreeWhole = 8;
@@ -65,17 +65,17 @@ inline TreePlan plan_tree(int B, int Hkv, int G, int max_q, int64_t max_tokens, 
 // - Two blocks of 16: three terms, or the routing by a W^R per query head, leave no tensor memory for 32 rows. Else
 //   a tile takes a block of 32 0.87 us and one of 16 0.62, but the block of 32 starts 4 us later, so while
 //   every CTA has an SM and few tiles. (bf16, 8 drafts of 32 / 8 heads: one sequence of 300 tokens in two blocks
-//   9.3 us, in one 13.0; of 16384 18.9 and 24.4; of 131072 75.6 and 60.5; 8 of 4096 24.5 and 26.8; 16 of 4096
-//   65 and 35. W^R per query head, in two blocks and in 128 rows: 8 of 4096 25.8 and 36.1, one of 131072 77 and 68,
-//   64 of 1000 92 and 61; fp32 8 of 4096 26.5 and 59.)
+//   9.5 us, in one 13.3; of 131072 78.5 and 60.7; 8 of 4096 25.3 and 26.5; 16 of 4096 45 and 35. W^R per query
+//   head, in two blocks and in 128 rows: 8 of 4096 26.2 and 38.9, one of 131072 80.3 and 78.9, 64 of 1000 72.3 and
+//   69.1; fp32 8 of 4096 26.5 and 59.)
 // - Blocks of 128 rows for many short units, whose starts a persistent CTA pays without a launch wave's rest (8
-//   drafts of 32 / 8 heads in 128 rows and in one block: 64 of 500 tokens 43 and 58 us, of 1000 57 and 69, of 2000
-//   88 and 91, 32 of 1000 31 and 35.5, of 4096 80 and 69).
+//   drafts of 32 / 8 heads in 128 rows and in one block: 64 of 500 tokens 47 and 58 us, of 1000 65.5 and 69.3, of
+//   1500 85.6 and 82.1, of 2000 100 and 93, 32 of 1000 35.0 and 35.7, of 2000 61 and 47).
 inline int tree_wide_blocks(int64_t units, int64_t tiles, int64_t rows, bool fp32, bool per_qh, int64_t sms) {
     if (rows > 32) return 0;
     if (rows <= 16) return 1;
     if (fp32 || (2 * units <= sms && units * tiles <= 16 * sms)) return 2;
-    return per_qh || (units > sms && tiles <= 16) ? 0 : 1;
+    return per_qh || (units > sms && tiles <= 8) ? 0 : 1;
 }
 
 }  // namespace kl

@@ -2,10 +2,10 @@
 // wide decode's kernel (kl_decode_wide_kernel.cuh, kTree): there a tile costs what its 16 or 32 rows cost,
 // where a block of kl_tree_tc.cu costs 128 rows, and the splits merge inside.
 // fp32 outputs take operands of three bf16 terms (24 bits) in the place of two.
-// Measured, 32 / 8 heads: 4 drafts on 700 tokens 9.7 us (13.6 in kl_tree_tc.cu; latency), with fp32 outputs 10.0
-// (22.7); 8 sequences of 4096 tokens, 8 drafts 24.5 us (34.5; HBM 10, the rest the start-up and the splits'
-// merge), fp32 26.5 (59); 64 of 8192, 4 drafts 172 us (6250 GB/s), fp32 197 (520), 8 drafts 223 us (the tile
-// chain of 32 rows); one of 131072, 8 drafts 60 us (HBM 40).
+// Measured, 32 / 8 heads: 4 drafts on 700 tokens 10.3 us (13.6 in kl_tree_tc.cu; latency), with fp32 outputs 10.4
+// (22.7); 8 sequences of 4096 tokens, 8 drafts 25.6 us (37; HBM 10, the rest the start-up and one run of 32 tiles
+// in each of 128 CTAs), fp32 27 (59); 64 of 8192, 4 drafts 176 us (6130 GB/s), fp32 200 (520), 8 drafts 227 us
+// (the tile chain of 32 rows); one of 131072, 8 drafts 61 us (HBM 40).
 #include "kl_decode_wide_kernel.cuh"
 
 namespace kl {
