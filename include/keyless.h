@@ -325,6 +325,116 @@ kl_status kl_tree_commit(const kl_shape *shape, const int32_t *cu_q_lens, const 
                          const int32_t *seq_lens, int32_t *new_lens, void *v_cache, int32_t *err,
                          kl_stream_t stream);
 
+/* ---- A cache that stays bounded while a sequence goes on -----------------------------------------
+ *
+ * Two ways to serve long streams with a cache of fixed size. Either new tokens see a window of the last
+ * tokens and a few first ones (kl_window_attention), so that pages behind the window may be freed. Or the
+ * attention that each cached row receives is added up as decoding goes on (kl_attention_weights), and from
+ * time to time the rows with the least are evicted (kl_evict). The paper has no counterpart: scores and
+ * outputs are those of its decode formula over the tokens that a position sees. */
+
+/* Bytes of device workspace kl_window_attention needs for either type of output (0 on bad arguments). The
+ * contract of kl_decode_workspace_size: zero-filled before its first use, then shared by any sequence of
+ * calls and shapes, decodes included. */
+size_t kl_window_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t window,
+                                int32_t sinks, int32_t num_splits);
+
+/*
+ * Causal attention with a sliding window and first tokens that stay visible (attention sinks): sequence b's
+ * n_b = cu_q_lens[b + 1] - cu_q_lens[b] new tokens are its last n_b cached rows (append them first); row
+ * r = cu_q_lens[b] + i sits at position p = seq_lens[b] - n_b + i and, per query head h,
+ *   q_r = q[r][h] W^R[w(h)],  s_t = scale * <q_r, v_t>,  out[r][h] = sum_t softmax(s)_t v_t
+ * over the tokens t <= p with t < sinks or t > p - window (window >= 1: a position always sees itself;
+ * sinks >= 0). n_b = 1 is the decode step, n_b = seq_lens[b] a whole prompt; a window of the longest sequence
+ * is full causal attention. Pages of which no row is seen by a new token are not read, and their entries in
+ * the block table may be anything.
+ * q, out: [total_q][Hq][D] (q bf16, out of out_dtype); cu_q_lens: [B + 1] int32 on the device,
+ * non-decreasing from 0; max_q_len: a host-side bound on every n_b (it chooses the kernel's blocks: a tight
+ * one is faster); w_r (NULL: q is the composed query), v_cache, block_table, seq_lens, num_splits as in
+ * kl_tree_attention. Workspace: kl_window_workspace_size bytes of the same arguments, 256-byte aligned. One
+ * launch. head_dim 128, page size 16, 32, 64 or 128, compute capability
+ * 10.3 (KL_ERR_UNSUPPORTED otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or
+ * seq_lens[b] <= max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine:
+ * nothing is written); a bad id of a page that is read raises KL_FLAG_BAD_PAGE and leaves the affected
+ * outputs unspecified (they may raise KL_FLAG_RANGE). A row that is not finite makes the outputs of the
+ * positions that see it NaN, and reaches no others.
+ * Precision: scores, softmax and sums in fp32. fp32 outputs: the routed query and the weights carry 24
+ * significant bits (error about 1e-6). bf16 outputs with R = (Hq / Hkv) * max_q_len <= 32: 16 bits. Other bf16
+ * outputs as in kl_prefill_attention: a query of 16 bits, weights and cached values in fp16; there a cached
+ * value of magnitude 65536 or more counts as not finite, and a non-finite output raises KL_FLAG_RANGE. (fp32
+ * outputs are computed in blocks of 16 rows: long chunks take several times as long as with bf16 outputs.)
+ */
+kl_status kl_window_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
+                              const int32_t *block_table, const int32_t *seq_lens,
+                              const int32_t *cu_q_lens, int32_t total_q, int32_t max_q_len, int32_t window,
+                              int32_t sinks, int32_t num_splits, void *out, kl_dtype out_dtype,
+                              void *workspace, size_t workspace_bytes, int32_t *err, kl_stream_t stream);
+
+/* Most new tokens per sequence of kl_attention_weights. */
+#define KL_WEIGHTS_MAX_ROWS 128
+
+/* Bytes of device workspace kl_attention_weights needs (0 on bad arguments): the contract of
+ * kl_decode_workspace_size. It holds the scores, 4 bytes for each row of a group and cached token. */
+size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len,
+                                 int32_t weights_stride, int32_t num_splits);
+
+/*
+ * Causal attention of a sequence's last rows that also adds up the weight each cached row receives:
+ * out as kl_window_attention gives it with a window of the longest sequence, and for every sequence b, value
+ * head g and token t < seq_lens[b], with a = softmax(s) of each row,
+ *   new_weights[b][g][t] = decay * weights[b][g][t] + sum over the n_b rows and the heads h of g of a_t
+ * (0 for the tokens behind a row's position). decay: finite and >= 0; with 0 the old weights are not read (and
+ * may be NULL). weights, new_weights: [B][Hkv][weights_stride] fp32, dense; they may be the same.
+ * Entries from seq_lens[b] on are neither read nor written; the old weight of a token that is new with this
+ * call has to be there (0). A sequence with n_b = 0 gets decay * weights. A longer chunk goes in pieces of
+ * KL_WEIGHTS_MAX_ROWS with seq_lens of their own, decay 1 from the second on.
+ * max_q_len <= KL_WEIGHTS_MAX_ROWS (KL_ERR_UNSUPPORTED otherwise); a sequence of more than weights_stride tokens
+ * raises KL_FLAG_BAD_LENGTH and is skipped, like those of kl_window_attention; a bad page leaves the
+ * sequence's outputs and weights unspecified. A row that is not finite makes the outputs of the positions
+ * that see it NaN, and where their scores are not finite the weights that they add as well. Other arguments,
+ * shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every run. Two
+ * launches. Query, weights and sums carry 24 significant bits for either type of output. Workspace:
+ * kl_weights_workspace_size bytes of the same arguments, 256-byte aligned.
+ */
+kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
+                               const int32_t *block_table, const int32_t *seq_lens,
+                               const int32_t *cu_q_lens, int32_t total_q, int32_t max_q_len,
+                               const float *weights, int32_t weights_stride, float decay, float *new_weights,
+                               int32_t num_splits, void *out, kl_dtype out_dtype, void *workspace,
+                               size_t workspace_bytes, int32_t *err, kl_stream_t stream);
+
+/* Longest sequence of kl_evict. */
+#define KL_EVICT_MAX_TOKENS 393216
+
+/* Bytes of device workspace kl_evict needs (0 on bad arguments): the contract of kl_decode_workspace_size. */
+size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, int32_t budget);
+
+/*
+ * Evict the rows with the least weight: of every sequence b of more than `budget` rows each value head g keeps
+ * the first `sinks` rows, the last `recent` and, of those between, the ones with the largest weights[b][g][t]
+ * (ties: the lowest index; negative weights and NaN count as 0), `budget` in all; 1 <= budget, 0 <= sinks,
+ * 0 <= recent, sinks + recent <= budget (KL_ERR_INVALID_ARG otherwise). A sequence of at most `budget` rows
+ * keeps them all. With t_0 < t_1 < ... the rows that stay and m = min(seq_lens[b], budget) their number,
+ *   row t_j of value head g -> row j of value head g, through new_block_table
+ *   kept[b][g][j] = t_j,  new_weights[b][g][j] = weights[b][g][t_j]    (j < m)
+ *   kept[b][g][j] = -1 (m <= j < budget),  new_weights[b][g][t] = 0 (m <= t < seq_lens[b]),  new_lens[b] = m
+ * and entries of new_weights from seq_lens[b] on are not written. weights, new_weights:
+ * [B][Hkv][weights_stride] fp32; kept: [B][Hkv][budget] int32; new_lens: [B] int32; new_weights may be weights
+ * and new_lens may be seq_lens. block_table and new_block_table: [B][max_pages_per_seq]; page i of a sequence's
+ * new table is its page i (rows then move in place; new_block_table may be block_table) or a page that no
+ * sequence of the call reads. A page that is written must belong to one sequence alone. head_dim 64 or 128, any
+ * page size. min(max_pages_per_seq * P, weights_stride) at most KL_EVICT_MAX_TOKENS (KL_ERR_UNSUPPORTED). A
+ * sequence whose length is negative, or more than weights_stride or max_pages_per_seq * P
+ * (KL_FLAG_BAD_LENGTH), or one of whose pages, old or new, lies outside the pool (KL_FLAG_BAD_PAGE) is
+ * left as it is, its entries of all outputs included. Two launches. Workspace: kl_evict_workspace_size bytes,
+ * 256-byte aligned.
+ */
+kl_status kl_evict(const kl_shape *shape, const float *weights, int32_t weights_stride, int32_t budget,
+                   int32_t sinks, int32_t recent, const int32_t *block_table, const int32_t *seq_lens,
+                   const int32_t *new_block_table, void *v_cache, float *new_weights, int32_t *kept,
+                   int32_t *new_lens, void *workspace, size_t workspace_bytes, int32_t *err,
+                   kl_stream_t stream);
+
 /* Most alternatives per row of kl_token_logprobs. */
 #define KL_LOGPROBS_MAX_TOP 32
 
@@ -523,7 +633,8 @@ int32_t kl_decode_kernel_available(const kl_shape *shape, int32_t kernel, int32_
  * undefined, and a workspace it used must be zero-filled again before the next call. This sets
  * that limit, in nanoseconds, for every decode launched afterwards by kl_decode_attention(_ex),
  * kl_decode_step, kl_standard_decode, kl_decode_attention_noalloc, the latent decodes and the FP8
- * decodes, and in the same way for kl_tree_attention and for the waits of kl_token_logprobs for its copies,
+ * decodes, and in the same way for kl_tree_attention, for kl_attention_weights and kl_window_attention (but its bf16 outputs
+ * with R > 32) and for the waits of kl_token_logprobs for its copies,
  * process-wide; 0 restores the default. Returns the limit in force before the call. A
  * small value makes the waits run out on purpose: this is how the timeout path is tested. The
  * paper has no counterpart.

@@ -22,4 +22,7 @@ from ._lib import (  # noqa: F401
     KL_FLAG_BAD_TOKEN, KL_FLAG_BAD_TREE, KL_LOGPROBS_MAX_TOP, KL_TREE_MAX_DRAFTS,
     kl_logprobs_workspace_size, kl_token_logprobs, kl_tree_attention, kl_tree_commit,
     kl_tree_workspace_size,
+    KL_EVICT_MAX_TOKENS, KL_WEIGHTS_MAX_ROWS,
+    kl_attention_weights, kl_evict, kl_evict_workspace_size, kl_weights_workspace_size, kl_window_attention,
+    kl_window_workspace_size,
 )

@@ -24,6 +24,7 @@ KL_FLAG_BAD_PAGE, KL_FLAG_BAD_POSITION, KL_FLAG_BAD_LENGTH, KL_FLAG_TIMEOUT, KL_
 KL_FLAG_BAD_TREE, KL_FLAG_BAD_TOKEN = 32, 64
 KL_NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024
 KL_TREE_MAX_DRAFTS, KL_LOGPROBS_MAX_TOP = 128, 32
+KL_WEIGHTS_MAX_ROWS, KL_EVICT_MAX_TOKENS = 128, 393216
 
 HEADER = os.path.join(_build.INCLUDE, "keyless.h")
 
@@ -101,6 +102,12 @@ def load() -> ctypes.CDLL:
         "kl_tree_workspace_size": ([SH, I32, I32, I32], SZ),
         "kl_tree_attention": ([SH, P, P, P, P, P, P, P, I32, I32, I32, P, I32, P, SZ, P, P], I32),
         "kl_tree_commit": ([SH, P, P, P, I32, P, P, P, P, P, P], I32),
+        "kl_window_workspace_size": ([SH, I32, I32, I32, I32, I32], SZ),
+        "kl_window_attention": ([SH, P, P, P, P, P, P, I32, I32, I32, I32, I32, P, I32, P, SZ, P, P], I32),
+        "kl_weights_workspace_size": ([SH, I32, I32, I32, I32], SZ),
+        "kl_attention_weights": ([SH, P, P, P, P, P, P, I32, I32, P, I32, F32, P, I32, P, I32, P, SZ, P, P], I32),
+        "kl_evict_workspace_size": ([SH, I32, I32], SZ),
+        "kl_evict": ([SH, P, I32, I32, I32, I32, P, P, P, P, P, P, P, P, SZ, P, P], I32),
         "kl_logprobs_workspace_size": ([I32, I32, I32], SZ),
         "kl_token_logprobs": ([I32, I32, I64, P, I32, F32, P, I32, I32, P, P, P, P, P, SZ, P, P], I32),
         "kl_set_wait_timeout_ns": ([ctypes.c_uint64], ctypes.c_uint64),
@@ -339,6 +346,44 @@ def kl_tree_commit(shape, cu_q_lens, path, path_lens, max_path, block_table, seq
     """Move the accepted path's rows to the front of the drafted region and set the new lengths."""
     _check(_call().kl_tree_commit(shape, cu_q_lens, path, path_lens, max_path, block_table, seq_lens,
                                   new_lens, v_cache, err, stream), "kl_tree_commit")
+
+
+def kl_window_workspace_size(shape, total_q, max_q_len, window, sinks, num_splits=0) -> int:
+    return int(load().kl_window_workspace_size(ctypes.byref(shape), total_q, max_q_len, window, sinks, num_splits))
+
+
+def kl_window_attention(shape, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q, max_q_len, window,
+                        sinks, num_splits, out, out_dtype, workspace, err=None, stream=None):
+    """Causal attention with a sliding window and first tokens that stay visible."""
+    _check(_call().kl_window_attention(shape, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q,
+                                       max_q_len, window, sinks, num_splits, out, out_dtype, workspace, err,
+                                       stream), "kl_window_attention")
+
+
+def kl_weights_workspace_size(shape, total_q, max_q_len, weights_stride, num_splits=0) -> int:
+    return int(load().kl_weights_workspace_size(ctypes.byref(shape), total_q, max_q_len, weights_stride,
+                                                num_splits))
+
+
+def kl_attention_weights(shape, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q, max_q_len, weights,
+                         weights_stride, decay, new_weights, num_splits, out, out_dtype, workspace, err=None,
+                         stream=None):
+    """Causal attention that also adds up the weight which each cached row receives."""
+    _check(_call().kl_attention_weights(shape, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q,
+                                        max_q_len, weights, weights_stride, decay, new_weights, num_splits, out,
+                                        out_dtype, workspace, err, stream), "kl_attention_weights")
+
+
+def kl_evict_workspace_size(shape, weights_stride, budget) -> int:
+    return int(load().kl_evict_workspace_size(ctypes.byref(shape), weights_stride, budget))
+
+
+def kl_evict(shape, weights, weights_stride, budget, sinks, recent, block_table, seq_lens, new_block_table,
+             v_cache, new_weights, kept, new_lens, workspace, err=None, stream=None):
+    """Keep the first rows, the last ones and those with the most weight; they move together in their order."""
+    _check(_call().kl_evict(shape, weights, weights_stride, budget, sinks, recent, block_table, seq_lens,
+                            new_block_table, v_cache, new_weights, kept, new_lens, workspace, err, stream),
+           "kl_evict")
 
 
 def kl_logprobs_workspace_size(num_rows, vocab, num_top=0) -> int:

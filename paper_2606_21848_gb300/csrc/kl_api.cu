@@ -7,6 +7,7 @@
 
 #include "kl_internal.cuh"
 #include "kl_tree_plan.cuh"
+#include "kl_window.cuh"
 
 namespace kl {
 
@@ -41,6 +42,29 @@ bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// The splits of up to Lmax tokens for `units` CTAs per split.
+void plan_splits(int32_t num_splits, int64_t Lmax, int64_t units, Geometry *g) {
+    int64_t S = num_splits;
+    if (S == 0) {
+        // As many splits as fit one wave of two CTAs per SM over the (value head, sequence)
+        // units, and splits of at most 8192 tokens so that ragged batches balance; never
+        // below 256 tokens per split.
+        const int64_t slots = 2 * (int64_t)device_sm_count();
+        const int64_t fill = units < slots ? slots / units : 1;
+        const int64_t cap = (Lmax + 8191) / 8192;
+        S = fill > cap ? fill : cap;
+        const int64_t smax = (Lmax + 255) / 256;
+        if (S > smax) S = smax;
+        if (S > kMaxSplits) S = kMaxSplits;
+        if (S < 1) S = 1;
+    }
+    int64_t chunk = (Lmax + S - 1) / S;
+    chunk = (chunk + kChunkQuantum - 1) / kChunkQuantum * kChunkQuantum;
+    g->chunk = (int)chunk;
+    g->S = (int)((Lmax + chunk - 1) / chunk);
+    if (g->S < 1) g->S = 1;
+}
+
 // Validate the shape and resolve the split plan. `num_splits` < 0 skips split planning.
 kl_status resolve(const kl_shape *s, int32_t num_splits, Geometry *g) {
     if (!s) return KL_ERR_INVALID_ARG;
@@ -72,27 +96,8 @@ kl_status resolve(const kl_shape *s, int32_t num_splits, Geometry *g) {
     if (num_splits < 0) return KL_OK;
     if (num_splits > kMaxSplits) return KL_ERR_INVALID_ARG;
 
-    const int64_t Lmax = (int64_t)g->max_pages * g->P;
-    int64_t S = num_splits;
-    if (S == 0) {
-        // As many splits as fit one wave of two CTAs per SM over the (value head, sequence)
-        // units, and splits of at most 8192 tokens so that ragged batches balance; never
-        // below 256 tokens per split.
-        const int64_t units = (int64_t)(g->B > 0 ? g->B : 1) * (g->Hkv / g->vpc) * g->nhb;
-        const int64_t slots = 2 * (int64_t)device_sm_count();
-        const int64_t fill = units < slots ? slots / units : 1;
-        const int64_t cap = (Lmax + 8191) / 8192;
-        S = fill > cap ? fill : cap;
-        const int64_t smax = (Lmax + 255) / 256;
-        if (S > smax) S = smax;
-        if (S > kMaxSplits) S = kMaxSplits;
-        if (S < 1) S = 1;
-    }
-    int64_t chunk = (Lmax + S - 1) / S;
-    chunk = (chunk + kChunkQuantum - 1) / kChunkQuantum * kChunkQuantum;
-    g->chunk = (int)chunk;
-    g->S = (int)((Lmax + chunk - 1) / chunk);
-    if (g->S < 1) g->S = 1;
+    plan_splits(num_splits, (int64_t)g->max_pages * g->P,
+                (int64_t)(g->B > 0 ? g->B : 1) * (g->Hkv / g->vpc) * g->nhb, g);
     return KL_OK;
 }
 
@@ -499,6 +504,263 @@ kl_status kl_tree_commit(const kl_shape *shape, const int32_t *cu_q_lens, const 
     return from_cuda(launch_tree_commit(g, cu_q_lens, path, path_lens, max_path, block_table, seq_lens,
                                         new_lens, static_cast<uint16_t *>(v_cache), err,
                                         reinterpret_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+// What kl_window_attention and kl_attention_weights check alike behind their sizes; with nothing to do *some is
+// false.
+kl_status check_causal(const Geometry &g, const void *q, const void *w_r, const void *v_cache,
+                       const int32_t *block_table, const int32_t *seq_lens, const int32_t *cu_q_lens,
+                       int32_t total_q, int32_t max_q_len, const void *out, bool *some) {
+    *some = false;
+    if (!prefill_tc_supported(g)) return KL_ERR_UNSUPPORTED;
+    if (g.B == 0 || total_q == 0 || max_q_len == 0) return KL_OK;
+    if (!q || !v_cache || !block_table || !seq_lens || !cu_q_lens || !out) return KL_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || (w_r && !aligned(w_r, 16)) || !aligned(v_cache, 16) || !aligned(out, 16))
+        return KL_ERR_INVALID_ARG;
+    *some = true;
+    return KL_OK;
+}
+
+// Blocks of up to NH rows, rpb positions of hp heads each, on the wide decode's kernel.
+void plan_causal(int NH, int32_t max_q_len, DecodeArgs *d) {
+    Geometry &g = d->geo;
+    auto &c = d->causal;
+    c.hp = g.G < NH ? g.G : NH;
+    c.rpb = NH / c.hp < max_q_len ? NH / c.hp : max_q_len;
+    c.nhg = (g.G + c.hp - 1) / c.hp;
+    c.rows = c.hp * c.rpb;
+    g.nhb = c.nhg * ((max_q_len + c.rpb - 1) / c.rpb);
+}
+
+// Splits of blocks of up to Lmax tokens. Whole where the blocks have more counters than the front region that
+// every workspace shares.
+void plan_causal_splits(int32_t num_splits, int64_t Lmax, Geometry *g) {
+    const int64_t ctas = (int64_t)(g->B > 0 ? g->B : 1) * g->Hkv * g->nhb;
+    plan_splits(ctas > (int64_t)kCounterFloor ? 1 : num_splits, Lmax, ctas, g);
+}
+
+// A kl_window_attention call: on the wide decode's kernel (d), or on the prefill's, which needs no workspace.
+struct WindowPlan {
+    bool wide;
+    DecodeArgs d;
+    SharedLayout w;
+};
+kl_status plan_window_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t window, int32_t sinks,
+                           int32_t num_splits, bool fp32, WindowPlan *c) {
+    Geometry &g = c->d.geo;
+    const kl_status st = resolve(shape, -1, &g);
+    if (st != KL_OK) return st;
+    if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits || window < 1 || sinks < 0)
+        return KL_ERR_INVALID_ARG;
+    const int64_t longest = (int64_t)g.max_pages * g.P;
+    c->d.causal.window = window < longest ? window : (int)longest;
+    c->d.causal.sinks = sinks < longest ? sinks : (int)longest;
+    const int max_q = max_q_len > 0 ? (max_q_len < longest ? max_q_len : (int)longest) : 1;
+    const int64_t units = (int64_t)g.B * g.Hkv, rows = (int64_t)g.G * max_q;
+    const int NH = window_rows(rows, fp32, g.wr_per_qh != 0);
+    c->wide = NH > 0;
+    if (!c->wide) {
+        c->w.total = 0;
+        return KL_OK;
+    }
+    plan_causal(NH, max_q, &c->d);
+    plan_causal_splits(num_splits, window_line(c->d.causal.rpb, c->d.causal.window, c->d.causal.sinks, longest), &g);
+    const size_t state_rows = (size_t)units * g.nhb * NH * g.S;
+    c->w = shared_layout((size_t)units * g.nhb, state_rows * g.D * sizeof(float), state_rows * 2 * sizeof(float));
+    return KL_OK;
+}
+
+// The geometry, layout and workspace of a kl_attention_weights call; the scores lie behind the runs' {maximum, sum}
+// in the last region.
+struct WeightsPlan {
+    DecodeArgs d;
+    SharedLayout w;
+    size_t stats, scores;
+};
+kl_status plan_weights_call(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t weights_stride,
+                            int32_t num_splits, WeightsPlan *c) {
+    Geometry &g = c->d.geo;
+    const kl_status st = resolve(shape, -1, &g);
+    if (st != KL_OK) return st;
+    if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits || weights_stride < 1)
+        return KL_ERR_INVALID_ARG;
+    if (max_q_len > KL_WEIGHTS_MAX_ROWS) return KL_ERR_UNSUPPORTED;
+    const int64_t tokens = (int64_t)g.max_pages * g.P, longest = tokens < weights_stride ? tokens : weights_stride;
+    const int64_t units = (int64_t)g.B * g.Hkv;
+    plan_causal(16, max_q_len > 0 ? max_q_len : 1, &c->d);
+    plan_causal_splits(num_splits, longest, &g);
+    c->d.causal.stride = weights_stride;
+    c->d.causal.pitch = (longest + 31) / 32 * 32;
+    const size_t blocks = (size_t)units * g.nhb, rows = blocks * 16 * g.S;
+    c->stats = round_up(rows * 2 * sizeof(float), 256);
+    c->scores = 2 * c->stats;
+    c->w = shared_layout(blocks, rows * g.D * sizeof(float),
+                         c->scores + blocks * c->d.causal.rows * c->d.causal.pitch * sizeof(float));
+    return KL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kl_window_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t window,
+                                int32_t sinks, int32_t num_splits) {
+    size_t most = 0;
+    for (int fp32 = 0; fp32 < 2; ++fp32) {
+        WindowPlan c{};
+        if (plan_window_call(shape, total_q, max_q_len, window, sinks, num_splits, fp32 != 0, &c) != KL_OK) return 0;
+        if (c.w.total > most) most = c.w.total;
+    }
+    return most;
+}
+
+kl_status kl_window_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
+                              const int32_t *block_table, const int32_t *seq_lens, const int32_t *cu_q_lens,
+                              int32_t total_q, int32_t max_q_len, int32_t window, int32_t sinks, int32_t num_splits,
+                              void *out, kl_dtype out_dtype, void *workspace, size_t workspace_bytes, int32_t *err,
+                              kl_stream_t stream) {
+    WindowPlan c{};
+    bool some;
+    if (out_dtype != KL_BF16 && out_dtype != KL_FP32) return KL_ERR_INVALID_ARG;
+    kl_status st = plan_window_call(shape, total_q, max_q_len, window, sinks, num_splits, out_dtype == KL_FP32, &c);
+    // (blocks of 128 positions and more are the prefill's grid's z extent)
+    if (st == KL_OK && (int64_t)max_q_len > (int64_t)65535 * 128) st = KL_ERR_UNSUPPORTED;
+    if (st == KL_OK)
+        st = check_causal(c.d.geo, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q, max_q_len, out, &some);
+    if (st != KL_OK || !some) return st;
+    if (c.w.total > 0 && (!workspace || workspace_bytes < c.w.total || !aligned(workspace, 256)))
+        return KL_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    if (c.wide) {
+        DecodeArgs &d = c.d;
+        d.q = static_cast<const uint16_t *>(q);
+        d.w_r = static_cast<const uint16_t *>(w_r);
+        d.v_cache = static_cast<const uint16_t *>(v_cache);
+        d.block_table = block_table;
+        d.seq_lens = seq_lens;
+        d.tree.cu_q = cu_q_lens;
+        d.tree.total_q = total_q;
+        d.tree.max_q = max_q_len;
+        d.counters = reinterpret_cast<unsigned int *>(ws);
+        d.part_o = reinterpret_cast<float *>(ws + c.w.states);
+        d.part_ml = reinterpret_cast<float *>(ws + c.w.extra);
+        d.out = out;
+        d.direct_out = d.geo.S == 1;
+        d.out_dtype = out_dtype;
+        d.err = err;
+        d.wait_ns = current_wait_ns();
+        d.stream = reinterpret_cast<cudaStream_t>(stream);
+        return from_cuda(launch_window_wide(d));
+    }
+    PrefillArgs a{};
+    a.geo = c.d.geo;
+    a.total_q = total_q;
+    a.max_q = max_q_len;
+    a.window = c.d.causal.window;
+    a.sinks = c.d.causal.sinks;
+    a.q = static_cast<const uint16_t *>(q);
+    a.w_r = static_cast<const uint16_t *>(w_r);
+    a.v_cache = static_cast<const uint16_t *>(v_cache);
+    a.block_table = block_table;
+    a.seq_lens = seq_lens;
+    a.cu_q = cu_q_lens;
+    a.out = out;
+    a.out_dtype = out_dtype;
+    a.err = err;
+    a.stream = reinterpret_cast<cudaStream_t>(stream);
+    return from_cuda(launch_window_tc(a));
+}
+
+size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t weights_stride,
+                                 int32_t num_splits) {
+    WeightsPlan c{};
+    return plan_weights_call(shape, total_q, max_q_len, weights_stride, num_splits, &c) == KL_OK ? c.w.total : 0;
+}
+
+kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
+                               const int32_t *block_table, const int32_t *seq_lens, const int32_t *cu_q_lens,
+                               int32_t total_q, int32_t max_q_len, const float *weights, int32_t weights_stride,
+                               float decay, float *new_weights, int32_t num_splits, void *out, kl_dtype out_dtype,
+                               void *workspace, size_t workspace_bytes, int32_t *err, kl_stream_t stream) {
+    WeightsPlan c{};
+    bool some;
+    if ((out_dtype != KL_BF16 && out_dtype != KL_FP32) || !(decay >= 0.f) || isinf(decay)) return KL_ERR_INVALID_ARG;
+    kl_status st = plan_weights_call(shape, total_q, max_q_len, weights_stride, num_splits, &c);
+    if (st == KL_OK)
+        st = check_causal(c.d.geo, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q, max_q_len, out, &some);
+    if (st != KL_OK || !some) return st;
+    if (!new_weights || (!weights && decay != 0.f) || !aligned(new_weights, 4) || !aligned(weights, 4))
+        return KL_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < c.w.total || !aligned(workspace, 256)) return KL_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    DecodeArgs &d = c.d;
+    d.q = static_cast<const uint16_t *>(q);
+    d.w_r = static_cast<const uint16_t *>(w_r);
+    d.v_cache = static_cast<const uint16_t *>(v_cache);
+    d.block_table = block_table;
+    d.seq_lens = seq_lens;
+    d.tree.cu_q = cu_q_lens;
+    d.tree.total_q = total_q;
+    d.tree.max_q = max_q_len;
+    d.counters = reinterpret_cast<unsigned int *>(ws);
+    d.part_o = reinterpret_cast<float *>(ws + c.w.states);
+    d.part_ml = reinterpret_cast<float *>(ws + c.w.extra);
+    d.causal.stats = reinterpret_cast<float2 *>(ws + c.w.extra + c.stats);
+    d.causal.scores = reinterpret_cast<float *>(ws + c.w.extra + c.scores);
+    d.out = out;
+    d.direct_out = d.geo.S == 1;
+    d.out_dtype = out_dtype;
+    d.err = err;
+    d.wait_ns = current_wait_ns();
+    d.stream = reinterpret_cast<cudaStream_t>(stream);
+    return from_cuda(launch_attention_weights(d, WeightArgs{weights, decay, new_weights}));
+}
+
+size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, int32_t budget) {
+    Geometry g;
+    if (resolve(shape, -1, &g) != KL_OK || weights_stride < 1 || budget < 1) return 0;
+    return shared_layout(0, (size_t)g.B * g.Hkv * kEvictUnitBytes, 0).total;
+}
+
+kl_status kl_evict(const kl_shape *shape, const float *weights, int32_t weights_stride, int32_t budget, int32_t sinks,
+                   int32_t recent, const int32_t *block_table, const int32_t *seq_lens, const int32_t *new_block_table,
+                   void *v_cache, float *new_weights, int32_t *kept, int32_t *new_lens, void *workspace,
+                   size_t workspace_bytes, int32_t *err, kl_stream_t stream) {
+    Geometry g;
+    const kl_status st = resolve(shape, -1, &g);
+    if (st != KL_OK) return st;
+    if (weights_stride < 1 || budget < 1 || sinks < 0 || recent < 0 || sinks > budget - recent)
+        return KL_ERR_INVALID_ARG;
+    const int64_t tokens = (int64_t)g.max_pages * g.P;
+    if ((tokens < weights_stride ? tokens : weights_stride) > KL_EVICT_MAX_TOKENS) return KL_ERR_UNSUPPORTED;
+    if (g.B == 0) return KL_OK;
+    if (!weights || !block_table || !seq_lens || !new_block_table || !v_cache || !new_weights || !kept || !new_lens)
+        return KL_ERR_INVALID_ARG;
+    if (!aligned(v_cache, 16) || !aligned(weights, 4) || !aligned(new_weights, 4)) return KL_ERR_INVALID_ARG;
+    const size_t need = kl_evict_workspace_size(shape, weights_stride, budget);
+    if (!workspace || workspace_bytes < need || !aligned(workspace, 256)) return KL_ERR_WORKSPACE;
+    EvictArgs a{};
+    a.geo = g;
+    a.weights = weights;
+    a.stride = weights_stride;
+    a.budget = budget;
+    a.sinks = sinks;
+    a.recent = recent;
+    a.block_table = block_table;
+    a.new_table = new_block_table;
+    a.seq_lens = seq_lens;
+    a.v_cache = static_cast<uint16_t *>(v_cache);
+    a.new_weights = new_weights;
+    a.kept = kept;
+    a.new_lens = new_lens;
+    a.workspace = static_cast<char *>(workspace) + shared_layout(0, 0, 0).states;
+    a.err = err;
+    a.stream = reinterpret_cast<cudaStream_t>(stream);
+    return from_cuda(launch_evict(a));
 }
 
 }  // extern "C"

@@ -7,8 +7,8 @@ namespace {
 template <int NH, int NG>
 cudaError_t launch_wide(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
                         const CUtensorMap &qmap) {
-    return la.wait_ns < kExactWaitNs ? launch_kernel_wide<NH, NG, true, false>(la, vmap, wmap, qmap)
-                                     : launch_kernel_wide<NH, NG, false, false>(la, vmap, wmap, qmap);
+    return la.wait_ns < kExactWaitNs ? launch_kernel_wide<NH, NG, true, kHeads>(la, vmap, wmap, qmap)
+                                     : launch_kernel_wide<NH, NG, false, kHeads>(la, vmap, wmap, qmap);
 }
 
 }  // namespace

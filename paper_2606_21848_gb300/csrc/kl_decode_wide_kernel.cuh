@@ -42,13 +42,23 @@
 // n % G, and a tile that holds drafts gives weight 0 to the rows that do not see a token. W^R per query head:
 // NH = 16. T = 3 (kTree, fp32 outputs): query and weights of three bf16 terms, N = 3 NH columns; the terms'
 // products meet in fp32, rounded to nearest.
+//
+// kWindow: the rows of consecutive positions (kl_window_attention): a CTA's rows are a block of drafts and heads of
+// its own (a.causal), its runs lie on the line of tiles that the block may see (window_span), and pages without
+// a visible row are not read. A tile with rows that not every position sees gives them weight 0 where they are not
+// seen; those that no position sees become zeros, whatever lies there.
+// kWeights: the same with all tokens before a position visible; the scores are written as well (a.causal.scores),
+// with the run's {maximum, sum} per row, from which kl_attention_weights forms the weights.
 #pragma once
 
 #include "kl_decode_tc_kernel.cuh"
+#include "kl_window.cuh"
 
 namespace kl {
 namespace {
 
+// What the rows of a CTA are.
+enum { kHeads = 0, kForest = 1, kWindow = 2, kWeights = 3 };
 constexpr int kWideGroupThreads = 256;               // 8 compute warps per softmax group
 constexpr uint32_t kBarGroup = 3;                    // + group: vote of one group's warps
 constexpr int kWideMaxRuns = 256;                    // states merged per (b, g, head block)
@@ -172,11 +182,12 @@ __device__ __forceinline__ float warp_max_redux(float f) {
     return __int_as_float(k >= 0 ? k : k ^ 0x7FFFFFFF);
 }
 
-template <int NH, int NG, bool kExact, bool kTree, int T>
+template <int NH, int NG, bool kExact, int kRows, int T>
 __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kCtas)
     decode_wide_kernel(const __grid_constant__ CUtensorMap vmap,
                        const __grid_constant__ CUtensorMap wmap,
                        const __grid_constant__ CUtensorMap qmap, const DecodeArgs a) {
+    constexpr bool kTree = kRows != kHeads, kCausal = kRows >= kWindow;
     using S = WideSmem<NH, NG, T>;
     using W = Wide<NH, NG, T>;
     constexpr int NS = W::kStages, kWideWarps = W::kWarps, kWideComputeThreads = 32 * W::kWarps;
@@ -203,20 +214,25 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     int G = min(NH, geo.G - NH * hb);                    // query heads (rows) of this CTA
-    const int qh0 = g * geo.G + (kTree ? 0 : NH * hb);   // its first query head
-    const int row0 = kTree ? NH * hb : 0;                // kTree: its first row
+    // kCausal: its heads, first of them and first draft; row r is draft m0 + r / hp with head r % hp
+    const int hp = kCausal ? a.causal.hp : geo.G;
+    const int hg = kCausal ? hb % a.causal.nhg * hp : 0, m0 = kCausal ? hb / a.causal.nhg * a.causal.rpb : 0;
+    const int qh0 = g * geo.G + (kCausal ? hg : kTree ? 0 : NH * hb);   // its first query head
+    const int row0 = kTree && !kCausal ? NH * hb : 0;    // kForest: its first row
     // rows of q and out, and of the split states
     auto out_row = [&](int h) -> size_t {
+        if constexpr (kCausal) return (size_t)(drafts0 + m0 + h / hp) * geo.Hq + qh0 + h % hp;
         if constexpr (kTree) return (size_t)(drafts0 + (row0 + h) / geo.G) * geo.Hq + qh0 + (row0 + h) % geo.G;
         return (size_t)b * geo.Hq + qh0 + h;
     };
     const size_t state0 =
-        kTree ? ((size_t)b * geo.Hkv + g) * geo.G * a.tree.max_q + row0 : (size_t)b * geo.Hq + qh0;
+        kCausal ? (((size_t)b * geo.Hkv + g) * geo.nhb + hb) * NH
+        : kTree ? ((size_t)b * geo.Hkv + g) * geo.G * a.tree.max_q + row0 : (size_t)b * geo.Hq + qh0;
     const bool route = a.w_r != nullptr;                 // else q is the composed query
     const bool route_pq = route && geo.wr_per_qh;
     // ring positions of W^R matrices (kTree, per query head: that of head (row0 + r) % G at position r; row n
     // of the CTA takes position n % G's result)
-    const int ro = !route ? 0 : !route_pq ? 1 : kTree ? min(geo.G, NH) : G;
+    const int ro = !route ? 0 : !route_pq ? 1 : kTree ? min(hp, NH) : G;
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) {
@@ -257,32 +273,47 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         drafts0 = a.tree.cu_q[b];
         const int end = a.tree.cu_q[b + 1];
         drafts = end - drafts0;
-        G = min(NH, drafts * geo.G - row0);
+        G = kCausal ? min(hp, geo.G - hg) + (min(a.causal.rpb, drafts - m0) - 1) * hp
+                    : min(NH, drafts * geo.G - row0);
+        if (kCausal && drafts <= m0) G = 0;
         if (drafts0 < 0 || drafts < 0 || end > a.tree.total_q || drafts > a.tree.max_q || L_raw < drafts) L_raw = -1;
+        else if (kRows == kWeights && L_raw > a.causal.stride) L_raw = -1;
         else if (G <= 0 && L_raw <= geo.max_pages * geo.P) L_raw = 0;    // (no rows: an empty run)
     }
+    // kCausal: the block's positions, and the line of tiles that they see
+    const int p0 = L_raw - drafts + m0, p1 = p0 + min(a.causal.rpb, drafts - m0) - 1;
+    const int window = kRows == kWindow ? a.causal.window : INT32_MAX / 2, sinks = kRows == kWindow ? a.causal.sinks : 0;
+    WindowSpan span{0, 0, 0};
+    if (kCausal && L_raw > 0 && L_raw <= geo.max_pages * geo.P) {
+        span = window_span(p0, p1, window, sinks);
+        L_raw = span.len;
+    }
+    // the token of a token of the line, and the page of a page
+    auto token_at = [&](int x) { return kRows == kWindow && x >= span.first ? x + span.shift : x; };
+    auto page_at = [&](int x) { return kRows == kWindow && x * geo.P >= span.first ? x + span.shift / geo.P : x; };
     const int pos_raw = a.v_new ? a.positions[b] : -1;
     const int t_begin = split0 * geo.chunk;
     const int first_page = t_begin / geo.P;
     const int32_t *bt = a.block_table + (size_t)b * geo.max_pages;
     int bt_cur = -1, bt_nxt = -1;
     if (warp == kWideProducer) {
-        if (first_page + lane < geo.max_pages) bt_cur = bt[first_page + lane];
-        if (first_page + 32 + lane < geo.max_pages) bt_nxt = bt[first_page + 32 + lane];
+        const int pa = page_at(first_page + lane), pb = page_at(first_page + 32 + lane);
+        if (pa < geo.max_pages) bt_cur = bt[pa];
+        if (pb < geo.max_pages) bt_nxt = bt[pb];
     }
     // Ring position r < ro: W^R as the MN-major A operand [j half][128 k rows][128 B]; position 0
     // also brings the CTA's query rows, the K-major B operand, into the front of the q_r buffer.
     auto issue_route = [&](int r) {
         const int s = r % NS;
         if (lane == 0) {
-            const int wrow = (!route_pq ? g : qh0 + (kTree ? (row0 + r) % geo.G : r)) * kD;
+            const int wrow = (!route_pq ? g : qh0 + (kCausal ? r : kTree ? (row0 + r) % geo.G : r)) * kD;
             ptx::mbar_arrive_expect_tx(&sm.full[s],
                                        kTileBytes + (r == 0 ? 2u * (uint32_t)geo.qbox * 128u : 0u));
             ptx::tma_load_2d(sm.tiles[s], &wmap, &sm.full[s], 0, wrow);
             ptx::tma_load_2d(sm.tiles[s] + kHalfBytes, &wmap, &sm.full[s], 64, wrow);
             if (r == 0 && kTree) {
-                ptx::tma_load_3d(sm.qr, &qmap, &sm.full[s], 0, qh0, drafts0);
-                ptx::tma_load_3d(sm.qr + kQHalf, &qmap, &sm.full[s], 64, qh0, drafts0);
+                ptx::tma_load_3d(sm.qr, &qmap, &sm.full[s], 0, qh0, drafts0 + m0);
+                ptx::tma_load_3d(sm.qr + kQHalf, &qmap, &sm.full[s], 64, qh0, drafts0 + m0);
             } else if (r == 0) {
                 ptx::tma_load_2d(sm.qr, &qmap, &sm.full[s], 0, b * geo.Hq + qh0);
                 ptx::tma_load_2d(sm.qr + kQHalf, &qmap, &sm.full[s], 64, b * geo.Hq + qh0);
@@ -375,18 +406,23 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             issued = r + 1;
         }
         const int split_pages = end_page - first_page;
+        const int low = p0 - window + 1;                 // kWindow: the first token that the window shows
         int bt_batch = 0;
         for (int i = 0; ok && i < n_tiles; ++i) {
             const int r = i + ro, s = r % NS;
-            const int p0 = i * ppt;                       // first page of the tile in the run
-            if ((p0 >> 5) != bt_batch) {
-                bt_batch = p0 >> 5;
+            const int pt = i * ppt;                       // first page of the tile in the run
+            if ((pt >> 5) != bt_batch) {
+                bt_batch = pt >> 5;
                 bt_cur = bt_nxt;
                 const int q = (bt_batch + 1) * 32 + lane;
-                bt_nxt = q < split_pages ? bt[first_page + q] : -1;
+                bt_nxt = q < split_pages ? bt[page_at(first_page + q)] : -1;
             }
-            const int page = __shfl_sync(0xffffffffu, bt_cur, ((p0 & 31) + lane) & 31);
-            const bool exists = lane < ppt && p0 + lane < split_pages;
+            const int page = __shfl_sync(0xffffffffu, bt_cur, ((pt & 31) + lane) & 31);
+            bool exists = lane < ppt && pt + lane < split_pages;
+            if constexpr (kRows == kWindow) {            // (pages without a visible row may be anyone's by now)
+                const int first = page_at(first_page + pt + lane) * P;
+                exists = exists && (first < sinks || first + P > low);
+            }
             if (r >= NS && !wait(&sm.empty[s], ((r / NS) & 1) ^ 1)) break;
             const bool in_range = exists && page >= 0 && page < geo.num_pages;
             if (exists && !in_range) bad = true;
@@ -520,7 +556,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                     if (route)
                         acc[e] = ptx::tmem_ld1(tmem + lane_base +
                                                (!route_pq ? kColO + h
-                                                : kTree   ? 16 * (h % geo.G) + h
+                                                : kTree   ? 16 * (h % hp) + h
                                                           : 16 * h + (h & 15)));
                     else
                         acc[e] = __uint_as_float((uint32_t)a.q[out_row(h) * kD + t] << 16);
@@ -587,7 +623,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         const int base = L - drafts;
         int parent = -1;
         uint32_t line = 0;
-        if (kTree && t_end > base && lane < drafts) {
+        if (kRows == kForest && t_end > base && lane < drafts) {
             parent = a.tree.parents[drafts0 + lane];
             if (parent < -1 || parent >= lane) {
                 if (warp == 0) raise_flag(a.err, KL_FLAG_BAD_TREE);
@@ -613,6 +649,27 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             }
             return m;
         };
+        // kCausal: the same for the block's positions; and whether none of them sees the token, and not all do
+        auto unseen = [&](int token, bool &none, bool &some) -> uint32_t {
+            const int n = p1 - p0 + 1, d = token - p0;
+            const int lo = max(d, 0), hi = token < sinks ? n : min(n, d + window);   // drafts lo .. hi - 1 see it
+            none = lo >= hi;
+            some = !none && (lo > 0 || hi < n);
+            if (none) return (1u << KH) - 1;
+            uint32_t m = 0;
+            if (some)
+#pragma unroll
+                for (int e = 0; e < KH; ++e) {
+                    const int i = (h0 + e) / hp;
+                    if (i < lo || i >= hi) m |= 1u << e;
+                }
+            return m;
+        };
+        // kWeights: row h0 of the scores
+        float *const scores =
+            kRows == kWeights
+                ? a.causal.scores + ((((size_t)b * geo.Hkv + g) * geo.nhb + hb) * a.causal.rows + h0) * a.causal.pitch
+                : nullptr;
         bool carried = ok;
         ok = true;
         for (int i = grp; i < n_tiles; i += NG) {
@@ -620,14 +677,18 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             const uint32_t sc = tmem + kColS + sb * N + h0 + lane_base;
             const int nvalid = min(kTile, t_end - (t_begin + i * kTile));
             const bool past = t >= nvalid;               // a token past the end: weight 0
-            const bool drafts_here = kTree && t_begin + i * kTile + nvalid > base;
-            const uint32_t hidden = drafts_here ? blind(t_begin + i * kTile) : 0;
+            const int tt = kCausal ? token_at(t_begin + i * kTile) : t_begin + i * kTile;   // the tile's first token
+            const bool drafts_here =
+                kCausal ? tt + nvalid - 1 > p0 || max(tt, sinks) <= min(tt + nvalid - 1, p1 - window)
+                        : kTree && tt + nvalid > base;
+            bool none = false, some = kRows == kForest && tt + t >= base;
+            const uint32_t hidden = !drafts_here ? 0 : kCausal ? unseen(tt + t, none, some) : blind(tt);
             // A drafted row that is not finite, which not every row sees, becomes zeros for the output MMAs, and
             // those who see it get NaN (their scores may be -inf). Both warps of the lane quarter look at all of
             // it while the scores are on their way; behind the group's barrier each clears a half.
             bool bad = false;
             if (drafts_here && carried && wait(&sm.full[(i + ro) % NS], ((i + ro) / NS) & 1) && !past &&
-                t_begin + i * kTile + t >= base) {
+                some) {
                 // (an exponent of all ones, plus one, sets the bit above it; a short loop, since its instructions
                 // are fetched for this tile alone)
                 const uint4 *row = reinterpret_cast<const uint4 *>(sm.tiles[(i + ro) % NS] + t * 128);
@@ -640,6 +701,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 }
                 bad = (all & 0x80008000u) != 0;
             }
+            if constexpr (kCausal) __syncwarp();         // (the lanes part above, and the loads are the warp's)
             bool ready = carried && wait(&sm.s_full[sb], (k >> 1) & 1);
             // the weights against the current references, 8 heads at a time
             float p[KH];
@@ -659,11 +721,21 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                     *reinterpret_cast<float4 *>(m + 4) = *reinterpret_cast<const float4 *>(mref + c + 4);
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
-                        const F2 d = sub2(add2(f2(hi[e], hi[e + 1]), f2(lo[e], lo[e + 1])),
-                                          f2(m[e], m[e + 1]));
+                        const F2 x = add2(f2(hi[e], hi[e + 1]), f2(lo[e], lo[e + 1]));
+                        if constexpr (kRows == kWeights) {
+                            hi[e] = x.x;
+                            hi[e + 1] = x.y;
+                        }
+                        const F2 d = sub2(x, f2(m[e], m[e + 1]));
                         p[c + e] = past ? 0.f : ptx::ex2(d.x);
                         p[c + e + 1] = past ? 0.f : ptx::ex2(d.y);
                         pmax = max3(pmax, p[c + e], p[c + e + 1]);
+                    }
+                    if constexpr (kRows == kWeights) {
+                        if (!past)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (h0 + c + e < G) scores[(size_t)(c + e) * a.causal.pitch + tt + t] = hi[e];
                     }
                 }
                 if (drafts_here) {
@@ -805,7 +877,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 if (nvalid < kTile || drafts_here) {
                     const int st = (i + ro) % NS;
                     carried = wait(&sm.full[st], ((i + ro) / NS) & 1);
-                    if (carried && ((drafts_here && bad) || (past && t < ((nvalid + 15) & ~15)))) {
+                    if (carried && ((drafts_here && (bad || none)) || (past && t < ((nvalid + 15) & ~15)))) {
                         uint4 *z = reinterpret_cast<uint4 *>(sm.tiles[st] + hs * kHalfBytes + t * 128);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) z[c] = make_uint4(0, 0, 0, 0);
@@ -880,6 +952,9 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                     o += w1 * o1[e];
                 }
                 float val = o / lt;
+                if constexpr (kRows == kWeights) {
+                    if (t == 0) a.causal.stats[(state0 + h) * geo.S + cta] = make_float2(M, lt);
+                }
                 if constexpr (kTree) {
                     // a run in which the row sees nothing; and the merge, which leaves out states without a
                     // positive sum, keeps one that a NaN score made NaN
@@ -929,14 +1004,14 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
     }
 }
 
-template <int NH, int NG, bool kExact, bool kTree, int T = 2>
+template <int NH, int NG, bool kExact, int kRows, int T = 2>
 cudaError_t launch_kernel_wide(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
                                const CUtensorMap &qmap) {
     const Geometry &g = la.geo;
     const size_t smem = sizeof(WideSmem<NH, NG, T>);
     static PerDeviceOnce once;
     const cudaError_t e = once.run([&] {
-        return cudaFuncSetAttribute(decode_wide_kernel<NH, NG, kExact, kTree, T>,
+        return cudaFuncSetAttribute(decode_wide_kernel<NH, NG, kExact, kRows, T>,
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     if (e != cudaSuccess) return e;
@@ -946,7 +1021,7 @@ cudaError_t launch_kernel_wide(const DecodeArgs &la, const CUtensorMap &vmap, co
     cfg.dynamicSmemBytes = smem;
     cfg.stream = la.stream;
     const OverlapAttr overlap(cfg);
-    return cudaLaunchKernelEx(&cfg, decode_wide_kernel<NH, NG, kExact, kTree, T>, vmap, wmap, qmap, la);
+    return cudaLaunchKernelEx(&cfg, decode_wide_kernel<NH, NG, kExact, kRows, T>, vmap, wmap, qmap, la);
 }
 
 // Consecutive splits per CTA: the fewest that fit one wave of `slots` CTAs (when the units alone do not fill

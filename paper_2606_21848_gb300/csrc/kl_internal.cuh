@@ -82,6 +82,42 @@ struct DecodeArgs {
         const int32_t *cu_q = nullptr, *parents = nullptr;
         int total_q = 0, max_q = 1;
     } tree;
+    // Its forms for consecutive positions (kl_window_attention, kl_attention_weights; tree.cu_q, total_q and max_q
+    // as above): a block is rpb positions of hp heads, a value head's nhg blocks of heads next to each other.
+    struct {
+        int hp = 1, rpb = 1, nhg = 1;
+        int window = 0, sinks = 0;
+        // kl_attention_weights: the scores times log2 e, [B][Hkv][nhb][rows][pitch], each run's {maximum (of
+        // these), sum}, [B][Hkv][nhb][16][S], and the longest sequence
+        int rows = 1, stride = 0;
+        int64_t pitch = 0;
+        float *scores = nullptr;
+        float2 *stats = nullptr;
+    } causal;
+};
+
+// What kl_attention_weights adds to its attention's arguments.
+struct WeightArgs {
+    const float *weights;     // [B][Hkv][stride]; not read where decay is 0
+    float decay;
+    float *new_weights;       // [B][Hkv][stride]
+};
+
+// Arguments of a kl_evict launch. The workspace holds kEvictUnitBytes for every sequence and value head.
+constexpr int kEvictUnitBytes = 8;
+struct EvictArgs {
+    Geometry geo;             // S and chunk unused
+    const float *weights;     // [B][Hkv][stride]
+    int stride, budget, sinks, recent;
+    const int32_t *block_table, *new_table;
+    const int32_t *seq_lens;
+    uint16_t *v_cache;
+    float *new_weights;       // [B][Hkv][stride]
+    int32_t *kept;            // [B][Hkv][budget]
+    int32_t *new_lens;        // [B]
+    void *workspace;
+    int32_t *err;
+    cudaStream_t stream;
 };
 
 // Arguments of a chunked-prefill launch (kl_prefill_attention). Sequence b's query rows are
@@ -94,6 +130,7 @@ struct PrefillArgs {
     // Layout (set by the launcher, plan_prefill): a block of 128 rows holds hp heads of one value head's group,
     // rpb query rows each; a cluster of cs CTAs splits a block's cache tiles.
     int hp = 1, rpb = 128, cs = 1;
+    int window = 0, sinks = 0;   // kl_window_attention (where w_r may be nullptr: q is the composed query)
     const uint16_t *q;        // [total_q][Hq][D] bf16
     const uint16_t *w_r;      // [Hw][D][D] bf16
     const uint16_t *v_cache;  // [num_pages][Hkv][P][D] bf16
@@ -292,6 +329,12 @@ cudaError_t launch_append_chunk(const Geometry &g, int total_q, int max_q, const
 cudaError_t launch_tree_tc(const TreeArgs &a);
 // The same by the wide decode's kernel (tree_wide_blocks): a.geo with its splits and blocks (nhb), a.tree.
 cudaError_t launch_tree_wide(const DecodeArgs &a);
+// Attention of consecutive positions with a sliding window, on the wide decode's kernel (a.causal) and on the
+// prefill's; with all tokens before a position and each cached row's weight added up.
+cudaError_t launch_window_wide(const DecodeArgs &a);
+cudaError_t launch_window_tc(const PrefillArgs &a);
+cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w);
+cudaError_t launch_evict(const EvictArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
                                const int32_t *path_lens, int max_path, const int32_t *block_table,
                                const int32_t *seq_lens, int32_t *new_lens, uint16_t *v_cache,

@@ -69,12 +69,20 @@
 //              not queue behind the next scores
 // Every wait is bounded (about one second); a wait that runs out raises KL_FLAG_TIMEOUT, makes
 // every role leave its loop, drains outstanding copies and MMAs and frees TMEM.
+//
+// kWindow (kl_window_attention, bf16 outputs of more than 32 rows per value head): the same with a sliding window and
+// first tokens that stay visible. A block's tiles are those that its positions see, laid end to end (window_span), and
+// pages without a visible row are not read. In a half tile that not all positions see entirely, rows that none sees
+// become zeros, whatever lies there; one that some see and that has no finite fp16 form becomes zeros as well, and a
+// bit makes the outputs of those who see it NaN. The query may be composed already (no W^R: the ring starts with
+// the tiles).
 #include <cudaTypedefs.h>
 #include <math.h>
 
 #include "kl_internal.cuh"
 #include "kl_prefill_plan.cuh"
 #include "kl_tc_rows.cuh"
+#include "kl_window.cuh"
 
 namespace kl {
 namespace {
@@ -101,6 +109,12 @@ constexpr uint32_t kColQ = 384;                   // Q_hi: 384 .. 447, Q_lo: 448
 constexpr uint32_t kLoCols = 64;                  // hi -> lo of a packed bf16 operand
 constexpr float kRescaleLog2 = 7.f;
 constexpr uint64_t kTimeoutNs = kRowsTimeoutNs;
+constexpr uint32_t kBarWindow = 5;                // named barrier of all softmax warps (1 .. 4: of pairs)
+
+// The bits below k, of 64.
+__device__ __forceinline__ uint64_t bits_below(int k) {
+    return k <= 0 ? 0 : k >= 64 ? ~0ull : (1ull << k) - 1;
+}
 
 struct __align__(1024) PrefillSmem {
     // The query block (A operand of the routing MMA); K-major, 128B-swizzled:
@@ -118,13 +132,16 @@ struct __align__(1024) PrefillSmem {
     float lsum[2][kBM];        // the two groups' shares of the row sums, for the epilogue (before:
                                // [1] the maxima of half tile 1, for the first reference)
     float2 ml[kBM];            // the rows' references and sums, for the cluster's merge
+    // kWindow: rows that some positions see and that are not finite as fp16: [0] of the tokens behind the block's
+    // first position, [1] of those that leave the window within the block, each from its first
+    uint32_t over[2][kBM / 32];
     uint32_t tmem_base;
     int abort;
 };
 
 // kShared: several heads per block or CTAs per cluster (a.hp, a.rpb, a.cs); otherwise one head per
 // block and one CTA per block, as constants.
-template <bool kShared>
+template <bool kShared, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
     prefill_tc_kernel(const __grid_constant__ CUtensorMap vmap,
                       const __grid_constant__ CUtensorMap wmap,
@@ -142,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
     const int L = a.seq_lens[b];
     const int n = q1 - q0;
-    if (q0 < 0 || n < 0 || q1 > a.total_q || L < n || L > geo.max_pages * geo.P) {
+    if (q0 < 0 || n < 0 || q1 > a.total_q || L < n || L > geo.max_pages * geo.P || (kWindow && n > a.max_q)) {
         if (tid == 0 && blockIdx.x == 0 && mblk == 0) raise_flag(a.err, KL_FLAG_BAD_LENGTH);
         return;
     }
@@ -160,11 +177,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     // The cluster's CTAs take consecutive shares of the block's cache tiles; this one's are tiles
     // tile0 .. tile0 + n_tiles - 1, half tiles 0 .. n_sub - 1 from there (none for the last ranks
     // of a short sequence).
-    const int all_tiles = pos_last / kBN + 1;
+    // (kWindow: shares of the line of tiles that the block sees)
+    WindowSpan span{0, 0, 0};
+    if (kWindow) span = window_span(pos0, pos_last, a.window, a.sinks);
+    const int len = kWindow ? span.len : pos_last + 1;
+    auto token_at = [&](int x) { return kWindow && x >= span.first ? x + span.shift : x; };
+    const int all_tiles = (len - 1) / kBN + 1;
     const int share = (all_tiles + cs - 1) / cs;
     const int tile0 = min(all_tiles, rank * share);
     const int n_tiles = min(share, all_tiles - tile0);
-    const int n_sub = max(0, min(2 * n_tiles, pos_last / kBS + 1 - 2 * tile0));
+    const int n_sub = max(0, min(2 * n_tiles, (len - 1) / kBS + 1 - 2 * tile0));
+    const bool route = !kWindow || a.w_r != nullptr;
+    const int ro = route ? 1 : 0;                // ring positions before the tiles
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -192,6 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         sm.abort = 0;
         ptx::fence_mbar_init();
     }
+    if (kWindow && tid < 2 * kBM / 32) sm.over[0][tid] = 0;
     if (warp == kMmaWarp) {
         ptx::tmem_alloc(&sm.tmem_base, kTmemCols);
         ptx::tmem_relinquish();
@@ -205,8 +230,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (warp == kProducerWarp && lane == 0) {
         ptx::prefetch_tensormap(&vmap);
-        ptx::prefetch_tensormap(&wmap);
-        ptx::prefetch_tensormap(&qmap);
+        if (route) {
+            ptx::prefetch_tensormap(&wmap);
+            ptx::prefetch_tensormap(&qmap);
+        }
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -232,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int issued = 0;
         bool bad = false;
         // position 0: W^R[w(h)] (B operand of the routing MMA) and the query block
-        if (lane == 0) {
+        if (route && lane == 0) {
             ptx::mbar_arrive_expect_tx(&sm.full[0], kTileBytes + hp * rpb * kD * 2);
             ptx::tma_load_2d(sm.tiles[0], &wmap, &sm.full[0], 0, wsel * kD);
             ptx::tma_load_2d(sm.tiles[0] + kHalfBytes, &wmap, &sm.full[0], 64, wsel * kD);
@@ -240,11 +267,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             ptx::tma_load_3d(sm.q + kHalfBytes, &qmap, &sm.full[0], 64, h, q0 + m0);
         }
         __syncwarp();
-        issued = 1;
+        issued = ro;
         for (int i = 0; i < n_tiles; ++i) {
-            const int r = i + 1, s = r % kStages;
-            const int pg = (tile0 + i) * ppt + lane;      // page index within the sequence
-            const bool exists = lane < ppt && pg < seq_pages;
+            const int r = i + ro, s = r % kStages;
+            const int pg = token_at((tile0 + i) * kBN) / P + lane;   // page index within the sequence
+            bool exists = lane < ppt && pg < seq_pages;
+            // (pages without a visible row may be anyone's by now)
+            if (kWindow)
+                exists = exists && pg * P <= pos_last && (pg * P < a.sinks || pg * P + P > pos0 - a.window + 1);
             const int page = exists ? bt[pg] : -1;
             if (r >= kStages && !wait(&sm.empty[s], ((r / kStages) & 1) ^ 1)) break;
             const bool in_range = exists && page >= 0 && page < geo.num_pages;
@@ -287,8 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         if (warp == kMmaWarp) {
             // routing, then the score MMAs of every tile
-            ok = wait(&sm.full[0], 0);
-            if (ok) {
+            ok = !route || wait(&sm.full[0], 0);
+            if (route && ok) {
                 ptx::tc_fence_after();
                 if (ptx::elect_one()) {
                     // Q_r = Q . W^R: A = query block (K-major), B = W^R (N = output dim j,
@@ -308,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ok && ptx::elect_one()) {
                 ptx::tc_fence_after();
                 for (int u = 0; u < n_sub; ++u) {
-                    const int r = (u >> 1) + 1, s = r % kStages, sb = u % kSub;
+                    const int r = (u >> 1) + ro, s = r % kStages, sb = u % kSub;
                     if (!wait.one(&sm.full[s], (r / kStages) & 1)) break;
                     // the output MMAs of half tile u - kSub have read buffer sb (its P)
                     if (u >= kSub && !wait.one(&sm.s_free[sb], (u / kSub - 1) & 1)) break;
@@ -329,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // columns of its score buffer), B = 64 rows of the tile (N = dims, MN-major),
             // converted to fp16 by the softmax warps before they arrive on p_full
             for (int u = 0; u < n_sub; ++u) {
-                const int s = ((u >> 1) + 1) % kStages, sb = u % kSub;
+                const int s = ((u >> 1) + ro) % kStages, sb = u % kSub;
                 if (!wait.one(&sm.p_full[sb], (u / kSub) & 1)) break;
                 ptx::tc_fence_after();
                 const uint64_t b0 = mn_desc + ((s * kTileBytes + (u & 1) * kBS * 128) >> 4);
@@ -364,18 +394,39 @@ __global__ void __launch_bounds__(kThreads, 1)
         // rows past the block's end take the last valid position: finite, never stored
         const int pos_r = min(pos0 + r / hp, pos_last);
         const float sl2 = geo.scale * kLog2e;
-        bool ok = wait(&sm.r_full, 0);
+        bool ok = !route || wait(&sm.r_full, 0);
 
         // Routed query row, this warp's 64 columns: Q_r * scale * log2 e as hi + lo bf16 pairs
         // into the Q columns (32 packed columns each).
         if (ok) {
             ptx::tc_fence_after();
             uint32_t u0[32], u1[32];
-            ptx::tmem_ld32(tmem + kColS + c0 + lane_base, u0);
-            ptx::tmem_ld32(tmem + kColS + c0 + 32 + lane_base, u1);
-            ptx::tmem_wait_ld();
-            ptx::reg_fence(u0);
-            ptx::reg_fence(u1);
+            if (route) {
+                ptx::tmem_ld32(tmem + kColS + c0 + lane_base, u0);
+                ptx::tmem_ld32(tmem + kColS + c0 + 32 + lane_base, u1);
+                ptx::tmem_wait_ld();
+                ptx::reg_fence(u0);
+                ptx::reg_fence(u1);
+            } else {
+                // the composed query, as it is
+                const int ri = r / hp, hh = r - ri * hp;
+                const bool live = ri < rows && hh < hn;
+                const uint4 *src = reinterpret_cast<const uint4 *>(
+                    a.q + (live ? ((size_t)(q0 + m0 + ri) * geo.Hq + h + hh) * kD + c0 : 0));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 x = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+                    const uint4 y = live ? src[c + 4] : make_uint4(0u, 0u, 0u, 0u);
+                    const uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        u0[8 * c + 2 * e] = wx[e] << 16;
+                        u0[8 * c + 2 * e + 1] = wx[e] & 0xffff0000u;
+                        u1[8 * c + 2 * e] = wy[e] << 16;
+                        u1[8 * c + 2 * e + 1] = wy[e] & 0xffff0000u;
+                    }
+                }
+            }
             uint32_t hi[32], lo[32];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -397,22 +448,44 @@ __global__ void __launch_bounds__(kThreads, 1)
         float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
         bool okl = ok;
         for (int u = hf; okl && u < n_sub; u += 2) {
-            const int t0 = tile0 * kBN + u * kBS, k = u >> 1, sb = u % kSub;
+            const int t0 = token_at(tile0 * kBN + u * kBS), k = u >> 1, sb = u % kSub;
             const uint32_t sbuf = tmem + kColS + (uint32_t)sb * kBS + lane_base;   // S, then P
             // This thread's half (64 dims) of a cache row of the half tile as fp16, formed while
             // the scores are still on their way: the output MMAs read the tile as fp16. Rows at
             // or past the sequence's end (an unwritten page tail, or a page slot no TMA filled)
             // become zeros, so that 0-weights never meet a non-finite value. The lanes start at
             // different 16-byte chunks so that a warp's accesses spread over all banks.
-            const int stage = (k + 1) % kStages;
-            okl = wait(&sm.full[stage], ((k + 1) / kStages) & 1);
+            const int stage = (k + ro) % kStages;
+            okl = wait(&sm.full[stage], ((k + ro) / kStages) & 1);
             if (!okl) break;
             const uint32_t v_s = ptx::smem_addr(sm.tiles[stage]) + (r >> 6) * kHalfBytes +
                                  (hf * kBS + (r & 63)) * 128;
+            // kWindow: whether not all positions see all of the half tile; of its row here: whether any
+            // does (rows lo .. hi - 1 of the block), and where some do, a bit if it is not finite
+            const bool partial = kWindow && (t0 + kBS - 1 > pos0 ||
+                                             max(t0, a.sinks) <= min(t0 + kBS - 1, pos_last - a.window));
+            bool seen = kWindow || t0 + (r & 63) < L, some = false;
+            if (kWindow && partial) {
+                const int t = t0 + (r & 63), d = t - pos0;
+                const int lo = max(d, 0), hi = t < a.sinks ? rows : min(rows, d + a.window);
+                seen = lo < hi;
+                some = lo > 0 || hi < rows;
+            }
             uint32_t vr[32];
-            if (t0 + (r & 63) < L) {
+            if (seen) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) ld_shared_v4(v_s + ((c + lane) & 7) * 16, vr + 4 * c);
+                if (kWindow && some) {
+                    bool over = false;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) over |= past_fp16(vr[e]);
+                    if (over) {
+                        const int t = t0 + (r & 63), bit = t > pos0 ? t - pos0 - 1 : t - (pos0 - a.window + 1);
+                        atomicOr(&sm.over[t > pos0 ? 0 : 1][bit >> 5], 1u << (bit & 31));
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) vr[e] = 0u;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                     vr[e] = pack_f16(__uint_as_float(vr[e] << 16), __uint_as_float(vr[e] & 0xffff0000u));
@@ -435,7 +508,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             ptx::reg_fence(s0);
             ptx::reg_fence(s1);
             // causal mask: token t0 + c is visible to the row when it is <= pos_r
-            if (t0 + kBS - 1 > pos0) {
+            if (kWindow && partial) {
+                // (and in the window or among the first tokens)
+                const uint64_t see = bits_below(pos_r + 1 - t0) &
+                                     (~bits_below(pos_r - a.window + 1 - t0) | bits_below(a.sinks - t0));
+                const uint32_t v0 = (uint32_t)see, v1 = (uint32_t)(see >> 32);
+#pragma unroll
+                for (int c = 0; c < 32; ++c) {
+                    if (!(v0 & (1u << c))) s0[c] = 0xff800000u;
+                    if (!(v1 & (1u << c))) s1[c] = 0xff800000u;
+                }
+            } else if (!kWindow && t0 + kBS - 1 > pos0) {
                 const int lim = pos_r - t0;
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
@@ -545,13 +628,28 @@ __global__ void __launch_bounds__(kThreads, 1)
             l = m_used == -INFINITY ? 0.f : l * ptx::ex2(m_used - m_fin);
         }
         sm.lsum[hf][r] = l;
-        const bool okp = ptx::bar_and(pair_bar, 64, oke);
-        const float lt = l + sm.lsum[hf ^ 1][r];
+        // (kWindow: all eight warps', so that every bit of `over` is here)
+        const bool okp = ptx::bar_and(kWindow ? kBarWindow : pair_bar, kWindow ? 32 * kComputeWarps : 64, oke);
+        float lt = l + sm.lsum[hf ^ 1][r];
+        if constexpr (kWindow) {
+            // bit j of the first set: token pos0 + 1 + j; of the second: pos0 - window + 1 + j
+            const uint64_t o0 = sm.over[0][0] | (uint64_t)sm.over[0][1] << 32;
+            const uint64_t o1 = sm.over[0][2] | (uint64_t)sm.over[0][3] << 32;
+            const uint64_t w0 = sm.over[1][0] | (uint64_t)sm.over[1][1] << 32;
+            const uint64_t w1 = sm.over[1][2] | (uint64_t)sm.over[1][3] << 32;
+            if (o0 | o1 | w0 | w1) {
+                const int i = pos_r - pos0, first = pos0 + 1;
+                auto sees = [&](int off) {       // 64 tokens from first + off on
+                    return bits_below(i - off) & (~bits_below(i - a.window - off) | bits_below(a.sinks - first - off));
+                };
+                if ((sees(0) & o0) | (sees(64) & o1) | (~bits_below(i) & w0) | (~bits_below(i - 64) & w1)) lt = NAN;
+            }
+        }
         if (kShared && cs > 1) {
             if (hf == 0) sm.ml[r] = okp ? make_float2(sm.mref[lb2][r], lt) : make_float2(-INFINITY, 0.f);
         } else if (okp) {
             ptx::tc_fence_after();
-            const float inv = lt > 0.f ? 1.f / lt : 0.f;
+            const float inv = lt > 0.f ? 1.f / lt : kWindow ? lt : 0.f;    // (NaN stays NaN)
             float nf = 0.f;   // x * 0 is NaN exactly when x is not finite
             const int ri = r / hp, hh = r - ri * hp;
             const size_t orow = ((size_t)(q0 + m0 + ri) * geo.Hq + h + hh) * kD + c0;
@@ -563,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ptx::reg_fence(u);
                 if (ri < rows && hh < hn) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) nf = fmaf(__uint_as_float(u[e]), 0.f, nf);
+                    for (int e = 0; e < 32; ++e) nf = fmaf(__uint_as_float(u[e]), kWindow ? inv * 0.f : 0.f, nf);
                     if (a.out_dtype == KL_FP32) {
                         float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(a.out) + orow + c4 * 32);
 #pragma unroll
@@ -750,11 +848,15 @@ bool prefill_tc_supported(const Geometry &g) {
     return major == 10 && minor == 3;
 }
 
-cudaError_t launch_prefill_tc(const PrefillArgs &a) {
+namespace {
+
+// longest: the most tokens of a block's line.
+template <bool kWindow>
+cudaError_t launch_rows(const PrefillArgs &a, int64_t longest) {
     const Geometry &g = a.geo;
     if (g.B == 0 || a.total_q == 0 || a.max_q == 0) return cudaSuccess;
     PrefillArgs la = a;
-    const PrefillPlan plan = plan_prefill(g.B, g.Hkv, g.G, a.max_q, (int64_t)g.max_pages * g.P,
+    const PrefillPlan plan = plan_prefill(g.B, g.Hkv, g.G, a.max_q, longest,
                                           g.wr_per_qh != 0, device_sm_count());
     la.hp = plan.hp;
     la.rpb = plan.rpb;
@@ -767,7 +869,8 @@ cudaError_t launch_prefill_tc(const PrefillArgs &a) {
         const cuuint32_t box[2] = {64, (cuuint32_t)g.P};
         if (!encode(&vmap, a.v_cache, 2, dims, strides, box)) return cudaErrorInvalidValue;
     }
-    {
+    wmap = qmap = vmap;                 // (not read with a composed query)
+    if (a.w_r) {
         // W^R as [Hw * 128 k rows][128 j], one box = a 64-column half of one matrix
         const cuuint64_t hw = g.wr_per_qh ? (cuuint64_t)g.Hq : (cuuint64_t)g.Hkv;
         const cuuint64_t dims[2] = {kD, hw * kD};
@@ -775,7 +878,7 @@ cudaError_t launch_prefill_tc(const PrefillArgs &a) {
         const cuuint32_t box[2] = {64, kD};
         if (!encode(&wmap, a.w_r, 2, dims, strides, box)) return cudaErrorInvalidValue;
     }
-    {
+    if (a.w_r) {
         // q as [total_q][Hq][128], one box = rpb consecutive rows of hp heads (64 dims); rows past
         // total_q and heads past Hq read as zeros
         const cuuint64_t dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)a.total_q};
@@ -786,7 +889,7 @@ cudaError_t launch_prefill_tc(const PrefillArgs &a) {
     const size_t smem = sizeof(PrefillSmem) + 1024;
     while (true) {
         const bool shared = la.hp > 1 || la.cs > 1;
-        const auto kernel = shared ? prefill_tc_kernel<true> : prefill_tc_kernel<false>;
+        const auto kernel = shared ? prefill_tc_kernel<true, kWindow> : prefill_tc_kernel<false, kWindow>;
         static PerDeviceOnce once[2];
         cudaError_t e = once[shared].run([&] {
             return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -810,6 +913,16 @@ cudaError_t launch_prefill_tc(const PrefillArgs &a) {
         (void)cudaGetLastError();
         la.cs = 1;
     }
+}
+
+}  // namespace
+
+cudaError_t launch_prefill_tc(const PrefillArgs &a) {
+    return launch_rows<false>(a, (int64_t)a.geo.max_pages * a.geo.P);
+}
+
+cudaError_t launch_window_tc(const PrefillArgs &a) {
+    return launch_rows<true>(a, window_line(kPrefillRows, a.window, a.sinks, (int64_t)a.geo.max_pages * a.geo.P));
 }
 
 cudaError_t launch_append_chunk(const Geometry &g, int total_q, int max_q, const uint16_t *v_new,

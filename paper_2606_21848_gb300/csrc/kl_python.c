@@ -30,7 +30,8 @@ static PyObject *g_initialized, *g_get_device, *g_raw_stream, *g_current_stream;
     X(route_query) X(append_v) X(decode_attention) X(decode_attention_ex) X(decode_step) X(combine) \
     X(standard_decode) X(decode_attention_noalloc) X(append_v_chunk) X(prefill_attention) \
     X(append_v_fp8) X(quantize_cache_fp8) X(decode_attention_fp8) X(decode_step_fp8) \
-    X(latent_decode) X(latent_decode_step) X(tree_attention) X(tree_commit) X(token_logprobs)
+    X(latent_decode) X(latent_decode_step) X(tree_attention) X(tree_commit) X(token_logprobs) \
+    X(window_attention) X(attention_weights) X(evict)
 #define POINTER(n) static __typeof__(kl_##n) *f_##n;
 ENTRIES(POINTER)
 #define SLOT(n) {"kl_" #n, &f_##n},
@@ -323,6 +324,20 @@ CALL(f_tree_attention(&sh, q, w, c, bt, sl, cu, pa, tq, mq, ns, out, (kl_dtype)d
 FN(tree_commit, 11) SHAPE(0); PTR(1, cu); PTR(2, pa); PTR(3, pl); INT(4, mp); PTR(5, bt); PTR(6, sl);
 PTR(7, nl); PTR(8, c); PTR(9, e); STREAM(10);
 CALL(f_tree_commit(&sh, cu, pa, pl, mp, bt, sl, nl, c, e, st))
+
+FN(window_attention, 17) SHAPE(0); PTR(1, q); PTR(2, w); PTR(3, c); PTR(4, bt); PTR(5, sl); PTR(6, cu);
+INT(7, tq); INT(8, mq); INT(9, wi); INT(10, si); INT(11, ns); PTR(12, out); INT(13, dt); WORK(14); PTR(15, e);
+STREAM(16);
+CALL(f_window_attention(&sh, q, w, c, bt, sl, cu, tq, mq, wi, si, ns, out, (kl_dtype)dt, ws, wsn, e, st))
+
+FN(attention_weights, 19) SHAPE(0); PTR(1, q); PTR(2, w); PTR(3, c); PTR(4, bt); PTR(5, sl); PTR(6, cu);
+INT(7, tq); INT(8, mq); PTR(9, aw); INT(10, as); FLOAT(11, de); PTR(12, nw); INT(13, ns); PTR(14, out); INT(15, dt);
+WORK(16); PTR(17, e); STREAM(18);
+CALL(f_attention_weights(&sh, q, w, c, bt, sl, cu, tq, mq, aw, as, de, nw, ns, out, (kl_dtype)dt, ws, wsn, e, st))
+
+FN(evict, 16) SHAPE(0); PTR(1, aw); INT(2, as); INT(3, bu); INT(4, si); INT(5, re); PTR(6, bt); PTR(7, sl);
+PTR(8, nt); PTR(9, c); PTR(10, nw); PTR(11, k); PTR(12, nl); WORK(13); PTR(14, e); STREAM(15);
+CALL(f_evict(&sh, aw, as, bu, si, re, bt, sl, nt, c, nw, k, nl, ws, wsn, e, st))
 
 FN(token_logprobs, 16) INT(0, nr); INT(1, vo); LONG(2, rs); PTR(3, lg); INT(4, dt); FLOAT(5, sc); PTR(6, tk);
 INT(7, tr); INT(8, nt); PTR(9, lp); PTR(10, en); PTR(11, tl); PTR(12, ti); WORK(13); PTR(14, e); STREAM(15);

@@ -1,0 +1,121 @@
+// Causal attention of a sequence's last rows that also adds up the weight that each cached row receives, for
+// sm_103a; head_dim 128:
+//
+//   out as kl_window_attention without a window, and per sequence, value head and cached row
+//   new_t = decay old_t + sum over the new rows r and the group's heads of softmax(s_r)_t
+//
+// The attention is the wide decode's kernel (kl_decode_wide_kernel.cuh, kWeights) in blocks of up to 16 (position,
+// head) rows, with query and weights of three bf16 terms, since the weights are fp32 results whatever type the
+// outputs have. A weight needs its row's whole softmax: the kernel writes the scores (4 bytes per row and token, 32
+// per cached row of 256 where a group has 8 heads) and a second kernel, its programmatic dependent, reads them back
+// with the runs' {maximum, sum}. Rows are added in their order: the sums are the same on every run.
+#include "kl_rows_wide.cuh"
+
+namespace kl {
+namespace {
+
+constexpr int kAddThreads = 256, kAddPer = 4;            // tokens per thread, kAddThreads apart
+constexpr int kAddTokens = kAddThreads * kAddPer;
+constexpr int kAddRows = 256;                            // rows whose {maximum, 1 / sum} a CTA holds at a time
+
+// CTA (tokens, g, b).
+__global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeArgs a, const WeightArgs w) {
+    __shared__ float2 row[kAddRows];                     // {maximum, 1 / sum}
+    grid_dep_wait();
+    grid_dep_launch();
+    const Geometry &geo = a.geo;
+    const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+    const int q0 = a.tree.cu_q[b], q1 = a.tree.cu_q[b + 1], n = q1 - q0, L = a.seq_lens[b];
+    if (q0 < 0 || n < 0 || q1 > a.tree.total_q || n > a.tree.max_q || L < n || L > a.causal.stride ||
+        L > geo.max_pages * geo.P)
+        return;                                          // (reported by the attention)
+    const int t0 = blockIdx.x * kAddTokens + tid;
+    if (blockIdx.x * kAddTokens >= L) return;
+    const size_t unit = (size_t)b * geo.Hkv + g;
+    const int hp = a.causal.hp, rpb = a.causal.rpb, nhg = a.causal.nhg;
+    float old[kAddPer], sum[kAddPer];
+#pragma unroll
+    for (int k = 0; k < kAddPer; ++k) {
+        const int t = t0 + k * kAddThreads;
+        old[k] = w.decay != 0.f && t < L ? w.weights[unit * a.causal.stride + t] : 0.f;
+        sum[k] = 0.f;
+    }
+    // rows in blocks as the attention's, kAddRows / 16 blocks at a time
+    const int blocks = (n + rpb - 1) / rpb * nhg;
+    constexpr int kBatch = kAddRows / 16;
+    for (int k0 = 0; k0 < blocks; k0 += kBatch) {
+        if (k0) __syncthreads();
+        const int hb = k0 + tid / 16, r = tid & 15;      // (kAddThreads = kAddRows)
+        if (hb < blocks) {
+            const int m0 = hb / nhg * rpb, end = L - n + min(m0 + rpb, n);
+            const int runs = (end + geo.chunk * geo.spc - 1) / (geo.chunk * geo.spc);
+            const int live = min(hp, geo.G - hb % nhg * hp) + (min(rpb, n - m0) - 1) * hp;
+            if (r < live) {
+                const float2 *s = a.causal.stats + ((unit * geo.nhb + hb) * 16 + r) * geo.S;
+                float M = -INFINITY, z = 0.f;
+                for (int i = 0; i < runs; ++i) {
+                    const float2 x = __ldcg(s + i);
+                    const float top = fmaxf(M, x.x);
+                    // (a run of maximum -inf has sum 0, or NaN)
+                    z = (M == top ? z : z * ptx::ex2(M - top)) + (x.x == top ? x.y : x.y * ptx::ex2(x.x - top));
+                    M = top;
+                }
+                row[tid] = make_float2(M, 1.f / z);
+            }
+        }
+        __syncthreads();
+        for (int hb = k0; hb < min(blocks, k0 + kBatch); ++hb) {
+            const int m0 = hb / nhg * rpb, live = min(hp, geo.G - hb % nhg * hp) + (min(rpb, n - m0) - 1) * hp;
+            const float *s = a.causal.scores + (unit * geo.nhb + hb) * a.causal.rows * a.causal.pitch;
+            const float2 *of = row + (hb - k0) * 16;
+            const int p0 = L - n + m0;
+#pragma unroll 4
+            for (int r = 0; r < live; ++r) {
+                const int p = p0 + r / hp;
+                const float2 m = of[r];
+#pragma unroll
+                for (int k = 0; k < kAddPer; ++k) {
+                    const int t = t0 + k * kAddThreads;
+                    if (t <= p) sum[k] += ptx::ex2(__ldcs(s + r * a.causal.pitch + t) - m.x) * m.y;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kAddPer; ++k) {
+        const int t = t0 + k * kAddThreads;
+        if (t < L) w.new_weights[unit * a.causal.stride + t] = w.decay != 0.f ? fmaf(w.decay, old[k], sum[k]) : sum[k];
+    }
+}
+
+template <int NG>
+cudaError_t launch_scores(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
+                          const CUtensorMap &qmap) {
+    return la.wait_ns < kExactWaitNs ? launch_kernel_wide<16, NG, true, kWeights, 3>(la, vmap, wmap, qmap)
+                                     : launch_kernel_wide<16, NG, false, kWeights, 3>(la, vmap, wmap, qmap);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w) {
+    DecodeArgs la = a;
+    Geometry &g = la.geo;
+    const int64_t sms = device_sm_count(), ctas = (int64_t)g.B * g.Hkv * g.nhb;
+    const int64_t tiles = ((int64_t)g.max_pages * g.P + 127) / 128;
+    const bool two_per_sm = ctas > sms && tiles <= 32;
+    g.qbox = a.causal.hp * a.causal.rpb;
+    g.spc = rows_splits_per_cta(g, tiles, ctas, two_per_sm ? 2 * sms : sms);
+    CUtensorMap vmap, wmap, qmap;
+    if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
+    cudaError_t e = two_per_sm ? launch_scores<1>(la, vmap, wmap, qmap) : launch_scores<2>(la, vmap, wmap, qmap);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    const int64_t longest = (int64_t)g.max_pages * g.P < a.causal.stride ? (int64_t)g.max_pages * g.P : a.causal.stride;
+    cfg.gridDim = dim3((unsigned)((longest + kAddTokens - 1) / kAddTokens), g.Hkv, g.B);
+    cfg.blockDim = dim3(kAddThreads);
+    cfg.stream = a.stream;
+    const OverlapAttr overlap(cfg);
+    return cudaLaunchKernelEx(&cfg, add_weights_kernel, la, w);
+}
+
+}  // namespace kl

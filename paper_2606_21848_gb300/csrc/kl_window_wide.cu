@@ -1,0 +1,41 @@
+// Attention of consecutive positions with a sliding window and first tokens that stay visible, on the wide
+// decode's kernel (kl_decode_wide_kernel.cuh, kWindow): the last tokens of decoding, a few drafts in a row.
+//
+//   out_p = sum_t softmax(scale <q_p W^R, v_t>)_t v_t   over t <= p with t < sinks or t > p - window
+//
+// A block of up to 16 or 32 (position, head) rows reads the tiles that its positions see and no others, so a step
+// costs what the window costs, however long the sequence. HBM bounds it: 256 bytes per visible token and value head.
+#include "kl_rows_wide.cuh"
+
+namespace kl {
+namespace {
+
+template <int NH, int NG, int T>
+cudaError_t launch_window(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
+                          const CUtensorMap &qmap) {
+    return la.wait_ns < kExactWaitNs ? launch_kernel_wide<NH, NG, true, kWindow, T>(la, vmap, wmap, qmap)
+                                     : launch_kernel_wide<NH, NG, false, kWindow, T>(la, vmap, wmap, qmap);
+}
+
+}  // namespace
+
+cudaError_t launch_window_wide(const DecodeArgs &a) {
+    DecodeArgs la = a;
+    Geometry &g = la.geo;
+    const int64_t sms = device_sm_count(), ctas = (int64_t)g.B * g.Hkv * g.nhb;
+    const bool fp32 = a.out_dtype == KL_FP32, w32 = a.causal.hp * a.causal.rpb > 16;
+    // (two CTAs per SM as in launch_tree_wide; with three terms these have rings of two tiles)
+    const int64_t tiles = ((int64_t)g.S * g.chunk + 127) / 128;
+    const bool two_per_sm = !w32 && ctas > sms && (!fp32 || tiles <= 32);
+    g.qbox = a.causal.hp * a.causal.rpb;
+    g.spc = rows_splits_per_cta(g, tiles, ctas, two_per_sm ? 2 * sms : sms);
+    CUtensorMap vmap, wmap, qmap;
+    if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
+    if (fp32)
+        return two_per_sm ? launch_window<16, 1, 3>(la, vmap, wmap, qmap)
+                          : launch_window<16, 2, 3>(la, vmap, wmap, qmap);
+    if (w32) return launch_window<32, 2, 2>(la, vmap, wmap, qmap);
+    return two_per_sm ? launch_window<16, 1, 2>(la, vmap, wmap, qmap) : launch_window<16, 2, 2>(la, vmap, wmap, qmap);
+}
+
+}  // namespace kl
