@@ -3,20 +3,23 @@
 // the lowest index) stay, `budget` in all; they move together in their order, and their weights with them.
 //
 // Two kernels. The selection: a cluster of CTAs per (sequence, value head), each with a piece of the weights in
-// shared memory. The smallest weight that stays is found by four rounds over its bits, 8 at a time from the top: every
-// CTA counts its piece's weights under the bits found so far, all add the counts up through distributed shared memory
-// and find the same byte. Then each warp counts what stays of a stretch of the piece, the counts are summed before
-// it, and it writes. (All weights are in shared memory before the first is written: weights may move in place.)
-// The move: 512 bytes of traffic per row of 128 bf16 values. Rows only ever move down, row j to a place at most
-// where it was, so in place a CTA takes (sequence, value head, a stretch of each row) from the first row on and reads
-// a step ahead of what it writes: what it overwrites has been read. To other pages the rows are shared out.
+// shared memory. The smallest weight that stays is found by three rounds over its bits from the top, 11, 10 and 10
+// (a positive fp32's order is that of its bits): every CTA counts its piece's weights that have the bits found so
+// far by their next ones, all add the counts up through distributed shared memory and find the same bin. Few
+// weights are left to count after the first round. Then each warp counts what stays of a stretch of the piece, the
+// counts are summed before it, and it writes. (All weights are in shared memory before the first is written:
+// weights may move in place.)
+// The move: 512 bytes of traffic per row of 128 bf16 values, and HBM bounds it. Rows only ever move down: in place
+// the CTAs of a cluster take turns of consecutive rows from the first on, read a turn ahead and meet between the
+// reads and the writes of a turn; what they overwrite has been read by then. To other pages nothing waits.
 #include "kl_internal.cuh"
 
 namespace kl {
 namespace {
 
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
-constexpr int kBins = 256;
+constexpr int kBits0 = 11, kBits = 10;                   // of the first round, of the others
+constexpr int kBins = 1 << kBits0;
+constexpr int kPerThread = 4, kBinWarps = kBins / kPerThread / 32;   // the first warps find the bin
 constexpr int kMostCluster = 8;
 
 // What the move needs to know of a (sequence, value head): rows that stay (0: it is left alone) and whether its
@@ -27,7 +30,7 @@ struct EvictUnit {
 static_assert(sizeof(EvictUnit) == kEvictUnitBytes, "");
 
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -45,13 +48,42 @@ __device__ __forceinline__ int ld_cluster(const int *p, int rank) {
     return v;
 }
 
+// Sums of the four words at `p` (16-byte aligned) over CTAs rank .. rank + 3 (those below `cluster`), all four loads
+// on their way at once.
+__device__ __forceinline__ void add_cluster(const int *p, int rank, int cluster, int (&n)[4]) {
+    uint32_t at[4];
+    int v[16];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                     : "=r"(at[c])
+                     : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(min(rank + c, cluster - 1)));
+    asm volatile(
+        "ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%16];\n\t"
+        "ld.shared::cluster.v4.b32 {%4, %5, %6, %7}, [%17];\n\t"
+        "ld.shared::cluster.v4.b32 {%8, %9, %10, %11}, [%18];\n\t"
+        "ld.shared::cluster.v4.b32 {%12, %13, %14, %15}, [%19];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(at[0]), "r"(at[1]), "r"(at[2]), "r"(at[3])
+        : "memory");
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (rank + c < cluster)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) n[e] += v[4 * c + e];
+}
+
 // Weights in their order as whole numbers; what is not positive, and NaN, is 0.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
 
-// Cluster (b, g), CTA `rank` of it: tokens rank * piece ...
-__global__ void __launch_bounds__(kSelThreads) select_kernel(const EvictArgs a, EvictUnit *units, int cluster, int piece) {
-    extern __shared__ float held[];                      // [piece]
-    __shared__ int hist[2][kBins];
+// Cluster (b, g), CTA `rank` of it: tokens rank * piece ... kThreads: 512, of which an SM holds four CTAs, or 1024 where
+// there are few units.
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kernel(const EvictArgs a, EvictUnit *units, int cluster, int piece) {
+    constexpr int kSelWarps = kThreads / 32;
+    extern __shared__ __align__(16) float held[];        // [piece]
+    __shared__ __align__(16) int hist[2][kBins];
     __shared__ int count[2];                             // of this CTA's piece: above the border, on it
     __shared__ int warp_above[kSelWarps], warp_on[kSelWarps];
     __shared__ uint32_t border;
@@ -62,86 +94,124 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const EvictArgs a, 
     const int b = unit / geo.Hkv;
     grid_dep_wait();
     const int L = a.seq_lens[b], rows = min(L, a.budget);
+    const bool too_long = L < 0 || L > geo.max_pages * geo.P || L > a.stride;
     if (tid == 0) {
-        bad = L < 0 || L > geo.max_pages * geo.P || L > a.stride ? KL_FLAG_BAD_LENGTH : 0;
-        same = 0;
         border = 0;
         wanted = 0;
     }
-    __syncthreads();
-    grid_dep_launch();
-    // every page of the sequence and of where it goes (the same answer in all CTAs of the sequence)
+    // The pages of the sequence and of where it goes, shared out over the cluster, while the weights are on their way
     const int32_t *from = a.block_table + (size_t)b * geo.max_pages, *to = a.new_table + (size_t)b * geo.max_pages;
-    if (!bad) {
-        const int pages = (L + geo.P - 1) / geo.P, new_pages = (rows + geo.P - 1) / geo.P;
-        bool wrong = false, eq = false;
-        for (int i = tid; i < pages; i += kSelThreads) {
-            const int p = from[i];
-            wrong |= p < 0 || p >= geo.num_pages;
-            if (i < new_pages) {
-                const int q = to[i];
-                wrong |= q < 0 || q >= geo.num_pages;
-                eq |= p == q;
-            }
-        }
-        if (wrong) bad = KL_FLAG_BAD_PAGE;               // (any of them)
-        if (eq) same = 1;
-    }
-    __syncthreads();
-    const bool left = bad != 0;
-    if (tid == 0 && rank == 0) {
-        if (left && unit % geo.Hkv == 0) raise_flag(a.err, bad);
-        units[unit] = EvictUnit{left ? -1 : rows, same};
-    }
-    if (left) return;                                    // (every CTA of the cluster)
     const float *w = a.weights + (size_t)unit * a.stride;
-    const int t0 = min(rank * piece, L), t1 = min(t0 + piece, L);
-    for (int t = t0 + tid; t < t1; t += kSelThreads) held[t - t0] = w[t];
+    const int t0 = too_long ? 0 : min(rank * piece, L), t1 = too_long ? 0 : min(t0 + piece, L);
+    constexpr int kAhead = 8;
+    float ahead[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (t0 + tid + k * kThreads < t1) ahead[k] = w[t0 + tid + k * kThreads];
+    int fault = too_long, eq = 0;
+    if (!too_long) {
+        const int pages = (L + geo.P - 1) / geo.P, new_pages = (rows + geo.P - 1) / geo.P;
+#pragma unroll 2
+        for (int i = rank * kThreads + tid; i < pages; i += cluster * kThreads) {
+            const int p = from[i], q = i < new_pages ? to[i] : 0;
+            if (p < 0 || p >= geo.num_pages || q < 0 || q >= geo.num_pages) fault = 1;
+            if (i < new_pages && p == q) eq = 1;
+        }
+    }
+    fault = __syncthreads_or(fault) ? (too_long ? KL_FLAG_BAD_LENGTH : KL_FLAG_BAD_PAGE) : 0;
+    eq = __syncthreads_or(eq);
+    if (cluster > 1) {
+        if (tid == 0) {
+            bad = fault;
+            same = eq;
+        }
+        cluster_sync();
+        fault = eq = 0;
+#pragma unroll
+        for (int c = 0; c < kMostCluster; ++c)
+            if (c < cluster) {
+                fault |= ld_cluster(&bad, c);
+                eq |= ld_cluster(&same, c);
+            }
+    }
+    if (tid == 0 && rank == 0) {
+        if (fault && unit % geo.Hkv == 0) raise_flag(a.err, fault);
+        units[unit] = EvictUnit{fault ? -1 : rows, eq};
+    }
+    if (fault) {                                         // (every CTA of the cluster, once all have read)
+        if (cluster > 1) cluster_sync();
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (t0 + tid + k * kThreads < t1) held[tid + k * kThreads] = ahead[k];
+    for (int t = t0 + tid + kAhead * kThreads; t < t1; t += kAhead * kThreads) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (t + k * kThreads < t1) ahead[k] = w[t + k * kThreads];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (t + k * kThreads < t1) held[t - t0 + k * kThreads] = ahead[k];
+    }
     // the tokens between the first and the last ones, of which `want` stay
     const bool all = L <= a.budget;
     const int mid0 = a.sinks, mid1 = L - a.recent;
     int want = all ? 0 : a.budget - a.sinks - a.recent;
     uint32_t key = 0;
-    for (int round = 0; round < 4 && want > 0; ++round) {
-        const int shift = 24 - 8 * round;
+    __shared__ int warp_sum[kBinWarps];
+    int shift = 31;
+    for (int round = 0; round < 3 && want > 0; ++round) {
+        const int bits = round == 0 ? kBits0 : kBits;
+        const uint32_t known = round == 0 ? 0u : ~0u << shift;   // bits found so far
+        shift -= bits;
         int *const h = hist[round & 1];
-        if (tid < kBins) h[tid] = 0;
+        for (int i = tid; i < kBins; i += kThreads) h[i] = 0;
         __syncthreads();
-        for (int base = t0; base < t1; base += kSelThreads) {
-            const int t = base + tid;
-            const uint32_t k = t < t1 ? weight_key(held[t - t0]) : 0;
-            const bool in = t < t1 && t >= mid0 && t < mid1 && (round == 0 || (k >> (shift + 8)) == (key >> (shift + 8)));
-            // (one addition per distinct byte of a warp: weights share their upper bits)
-            const uint32_t bin = in ? (k >> shift) & 255u : kBins;
-            const uint32_t mates = __match_any_sync(0xffffffffu, bin);
-            if (in && lane == __ffs(mates) - 1) atomicAdd(h + bin, __popc(mates));
+        // four consecutive weights per thread
+        for (int base = 0; base < t1 - t0; base += 4 * kThreads) {
+            const int at = base + 4 * tid;
+            if (t0 + at >= t1) break;
+            const float4 x = *reinterpret_cast<const float4 *>(held + at);
+            const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t k = weight_key(xs[e]);
+                const int t = t0 + at + e;
+                if ((k & known) == key && t >= mid0 && t < min(t1, mid1)) atomicAdd(h + ((k >> shift) & ((1u << bits) - 1)), 1);
+            }
         }
         if (cluster > 1) cluster_sync();
         else __syncthreads();
-        // the byte of the want-th largest: bins from the top, 8 per lane of one warp
-        if (warp == 0) {
-            int n[8], sum = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int bin = 255 - 8 * lane - e;
-                n[e] = 0;
-                if (cluster > 1)
-                    for (int c = 0; c < cluster; ++c) n[e] += ld_cluster(h + bin, c);
-                else n[e] = h[bin];
-                sum += n[e];
+        // the bin of the want-th largest: bins from the top, kPerThread per thread
+        const int low = kBins - kPerThread * (tid + 1);          // its lowest bin
+        int n[kPerThread] = {0, 0, 0, 0}, sum = 0, upto = 0;
+        if (warp < kBinWarps) {
+            if (cluster > 1) {
+                for (int c = 0; c < cluster; c += 4) add_cluster(h + low, c, cluster, n);
+            } else {
+                const int4 x = *reinterpret_cast<const int4 *>(h + low);
+                n[0] = x.x;
+                n[1] = x.y;
+                n[2] = x.z;
+                n[3] = x.w;
             }
-            int upto = sum;
+            sum = upto = n[0] + n[1] + n[2] + n[3];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int x = __shfl_up_sync(0xffffffffu, upto, o);
                 if (lane >= o) upto += x;
             }
+            if (lane == 31) warp_sum[warp] = upto;
+        }
+        __syncthreads();
+        if (warp < kBinWarps) {
+            upto += __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0);
             int above = upto - sum;
             if (above < want && want <= upto) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = kPerThread - 1; e >= 0; --e) {
                     if (above < want && want <= above + n[e]) {
-                        border = key | (uint32_t)(255 - 8 * lane - e) << shift;
+                        border = key | (uint32_t)(low + e) << shift;
                         wanted = want - above;
                     }
                     above += n[e];
@@ -154,113 +224,155 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const EvictArgs a, 
     }
     // `want` of those on the border `key` stay, the first ones; with none wanted nothing between stays
     const bool none = !all && a.budget == a.sinks + a.recent;
-    auto above = [&](int t) { return all || t < mid0 || t >= mid1 || (!none && weight_key(held[t - t0]) > key); };
-    auto on = [&](int t) { return !all && !none && t >= mid0 && t < mid1 && weight_key(held[t - t0]) == key; };
-    const int per = ((t1 - t0 + kSelWarps - 1) / kSelWarps + 31) & ~31;
+    // Four consecutive tokens per lane and step: how many are above, and (<< 16) on the border; of which bits they are.
+    auto look = [&](int t, uint32_t &bits) -> uint32_t {
+        bits = 0;
+        if (t >= t1) return 0;
+        const float4 x = *reinterpret_cast<const float4 *>(held + (t - t0));
+        const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (t + e >= t1) continue;
+            const bool inner = !all && t + e >= mid0 && t + e < mid1;
+            const uint32_t k = weight_key(xs[e]);
+            if (!inner || (!none && k > key)) bits |= 1u << e;
+            else if (!none && k == key) bits |= 16u << e;
+        }
+        return __popc(bits & 15u) | __popc(bits >> 4) << 16;
+    };
+    const int per = ((t1 - t0 + kSelWarps - 1) / kSelWarps + 127) & ~127;
     const int s0 = min(t0 + warp * per, t1), s1 = min(s0 + per, t1);
     if (want == 0 || all || none) __syncthreads();       // (held is complete)
     int na = 0, no = 0;
-    for (int t = s0; t < s1; t += 32) {
-        na += __popc(__ballot_sync(0xffffffffu, t + lane < s1 && above(t + lane)));
-        no += __popc(__ballot_sync(0xffffffffu, t + lane < s1 && on(t + lane)));
+    for (int t = s0; t < s1; t += 128) {
+        uint32_t bits;
+        const uint32_t n = __reduce_add_sync(0xffffffffu, look(t + 4 * lane, bits));
+        na += n & 0xffffu;
+        no += n >> 16;
     }
     if (lane == 0) {
         warp_above[warp] = na;
         warp_on[warp] = no;
     }
     __syncthreads();
-    if (tid == 0) {
-        int x = 0, y = 0;
-        for (int i = 0; i < kSelWarps; ++i) {
-            x += warp_above[i];
-            y += warp_on[i];
+    if (warp == 0) {
+        const int x = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? warp_above[lane] : 0);
+        const int y = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? warp_on[lane] : 0);
+        if (lane == 0) {
+            count[0] = x;
+            count[1] = y;
         }
-        count[0] = x;
-        count[1] = y;
     }
     if (cluster > 1) cluster_sync();                     // (and every CTA holds its weights)
     else __syncthreads();
-    int before = 0, on_before = 0;                       // this warp's stretch: above the border and on it before
-    for (int c = 0; c < rank; ++c) {
-        before += ld_cluster(count, c);
-        on_before += ld_cluster(count + 1, c);
+    // above the border and on it before this warp's stretch
+    int before = lane < warp ? warp_above[lane] : 0, on_before = lane < warp ? warp_on[lane] : 0;
+    if (lane < rank) {
+        before += ld_cluster(count, lane);
+        on_before += ld_cluster(count + 1, lane);
     }
-    for (int i = 0; i < warp; ++i) {
-        before += warp_above[i];
-        on_before += warp_on[i];
-    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    on_before = __reduce_add_sync(0xffffffffu, on_before);
+    // (Here and not earlier: CTAs of the move that come while only some SMs have room crowd those. 64 sequences of
+    // 8192 rows, 4096 of which stay: 259 us with the signal at the top.)
+    grid_dep_launch();
     int32_t *kept = a.kept + (size_t)unit * a.budget;
     float *nw = a.new_weights + (size_t)unit * a.stride;
-    for (int t = s0; t < s1; t += 32) {
-        const bool live = t + lane < s1, x = live && above(t + lane), y = live && on(t + lane);
-        const uint32_t mx = __ballot_sync(0xffffffffu, x), my = __ballot_sync(0xffffffffu, y);
-        const uint32_t under = (1u << lane) - 1;
-        const int ox = before + __popc(mx & under), oy = on_before + __popc(my & under);
-        if (x || (y && oy < want)) {
-            const int at = ox + min(oy, want);
-            kept[at] = t + lane;
-            nw[at] = held[t + lane - t0];
+    for (int t = s0; t < s1; t += 128) {
+        uint32_t bits, upto = look(t + 4 * lane, bits);
+        const uint32_t mine = upto;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
         }
-        before += __popc(mx);
-        on_before += __popc(my);
+        int ox = before + (int)((upto - mine) & 0xffffu), oy = on_before + (int)((upto - mine) >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool x = bits >> e & 1, y = bits >> (4 + e) & 1;
+            if (x || (y && oy < want)) {
+                const int at = ox + min(oy, want);
+                kept[at] = t + 4 * lane + e;
+                nw[at] = held[t + 4 * lane + e - t0];
+            }
+            ox += x;
+            oy += y;
+        }
+        const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
+        before += total & 0xffffu;
+        on_before += total >> 16;
     }
     // (the whole cluster writes the rest; nothing there is read again)
-    for (int t = rows + rank * kSelThreads + tid; t < L; t += cluster * kSelThreads) nw[t] = 0.f;
-    for (int t = rows + rank * kSelThreads + tid; t < a.budget; t += cluster * kSelThreads) kept[t] = -1;
+    for (int t = rows + rank * kThreads + tid; t < L; t += cluster * kThreads) nw[t] = 0.f;
+    for (int t = rows + rank * kThreads + tid; t < a.budget; t += cluster * kThreads) kept[t] = -1;
     if (cluster > 1) cluster_sync();                     // (the counts are read)
 }
 
 constexpr int kMoveThreads = 256;
-constexpr int kMoveDepth = 4;                            // 16-byte pieces per thread and step
+constexpr int kMoveDepth = 4;                            // 16-byte pieces per thread and turn
 
-// CTA (unit * slices + slice) * parts + part: a stretch of 2^cshift 16-byte pieces of every row.
-__global__ void __launch_bounds__(kMoveThreads) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
-                                                            int cshift, int parts) {
+// t / P and t % P: P a power of two (its shift), or any (shift -1).
+struct Paging {
+    int P, shift;
+    __device__ __forceinline__ int page(int t) const { return shift >= 0 ? t >> shift : t / P; }
+    __device__ __forceinline__ int row(int t) const { return shift >= 0 ? t & (P - 1) : t % P; }
+};
+
+// CTA ((unit * slices + slice) * groups + group) * cluster + rank: a stretch of 2^cshift 16-byte pieces of every row.
+// In turn s of its group (groups * cluster of them share the rows that move to other pages) CTA `rank` takes
+// `step` rows. Three turns ahead of the write it reads which rows, two ahead their pages, one ahead the rows.
+__global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
+                                                            int cshift, int groups, int cluster, const Paging pg) {
     grid_dep_wait();
     grid_dep_launch();
     const Geometry &geo = a.geo;
-    const int part = blockIdx.x % parts, slice = blockIdx.x / parts % slices, unit = blockIdx.x / parts / slices;
+    const int rank = blockIdx.x % cluster, group = blockIdx.x / cluster % groups;
+    const int slice = blockIdx.x / cluster / groups % slices, unit = blockIdx.x / cluster / groups / slices;
     const int tid = threadIdx.x;
-    const int b = unit / geo.Hkv, g = unit % geo.Hkv, P = geo.P;
+    const int b = unit / geo.Hkv, g = unit % geo.Hkv;
     const EvictUnit u = units[unit];
+    // (the whole cluster leaves)
     if (u.rows < 0) return;
-    if (g == 0 && slice == 0 && part == 0 && tid == 0) a.new_lens[b] = u.rows;
-    int j0 = 0, j1 = u.rows;
+    if (g == 0 && slice == 0 && group == 0 && rank == 0 && tid == 0) a.new_lens[b] = u.rows;
+    if (u.in_place && group > 0) return;
     constexpr int kStep = kMoveThreads * kMoveDepth;
-    const int step = kStep >> cshift;                    // rows per step
-    if (u.in_place) {
-        if (part > 0) return;
-    } else {
-        const int per = ((u.rows + parts - 1) / parts + step - 1) / step * step;
-        j0 = min(part * per, u.rows);
-        j1 = min(j0 + per, u.rows);
-    }
+    const int step = kStep >> cshift;                    // rows of a CTA per turn
+    const int turn = step * cluster * (u.in_place ? 1 : groups);
     const int32_t *from = a.block_table + (size_t)b * geo.max_pages, *to = a.new_table + (size_t)b * geo.max_pages;
     const int32_t *kept = a.kept + (size_t)unit * a.budget;
-    const int cpr = geo.D / 8, c = (slice << cshift) + (tid & ((1 << cshift) - 1)), r = tid >> cshift;
+    const int cpr = geo.D / 8, c = (slice << cshift) + (tid & ((1 << cshift) - 1));
     const int rstep = kMoveThreads >> cshift;
     uint4 *const v = reinterpret_cast<uint4 *>(a.v_cache);
-    auto piece = [&](const int32_t *table, int t) -> uint4 * {
-        return v + (((int64_t)table[t / P] * geo.Hkv + g) * P + t % P) * cpr + c;
+    auto piece = [&](int page, int t) -> uint4 * {
+        return v + (((int64_t)page * geo.Hkv + g) * geo.P + pg.row(t)) * cpr + c;
     };
+    const int first = (u.in_place ? rank : group * cluster + rank) * step + (tid >> cshift);
+    // of this thread's kMoveDepth rows: which (of turn s + 2 at the loop's head), their pages and rows (s + 1)
     uint4 x[kMoveDepth], y[kMoveDepth];
-    auto load = [&](int j, uint4 (&d)[kMoveDepth]) {
+    int id[kMoveDepth], page[kMoveDepth], next[kMoveDepth];
+    auto each = [&](int j, auto &&f) {
 #pragma unroll
-        for (int k = 0; k < kMoveDepth; ++k) {
-            const int at = j + r + k * rstep;
-            if (at < j1) d[k] = *piece(from, kept[at]);
-        }
+        for (int k = 0; k < kMoveDepth; ++k)
+            if (j + k * rstep < u.rows) f(k, j + k * rstep);
     };
-    load(j0, x);
-    for (int j = j0; j < j1; j += step) {
-        load(j + step, y);
-        if (u.in_place) __syncthreads();                 // this step's and the next one's rows have been read
-#pragma unroll
-        for (int k = 0; k < kMoveDepth; ++k) {
-            const int at = j + r + k * rstep;
-            if (at < j1) *piece(to, at) = x[k];
-            x[k] = y[k];
+    each(first, [&](int k, int at) { id[k] = kept[at]; });
+    each(first + turn, [&](int k, int at) { next[k] = kept[at]; });
+    each(first, [&](int k, int) { page[k] = from[pg.page(id[k])]; });
+    each(first, [&](int k, int) { x[k] = *piece(page[k], id[k]); });
+    each(first + turn, [&](int k, int) { page[k] = from[pg.page(next[k])]; id[k] = next[k]; });
+    each(first + 2 * turn, [&](int k, int at) { next[k] = kept[at]; });
+    const int turns = (u.rows + turn - 1) / turn;        // (as many in all CTAs: they meet)
+    for (int s = 0, j = first; s < turns; ++s, j += turn) {
+        each(j + turn, [&](int k, int) { y[k] = *piece(page[k], id[k]); });
+        each(j + 2 * turn, [&](int k, int) { page[k] = from[pg.page(next[k])]; id[k] = next[k]; });
+        each(j + 3 * turn, [&](int k, int at) { next[k] = kept[at]; });
+        if (u.in_place) {                                // the rows of this turn and the next one have been read
+            if (cluster > 1) cluster_sync();
+            else __syncthreads();
         }
+        each(j, [&](int k, int at) { *piece(to[pg.page(at)], at) = x[k]; });
+#pragma unroll
+        for (int k = 0; k < kMoveDepth; ++k) x[k] = y[k];
     }
 }
 
@@ -276,17 +388,19 @@ cudaError_t launch_evict(const EvictArgs &a) {
            ((longest > (int64_t)cluster * KL_EVICT_MAX_TOKENS / kMostCluster) ||
             (2 * (int64_t)units * cluster <= sms && longest >= 4096 * (int64_t)cluster)))
         cluster *= 2;
-    const int piece = (int)((longest + cluster - 1) / cluster + 31) & ~31;
+    const int piece = (int)((longest + cluster - 1) / cluster + 127) & ~127;
     EvictUnit *info = static_cast<EvictUnit *>(a.workspace);
-    static PerDeviceOnce once;
-    const cudaError_t e = once.run([&] {
-        return cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const bool few = units * cluster <= sms;
+    const auto kernel = few ? select_kernel<1024> : select_kernel<512>;
+    static PerDeviceOnce once[2];
+    const cudaError_t e = once[few].run([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     KL_EVICT_MAX_TOKENS / kMostCluster * (int)sizeof(float));
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(units * cluster));
-    cfg.blockDim = dim3(kSelThreads);
+    cfg.blockDim = dim3(few ? 1024 : 512);
     cfg.dynamicSmemBytes = piece * sizeof(float);
     cfg.stream = a.stream;
     cudaLaunchAttribute attr[2];
@@ -297,23 +411,30 @@ cudaError_t launch_evict(const EvictArgs &a) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t s = cudaLaunchKernelEx(&cfg, select_kernel, a, info, cluster, piece);
+    cudaError_t s = cudaLaunchKernelEx(&cfg, kernel, a, info, cluster, piece);
     if (s != cudaSuccess) return s;
-    // 64-byte stretches where there are few units, whole rows where they fill the GPU
+    // As many CTAs as the GPU holds at a time, four per SM: clusters of them while there are few units, then 64-byte
+    // stretches instead of whole rows, then (to other pages) groups of clusters.
     const int cpr = g.D / 8;
-    int cshift = 2;
-    while ((1 << cshift) < cpr && (int64_t)units * (cpr >> (cshift + 1)) >= 2 * sms) ++cshift;
+    const int64_t wanted = 4 * sms;
+    int team = 1, cshift = g.D == 128 ? 4 : 3;
+    while (team < kMostCluster && 2 * units * team <= wanted && (kMoveThreads * kMoveDepth >> cshift) * team < a.budget) team *= 2;
+    while (cshift > 2 && 2 * (int64_t)units * team * (cpr >> cshift) <= wanted) --cshift;
     const int slices = cpr >> cshift, step = kMoveThreads * kMoveDepth >> cshift;
-    int64_t parts = (4 * (int64_t)sms + units * slices - 1) / ((int64_t)units * slices);
-    const int64_t most = (a.budget + step - 1) / step;
-    parts = parts > most ? most : parts;
+    int64_t groups = wanted / ((int64_t)units * slices * team);
+    const int64_t most = (a.budget + (int64_t)step * team - 1) / ((int64_t)step * team);
+    groups = groups < 1 ? 1 : groups > most ? most : groups;
+    int shift = 0;
+    while (1 << shift < g.P) ++shift;
+    const Paging pg{g.P, 1 << shift == g.P ? shift : -1};
     cudaLaunchConfig_t mv = {};
-    parts = parts < 1 ? 1 : parts;
-    mv.gridDim = dim3((unsigned)(parts * units * slices));
+    mv.gridDim = dim3((unsigned)(groups * units * slices * team));
     mv.blockDim = dim3(kMoveThreads);
     mv.stream = a.stream;
-    const OverlapAttr overlap(mv);
-    return cudaLaunchKernelEx(&mv, move_kernel, a, (const EvictUnit *)info, slices, cshift, (int)parts);
+    attr[1].val.clusterDim.x = team;
+    mv.attrs = attr;
+    mv.numAttrs = 2;
+    return cudaLaunchKernelEx(&mv, move_kernel, a, (const EvictUnit *)info, slices, cshift, (int)groups, team, pg);
 }
 
 }  // namespace kl
