@@ -74,6 +74,16 @@ __device__ __forceinline__ void add_cluster(const int *p, int rank, int cluster,
             for (int e = 0; e < 4; ++e) n[e] += v[4 * c + e];
 }
 
+// Writes n to `p` (16-byte aligned) in the shared memory of CTA `rank`.
+__device__ __forceinline__ void st_cluster(int *p, int rank, const int (&n)[4]) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(at)
+                 : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(n[0]), "r"(n[1]), "r"(n[2]), "r"(n[3])
+                 : "memory");
+}
+
 // Weights in their order as whole numbers; what is not positive, and NaN, is 0.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
 
@@ -83,7 +93,7 @@ template <int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kernel(const EvictArgs a, EvictUnit *units, int cluster, int piece) {
     constexpr int kSelWarps = kThreads / 32;
     extern __shared__ __align__(16) float held[];        // [piece]
-    __shared__ __align__(16) int hist[2][kBins];
+    __shared__ __align__(16) int hist[kBins], sums[kBins];   // of this CTA, of the cluster
     __shared__ int count[2];                             // of this CTA's piece: above the border, on it
     __shared__ int warp_above[kSelWarps], warp_on[kSelWarps];
     __shared__ uint32_t border;
@@ -164,37 +174,49 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
         const int bits = round == 0 ? kBits0 : kBits;
         const uint32_t known = round == 0 ? 0u : ~0u << shift;   // bits found so far
         shift -= bits;
-        int *const h = hist[round & 1];
+        int *const h = hist;
         for (int i = tid; i < kBins; i += kThreads) h[i] = 0;
         __syncthreads();
-        // four consecutive weights per thread
-        for (int base = 0; base < t1 - t0; base += 4 * kThreads) {
-            const int at = base + 4 * tid;
-            if (t0 + at >= t1) break;
+        // four consecutive weights per thread (those at the ends of the middle one by one)
+        for (int at = 4 * tid; at < t1 - t0; at += 4 * kThreads) {
             const float4 x = *reinterpret_cast<const float4 *>(held + at);
-            const float xs[4] = {x.x, x.y, x.z, x.w};
+            uint32_t k[4] = {weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w)};
+            const int from_mid = t0 + at - mid0;
+            const uint32_t mids = (uint32_t)(min(t1, mid1) - mid0);
+            bool in[4], any = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t k = weight_key(xs[e]);
-                const int t = t0 + at + e;
-                if ((k & known) == key && t >= mid0 && t < min(t1, mid1)) atomicAdd(h + ((k >> shift) & ((1u << bits) - 1)), 1);
+                in[e] = ((k[e] ^ key) & known) == 0 && (uint32_t)(from_mid + e) < mids;
+                any |= in[e];
             }
+            if (any)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (in[e]) atomicAdd(h + ((k[e] >> shift) & ((1u << bits) - 1)), 1);
         }
-        if (cluster > 1) cluster_sync();
-        else __syncthreads();
+        if (cluster > 1) {
+            // each CTA adds up a share of the bins and gives it to all
+            cluster_sync();
+            const int share = kBins / cluster;
+            if (4 * tid < share) {
+                int *const mine = h + rank * share + 4 * tid;
+                int n[4] = {0, 0, 0, 0};
+                for (int c = 0; c < cluster; c += 4) add_cluster(mine, c, cluster, n);
+                for (int c = 0; c < cluster; ++c) st_cluster(sums + (mine - h), c, n);
+            }
+            cluster_sync();
+        } else {
+            __syncthreads();
+        }
         // the bin of the want-th largest: bins from the top, kPerThread per thread
         const int low = kBins - kPerThread * (tid + 1);          // its lowest bin
         int n[kPerThread] = {0, 0, 0, 0}, sum = 0, upto = 0;
         if (warp < kBinWarps) {
-            if (cluster > 1) {
-                for (int c = 0; c < cluster; c += 4) add_cluster(h + low, c, cluster, n);
-            } else {
-                const int4 x = *reinterpret_cast<const int4 *>(h + low);
-                n[0] = x.x;
-                n[1] = x.y;
-                n[2] = x.z;
-                n[3] = x.w;
-            }
+            const int4 x = *reinterpret_cast<const int4 *>((cluster > 1 ? sums : h) + low);
+            n[0] = x.x;
+            n[1] = x.y;
+            n[2] = x.z;
+            n[3] = x.w;
             sum = upto = n[0] + n[1] + n[2] + n[3];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -273,8 +295,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
     }
     before = __reduce_add_sync(0xffffffffu, before);
     on_before = __reduce_add_sync(0xffffffffu, on_before);
-    // (Here and not earlier: CTAs of the move that come while only some SMs have room crowd those. 64 sequences of
-    // 8192 rows, 4096 of which stay: 259 us with the signal at the top.)
     grid_dep_launch();
     int32_t *kept = a.kept + (size_t)unit * a.budget;
     float *nw = a.new_weights + (size_t)unit * a.stride;
@@ -308,7 +328,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
     if (cluster > 1) cluster_sync();                     // (the counts are read)
 }
 
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 128, kMoveCtas = 8;         // per SM
+constexpr int64_t kEarlyBytes = 256 << 20;               // of rows: up to here the move starts early
 constexpr int kMoveDepth = 4;                            // 16-byte pieces per thread and turn
 
 // t / P and t % P: P a power of two (its shift), or any (shift -1).
@@ -321,7 +342,7 @@ struct Paging {
 // CTA ((unit * slices + slice) * groups + group) * cluster + rank: a stretch of 2^cshift 16-byte pieces of every row.
 // In turn s of its group (groups * cluster of them share the rows that move to other pages) CTA `rank` takes
 // `step` rows. Three turns ahead of the write it reads which rows, two ahead their pages, one ahead the rows.
-__global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
+__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
                                                             int cshift, int groups, int cluster, const Paging pg) {
     grid_dep_wait();
     grid_dep_launch();
@@ -413,12 +434,13 @@ cudaError_t launch_evict(const EvictArgs &a) {
     cfg.numAttrs = 2;
     cudaError_t s = cudaLaunchKernelEx(&cfg, kernel, a, info, cluster, piece);
     if (s != cudaSuccess) return s;
-    // As many CTAs as the GPU holds at a time, four per SM: clusters of them while there are few units, then 64-byte
+    // As many CTAs as the GPU holds at a time, eight per SM: clusters of them while there are few units, then 64-byte
     // stretches instead of whole rows, then (to other pages) groups of clusters.
     const int cpr = g.D / 8;
-    const int64_t wanted = 4 * sms;
+    const int64_t wanted = kMoveCtas * sms;
     int team = 1, cshift = g.D == 128 ? 4 : 3;
-    while (team < kMostCluster && 2 * units * team <= wanted && (kMoveThreads * kMoveDepth >> cshift) * team < a.budget) team *= 2;
+    while (cshift > 3 && 2 * (int64_t)units * (cpr >> cshift) <= wanted) --cshift;
+    while (team < kMostCluster && 2 * (int64_t)units * team * (cpr >> cshift) <= wanted && (kMoveThreads * kMoveDepth >> cshift) * team < a.budget) team *= 2;
     while (cshift > 2 && 2 * (int64_t)units * team * (cpr >> cshift) <= wanted) --cshift;
     const int slices = cpr >> cshift, step = kMoveThreads * kMoveDepth >> cshift;
     int64_t groups = wanted / ((int64_t)units * slices * team);
@@ -432,6 +454,10 @@ cudaError_t launch_evict(const EvictArgs &a) {
     mv.blockDim = dim3(kMoveThreads);
     mv.stream = a.stream;
     attr[1].val.clusterDim.x = team;
+    // An early start saves a launch's latency, but the CTAs then crowd the SMs that the selection leaves first (64 x
+    // 8192 rows to 4096, 8 heads, 1 GB of traffic: 242 us with it)
+    if ((int64_t)units * (a.budget < longest ? a.budget : longest) * g.D * 4 > kEarlyBytes)
+        attr[0].val.programmaticStreamSerializationAllowed = 0;
     mv.attrs = attr;
     mv.numAttrs = 2;
     return cudaLaunchKernelEx(&mv, move_kernel, a, (const EvictUnit *)info, slices, cshift, (int)groups, team, pg);
