@@ -14,13 +14,15 @@
 namespace kl {
 namespace {
 
-constexpr int kAddThreads = 256, kAddPer = 4;            // tokens per thread, kAddThreads apart
-constexpr int kAddTokens = kAddThreads * kAddPer;
+constexpr int kAddThreads = 256;
 constexpr int kAddRows = 256;                            // rows whose {maximum, 1 / sum} a CTA holds at a time
+constexpr int kAddAhead = 8;                             // scores that a thread has on their way, times kAddPer
 
-// CTA (tokens, g, b).
+// CTA (tokens, g, b); kAddPer tokens per thread, kAddThreads apart.
+template <int kAddPer>
 __global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeArgs a, const WeightArgs w) {
     __shared__ float2 row[kAddRows];                     // {maximum, 1 / sum}
+    constexpr int kAddTokens = kAddThreads * kAddPer;
     grid_dep_wait();
     grid_dep_launch();
     const Geometry &geo = a.geo;
@@ -69,15 +71,40 @@ __global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeAr
             const float *s = a.causal.scores + (unit * geo.nhb + hb) * a.causal.rows * a.causal.pitch;
             const float2 *of = row + (hb - k0) * 16;
             const int p0 = L - n + m0;
-#pragma unroll 4
-            for (int r = 0; r < live; ++r) {
-                const int p = p0 + r / hp;
-                const float2 m = of[r];
+            if ((int)(blockIdx.x + 1) * kAddTokens - 1 <= p0) {
+                // all positions see all of these tokens
+                s += t0;
+                int r = 0;
+                for (; r + kAddAhead <= live; r += kAddAhead) {
+                    float x[kAddAhead][kAddPer];
 #pragma unroll
-                for (int k = 0; k < kAddPer; ++k) {
-                    const int t = t0 + k * kAddThreads;
-                    if (t <= p) sum[k] += ptx::ex2(__ldcs(s + r * a.causal.pitch + t) - m.x) * m.y;
+                    for (int e = 0; e < kAddAhead; ++e)
+#pragma unroll
+                        for (int k = 0; k < kAddPer; ++k) x[e][k] = __ldcs(s + (r + e) * a.causal.pitch + k * kAddThreads);
+#pragma unroll
+                    for (int e = 0; e < kAddAhead; ++e) {
+                        const float2 m = of[r + e];
+#pragma unroll
+                        for (int k = 0; k < kAddPer; ++k) sum[k] += ptx::ex2(x[e][k] - m.x) * m.y;
+                    }
                 }
+                for (; r < live; ++r) {
+                    const float2 m = of[r];
+#pragma unroll
+                    for (int k = 0; k < kAddPer; ++k)
+                        sum[k] += ptx::ex2(__ldcs(s + r * a.causal.pitch + k * kAddThreads) - m.x) * m.y;
+                }
+            } else {
+                // draft by draft; a position sees the tokens up to its own
+                for (int r0 = 0, p = p0; r0 < live; r0 += hp, ++p)
+#pragma unroll 4
+                    for (int r = r0; r < min(r0 + hp, live); ++r) {
+                        const float2 m = of[r];
+#pragma unroll
+                        for (int k = 0; k < kAddPer; ++k)
+                            if (t0 + k * kAddThreads <= p)
+                                sum[k] += ptx::ex2(__ldcs(s + r * a.causal.pitch + t0 + k * kAddThreads) - m.x) * m.y;
+                    }
             }
         }
     }
@@ -111,11 +138,14 @@ cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w) {
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     const int64_t longest = (int64_t)g.max_pages * g.P < a.causal.stride ? (int64_t)g.max_pages * g.P : a.causal.stride;
-    cfg.gridDim = dim3((unsigned)((longest + kAddTokens - 1) / kAddTokens), g.Hkv, g.B);
+    // (one token per thread while that leaves places empty)
+    const bool few = longest * g.Hkv * g.B <= 8 * kAddThreads * sms;
+    const int tokens = kAddThreads * (few ? 1 : 4);
+    cfg.gridDim = dim3((unsigned)((longest + tokens - 1) / tokens), g.Hkv, g.B);
     cfg.blockDim = dim3(kAddThreads);
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
-    return cudaLaunchKernelEx(&cfg, add_weights_kernel, la, w);
+    return cudaLaunchKernelEx(&cfg, few ? add_weights_kernel<1> : add_weights_kernel<4>, la, w);
 }
 
 }  // namespace kl
