@@ -670,6 +670,9 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             kRows == kWeights
                 ? a.causal.scores + ((((size_t)b * geo.Hkv + g) * geo.nhb + hb) * a.causal.rows + h0) * a.causal.pitch
                 : nullptr;
+        // kCausal: a warp without a row of the block keeps the barriers and clears rows, and forms no weights (what it
+        // leaves in its columns of P reaches only its columns of O, which nothing reads)
+        const bool live = !kCausal || h0 < G;
         bool carried = ok;
         ok = true;
         for (int i = grp; i < n_tiles; i += NG) {
@@ -706,7 +709,11 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             // the weights against the current references, 8 heads at a time
             float p[KH];
             float pmax = 0.f;
-            if (ready) {
+            if (kCausal && !live) {
+#pragma unroll
+                for (int e = 0; e < KH; ++e) p[e] = 0.f;
+            }
+            if (ready && live) {
                 ptx::tc_fence_after();
 #pragma unroll
                 for (int c = 0; c < KH; c += 8) {
@@ -754,7 +761,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 // the per-head maximum over the tile's 128 tokens becomes the reference
                 if (ready) {
 #pragma unroll
-                    for (int c = 0; c < KH; c += 8) {
+                    for (int c = 0; live && c < KH; c += 8) {
                         float s[8];
                         ld_terms(sc + c, s);
 #pragma unroll
@@ -772,7 +779,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 }
                 ptx::tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < KH; c += 8) {
+                for (int c = 0; live && c < KH; c += 8) {
                     float alpha[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -817,7 +824,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 // every warp has read the old references: the new ones take their place (the
                 // group's next barrier separates the maxima of two slow tiles the same way)
                 ptx::bar_sync(kBarGroup + grp, kWideGroupThreads);
-                if (qd == 0 && lane < KH) {
+                if (qd == 0 && lane < KH && live) {
                     const int h = h0 + lane;
                     mref[lane] = fmaxf(mref[lane], fmaxf(fmaxf(sm.red[grp][0][h], sm.red[grp][1][h]),
                                                          fmaxf(sm.red[grp][2][h], sm.red[grp][3][h])));
@@ -853,7 +860,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             }
             if (!freed) carried = wait(&sm.o_full[grp], (k - 1) & 1);
             if (carried) {
-                if (k > 0) {
+                if (k > 0 && live) {
                     // fold the group's previous tile; this tile's MMAs start over
                     ptx::tc_fence_after();
 #pragma unroll
@@ -863,7 +870,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 }
                 uint8_t *row = sm.p[grp] + (t >> 3) * kGroupBytes + (t & 7) * 16 + (h0 >> 3) * 128;
 #pragma unroll
-                for (int c = 0; c < KH / 8; ++c) {
+                for (int c = 0; live && c < KH / 8; ++c) {
                     *reinterpret_cast<uint4 *>(row + c * 128) =
                         make_uint4(ph[4 * c], ph[4 * c + 1], ph[4 * c + 2], ph[4 * c + 3]);
                     *reinterpret_cast<uint4 *>(row + (NH / 8 + c) * 128) =
