@@ -717,7 +717,10 @@ kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void 
     d.err = err;
     d.wait_ns = current_wait_ns();
     d.stream = reinterpret_cast<cudaStream_t>(stream);
-    return from_cuda(launch_attention_weights(d, WeightArgs{weights, decay, new_weights}));
+    d.causal.weights = weights;
+    d.causal.decay = decay;
+    d.causal.new_weights = new_weights;
+    return from_cuda(launch_attention_weights(d));
 }
 
 size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, int32_t budget) {

@@ -182,6 +182,64 @@ __device__ __forceinline__ float warp_max_redux(float f) {
     return __int_as_float(k >= 0 ? k : k ^ 0x7FFFFFFF);
 }
 
+// kWeights, one block of rows per value head: weights of the `rows` rows at positions p0 + r / hp of (b, g) from their
+// scores and the `runs` runs' {maximum, sum}, added to the old ones of the L tokens. Threads 0 .. kThreads - 1, all
+// behind a barrier that makes the scores visible; `of`: 16 float2 in shared memory that nobody else uses.
+template <int kThreads>
+__device__ void add_unit_weights(const DecodeArgs &a, int b, int g, int rows, int p0, int L, int runs, float2 *of,
+                                 int tid) {
+    const Geometry &geo = a.geo;
+    const size_t unit = (size_t)b * geo.Hkv + g;
+    if (tid < rows) {
+        const float2 *s = a.causal.stats + (unit * 16 + tid) * geo.S;
+        float M = -INFINITY, z = 0.f;
+        for (int i = 0; i < runs; ++i) {
+            const float2 x = __ldcg(s + i);
+            const float top = fmaxf(M, x.x);
+            // (a run of maximum -inf has sum 0, or NaN)
+            z = (M == top ? z : z * ptx::ex2(M - top)) + (x.x == top ? x.y : x.y * ptx::ex2(x.x - top));
+            M = top;
+        }
+        of[tid] = make_float2(M, 1.f / z);
+    }
+    ptx::bar_sync(kBarCompute, kThreads);
+    const float *s = a.causal.scores + unit * a.causal.rows * a.causal.pitch;
+    const float *old = a.causal.weights + unit * a.causal.stride;
+    float *out = a.causal.new_weights + unit * a.causal.stride;
+    const float decay = a.causal.decay;
+    const int hp = a.causal.hp;
+    // four consecutive tokens per thread, eight rows of them on their way
+    for (int t = 4 * tid; t < L; t += 4 * kThreads) {
+        float sum[4] = {0.f, 0.f, 0.f, 0.f}, was[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) was[k] = decay != 0.f && t + k < L ? old[t + k] : 0.f;
+        const bool all = t + 3 <= p0;                    // seen by all rows
+        int p = p0, left = hp;                           // row r's position, and the rows up to the next one
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (r0 + e < rows) x[e] = __ldcg(reinterpret_cast<const float4 *>(s + (r0 + e) * a.causal.pitch + t));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (r0 + e >= rows) break;
+                const float2 m = of[r0 + e];
+                const float xs[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (all || t + k <= p) sum[k] += ptx::ex2(xs[k] - m.x) * m.y;
+                if (--left == 0) {
+                    left = hp;
+                    ++p;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (t + k < L) out[t + k] = decay != 0.f ? fmaf(decay, was[k], sum[k]) : sum[k];
+    }
+}
+
 template <int NH, int NG, bool kExact, int kRows, int T>
 __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kCtas)
     decode_wide_kernel(const __grid_constant__ CUtensorMap vmap,
@@ -280,6 +338,11 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         else if (kRows == kWeights && L_raw > a.causal.stride) L_raw = -1;
         else if (G <= 0 && L_raw <= geo.max_pages * geo.P) L_raw = 0;    // (no rows: an empty run)
     }
+    // kWeights: a sequence without new tokens, whose weights fade
+    const int fades = kRows == kWeights && geo.nhb == 1 && drafts == 0 && a.seq_lens[b] <= a.causal.stride &&
+                              a.seq_lens[b] <= geo.max_pages * geo.P && L_raw == 0
+                          ? a.seq_lens[b]
+                          : 0;
     // kCausal: the block's positions, and the line of tiles that they see
     const int p0 = L_raw - drafts + m0, p1 = p0 + min(a.causal.rpb, drafts - m0) - 1;
     const int window = kRows == kWindow ? a.causal.window : INT32_MAX / 2, sinks = kRows == kWindow ? a.causal.sinks : 0;
@@ -361,6 +424,11 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 else static_cast<__nv_bfloat16 *>(a.out)[oi] = __float2bfloat16_rn(0.f);
             }
         }
+        if (kRows == kWeights && fades > 0 && cta == 0) {
+            const size_t at = ((size_t)b * geo.Hkv + g) * a.causal.stride;
+            for (int t0 = tid; t0 < fades; t0 += W::kThreads)
+                a.causal.new_weights[at + t0] = a.causal.decay != 0.f ? a.causal.decay * a.causal.weights[at + t0] : 0.f;
+        }
         if (warp == kWideMma) ptx::tmem_dealloc(sm.tmem_base, kWideTmemCols);
         if (warp == kWideProducer) {
             for (int r = 0; r < early_route; ++r) {
@@ -406,6 +474,8 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             issued = r + 1;
         }
         const int split_pages = end_page - first_page;
+        // kWeights: the cached rows leave L2 before the scores, which are read back soon
+        const uint64_t policy = kRows == kWeights ? ptx::policy_once() : 0;
         const int low = p0 - window + 1;                 // kWindow: the first token that the window shows
         int bt_batch = 0;
         for (int i = 0; ok && i < n_tiles; ++i) {
@@ -437,6 +507,11 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 [&] { ptx::mbar_arrive_expect_tx(&sm.full[s], __popc(mask) * page_bytes * 2u); },
                 [&](int p, int row) {
                     uint8_t *dst = sm.tiles[s] + p * page_bytes;
+                    if constexpr (kRows == kWeights) {
+                        ptx::tma_load_2d_policy(dst, &vmap, &sm.full[s], 0, row, policy);
+                        ptx::tma_load_2d_policy(dst + kHalfBytes, &vmap, &sm.full[s], 64, row, policy);
+                        return;
+                    }
                     ptx::tma_load_2d(dst, &vmap, &sm.full[s], 0, row);
                     ptx::tma_load_2d(dst + kHalfBytes, &vmap, &sm.full[s], 64, row);
                 });
@@ -990,6 +1065,14 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 ptx::bar_sync(kBarCompute, kWideComputeThreads);
                 if (sm.is_last)
                     merge_states<kWideWarps, kD>(sm, a, state0, out_row, G, n_cta_u, tid, warp, lane, wait);
+            }
+            if constexpr (kRows == kWeights) {
+                if (geo.nhb == 1 && (write_out || sm.is_last)) {
+                    // (the merge leaves the front of the query operand alone, and everything has been read there)
+                    ptx::bar_sync(kBarCompute, kWideComputeThreads);
+                    add_unit_weights<kWideComputeThreads>(a, b, g, G, p0, p1 + 1, n_cta_u,
+                                                          reinterpret_cast<float2 *>(sm.qr), tid);
+                }
             }
         }
     }

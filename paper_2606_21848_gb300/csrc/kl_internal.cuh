@@ -93,14 +93,10 @@ struct DecodeArgs {
         int64_t pitch = 0;
         float *scores = nullptr;
         float2 *stats = nullptr;
+        const float *weights = nullptr;   // [B][Hkv][stride]; not read where decay is 0
+        float decay = 0.f;
+        float *new_weights = nullptr;     // [B][Hkv][stride]
     } causal;
-};
-
-// What kl_attention_weights adds to its attention's arguments.
-struct WeightArgs {
-    const float *weights;     // [B][Hkv][stride]; not read where decay is 0
-    float decay;
-    float *new_weights;       // [B][Hkv][stride]
 };
 
 // Arguments of a kl_evict launch. The workspace holds kEvictUnitBytes for every sequence and value head.
@@ -333,7 +329,7 @@ cudaError_t launch_tree_wide(const DecodeArgs &a);
 // prefill's; with all tokens before a position and each cached row's weight added up.
 cudaError_t launch_window_wide(const DecodeArgs &a);
 cudaError_t launch_window_tc(const PrefillArgs &a);
-cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w);
+cudaError_t launch_attention_weights(const DecodeArgs &a);
 cudaError_t launch_evict(const EvictArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
                                const int32_t *path_lens, int max_path, const int32_t *block_table,

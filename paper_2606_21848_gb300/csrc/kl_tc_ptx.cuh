@@ -124,6 +124,23 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, u
         : "memory");
 }
 
+// An L2 policy for data that is read once: its lines are the first to go.
+__device__ __forceinline__ uint64_t policy_once() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+
+// tma_load_2d under an L2 policy.
+__device__ __forceinline__ void tma_load_2d_policy(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y,
+                                                   uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint "
+        "[%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_addr(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_addr(bar)), "l"(policy)
+        : "memory");
+}
+
 // The producers' page loop: lane p < 8 of the (converged) warp holds the row coordinate of page p
 // of a tile, `mask` the pages to load; one elected lane runs `load(p, row)` for each of them with
 // warp-uniform coordinates. TMA operands are uniform registers: issued by each page's own lane, a

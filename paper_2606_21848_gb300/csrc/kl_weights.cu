@@ -7,8 +7,9 @@
 // The attention is the wide decode's kernel (kl_decode_wide_kernel.cuh, kWeights) in blocks of up to 16 (position,
 // head) rows, with query and weights of three bf16 terms, since the weights are fp32 results whatever type the
 // outputs have. A weight needs its row's whole softmax: the kernel writes the scores (4 bytes per row and token, 32
-// per cached row of 256 where a group has 8 heads) and a second kernel, its programmatic dependent, reads them back
-// with the runs' {maximum, sum}. Rows are added in their order: the sums are the same on every run.
+// per cached row of 256 where a group has 8 heads), and the last CTA of a value head reads them back, mostly from
+// L2, with the runs' {maximum, sum}. Where a value head has several blocks of rows, a second kernel, the first's
+// programmatic dependent, does that. Rows are added in their order: the sums are the same on every run.
 #include "kl_rows_wide.cuh"
 
 namespace kl {
@@ -20,12 +21,13 @@ constexpr int kAddAhead = 8;                             // scores that a thread
 
 // CTA (tokens, g, b); kAddPer tokens per thread, kAddThreads apart.
 template <int kAddPer>
-__global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeArgs a, const WeightArgs w) {
+__global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeArgs a) {
     __shared__ float2 row[kAddRows];                     // {maximum, 1 / sum}
     constexpr int kAddTokens = kAddThreads * kAddPer;
     grid_dep_wait();
     grid_dep_launch();
     const Geometry &geo = a.geo;
+    const auto &w = a.causal;
     const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
     const int q0 = a.tree.cu_q[b], q1 = a.tree.cu_q[b + 1], n = q1 - q0, L = a.seq_lens[b];
     if (q0 < 0 || n < 0 || q1 > a.tree.total_q || n > a.tree.max_q || L < n || L > a.causal.stride ||
@@ -124,7 +126,7 @@ cudaError_t launch_scores(const DecodeArgs &la, const CUtensorMap &vmap, const C
 
 }  // namespace
 
-cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w) {
+cudaError_t launch_attention_weights(const DecodeArgs &a) {
     DecodeArgs la = a;
     Geometry &g = la.geo;
     const int64_t sms = device_sm_count(), ctas = (int64_t)g.B * g.Hkv * g.nhb;
@@ -135,7 +137,7 @@ cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w) {
     CUtensorMap vmap, wmap, qmap;
     if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
     cudaError_t e = two_per_sm ? launch_scores<1>(la, vmap, wmap, qmap) : launch_scores<2>(la, vmap, wmap, qmap);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || g.nhb == 1) return e;        // (one block per value head adds its weights itself)
     cudaLaunchConfig_t cfg = {};
     const int64_t longest = (int64_t)g.max_pages * g.P < a.causal.stride ? (int64_t)g.max_pages * g.P : a.causal.stride;
     // (one token per thread while that leaves places empty)
@@ -145,7 +147,7 @@ cudaError_t launch_attention_weights(const DecodeArgs &a, const WeightArgs &w) {
     cfg.blockDim = dim3(kAddThreads);
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
-    return cudaLaunchKernelEx(&cfg, few ? add_weights_kernel<1> : add_weights_kernel<4>, la, w);
+    return cudaLaunchKernelEx(&cfg, few ? add_weights_kernel<1> : add_weights_kernel<4>, la);
 }
 
 }  // namespace kl
