@@ -37,6 +37,7 @@ namespace {
 constexpr int kChunkQuantum = 128;  // split boundaries fall on multiples of 128 tokens
 constexpr int kSimtMaxGroup = 8;    // query heads per value head of the CUDA-core kernel
 constexpr int kMaxSplits = 1024;
+constexpr int kCausalMostRuns = 256;   // states of a block that one CTA merges
 
 bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -536,11 +537,21 @@ void plan_causal(int NH, int32_t max_q_len, DecodeArgs *d) {
     g.nhb = c.nhg * ((max_q_len + c.rpb - 1) / c.rpb);
 }
 
-// Splits of blocks of up to Lmax tokens. Whole where the blocks have more counters than the front region that
-// every workspace shares.
-void plan_causal_splits(int32_t num_splits, int64_t Lmax, Geometry *g) {
-    const int64_t ctas = (int64_t)(g->B > 0 ? g->B : 1) * g->Hkv * g->nhb;
-    plan_splits(ctas > (int64_t)kCounterFloor ? 1 : num_splits, Lmax, ctas, g);
+// The runs of blocks of NH rows and up to `longest` tokens (terms: of their operands). Whole where the blocks have more
+// counters than the front region that every workspace shares. Returns the rows of states that the runs leave.
+size_t plan_causal_runs(int32_t num_splits, int64_t longest, int NH, int terms, DecodeArgs *d) {
+    Geometry &g = d->geo;
+    const int64_t sms = device_sm_count(), units = (int64_t)(g.B > 0 ? g.B : 1) * g.Hkv * g.nhb;
+    // Two CTAs per SM where there are blocks for them; with three terms these have rings of two tiles, which suits
+    // short lines alone.
+    d->causal.two_per_sm = NH == 16 && units > sms && (terms == 2 || longest <= 32 * 128);
+    const CausalRuns r = plan_runs(units, longest, units > (int64_t)kCounterFloor ? 1 : num_splits,
+                                   d->causal.two_per_sm ? 2 * sms : sms, kCausalMostRuns);
+    g.S = r.splits;
+    g.chunk = r.chunk;
+    g.spc = r.spc;
+    d->causal.whole = units > (int64_t)kCounterFloor ? (int)units : r.whole;
+    return (size_t)(units - d->causal.whole) * NH * g.S;
 }
 
 // A kl_window_attention call: on the wide decode's kernel (d), or on the prefill's, which needs no workspace.
@@ -568,8 +579,8 @@ kl_status plan_window_call(const kl_shape *shape, int32_t total_q, int32_t max_q
         return KL_OK;
     }
     plan_causal(NH, max_q, &c->d);
-    plan_causal_splits(num_splits, window_line(c->d.causal.rpb, c->d.causal.window, c->d.causal.sinks, longest), &g);
-    const size_t state_rows = (size_t)units * g.nhb * NH * g.S;
+    const int64_t line = window_line(c->d.causal.rpb, c->d.causal.window, c->d.causal.sinks, longest);
+    const size_t state_rows = plan_causal_runs(num_splits, line, NH, fp32 ? 3 : 2, &c->d);
     c->w = shared_layout((size_t)units * g.nhb, state_rows * g.D * sizeof(float), state_rows * 2 * sizeof(float));
     return KL_OK;
 }
@@ -592,13 +603,13 @@ kl_status plan_weights_call(const kl_shape *shape, int32_t total_q, int32_t max_
     const int64_t tokens = (int64_t)g.max_pages * g.P, longest = tokens < weights_stride ? tokens : weights_stride;
     const int64_t units = (int64_t)g.B * g.Hkv;
     plan_causal(16, max_q_len > 0 ? max_q_len : 1, &c->d);
-    plan_causal_splits(num_splits, longest, &g);
+    const size_t state_rows = plan_causal_runs(num_splits, longest, 16, 3, &c->d);
     c->d.causal.stride = weights_stride;
     c->d.causal.pitch = (longest + 31) / 32 * 32;
     const size_t blocks = (size_t)units * g.nhb, rows = blocks * 16 * g.S;
-    c->stats = round_up(rows * 2 * sizeof(float), 256);
-    c->scores = 2 * c->stats;
-    c->w = shared_layout(blocks, rows * g.D * sizeof(float),
+    c->stats = round_up(state_rows * 2 * sizeof(float), 256);
+    c->scores = c->stats + round_up(rows * 2 * sizeof(float), 256);
+    c->w = shared_layout(blocks, state_rows * g.D * sizeof(float),
                          c->scores + blocks * c->d.causal.rows * c->d.causal.pitch * sizeof(float));
     return KL_OK;
 }

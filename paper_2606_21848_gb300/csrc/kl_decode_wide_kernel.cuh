@@ -264,11 +264,18 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
     S &sm = *reinterpret_cast<S *>(smem_wide);
 
     const Geometry &geo = a.geo;
-    const int hb = blockIdx.x % geo.nhb, cta = blockIdx.x / geo.nhb;
-    const int g = blockIdx.y, b = blockIdx.z;
+    // kCausal: a line of CTAs, units in the order of (b, g, block of rows)
+    const int runs = kCausal ? (geo.S + geo.spc - 1) / geo.spc : 1;
+    const bool whole = kCausal && (int)blockIdx.x < a.causal.whole;
+    const int part = (int)blockIdx.x - a.causal.whole;
+    const int unit = !kCausal ? 0 : whole ? (int)blockIdx.x : a.causal.whole + part / runs;
+    const int hb = kCausal ? unit % geo.nhb : blockIdx.x % geo.nhb;
+    const int cta = !kCausal ? blockIdx.x / geo.nhb : whole ? 0 : part % runs;
+    const int g = kCausal ? unit / geo.nhb % geo.Hkv : blockIdx.y, b = kCausal ? unit / geo.nhb / geo.Hkv : blockIdx.z;
+    const int spc = whole ? geo.S : geo.spc;             // splits per CTA
     // kTree: the sequence's drafts, rows drafts0 .. + drafts - 1 of q and out, its last cached rows
     int drafts0 = 0, drafts = 1;
-    const int split0 = cta * geo.spc;
+    const int split0 = cta * spc;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     int G = min(NH, geo.G - NH * hb);                    // query heads (rows) of this CTA
@@ -284,7 +291,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         return (size_t)b * geo.Hq + qh0 + h;
     };
     const size_t state0 =
-        kCausal ? (((size_t)b * geo.Hkv + g) * geo.nhb + hb) * NH
+        kCausal ? ((size_t)unit - a.causal.whole) * NH
         : kTree ? ((size_t)b * geo.Hkv + g) * geo.G * a.tree.max_q + row0 : (size_t)b * geo.Hq + qh0;
     const bool route = a.w_r != nullptr;                 // else q is the composed query
     const bool route_pq = route && geo.wr_per_qh;
@@ -398,11 +405,11 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
         if (tid == 0 && cta == 0 && g == 0) raise_flag(a.err, KL_FLAG_BAD_LENGTH);
         L = 0;
     }
-    const int t_end = min(t_begin + geo.spc * geo.chunk, L);
+    const int t_end = min(t_begin + spc * geo.chunk, L);
     const int n_tiles = t_end > t_begin ? (t_end - t_begin + kTile - 1) / kTile : 0;
     const bool pos_ok = pos_raw >= 0 && pos_raw < geo.max_pages * geo.P;
     if (a.v_new && !pos_ok && tid == 0 && cta == 0 && g == 0) raise_flag(a.err, KL_FLAG_BAD_POSITION);
-    const bool app_owner = a.v_new && pos_ok && pos_raw / (geo.chunk * geo.spc) == cta;
+    const bool app_owner = a.v_new && pos_ok && pos_raw / (geo.chunk * spc) == cta;
 
     // An empty run: the new row if it lies there, the zero output of an empty sequence, and no
     // part in the merge (which counts only the runs that hold tokens).
@@ -988,7 +995,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
             ptx::tc_fence_after();
             // merge of the two groups' states, thread = output dim t, heads h1 .. h1 + KR - 1:
             // one run of the whole sequence writes the output, else the run's state
-            const int n_cta_u = (L + geo.chunk * geo.spc - 1) / (geo.chunk * geo.spc);
+            const int n_cta_u = (L + geo.chunk * spc - 1) / (geo.chunk * spc);
             const bool write_out = a.direct_out || n_cta_u == 1;
             const bool two = NG == 2 && n_tiles > 1;
             const int mine0 = (n_tiles + NG - 1) / NG;
@@ -1035,7 +1042,7 @@ __global__ void __launch_bounds__(Wide<NH, NG, T>::kThreads, Wide<NH, NG, T>::kC
                 }
                 float val = o / lt;
                 if constexpr (kRows == kWeights) {
-                    if (t == 0) a.causal.stats[(state0 + h) * geo.S + cta] = make_float2(M, lt);
+                    if (t == 0) a.causal.stats[((size_t)unit * NH + h) * geo.S + cta] = make_float2(M, lt);
                 }
                 if constexpr (kTree) {
                     // a run in which the row sees nothing; and the merge, which leaves out states without a
@@ -1107,6 +1114,12 @@ cudaError_t launch_kernel_wide(const DecodeArgs &la, const CUtensorMap &vmap, co
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((g.S + g.spc - 1) / g.spc * g.nhb, g.Hkv, g.B);
+    if (kRows >= kWindow) {
+        const int64_t units = (int64_t)g.B * g.Hkv * g.nhb, whole = la.causal.whole;
+        const int64_t ctas = whole + (units - whole) * ((g.S + g.spc - 1) / g.spc);
+        if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+        cfg.gridDim = dim3((unsigned)ctas);
+    }
     cfg.blockDim = dim3(Wide<NH, NG, T>::kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = la.stream;

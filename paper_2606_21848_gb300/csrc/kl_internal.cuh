@@ -84,8 +84,11 @@ struct DecodeArgs {
     } tree;
     // Its forms for consecutive positions (kl_window_attention, kl_attention_weights; tree.cu_q, total_q and max_q
     // as above): a block is rpb positions of hp heads, a value head's nhg blocks of heads next to each other.
+    // CTAs: the first `whole` units (b, g, block of rows) in one run each, the others in runs of geo.spc splits;
+    // states and sums of the units behind those alone.
     struct {
         int hp = 1, rpb = 1, nhg = 1;
+        int whole = 0, two_per_sm = 0;
         int window = 0, sinks = 0;
         // kl_attention_weights: the scores times log2 e, [B][Hkv][nhb][rows][pitch], each run's {maximum (of
         // these), sum}, [B][Hkv][nhb][16][S], and the longest sequence

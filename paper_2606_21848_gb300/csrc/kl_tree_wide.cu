@@ -11,6 +11,26 @@
 namespace kl {
 namespace {
 
+// Splits per CTA of g.S splits of up to `tiles` tiles for `ctas` blocks (units times blocks of rows) on `slots`
+// places.
+inline int rows_splits_per_cta(const Geometry &g, int64_t tiles, int64_t ctas, int64_t slots) {
+    int spc = splits_per_cta(g.S, ctas, slots);
+    // That fits one wave where it can, even if it leaves places empty; shorter runs in several waves where they are
+    // done a tenth sooner, a CTA costing 8 tiles' time by itself (10 sequences of 40000 tokens, 4 drafts of 64 / 8
+    // heads 215 -> 168 us, 2 drafts 162 -> 140).
+    const auto cost = [&](int n) {
+        return (ctas * ((g.S + n - 1) / n) + slots - 1) / slots * ((tiles * n + g.S - 1) / g.S + 8);
+    };
+    int best = spc;
+    for (int n = (g.S + kWideMaxRuns - 1) / kWideMaxRuns; n < spc; ++n)
+        if (cost(n) < cost(best)) best = n;
+    if (cost(best) * 10 < cost(spc) * 9) spc = best;
+    // (and no more than four waves of CTAs, each of which pays a start: a split count of the caller's may ask for
+    // any number of short runs)
+    while (spc < g.S && (g.S + spc - 1) / spc * ctas > 4 * slots) ++spc;
+    return spc;
+}
+
 template <int NH, int NG, int T>
 cudaError_t launch_tree(const DecodeArgs &la, const CUtensorMap &vmap, const CUtensorMap &wmap,
                         const CUtensorMap &qmap) {

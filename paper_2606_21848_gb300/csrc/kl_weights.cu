@@ -52,7 +52,8 @@ __global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeAr
         const int hb = k0 + tid / 16, r = tid & 15;      // (kAddThreads = kAddRows)
         if (hb < blocks) {
             const int m0 = hb / nhg * rpb, end = L - n + min(m0 + rpb, n);
-            const int runs = (end + geo.chunk * geo.spc - 1) / (geo.chunk * geo.spc);
+            const int spc = (int)(unit * geo.nhb + hb) < a.causal.whole ? geo.S : geo.spc;
+            const int runs = (end + geo.chunk * spc - 1) / (geo.chunk * spc);
             const int live = min(hp, geo.G - hb % nhg * hp) + (min(rpb, n - m0) - 1) * hp;
             if (r < live) {
                 const float2 *s = a.causal.stats + ((unit * geo.nhb + hb) * 16 + r) * geo.S;
@@ -129,11 +130,9 @@ cudaError_t launch_scores(const DecodeArgs &la, const CUtensorMap &vmap, const C
 cudaError_t launch_attention_weights(const DecodeArgs &a) {
     DecodeArgs la = a;
     Geometry &g = la.geo;
-    const int64_t sms = device_sm_count(), ctas = (int64_t)g.B * g.Hkv * g.nhb;
-    const int64_t tiles = ((int64_t)g.max_pages * g.P + 127) / 128;
-    const bool two_per_sm = ctas > sms && tiles <= 32;
+    const int64_t sms = device_sm_count();
+    const bool two_per_sm = a.causal.two_per_sm;
     g.qbox = a.causal.hp * a.causal.rpb;
-    g.spc = rows_splits_per_cta(g, tiles, ctas, two_per_sm ? 2 * sms : sms);
     CUtensorMap vmap, wmap, qmap;
     if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
     cudaError_t e = two_per_sm ? launch_scores<1>(la, vmap, wmap, qmap) : launch_scores<2>(la, vmap, wmap, qmap);

@@ -35,4 +35,56 @@ inline int window_rows(int64_t rows, bool fp32, bool per_qh) {
     return 0;
 }
 
+// How blocks of up to `tiles` tiles of 128 tokens are cut into runs, one per CTA.
+struct CausalRuns {
+    int splits;      // pieces of a line, of `chunk` tokens each
+    int chunk;
+    int spc;         // pieces per run
+    int whole;       // the first units are one run each
+};
+// `units` blocks of rows on `slots` places; num_splits: most runs of a block, 0: chosen here. A CTA costs 8 tiles' time
+// by itself.
+// - Fewer blocks than places: as many runs as fit one wave, or several waves of shorter runs where these are done a
+//   tenth sooner.
+// - More: the last wave's blocks alone are cut, where that is done sooner. (128 sequences with a window of 4160, 8 value
+//   heads: 1024 blocks on 304 places, in 3.4 waves 197 us; 512 blocks of 64 tiles with weights on 152 places 243.)
+inline CausalRuns plan_runs(int64_t units, int64_t max_tokens, int num_splits, int64_t slots, int most_states) {
+    const int64_t tiles = (max_tokens + 127) / 128;
+    const auto cost = [&](int64_t n, int64_t runs) {
+        return (n * runs + slots - 1) / slots * ((tiles + runs - 1) / runs + 8);
+    };
+    const auto cut = [&](int64_t runs, int64_t whole) {
+        CausalRuns r;
+        r.chunk = (int)((tiles + runs - 1) / runs * 128);
+        r.splits = (int)((max_tokens + r.chunk - 1) / r.chunk);
+        r.spc = 1;
+        r.whole = (int)(r.splits > 1 ? whole : units);
+        return r;
+    };
+    if (num_splits > 0) {
+        // (no more than four waves of CTAs, each of which pays a start)
+        int64_t runs = num_splits < tiles ? num_splits : tiles;
+        while (runs > 1 && runs * units > 4 * slots) --runs;
+        return cut(runs, 0);
+    }
+    const int64_t most = tiles / 2 < most_states ? tiles / 2 : most_states;
+    int64_t best = 1;
+    if (units < slots) {
+        for (int64_t runs = 2; runs <= most && runs * units <= slots; ++runs) best = runs;
+        const int64_t one_wave = cost(units, best);
+        int64_t other = best;
+        for (int64_t runs = best + 1; runs <= most && runs * units <= 4 * slots; ++runs)
+            if (cost(units, runs) < cost(units, other)) other = runs;
+        if (cost(units, other) * 10 < one_wave * 9) best = other;
+        return cut(best, 0);
+    }
+    // long lines: runs of at most 8192 tokens, so that batches of any lengths balance
+    const int64_t cap = (max_tokens + 8191) / 8192;
+    if (cap > 1) return cut(cap, 0);
+    const int64_t rest = units % slots;
+    for (int64_t runs = 2; runs <= 4 && runs <= most; ++runs)
+        if (rest && cost(rest, runs) < cost(rest, best)) best = runs;
+    return cut(best, units - rest);
+}
+
 }  // namespace kl

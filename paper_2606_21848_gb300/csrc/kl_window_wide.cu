@@ -22,13 +22,8 @@ cudaError_t launch_window(const DecodeArgs &la, const CUtensorMap &vmap, const C
 cudaError_t launch_window_wide(const DecodeArgs &a) {
     DecodeArgs la = a;
     Geometry &g = la.geo;
-    const int64_t sms = device_sm_count(), ctas = (int64_t)g.B * g.Hkv * g.nhb;
-    const bool fp32 = a.out_dtype == KL_FP32, w32 = a.causal.hp * a.causal.rpb > 16;
-    // (two CTAs per SM as in launch_tree_wide; with three terms these have rings of two tiles)
-    const int64_t tiles = ((int64_t)g.S * g.chunk + 127) / 128;
-    const bool two_per_sm = !w32 && ctas > sms && (!fp32 || tiles <= 32);
+    const bool fp32 = a.out_dtype == KL_FP32, w32 = a.causal.hp * a.causal.rpb > 16, two_per_sm = a.causal.two_per_sm;
     g.qbox = a.causal.hp * a.causal.rpb;
-    g.spc = rows_splits_per_cta(g, tiles, ctas, two_per_sm ? 2 * sms : sms);
     CUtensorMap vmap, wmap, qmap;
     if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
     if (fp32)
