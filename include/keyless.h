@@ -359,10 +359,10 @@ size_t kl_window_workspace_size(const kl_shape *shape, int32_t total_q, int32_t 
  * outputs unspecified (they may raise KL_FLAG_RANGE). A row that is not finite makes the outputs of the
  * positions that see it NaN, and reaches no others.
  * Precision: scores, softmax and sums in fp32. fp32 outputs: the routed query and the weights carry 24
- * significant bits (error about 1e-6). bf16 outputs with R = (Hq / Hkv) * max_q_len <= 32: 16 bits. Other bf16
- * outputs as in kl_prefill_attention: a query of 16 bits, weights and cached values in fp16; there a cached
- * value of magnitude 65536 or more counts as not finite, and a non-finite output raises KL_FLAG_RANGE. (fp32
- * outputs are computed in blocks of 16 rows: long chunks take several times as long as with bf16 outputs.)
+ * significant bits (error about 1e-6). bf16 outputs with R <= 32, R = (Hq / Hkv) * max_q_len (with a W^R per
+ * query head: R <= 16 or max_q_len <= 32): 16 bits. Other bf16 outputs as in kl_prefill_attention: a query of 16
+ * bits, weights and cached values in fp16; there a cached value of magnitude 65536 or more counts as not finite,
+ * and a non-finite output raises KL_FLAG_RANGE.
  */
 kl_status kl_window_attention(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
                               const int32_t *block_table, const int32_t *seq_lens,
@@ -392,8 +392,9 @@ size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t
  * raises KL_FLAG_BAD_LENGTH and is skipped, like those of kl_window_attention; a bad page leaves the
  * sequence's outputs and weights unspecified. A row that is not finite makes the outputs of the positions
  * that see it NaN, and where their scores are not finite the weights that they add as well. Other arguments,
- * shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every run. Two
- * launches. Query, weights and sums carry 24 significant bits for either type of output. Workspace:
+ * shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every run. One
+ * launch, or two. The routed query carries 24 significant bits for either type of output, and so do the weights;
+ * bf16 outputs that kl_window_attention would sum up from fp16 weights and values are so here as well. Workspace:
  * kl_weights_workspace_size bytes of the same arguments, 256-byte aligned.
  */
 kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
@@ -633,8 +634,8 @@ int32_t kl_decode_kernel_available(const kl_shape *shape, int32_t kernel, int32_
  * undefined, and a workspace it used must be zero-filled again before the next call. This sets
  * that limit, in nanoseconds, for every decode launched afterwards by kl_decode_attention(_ex),
  * kl_decode_step, kl_standard_decode, kl_decode_attention_noalloc, the latent decodes and the FP8
- * decodes, and in the same way for kl_tree_attention, for kl_attention_weights and kl_window_attention (but its bf16 outputs
- * with R > 32) and for the waits of kl_token_logprobs for its copies,
+ * decodes, and in the same way for kl_tree_attention, for kl_attention_weights and kl_window_attention where they run on
+ * the decodes' kernels (R <= 32 as defined there) and for the waits of kl_token_logprobs for its copies,
  * process-wide; 0 restores the default. Returns the limit in force before the call. A
  * small value makes the waits run out on purpose: this is how the timeout path is tested. The
  * paper has no counterpart.

@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "kl_internal.cuh"
+#include "kl_prefill_plan.cuh"
 #include "kl_tree_plan.cuh"
 #include "kl_window.cuh"
 
@@ -571,8 +572,8 @@ kl_status plan_window_call(const kl_shape *shape, int32_t total_q, int32_t max_q
     c->d.causal.window = window < longest ? window : (int)longest;
     c->d.causal.sinks = sinks < longest ? sinks : (int)longest;
     const int max_q = max_q_len > 0 ? (max_q_len < longest ? max_q_len : (int)longest) : 1;
-    const int64_t units = (int64_t)g.B * g.Hkv, rows = (int64_t)g.G * max_q;
-    const int NH = window_rows(rows, fp32, g.wr_per_qh != 0);
+    const int64_t units = (int64_t)g.B * g.Hkv;
+    const int NH = window_rows(g.G, max_q, fp32, g.wr_per_qh != 0);
     c->wide = NH > 0;
     if (!c->wide) {
         c->w.total = 0;
@@ -585,10 +586,12 @@ kl_status plan_window_call(const kl_shape *shape, int32_t total_q, int32_t max_q
     return KL_OK;
 }
 
-// The geometry, layout and workspace of a kl_attention_weights call; the scores lie behind the runs' {maximum, sum}
-// in the last region.
+// The geometry, layout and workspace of a kl_attention_weights call, on the wide decode's kernel (d) or the prefill's;
+// the scores lie behind the runs' {maximum, sum} in the last region.
 struct WeightsPlan {
+    bool wide;
     DecodeArgs d;
+    int64_t pitch;
     SharedLayout w;
     size_t stats, scores;
 };
@@ -602,10 +605,21 @@ kl_status plan_weights_call(const kl_shape *shape, int32_t total_q, int32_t max_
     if (max_q_len > KL_WEIGHTS_MAX_ROWS) return KL_ERR_UNSUPPORTED;
     const int64_t tokens = (int64_t)g.max_pages * g.P, longest = tokens < weights_stride ? tokens : weights_stride;
     const int64_t units = (int64_t)g.B * g.Hkv;
-    plan_causal(16, max_q_len > 0 ? max_q_len : 1, &c->d);
+    const int max_q = max_q_len > 0 ? max_q_len : 1;
+    c->pitch = (longest + 63) / 64 * 64;
+    c->wide = window_rows(g.G, max_q, true, g.wr_per_qh != 0) > 0;
+    if (!c->wide) {
+        const PrefillPlan p = plan_prefill(g.B, g.Hkv, g.G, max_q, longest, g.wr_per_qh != 0, device_sm_count());
+        const size_t blocks = (size_t)units * ((g.G + p.hp - 1) / p.hp) * ((max_q + p.rpb - 1) / p.rpb);
+        c->stats = 0;
+        c->scores = round_up(blocks * kPrefillRows * 8 * sizeof(float2), 256);
+        c->w = shared_layout(0, 0, c->scores + blocks * kPrefillRows * c->pitch * sizeof(float));
+        return KL_OK;
+    }
+    plan_causal(16, max_q, &c->d);
     const size_t state_rows = plan_causal_runs(num_splits, longest, 16, 3, &c->d);
     c->d.causal.stride = weights_stride;
-    c->d.causal.pitch = (longest + 31) / 32 * 32;
+    c->d.causal.pitch = c->pitch;
     const size_t blocks = (size_t)units * g.nhb, rows = blocks * 16 * g.S;
     c->stats = round_up(state_rows * 2 * sizeof(float), 256);
     c->scores = c->stats + round_up(rows * 2 * sizeof(float), 256);
@@ -708,6 +722,30 @@ kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void 
         return KL_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < c.w.total || !aligned(workspace, 256)) return KL_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
+    if (!c.wide) {
+        PrefillArgs a{};
+        a.geo = c.d.geo;
+        a.total_q = total_q;
+        a.max_q = max_q_len;
+        a.q = static_cast<const uint16_t *>(q);
+        a.w_r = static_cast<const uint16_t *>(w_r);
+        a.v_cache = static_cast<const uint16_t *>(v_cache);
+        a.block_table = block_table;
+        a.seq_lens = seq_lens;
+        a.cu_q = cu_q_lens;
+        a.pitch = c.pitch;
+        a.stats = reinterpret_cast<float2 *>(ws + c.w.extra + c.stats);
+        a.scores = reinterpret_cast<float4 *>(ws + c.w.extra + c.scores);
+        a.stride = weights_stride;
+        a.weights = weights;
+        a.decay = decay;
+        a.new_weights = new_weights;
+        a.out = out;
+        a.out_dtype = out_dtype;
+        a.err = err;
+        a.stream = reinterpret_cast<cudaStream_t>(stream);
+        return from_cuda(launch_weights_tc(a));
+    }
     DecodeArgs &d = c.d;
     d.q = static_cast<const uint16_t *>(q);
     d.w_r = static_cast<const uint16_t *>(w_r);

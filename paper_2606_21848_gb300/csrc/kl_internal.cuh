@@ -130,6 +130,15 @@ struct PrefillArgs {
     // rpb query rows each; a cluster of cs CTAs splits a block's cache tiles.
     int hp = 1, rpb = 128, cs = 1;
     int window = 0, sinks = 0;   // kl_window_attention (where w_r may be nullptr: q is the composed query)
+    // kl_attention_weights: the scores times log2 e, [block][pitch / 4][128 rows] of four tokens each, and every CTA's
+    // {maximum (of these), sum}, [block][128][8]
+    int64_t pitch = 0;
+    float4 *scores = nullptr;
+    float2 *stats = nullptr;
+    int stride = 0;
+    const float *weights = nullptr;
+    float decay = 0.f;
+    float *new_weights = nullptr;
     const uint16_t *q;        // [total_q][Hq][D] bf16
     const uint16_t *w_r;      // [Hw][D][D] bf16
     const uint16_t *v_cache;  // [num_pages][Hkv][P][D] bf16
@@ -333,6 +342,7 @@ cudaError_t launch_tree_wide(const DecodeArgs &a);
 cudaError_t launch_window_wide(const DecodeArgs &a);
 cudaError_t launch_window_tc(const PrefillArgs &a);
 cudaError_t launch_attention_weights(const DecodeArgs &a);
+cudaError_t launch_weights_tc(const PrefillArgs &a);
 cudaError_t launch_evict(const EvictArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,
                                const int32_t *path_lens, int max_path, const int32_t *block_table,

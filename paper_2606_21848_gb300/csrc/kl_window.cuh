@@ -26,13 +26,14 @@ __host__ __device__ inline int64_t window_line(int64_t rows, int64_t window, int
     return n < max_tokens ? n : max_tokens;
 }
 
-// The rows of a block with `rows` rows per value head (positions x heads of a group): 16 or 32 on the wide
-// decode's kernel, 0: 128 on the prefill's. fp32 outputs take operands of three bf16 terms, and a W^R per query head
-// a place in tensor memory each, which leaves room for 16.
-inline int window_rows(int64_t rows, bool fp32, bool per_qh) {
-    if (rows <= 16 || fp32) return 16;
-    if (rows <= 32) return per_qh ? 16 : 32;
-    return 0;
+// The rows of a block for max_q positions of G heads per value head: 16 or 32 on the wide decode's kernel, 0: 128 on
+// the prefill's. Operands of three bf16 terms (`fine`), and a W^R per query head a place in tensor memory each, leave
+// room for 16 there; the prefill's blocks hold one head's rows where each has its W^R.
+inline int window_rows(int64_t G, int64_t max_q, bool fine, bool per_qh) {
+    const int64_t rows = G * max_q;
+    if (rows <= 16) return 16;
+    if (per_qh ? max_q > 32 : rows > 32) return 0;
+    return fine || per_qh ? 16 : 32;
 }
 
 // How blocks of up to `tiles` tiles of 128 tokens are cut into runs, one per CTA.

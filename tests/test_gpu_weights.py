@@ -179,6 +179,7 @@ def test_a_workspace_shared_with_a_graph_and_the_same_sums_on_every_run():
             n.fill_(-7.0)
 
 
-def test_a_long_sequence():
-    x = inputs((40000, 3), (2, 1), 8, 1, 64)
+@pytest.mark.parametrize("n", [2, 6, 40])
+def test_a_long_sequence(n):
+    x = inputs((40000, 3), (n, 1), 8, 1, 64)
     check(x, 1.0)

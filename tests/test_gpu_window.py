@@ -200,6 +200,19 @@ def test_results_are_the_same_on_every_run():
                 assert torch.equal(window(g, 300, 5, dtype), a)
 
 
+@pytest.mark.parametrize("L", [4096, 4097, 4200, 8192, 8300, 20000])
+@pytest.mark.parametrize("grow", [0.0, 3.0])
+def test_long_lines(L, grow):
+    """Many tiles per block, with scores that stay alike or grow along the sequence (the references move)."""
+    x = inputs((L, 300), (40, 40), 4, 1, 64)
+    if grow:
+        up = torch.linspace(0.2, grow, L)
+        for t in range(L):
+            x["v_cache"][int(x["block_table"][0, t // 64]), :, t % 64] *= up[t].to(torch.bfloat16)
+    for W in (1 << 30, L - 100):
+        both(x, W, 3)
+
+
 @pytest.mark.parametrize("n", [1, 200])
 def test_another_stream(n):
     g = on(inputs((900,), (n,), 16, 2))
