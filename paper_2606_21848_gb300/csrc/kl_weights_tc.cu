@@ -45,32 +45,42 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_weights_kernel(const Prefi
     for (int k = 0; k < blocks; ++k) {
         const int hg = k % nhg, m0 = k / nhg * rpb, hn = min(hp, geo.G - hg * hp), rows = min(rpb, n - m0);
         const size_t blk = ((size_t)(b * geo.Hkv + g) * nhg + hg) * nm + m0 / rpb;
-        const int live = (rows - 1) * hp + hn, end = L - n + m0 + rows;
+        const int live = (rows - 1) * hp + hn, end = L - n + m0 + rows, stop = (end + 63) & ~63;
+        const float4 *const s = a.scores + (blk * (a.pitch / 4) + t0 / 4) * kBM;
+        // (scores behind a position's own token are -inf; behind the block's last half tile there are none)
+        auto load = [&](int r, float4(&x)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                if (r < live && t0 + 4 * i < stop) x[i] = __ldcg(s + i * kBM + r);
+            }
+        };
+        float4 x[8];
+        load(lane, x);                                       // (on their way with the sums)
         if (k) __syncthreads();
         if (tid < live) {
             // every CTA's sum moves to the largest maximum
-            const float2 *s = a.stats + (blk * kBM + tid) * 8;
+            const float2 *of_row = a.stats + (blk * kBM + tid) * 8;
+            float2 y[8];
             float M = -INFINITY, z = 0.f;
-            for (int i = 0; i < cs; ++i) {
-                const float2 x = __ldcg(s + i);
-                const float top = fmaxf(M, x.x);
-                z = (M == top ? z : z * ptx::ex2(M - top)) + (x.x == top ? x.y : x.y * ptx::ex2(x.x - top));
-                M = top;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                y[i] = make_float2(-INFINITY, 0.f);
+                if (i < cs) y[i] = __ldcg(of_row + i);
             }
-            // (heads past the group's have no scores)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) M = fmaxf(M, y[i].x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < cs) z += y[i].x == M ? y[i].y : y[i].y * ptx::ex2(y[i].x - M);
+            // (heads past the group's have no scores: weight 0)
             of[tid] = tid % hp < hn ? make_float2(M, 1.f / z) : make_float2(INFINITY, 0.f);
         }
         __syncthreads();
-        if (t0 >= end) continue;                             // (scores behind a position's own token are -inf)
         for (int r = lane; r < live; r += 32) {
+            if (r != lane) load(r, x);
             const float2 m = of[r];
             if (m.x == INFINITY && m.y == 0.f) continue;
-            const float4 *s = a.scores + (blk * (a.pitch / 4) + t0 / 4) * kBM + r;
-            float4 x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                x[i] = t0 + 4 * i < ((end + 63) & ~63) ? __ldcg(s + i * kBM)
-                                                       : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 sum[4 * i] += ptx::ex2(x[i].x - m.x) * m.y;
