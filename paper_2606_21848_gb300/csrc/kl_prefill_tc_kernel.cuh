@@ -152,6 +152,7 @@ struct __align__(1024) PrefillSmem {
     // kWindow, kWeights: rows that some positions see and that are not finite as fp16: [0] of the tokens behind the block's
     // first position, [1] of those that leave the window within the block, each from its first
     uint32_t over[2][kBM / 32];
+    uint4 stage[kComputeWarps][32 * 4];   // kWindow: a warp's 32 rows of 32 outputs on their way
     uint32_t tmem_base;
     int abort;
 };
@@ -798,7 +799,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ptx::tmem_wait_ld();
                 ptx::reg_fence(u);
                 if constexpr (PT == 3) add_sum(c0 + c4 * 32, u);
-                if (ri < rows && hh < hn) {
+                if (kWindow && PT == 1 && a.out_dtype == KL_BF16) {
+                    // through shared memory, so that four lanes write 64 consecutive bytes (a row each, the stores alone
+                    // took 2000 cycles per block: 32 lines each)
+                    if (ri < rows && hh < hn)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) nf = fmaf(__uint_as_float(u[e]), inv * 0.f, nf);
+                    uint4 *const stage = sm.stage[warp];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = pack2(__uint_as_float(u[8 * c + 2 * e]) * inv, __uint_as_float(u[8 * c + 2 * e + 1]) * inv);
+                        stage[lane * 4 + (c ^ (lane >> 1 & 3))] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int row = 8 * c + (lane >> 2), rr = qd * 32 + row, qi = rr / hp, h2 = rr - qi * hp;
+                        const uint4 x = stage[row * 4 + ((lane & 3) ^ (row >> 1 & 3))];
+                        if (qi < rows && h2 < hn)
+                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) +
+                                                       ((size_t)(q0 + m0 + qi) * geo.Hq + h + h2) * kD + c0 + c4 * 32 +
+                                                       (lane & 3) * 8) = x;
+                    }
+                    __syncwarp();
+                } else if (ri < rows && hh < hn) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) nf = fmaf(__uint_as_float(u[e]), kWindow ? inv * 0.f : 0.f, nf);
                     if (a.out_dtype == KL_FP32) {
