@@ -9,9 +9,17 @@
 // weights are left to count after the first round. Then each warp counts what stays of a stretch of the piece, the
 // counts are summed before it, and it writes. (All weights are in shared memory before the first is written:
 // weights may move in place.)
-// The move: 512 bytes of traffic per row of 128 bf16 values, and HBM bounds it. Rows only ever move down: in place
-// the CTAs of a cluster take turns of consecutive rows from the first on, read a turn ahead and meet between the
-// reads and the writes of a turn; what they overwrite has been read by then. To other pages nothing waits.
+// The move: 512 bytes of traffic per row of 128 bf16 values, and HBM bounds it. Rows only ever move down, so in place
+// what a chunk of consecutive rows overwrites has been read once all chunks before it have been read.
+// - Many (sequence, value head)s: one CTA per stretch of 128 bytes of their rows goes through the chunks and reads a
+//   chunk ahead of what it writes (64 x 8192 rows to 4096, 8 heads: 180 us, 5.9 TB/s).
+// - Fewer: a cluster of CTAs each, which meet between the reads and the writes of a turn (8 x 8 heads, 2048 of 2300 rows:
+//   17 us).
+// - Fewer than 48: as many CTAs as the GPU holds take the chunks in order, from a counter, announce each that they have
+//   read, and ahead of a write wait for the chunks that read what it overwrites, whose number the selection has counted
+//   (3 sequences of 90000 rows to 40821, 2 heads, 29 us, in clusters 103; one of 131072 rows to 65536, one head, 17 and 140;
+//   88 units of 5300 rows to 3589 42 and 45, 64 of 2300 to 2048 36 and 17).
+// To other pages nothing waits.
 #include "kl_internal.cuh"
 
 namespace kl {
@@ -21,11 +29,12 @@ constexpr int kBits0 = 11, kBits = 10;                   // of the first round, 
 constexpr int kBins = 1 << kBits0;
 constexpr int kPerThread = 4, kBinWarps = kBins / kPerThread / 32;   // the first warps find the bin
 constexpr int kMostCluster = 8;
+constexpr int kMovePieces = 512;                         // 16-byte pieces of a chunk of rows: one CTA's turn of the move
 
-// What the move needs to know of a (sequence, value head): rows that stay (0: it is left alone) and whether its
-// rows may move within their pages.
+// What the move needs to know of a (sequence, value head): rows that stay (-1: it is left alone), whether its rows
+// may move within their pages, and the chunks that CTAs have taken.
 struct EvictUnit {
-    int rows, in_place;
+    int rows, in_place, taken, spare;
 };
 static_assert(sizeof(EvictUnit) == kEvictUnitBytes, "");
 
@@ -90,7 +99,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __flo
 // Cluster (b, g), CTA `rank` of it: tokens rank * piece ... kThreads: 512, of which an SM holds four CTAs, or 1024 where
 // there are few units.
 template <int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kernel(const EvictArgs a, EvictUnit *units, int cluster, int piece) {
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
+    select_kernel(const EvictArgs a, EvictUnit *units, uint4 *read, int32_t *need, int marks, int cluster, int piece) {
     constexpr int kSelWarps = kThreads / 32;
     extern __shared__ __align__(16) float held[];        // [piece]
     __shared__ __align__(16) int hist[kBins], sums[kBins];   // of this CTA, of the cluster
@@ -146,8 +156,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
     }
     if (tid == 0 && rank == 0) {
         if (fault && unit % geo.Hkv == 0) raise_flag(a.err, fault);
-        units[unit] = EvictUnit{fault ? -1 : rows, eq};
+        units[unit] = EvictUnit{fault ? -1 : rows, eq, 0, 0};
     }
+    for (int i = rank * kThreads + tid; i < marks; i += cluster * kThreads)      // (no chunk has been read)
+        read[(size_t)unit * marks + i] = make_uint4(0u, 0u, 0u, 0u);
     if (fault) {                                         // (every CTA of the cluster, once all have read)
         if (cluster > 1) cluster_sync();
         return;
@@ -296,6 +308,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
     before = __reduce_add_sync(0xffffffffu, before);
     on_before = __reduce_add_sync(0xffffffffu, on_before);
     grid_dep_launch();
+    const int chunk = kMovePieces * 8 / geo.D;           // rows (a power of two)
     int32_t *kept = a.kept + (size_t)unit * a.budget;
     float *nw = a.new_weights + (size_t)unit * a.stride;
     for (int t = s0; t < s1; t += 128) {
@@ -317,6 +330,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
             }
             ox += x;
             oy += y;
+            // the rows that have to be read before the chunk that ends with this place is written
+            const int t1e = t + 4 * lane + e + 1;
+            if ((t1e & (chunk - 1)) == 0 && t1e <= rows && t1e <= t1) need[(size_t)unit * marks * 16 + t1e / chunk - 1] = ox + min(oy, want);
         }
         const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
         before += total & 0xffffu;
@@ -330,7 +346,31 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1) select_kern
 
 constexpr int kMoveThreads = 128, kMoveCtas = 8;         // per SM
 constexpr int64_t kEarlyBytes = 256 << 20;               // of rows: up to here the move starts early
-constexpr int kMoveDepth = 4;                            // 16-byte pieces per thread and turn
+constexpr uint64_t kMoveWaitNs = 1000000000ull;          // bound of a wait for other CTAs' reads
+constexpr int kShareUnits = 48;                          // fewer units: share_kernel
+constexpr int kMoveDepth = kMovePieces / kMoveThreads;                            // 16-byte pieces per thread and turn
+
+__device__ __forceinline__ uint64_t global_timer() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+
+// Whether the first n (or all 16) bytes at `p` are 1.
+__device__ __forceinline__ bool all_read(const uint4 *p, int n) {
+    bool all = true;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t v;
+        asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];"
+                     : "=r"(v)
+                     : "l"(reinterpret_cast<const uint32_t *>(p) + e)
+                     : "memory");
+        const int m = min(4, n - 4 * e);
+        if (m > 0) all = all && ((v ^ 0x01010101u) & (0xffffffffu >> (32 - 8 * m))) == 0;
+    }
+    return all;
+}
 
 // t / P and t % P: P a power of two (its shift), or any (shift -1).
 struct Paging {
@@ -339,61 +379,196 @@ struct Paging {
     __device__ __forceinline__ int row(int t) const { return shift >= 0 ? t & (P - 1) : t % P; }
 };
 
-// CTA ((unit * slices + slice) * groups + group) * cluster + rank: a stretch of 2^cshift 16-byte pieces of every row.
-// In turn s of its group (groups * cluster of them share the rows that move to other pages) CTA `rank` takes
-// `step` rows. Three turns ahead of the write it reads which rows, two ahead their pages, one ahead the rows.
-__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
-                                                            int cshift, int groups, int cluster, const Paging pg) {
-    grid_dep_wait();
-    grid_dep_launch();
-    const Geometry &geo = a.geo;
-    const int rank = blockIdx.x % cluster, group = blockIdx.x / cluster % groups;
-    const int slice = blockIdx.x / cluster / groups % slices, unit = blockIdx.x / cluster / groups / slices;
-    const int tid = threadIdx.x;
-    const int b = unit / geo.Hkv, g = unit % geo.Hkv;
-    const EvictUnit u = units[unit];
-    // (the whole cluster leaves)
-    if (u.rows < 0) return;
-    if (g == 0 && slice == 0 && group == 0 && rank == 0 && tid == 0) a.new_lens[b] = u.rows;
-    if (u.in_place && group > 0) return;
-    constexpr int kStep = kMoveThreads * kMoveDepth;
-    const int step = kStep >> cshift;                    // rows of a CTA per turn
-    const int turn = step * cluster * (u.in_place ? 1 : groups);
-    const int32_t *from = a.block_table + (size_t)b * geo.max_pages, *to = a.new_table + (size_t)b * geo.max_pages;
-    const int32_t *kept = a.kept + (size_t)unit * a.budget;
-    const int cpr = geo.D / 8, c = (slice << cshift) + (tid & ((1 << cshift) - 1));
-    const int rstep = kMoveThreads >> cshift;
-    uint4 *const v = reinterpret_cast<uint4 *>(a.v_cache);
-    auto piece = [&](int page, int t) -> uint4 * {
-        return v + (((int64_t)page * geo.Hkv + g) * geo.P + pg.row(t)) * cpr + c;
-    };
-    const int first = (u.in_place ? rank : group * cluster + rank) * step + (tid >> cshift);
-    // of this thread's kMoveDepth rows: which (of turn s + 2 at the loop's head), their pages and rows (s + 1)
-    uint4 x[kMoveDepth], y[kMoveDepth];
-    int id[kMoveDepth], page[kMoveDepth], next[kMoveDepth];
-    auto each = [&](int j, auto &&f) {
+// What both forms share: this thread's pieces of the rows of a chunk.
+struct Mover {
+    const int32_t *from, *to, *kept;
+    uint4 *v;
+    int64_t page_pieces;     // 16-byte pieces of a page
+    int head, cpr, c, first, rstep, rows;   // head: of the value head's first row in a page; c: of this thread in a row
+    Paging pg;
+    __device__ __forceinline__ uint4 *piece(int page, int t) const {
+        return v + page * page_pieces + head + pg.row(t) * cpr + c;
+    }
+    // f(k, row) for this thread's rows of the chunk from row j on
+    template <typename F>
+    __device__ __forceinline__ void each(int j, F &&f) const {
 #pragma unroll
         for (int k = 0; k < kMoveDepth; ++k)
-            if (j + k * rstep < u.rows) f(k, j + k * rstep);
-    };
-    each(first, [&](int k, int at) { id[k] = kept[at]; });
-    each(first + turn, [&](int k, int at) { next[k] = kept[at]; });
-    each(first, [&](int k, int) { page[k] = from[pg.page(id[k])]; });
-    each(first, [&](int k, int) { x[k] = *piece(page[k], id[k]); });
-    each(first + turn, [&](int k, int) { page[k] = from[pg.page(next[k])]; id[k] = next[k]; });
-    each(first + 2 * turn, [&](int k, int at) { next[k] = kept[at]; });
-    const int turns = (u.rows + turn - 1) / turn;        // (as many in all CTAs: they meet)
-    for (int s = 0, j = first; s < turns; ++s, j += turn) {
-        each(j + turn, [&](int k, int) { y[k] = *piece(page[k], id[k]); });
-        each(j + 2 * turn, [&](int k, int) { page[k] = from[pg.page(next[k])]; id[k] = next[k]; });
-        each(j + 3 * turn, [&](int k, int at) { next[k] = kept[at]; });
-        if (u.in_place) {                                // the rows of this turn and the next one have been read
-            if (cluster > 1) cluster_sync();
+            if (j + first + k * rstep < rows) f(k, j + first + k * rstep);
+    }
+    __device__ __forceinline__ void ids(int j, int (&id)[kMoveDepth]) const {
+        each(j, [&](int k, int at) { id[k] = kept[at]; });
+    }
+    __device__ __forceinline__ void pages(int j, const int (&id)[kMoveDepth], int (&page)[kMoveDepth]) const {
+        each(j, [&](int k, int) { page[k] = from[pg.page(id[k])]; });
+    }
+    __device__ __forceinline__ void load(int j, const int (&id)[kMoveDepth], const int (&page)[kMoveDepth],
+                                         uint4 (&x)[kMoveDepth]) const {
+        each(j, [&](int k, int) { x[k] = *piece(page[k], id[k]); });
+    }
+    __device__ __forceinline__ void store(int j, const uint4 (&x)[kMoveDepth]) const {
+        each(j, [&](int k, int at) { *piece(to[pg.page(at)], at) = x[k]; });
+    }
+};
+// A stretch of 2^cshift pieces, number `slice`, of the rows of a unit.
+__device__ __forceinline__ Mover mover(const EvictArgs &a, int unit, int rows, int slice, int cshift, const Paging &pg) {
+    const Geometry &geo = a.geo;
+    const int b = unit / geo.Hkv, g = unit % geo.Hkv, tid = threadIdx.x;
+    Mover m;
+    m.from = a.block_table + (size_t)b * geo.max_pages;
+    m.to = a.new_table + (size_t)b * geo.max_pages;
+    m.kept = a.kept + (size_t)unit * a.budget;
+    m.v = reinterpret_cast<uint4 *>(a.v_cache);
+    m.cpr = geo.D / 8;
+    m.page_pieces = (int64_t)geo.Hkv * geo.P * m.cpr;
+    m.head = g * geo.P * m.cpr;
+    m.c = (slice << cshift) + (tid & ((1 << cshift) - 1));
+    m.first = tid >> cshift;
+    m.rstep = kMoveThreads >> cshift;
+    m.rows = rows;
+    m.pg = pg;
+    return m;
+}
+
+// CTA ((unit * slices + slice) * groups + group) * team + rank: a cluster of `team` CTAs takes its chunks in turns, chunk
+// rank of each; `groups` of them share a unit that moves to other pages, in place the first does it alone. Three turns
+// ahead of the write a CTA reads which rows, two ahead their pages, one ahead the rows.
+__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
+                                                                       int cshift, int groups, int team, const Paging pg) {
+    grid_dep_wait();
+    grid_dep_launch();
+    const int rank = blockIdx.x % team, group = blockIdx.x / team % groups;
+    const int slice = blockIdx.x / team / groups % slices, unit = blockIdx.x / team / groups / slices;
+    const EvictUnit u = units[unit];
+    if (u.rows < 0) return;                              // (the whole cluster)
+    if (unit % a.geo.Hkv == 0 && slice == 0 && group == 0 && rank == 0 && threadIdx.x == 0)
+        a.new_lens[unit / a.geo.Hkv] = u.rows;
+    if (u.in_place && group > 0) return;
+    const Mover m = mover(a, unit, u.rows, slice, cshift, pg);
+    const int chunk = kMovePieces >> cshift, step = chunk * team * (u.in_place ? 1 : groups);
+    uint4 x[kMoveDepth], y[kMoveDepth];
+    int id[kMoveDepth], page[kMoveDepth], next[kMoveDepth];
+    int j = (u.in_place ? rank : group * team + rank) * chunk;
+    m.ids(j, id);
+    m.ids(j + step, next);
+    m.pages(j, id, page);
+    m.load(j, id, page, x);
+    m.pages(j + step, next, page);
+#pragma unroll
+    for (int k = 0; k < kMoveDepth; ++k) id[k] = next[k];
+    m.ids(j + 2 * step, next);
+    const int turns = (u.rows + step - 1) / step;        // (as many in all CTAs: they meet)
+    for (int s = 0; s < turns; ++s, j += step) {
+        m.load(j + step, id, page, y);
+        m.pages(j + 2 * step, next, page);
+#pragma unroll
+        for (int k = 0; k < kMoveDepth; ++k) id[k] = next[k];
+        m.ids(j + 3 * step, next);
+        if (u.in_place) {                                // this turn's and the next one's rows have been read
+            if (team > 1) cluster_sync();
             else __syncthreads();
         }
-        each(j, [&](int k, int at) { *piece(to[pg.page(at)], at) = x[k]; });
+        m.store(j, x);
 #pragma unroll
         for (int k = 0; k < kMoveDepth; ++k) x[k] = y[k];
+    }
+}
+
+// CTA unit * team + t, whole rows: the CTAs of a unit take its chunks in order, from a counter. read[unit][chunk]: bytes,
+// 1 once its rows have been read (marks: 16 of them each); need[unit][chunk]: the first rows that have to be read before it
+// is written. The last warp keeps the books: it takes tickets, announces chunks and looks at the other CTAs' while the
+// movers' loads are on their way. A ticket is taken when there is room to read its chunk at once, so that no chunk waits
+// for another's write before it is read: the chunks below one that waits are with CTAs that read them.
+// The marks need no fences: what was announced has been read, since its values are here, and a write that follows a mark
+// in the program cannot be ahead of it. (3 sequences of 90000 rows to 40821, 2 heads: with fences, which wait for the
+// writes of all warps, 122 instead of 86 us; with a wait for all chunks ahead instead of those that are needed 86
+// instead of 29; with chunks in turns of the whole team instead of tickets 36.)
+constexpr int kShareThreads = kMoveThreads + 32, kShareCtas = 6;
+constexpr uint32_t kBarTake = 1, kBarRead = 2, kBarWrite = 3;    // a ticket is here; a chunk is; its place may be written
+__device__ __forceinline__ void bar(uint32_t id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kShareThreads) : "memory"); }
+
+__global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const EvictArgs a, EvictUnit *units, uint4 *read,
+                                                                          const int32_t *need, int marks, int team, int cshift,
+                                                                          const Paging pg) {
+    __shared__ volatile int ticket, gone;
+    grid_dep_wait();
+    grid_dep_launch();
+    const int unit = blockIdx.x / team, tid = threadIdx.x, lane = tid & 31;
+    const int rows = units[unit].rows, in_place = units[unit].in_place;
+    if (rows < 0) return;
+    if (unit % a.geo.Hkv == 0 && blockIdx.x % team == 0 && tid == 0) a.new_lens[unit / a.geo.Hkv] = rows;
+    const int chunk = kMovePieces >> cshift;
+    if (tid >= kMoveThreads) {
+        uint8_t *const mine = reinterpret_cast<uint8_t *>(read + (size_t)unit * marks);
+        const int32_t *const first_rows = need + (size_t)unit * marks * 16;
+        auto take = [&]() -> int {
+            int c = 0;
+            if (lane == 0) ticket = c = atomicAdd(&units[unit].taken, 1);
+            return __shfl_sync(0xffffffffu, c, 0);
+        };
+        // chunk c may be written once those below this have been read
+        auto limit = [&](int c) -> int {
+            if (!in_place || c * chunk >= rows) return 0;
+            return (c + 1) * chunk > rows ? c : min(c, (__ldcg(first_rows + c) + chunk - 1) / chunk);
+        };
+        if (lane == 0) gone = 0;
+        int known = 0, c0 = take(), stop = limit(c0);    // known: all chunks below have been read
+        bar(kBarTake);
+        while (c0 * chunk < rows) {
+            bar(kBarRead);
+            if (in_place && lane == 0)
+                asm volatile("st.relaxed.gpu.global.u8 [%0], %1;" ::"l"(mine + c0), "r"(1) : "memory");
+            const int c1 = take();
+            bar(kBarTake);
+            const int next = limit(c1);
+            const uint64_t t0 = global_timer();
+            while (known < stop) {
+                // 16 marks per lane from the last whole 16 on; as many as follow each other from there
+                const int first = known & ~15, n = min(16, stop - first - 16 * lane);
+                const bool ok = n <= 0 || all_read(reinterpret_cast<const uint4 *>(mine + first) + lane, n);
+                const unsigned not_yet = ~__ballot_sync(0xffffffffu, ok);
+                known = not_yet ? max(known, first + 16 * (__ffs(not_yet) - 1)) : min(stop, first + 512);
+                if (known < stop && global_timer() - t0 > kMoveWaitNs) {
+                    gone = 1;
+                    break;
+                }
+            }
+            __syncwarp();
+            bar(kBarWrite);
+            if (gone) {                                  // (rows that are still to be read may not be overwritten)
+                if (lane == 0) raise_flag(a.err, KL_FLAG_TIMEOUT);
+                return;
+            }
+            c0 = c1;
+            stop = next;
+        }
+        return;
+    }
+    const Mover m = mover(a, unit, rows, 0, cshift, pg);
+    uint4 x[kMoveDepth], y[kMoveDepth];
+#pragma unroll
+    for (int k = 0; k < kMoveDepth; ++k) x[k] = y[k] = make_uint4(0u, 0u, 0u, 0u);
+    int id[kMoveDepth], page[kMoveDepth];
+    bar(kBarTake);
+    int c0 = ticket;
+    m.ids(c0 * chunk, id);
+    m.pages(c0 * chunk, id, page);
+    m.load(c0 * chunk, id, page, x);
+    while (c0 * chunk < rows) {
+        // (a word of every load goes into a branch, so that the rows are here and not only on their way)
+        if ((x[0].x ^ x[1].x ^ x[2].x ^ x[3].x) == 0x9e3779b9u) __nanosleep(0);
+        bar(kBarRead);
+        bar(kBarTake);
+        const int c1 = ticket;
+        m.ids(c1 * chunk, id);
+        m.pages(c1 * chunk, id, page);
+        m.load(c1 * chunk, id, page, y);
+        bar(kBarWrite);
+        if (gone) return;
+        m.store(c0 * chunk, x);
+#pragma unroll
+        for (int k = 0; k < kMoveDepth; ++k) x[k] = y[k];
+        c0 = c1;
     }
 }
 
@@ -410,7 +585,11 @@ cudaError_t launch_evict(const EvictArgs &a) {
             (2 * (int64_t)units * cluster <= sms && longest >= 4096 * (int64_t)cluster)))
         cluster *= 2;
     const int piece = (int)((longest + cluster - 1) / cluster + 127) & ~127;
-    EvictUnit *info = static_cast<EvictUnit *>(a.workspace);
+    // (the marks first: they are read 16 at a time)
+    const int marks = kl_evict_marks(a.budget);
+    uint4 *read = static_cast<uint4 *>(a.workspace);
+    int32_t *need = reinterpret_cast<int32_t *>(read + (size_t)units * marks);
+    EvictUnit *info = reinterpret_cast<EvictUnit *>(need + (size_t)units * marks * 16);
     const bool few = units * cluster <= sms;
     const auto kernel = few ? select_kernel<1024> : select_kernel<512>;
     static PerDeviceOnce once[2];
@@ -432,33 +611,43 @@ cudaError_t launch_evict(const EvictArgs &a) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t s = cudaLaunchKernelEx(&cfg, kernel, a, info, cluster, piece);
+    cudaError_t s = cudaLaunchKernelEx(&cfg, kernel, a, info, read, need, marks, cluster, piece);
     if (s != cudaSuccess) return s;
-    // As many CTAs as the GPU holds at a time, eight per SM: clusters of them while there are few units, then 64-byte
-    // stretches instead of whole rows, then (to other pages) groups of clusters.
-    const int cpr = g.D / 8;
-    const int64_t wanted = kMoveCtas * sms;
-    int team = 1, cshift = g.D == 128 ? 4 : 3;
-    while (cshift > 3 && 2 * (int64_t)units * (cpr >> cshift) <= wanted) --cshift;
-    while (team < kMostCluster && 2 * (int64_t)units * team * (cpr >> cshift) <= wanted && (kMoveThreads * kMoveDepth >> cshift) * team < a.budget) team *= 2;
-    while (cshift > 2 && 2 * (int64_t)units * team * (cpr >> cshift) <= wanted) --cshift;
-    const int slices = cpr >> cshift, step = kMoveThreads * kMoveDepth >> cshift;
-    int64_t groups = wanted / ((int64_t)units * slices * team);
-    const int64_t most = (a.budget + (int64_t)step * team - 1) / ((int64_t)step * team);
-    groups = groups < 1 ? 1 : groups > most ? most : groups;
     int shift = 0;
     while (1 << shift < g.P) ++shift;
     const Paging pg{g.P, 1 << shift == g.P ? shift : -1};
     cudaLaunchConfig_t mv = {};
-    mv.gridDim = dim3((unsigned)(groups * units * slices * team));
     mv.blockDim = dim3(kMoveThreads);
     mv.stream = a.stream;
-    attr[1].val.clusterDim.x = team;
     // An early start saves a launch's latency, but the CTAs then crowd the SMs that the selection leaves first (64 x
     // 8192 rows to 4096, 8 heads, 1 GB of traffic: 242 us with it)
     if ((int64_t)units * (a.budget < longest ? a.budget : longest) * g.D * 4 > kEarlyBytes)
         attr[0].val.programmaticStreamSerializationAllowed = 0;
     mv.attrs = attr;
+    mv.numAttrs = 1;
+    const int cpr = g.D / 8, wanted = kMoveCtas * sms;
+    const int64_t most = a.budget < longest ? a.budget : longest;
+    int cshift = g.D == 128 ? 4 : 3;
+    if (units < kShareUnits) {
+        const int chunks = (int)((most + (kMovePieces >> cshift) - 1) / (kMovePieces >> cshift));
+        const int places = kShareCtas * sms / units, team = places < chunks ? places : chunks;
+        mv.gridDim = dim3((unsigned)(units * team));
+        mv.blockDim = dim3(kShareThreads);
+        return cudaLaunchKernelEx(&mv, share_kernel, a, info, read, (const int32_t *)need, marks, team, cshift, pg);
+    }
+    // As many CTAs as the GPU holds at a time, eight per SM: 128-byte stretches, then clusters, then (to other pages)
+    // groups of clusters
+    while (cshift > 3 && 2 * (int64_t)units * (cpr >> cshift) <= wanted) --cshift;
+    int team = 1;
+    while (team < kMostCluster && 2 * (int64_t)units * team * (cpr >> cshift) <= wanted &&
+           (int64_t)(kMovePieces >> cshift) * team < most)
+        team *= 2;
+    const int slices = cpr >> cshift;
+    const int64_t turn = (int64_t)(kMovePieces >> cshift) * team, turns = (most + turn - 1) / turn;
+    int64_t groups = wanted / ((int64_t)units * slices * team);
+    groups = groups < 1 ? 1 : groups > turns ? turns : groups;
+    mv.gridDim = dim3((unsigned)(groups * units * slices * team));
+    attr[1].val.clusterDim.x = team;
     mv.numAttrs = 2;
     return cudaLaunchKernelEx(&mv, move_kernel, a, (const EvictUnit *)info, slices, cshift, (int)groups, team, pg);
 }

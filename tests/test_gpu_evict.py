@@ -146,6 +146,24 @@ def test_many_units():
     check(case([random.Random(3).randint(0, 400) for _ in range(70)], 8, 64, 16), 150, 4, 20)
 
 
+@pytest.mark.parametrize("B", [5, 6, 12, 40])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("spare", [0, 1])
+def test_numbers_of_units(B, D, spare):
+    """40 to 480 value heads in all: each form of the move, with several turns of its CTAs."""
+    r = random.Random(B)
+    lens = [r.randint(1, 1400) for _ in range(B)]
+    check(case(lens, 8, D, 16, spare=spare, kind="skewed"), 800, 4, 100)
+
+
+@pytest.mark.parametrize("budget", [2999, 2900, 1500, 70])
+@pytest.mark.parametrize("kind", ["rising", "falling", "random"])
+def test_one_long_unit_in_place(budget, kind):
+    """Rows that move by one place, by all that was evicted at once, or by more and more."""
+    check(case((3000,), 1, 128, 16, kind=kind), budget, 2, 5)
+    check(case((60000,), 1, 64, 16, kind=kind), 20 * budget, 2, 5)
+
+
 def test_a_budget_of_one_less():
     for kind in ("rising", "falling", "random"):
         c = case((4000, 3999, 4001), 2, 128, 16, kind=kind)
