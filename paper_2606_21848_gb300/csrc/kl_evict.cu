@@ -12,7 +12,7 @@
 // The move: 512 bytes of traffic per row of 128 bf16 values, and HBM bounds it. Rows only ever move down, so in place
 // what a chunk of consecutive rows overwrites has been read once all chunks before it have been read.
 // - Many (sequence, value head)s: one CTA per stretch of 128 bytes of their rows goes through the chunks and reads a
-//   chunk ahead of what it writes (64 x 8192 rows to 4096, 8 heads: 180 us, 5.9 TB/s).
+//   chunk ahead of what it writes (64 x 8192 rows to 4096, 8 heads: 163 us, 6.6 TB/s).
 // - Fewer: a cluster of CTAs each, which meet between the reads and the writes of a turn (8 x 8 heads, 2048 of 2300 rows:
 //   17 us).
 // - Fewer than 48: as many CTAs as the GPU holds take the chunks in order, from a counter, announce each that they have
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
             const float4 x = *reinterpret_cast<const float4 *>(held + at);
             uint32_t k[4] = {weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w)};
             const int from_mid = t0 + at - mid0;
-            const uint32_t mids = (uint32_t)(min(t1, mid1) - mid0);
+            const uint32_t mids = (uint32_t)max(min(t1, mid1) - mid0, 0);   // (0: the piece is all first tokens)
             bool in[4], any = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
     }
     // (the whole cluster writes the rest; nothing there is read again)
     for (int t = rows + rank * kThreads + tid; t < L; t += cluster * kThreads) nw[t] = 0.f;
-    for (int t = rows + rank * kThreads + tid; t < a.budget; t += cluster * kThreads) kept[t] = -1;
+    for (uint32_t t = rows + rank * kThreads + tid; t < (uint32_t)a.budget; t += cluster * kThreads) kept[t] = -1;
     if (cluster > 1) cluster_sync();                     // (the counts are read)
 }
 

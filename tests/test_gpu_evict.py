@@ -112,6 +112,15 @@ def check(c, budget, sinks, recent, in_place=False, **kw):
 KINDS = ["random", "skewed", "ties", "zero", "rising", "falling", "odd"]
 
 
+@pytest.mark.parametrize("sinks,recent,budget", [(6000, 0, 9000), (6000, 9000, 16000), (2560, 1, 2562), (19000, 900, 19901),
+                                                 (0, 18000, 18100)])
+def test_first_and_last_tokens_beyond_a_piece(sinks, recent, budget):
+    """A cluster's CTAs whose piece of the weights lies wholly among the first or the last tokens count none of it."""
+    for kind in ("random", "rising"):
+        check(case((20000,), Hkv=1, kind=kind), budget, sinks, recent)
+        check(case((20000, 6001), Hkv=1, D=64, kind=kind, spare=1), budget, sinks, recent)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("spare", [0, 1])
 def test_kinds_of_weights(kind, spare):
