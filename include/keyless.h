@@ -388,7 +388,7 @@ size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t
  * Entries from seq_lens[b] on are neither read nor written; the old weight of a token that is new with this
  * call has to be there (0). A sequence with n_b = 0 gets decay * weights. A longer chunk goes in pieces of
  * KL_WEIGHTS_MAX_ROWS with seq_lens of their own, decay 1 from the second on.
- * max_q_len <= KL_WEIGHTS_MAX_ROWS (KL_ERR_UNSUPPORTED otherwise); a sequence of more than weights_stride tokens
+ * max_q_len <= KL_WEIGHTS_MAX_ROWS, num_seqs and num_kv_heads <= 65535 (KL_ERR_UNSUPPORTED otherwise); a sequence of more than weights_stride tokens
  * raises KL_FLAG_BAD_LENGTH and is skipped, like those of kl_window_attention; a bad page leaves the
  * sequence's outputs and weights unspecified. A row that is not finite makes the outputs of the positions
  * that see it NaN, and where their scores are not finite the weights that they add as well. Other arguments,
@@ -427,8 +427,10 @@ size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, in
  * page size. min(max_pages_per_seq * P, weights_stride) at most KL_EVICT_MAX_TOKENS (KL_ERR_UNSUPPORTED). A
  * sequence whose length is negative, or more than weights_stride or max_pages_per_seq * P
  * (KL_FLAG_BAD_LENGTH), or one of whose pages, old or new, lies outside the pool (KL_FLAG_BAD_PAGE) is
- * left as it is, its entries of all outputs included. Two launches. Workspace: kl_evict_workspace_size bytes,
- * 256-byte aligned.
+ * left as it is, its entries of all outputs included. Two launches. Where a CTA of the move waits more than a second
+ * for others to read what it is about to overwrite (few value heads, in place), it raises KL_FLAG_TIMEOUT and leaves
+ * the rest of its rows unmoved; the cache is then undefined. Workspace: kl_evict_workspace_size bytes, 256-byte
+ * aligned.
  */
 kl_status kl_evict(const kl_shape *shape, const float *weights, int32_t weights_stride, int32_t budget,
                    int32_t sinks, int32_t recent, const int32_t *block_table, const int32_t *seq_lens,

@@ -602,7 +602,8 @@ kl_status plan_weights_call(const kl_shape *shape, int32_t total_q, int32_t max_
     if (st != KL_OK) return st;
     if (total_q < 0 || max_q_len < 0 || num_splits < 0 || num_splits > kMaxSplits || weights_stride < 1)
         return KL_ERR_INVALID_ARG;
-    if (max_q_len > KL_WEIGHTS_MAX_ROWS) return KL_ERR_UNSUPPORTED;
+    // (both are extents of the grid that adds the weights up)
+    if (max_q_len > KL_WEIGHTS_MAX_ROWS || g.B > 65535 || g.Hkv > 65535) return KL_ERR_UNSUPPORTED;
     const int64_t tokens = (int64_t)g.max_pages * g.P, longest = tokens < weights_stride ? tokens : weights_stride;
     const int64_t units = (int64_t)g.B * g.Hkv;
     const int max_q = max_q_len > 0 ? max_q_len : 1;

@@ -122,3 +122,9 @@ def test_evict_arguments():
         refused(WORKSPACE, evict, ws=ws)
     assert evict(sh=shape(num_seqs=0)) is None            # nothing to do
     assert kl.kl_evict_workspace_size(shape(), 512, 0) == 0
+
+
+def test_weights_of_more_sequences_than_a_grid_has():
+    for bad in (dict(num_seqs=65536), dict(num_q_heads=65536, num_kv_heads=65536)):
+        refused(UNSUPPORTED, weights, sh=shape(**bad))
+        assert kl.kl_weights_workspace_size(shape(**bad), 4, 2, 512, 0) == 0
