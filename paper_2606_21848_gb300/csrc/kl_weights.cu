@@ -10,6 +10,8 @@
 // per cached row of 256 where a group has 8 heads), and the last CTA of a value head reads them back, mostly from
 // L2, with the runs' {maximum, sum}. Where a value head has several blocks of rows, a second kernel, the first's
 // programmatic dependent, does that. Rows are added in their order: the sums are the same on every run.
+// HBM bounds it (256 bytes per token and value head), then the tile's chain with three terms. Measured: 64 sequences of
+// 8192 tokens, 64 / 8 heads 231 us (4.8 TB/s); 24 of 301 to 20011, 32 / 8 heads 129 us; one of 2000 11.5 us.
 #include "kl_rows_wide.cuh"
 
 namespace kl {

@@ -5,6 +5,8 @@
 // The scores lie as [block][tokens / 4][128 rows] float4: a warp of the attention writes 32 rows' four tokens as 512
 // consecutive bytes, and here a warp reads them so: lane = row, and the lanes' sums of 32 tokens meet in one
 // exchange of 31 shuffles. The order of all additions is fixed.
+// Measured: 16 rows behind 4 prompts of 4001 to 6007 tokens, 32 / 8 heads 45 us, 37 of them the attention (as blocks of
+// 16 rows on the wide decode's kernel 82).
 #include "kl_prefill_tc_kernel.cuh"
 
 namespace kl {

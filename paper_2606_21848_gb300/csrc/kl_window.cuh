@@ -48,7 +48,8 @@ struct CausalRuns {
 // - Fewer blocks than places: as many runs as fit one wave, or several waves of shorter runs where these are done a
 //   tenth sooner.
 // - More: the last wave's blocks alone are cut, where that is done sooner. (128 sequences with a window of 4160, 8 value
-//   heads: 1024 blocks on 304 places, in 3.4 waves 197 us; 512 blocks of 64 tiles with weights on 152 places 243.)
+//   heads: 1024 blocks on 304 places, in 3.4 waves 197 us, 187 with the last wave cut; 512 blocks of 64 tiles with weights
+//   on 152 places 243, 231.)
 inline CausalRuns plan_runs(int64_t units, int64_t max_tokens, int num_splits, int64_t slots, int most_states) {
     const int64_t tiles = (max_tokens + 127) / 128;
     const auto cost = [&](int64_t n, int64_t runs) {

