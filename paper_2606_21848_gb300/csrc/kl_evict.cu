@@ -5,9 +5,9 @@
 // Two kernels. The selection: a cluster of CTAs per (sequence, value head), each with a piece of the weights in
 // shared memory. The smallest weight that stays is found by three rounds over its bits from the top, 11, 10 and 10
 // (a positive fp32's order is that of its bits): every CTA counts its piece's weights that have the bits found so
-// far by their next ones, all add the counts up through distributed shared memory and find the same bin. Few
-// weights are left to count after the first round. Then each warp counts what stays of a stretch of the piece, the
-// counts are summed before it, and it writes. (All weights are in shared memory before the first is written:
+// far by their next ones, and by 32 of these together; all meet, add up the coarse counts through distributed shared
+// memory, then the 32 fine ones, and find the same bin. Few weights are left to count after the first round. Then each
+// warp counts what stays of a stretch of the piece, the counts are summed before it, and it writes. (All weights are in shared memory before the first is written:
 // weights may move in place.)
 // The move: 512 bytes of traffic per row of 128 bf16 values, and HBM bounds it. Rows only ever move down, so in place
 // what a chunk of consecutive rows overwrites has been read once all chunks before it have been read.
@@ -27,7 +27,6 @@ namespace {
 
 constexpr int kBits0 = 11, kBits = 10;                   // of the first round, of the others
 constexpr int kBins = 1 << kBits0;
-constexpr int kPerThread = 4, kBinWarps = kBins / kPerThread / 32;   // the first warps find the bin
 constexpr int kMostCluster = 8;
 constexpr int kMovePieces = 512;                         // 16-byte pieces of a chunk of rows: one CTA's turn of the move
 
@@ -46,90 +45,99 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-// The word at `p` of this CTA's shared memory in that of CTA `rank` of the cluster.
-__device__ __forceinline__ int ld_cluster(const int *p, int rank) {
-    uint32_t at;
-    int v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                 : "=r"(at)
-                 : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
-}
-
-// Sums of the four words at `p` (16-byte aligned) over CTAs rank .. rank + 3 (those below `cluster`), all four loads
-// on their way at once.
-__device__ __forceinline__ void add_cluster(const int *p, int rank, int cluster, int (&n)[4]) {
-    uint32_t at[4];
-    int v[16];
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                     : "=r"(at[c])
-                     : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(min(rank + c, cluster - 1)));
-    asm volatile(
-        "ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%16];\n\t"
-        "ld.shared::cluster.v4.b32 {%4, %5, %6, %7}, [%17];\n\t"
-        "ld.shared::cluster.v4.b32 {%8, %9, %10, %11}, [%18];\n\t"
-        "ld.shared::cluster.v4.b32 {%12, %13, %14, %15}, [%19];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(at[0]), "r"(at[1]), "r"(at[2]), "r"(at[3])
-        : "memory");
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (rank + c < cluster)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) n[e] += v[4 * c + e];
-}
-
-// Writes n to `p` (16-byte aligned) in the shared memory of CTA `rank`.
-__device__ __forceinline__ void st_cluster(int *p, int rank, const int (&n)[4]) {
+// The two words at `p` (8-byte aligned) of this CTA's shared memory in that of CTA `rank` of the cluster, or the first.
+__device__ __forceinline__ void ld_cluster(const int *p, int rank, int (&n)[2]) {
     uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
                  : "=r"(at)
                  : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(n[0]), "r"(n[1]), "r"(n[2]), "r"(n[3])
-                 : "memory");
+    asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(n[0]), "=r"(n[1]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ld_cluster(const int *p, int rank, int (&n)[1]) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(at)
+                 : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(n[0]) : "r"(at) : "memory");
+}
+// Their sums over the cluster, eight loads on their way at once.
+template <int kWords>
+__device__ __forceinline__ void add_cluster(const int *p, int cluster, int (&n)[kWords]) {
+#pragma unroll
+    for (int e = 0; e < kWords; ++e) n[e] = cluster > 1 ? 0 : p[e];
+    if (cluster == 1) return;
+    for (int c0 = 0; c0 < cluster; c0 += 8) {
+        int v[8][kWords];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) ld_cluster(p, min(c0 + c, cluster - 1), v[c]);
+#pragma unroll
+        for (int e = 0; e < kWords; ++e)
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c0 + c < cluster) n[e] += v[c][e];
+    }
+}
+
+// Writes x, y to `p` (8-byte aligned) in the shared memory of CTA `rank`.
+__device__ __forceinline__ void st_cluster(int *p, int rank, int x, int y) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(at)
+                 : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
+}
+
+// Sums of n over lanes 0 .. lane.
+__device__ __forceinline__ int upto_lane(int n, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, n, o);
+        if (lane >= o) n += x;
+    }
+    return n;
 }
 
 // Weights in their order as whole numbers; what is not positive, and NaN, is 0.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
 
 // Cluster (b, g), CTA `rank` of it: tokens rank * piece ... kThreads: 512, of which an SM holds four CTAs, or 1024 where
-// there are few units.
+// there are few units. Shared memory: the piece's weights, and two bits for each of them (above the border, on it).
 template <int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
     select_kernel(const EvictArgs a, EvictUnit *units, uint4 *read, int32_t *need, int marks, int cluster, int piece) {
     constexpr int kSelWarps = kThreads / 32;
-    extern __shared__ __align__(16) float held[];        // [piece]
-    __shared__ __align__(16) int hist[kBins], sums[kBins];   // of this CTA, of the cluster
-    __shared__ int count[2];                             // of this CTA's piece: above the border, on it
+    extern __shared__ __align__(16) float held[];        // [piece], then the bits
+    // of this CTA: the bins, and sums of 32 of them; the rounds take turns, since the cluster still reads the last one's
+    __shared__ __align__(16) int hists[2][kBins], coarse[2][kBins / 32];
+    __shared__ __align__(8) int counts[kMostCluster][2]; // of the CTAs' pieces: above the border, on it
     __shared__ int warp_above[kSelWarps], warp_on[kSelWarps];
     __shared__ uint32_t border;
-    __shared__ int wanted, bad, same;
+    __shared__ __align__(8) int found[2];                // pages outside the pool; pages that stay where they are
+    __shared__ int wanted, bad;
+    uint2 *const sel = reinterpret_cast<uint2 *>(held + piece);
     const Geometry &geo = a.geo;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = cluster > 1 ? (int)cluster_rank() : 0, unit = blockIdx.x / cluster;
     const int b = unit / geo.Hkv;
     grid_dep_wait();
     const int L = a.seq_lens[b], rows = min(L, a.budget);
-    const bool too_long = L < 0 || L > geo.max_pages * geo.P || L > a.stride;
-    if (tid == 0) {
-        border = 0;
-        wanted = 0;
+    const bool first = tid == 0 && rank == 0, tells = first && unit % geo.Hkv == 0;
+    if (L < 0 || L > geo.max_pages * geo.P || L > a.stride) {    // (the whole cluster)
+        if (tells) raise_flag(a.err, KL_FLAG_BAD_LENGTH);
+        if (first) units[unit] = EvictUnit{-1, 0, 0, 0};
+        return;
     }
     // The pages of the sequence and of where it goes, shared out over the cluster, while the weights are on their way
     const int32_t *from = a.block_table + (size_t)b * geo.max_pages, *to = a.new_table + (size_t)b * geo.max_pages;
     const float *w = a.weights + (size_t)unit * a.stride;
-    const int t0 = too_long ? 0 : min(rank * piece, L), t1 = too_long ? 0 : min(t0 + piece, L);
+    const int t0 = min(rank * piece, L), t1 = min(t0 + piece, L);
     constexpr int kAhead = 8;
     float ahead[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
         if (t0 + tid + k * kThreads < t1) ahead[k] = w[t0 + tid + k * kThreads];
-    int fault = too_long, eq = 0;
-    if (!too_long) {
+    int fault = 0, eq = 0;
+    {
         const int pages = (L + geo.P - 1) / geo.P, new_pages = (rows + geo.P - 1) / geo.P;
 #pragma unroll 2
         for (int i = rank * kThreads + tid; i < pages; i += cluster * kThreads) {
@@ -138,31 +146,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
             if (i < new_pages && p == q) eq = 1;
         }
     }
-    fault = __syncthreads_or(fault) ? (too_long ? KL_FLAG_BAD_LENGTH : KL_FLAG_BAD_PAGE) : 0;
-    eq = __syncthreads_or(eq);
-    if (cluster > 1) {
-        if (tid == 0) {
-            bad = fault;
-            same = eq;
-        }
-        cluster_sync();
-        fault = eq = 0;
-#pragma unroll
-        for (int c = 0; c < kMostCluster; ++c)
-            if (c < cluster) {
-                fault |= ld_cluster(&bad, c);
-                eq |= ld_cluster(&same, c);
-            }
-    }
-    if (tid == 0 && rank == 0) {
-        if (fault && unit % geo.Hkv == 0) raise_flag(a.err, fault);
-        units[unit] = EvictUnit{fault ? -1 : rows, eq, 0, 0};
-    }
     for (int i = rank * kThreads + tid; i < marks; i += cluster * kThreads)      // (no chunk has been read)
         read[(size_t)unit * marks + i] = make_uint4(0u, 0u, 0u, 0u);
-    if (fault) {                                         // (every CTA of the cluster, once all have read)
-        if (cluster > 1) cluster_sync();
-        return;
+    fault = __syncthreads_or(fault);
+    eq = __syncthreads_or(eq);
+    if (tid == 0) {
+        found[0] = fault;
+        found[1] = eq;
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
@@ -179,169 +169,153 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
     const bool all = L <= a.budget;
     const int mid0 = a.sinks, mid1 = L - a.recent;
     int want = all ? 0 : a.budget - a.sinks - a.recent;
+    auto meet = [&] {
+        if (cluster > 1) cluster_sync();
+        else __syncthreads();
+    };
+    // Warp 0, behind the first meeting: what the CTAs have found out about the pages.
+    auto look_around = [&] {
+        int x[2] = {0, 0};
+        if (lane < cluster) {
+            if (cluster > 1) ld_cluster(found, lane, x);
+            else x[0] = found[0], x[1] = found[1];
+        }
+        const bool fault = __any_sync(0xffffffffu, x[0]), eq = __any_sync(0xffffffffu, x[1]);
+        if (lane > 0) return;
+        bad = fault;
+        if (tells && fault) raise_flag(a.err, KL_FLAG_BAD_PAGE);
+        if (first) units[unit] = EvictUnit{fault ? -1 : rows, eq, 0, 0};
+    };
     uint32_t key = 0;
-    __shared__ int warp_sum[kBinWarps];
     int shift = 31;
+    if (want == 0) {
+        meet();
+        if (warp == 0) look_around();
+        __syncthreads();
+    }
     for (int round = 0; round < 3 && want > 0; ++round) {
-        const int bits = round == 0 ? kBits0 : kBits;
-        const uint32_t known = round == 0 ? 0u : ~0u << shift;   // bits found so far
+        const int bits = round == 0 ? kBits0 : kBits, known = shift;     // bits known .. 30 are found
         shift -= bits;
-        int *const h = hist;
+        int *const h = hists[round & 1], *const rough = coarse[round & 1];
         for (int i = tid; i < kBins; i += kThreads) h[i] = 0;
         __syncthreads();
-        // four consecutive weights per thread (those at the ends of the middle one by one)
-        for (int at = 4 * tid; at < t1 - t0; at += 4 * kThreads) {
+        // four consecutive weights per thread; the ends of the middle one by one
+        const uint32_t mask = (1u << bits) - 1, so_far = key >> known;
+        const int begin = max(mid0 - t0, 0), end = min(t1, mid1) - t0;   // of the middle in this piece
+        for (int at = 4 * tid; at < end; at += 4 * kThreads) {
             const float4 x = *reinterpret_cast<const float4 *>(held + at);
-            uint32_t k[4] = {weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w)};
-            const int from_mid = t0 + at - mid0;
-            const uint32_t mids = (uint32_t)max(min(t1, mid1) - mid0, 0);   // (0: the piece is all first tokens)
-            bool in[4], any = false;
+            const uint32_t k[4] = {weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w)};
+            bool hit[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                in[e] = ((k[e] ^ key) & known) == 0 && (uint32_t)(from_mid + e) < mids;
-                any |= in[e];
-            }
-            if (any)
+            for (int e = 0; e < 4; ++e) hit[e] = k[e] >> known == so_far;
+            if (!(hit[0] || hit[1] || hit[2] || hit[3])) continue;
+            const bool inside = at >= begin && at + 4 <= end;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (in[e]) atomicAdd(h + ((k[e] >> shift) & ((1u << bits) - 1)), 1);
-        }
-        if (cluster > 1) {
-            // each CTA adds up a share of the bins and gives it to all
-            cluster_sync();
-            const int share = kBins / cluster;
-            if (4 * tid < share) {
-                int *const mine = h + rank * share + 4 * tid;
-                int n[4] = {0, 0, 0, 0};
-                for (int c = 0; c < cluster; c += 4) add_cluster(mine, c, cluster, n);
-                for (int c = 0; c < cluster; ++c) st_cluster(sums + (mine - h), c, n);
-            }
-            cluster_sync();
-        } else {
-            __syncthreads();
-        }
-        // the bin of the want-th largest: bins from the top, kPerThread per thread
-        const int low = kBins - kPerThread * (tid + 1);          // its lowest bin
-        int n[kPerThread] = {0, 0, 0, 0}, sum = 0, upto = 0;
-        if (warp < kBinWarps) {
-            const int4 x = *reinterpret_cast<const int4 *>((cluster > 1 ? sums : h) + low);
-            n[0] = x.x;
-            n[1] = x.y;
-            n[2] = x.z;
-            n[3] = x.w;
-            sum = upto = n[0] + n[1] + n[2] + n[3];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += x;
-            }
-            if (lane == 31) warp_sum[warp] = upto;
+            for (int e = 0; e < 4; ++e)
+                if (hit[e] && (inside || (at + e >= begin && at + e < end))) atomicAdd(h + ((k[e] >> shift) & mask), 1);
         }
         __syncthreads();
-        if (warp < kBinWarps) {
-            upto += __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0);
-            int above = upto - sum;
-            if (above < want && want <= upto) {
-#pragma unroll
-                for (int e = kPerThread - 1; e >= 0; --e) {
-                    if (above < want && want <= above + n[e]) {
-                        border = key | (uint32_t)(low + e) << shift;
-                        wanted = want - above;
-                    }
-                    above += n[e];
-                }
+        for (int i = warp; i < kBins / 32; i += kSelWarps) {
+            const int n = __reduce_add_sync(0xffffffffu, h[32 * i + lane]);
+            if (lane == 0) rough[i] = n;
+        }
+        meet();
+        // the bin of the want-th largest, from the top: which 32 of them (a lane looks at two), then which of these
+        if (warp == 0) {
+            if (round == 0) look_around();
+            int n[2], f[1];
+            add_cluster(rough + kBins / 32 - 2 - 2 * lane, cluster, n);
+            const int sum = n[0] + n[1], upto = upto_lane(sum, lane);
+            const int l = __ffs(__ballot_sync(0xffffffffu, want <= upto)) - 1;
+            int above = __shfl_sync(0xffffffffu, upto - sum, l);
+            const int upper = __shfl_sync(0xffffffffu, n[1], l);
+            int group = kBins / 32 - 1 - 2 * l;
+            if (want > above + upper) {
+                above += upper;
+                --group;
+            }
+            add_cluster(h + 32 * group + 31 - lane, cluster, f);
+            const int here = above + upto_lane(f[0], lane);
+            if (lane == __ffs(__ballot_sync(0xffffffffu, want <= here)) - 1) {
+                border = key | (uint32_t)(32 * group + 31 - lane) << shift;
+                wanted = want - (here - f[0]);
             }
         }
         __syncthreads();
         key = border;
         want = wanted;
+        if (bad) break;
+    }
+    if (bad) {                                           // (every CTA of the cluster, once all have read)
+        if (cluster > 1) cluster_sync();
+        return;
     }
     // `want` of those on the border `key` stay, the first ones; with none wanted nothing between stays
     const bool none = !all && a.budget == a.sinks + a.recent;
-    // Four consecutive tokens per lane and step: how many are above, and (<< 16) on the border; of which bits they are.
-    auto look = [&](int t, uint32_t &bits) -> uint32_t {
-        bits = 0;
-        if (t >= t1) return 0;
-        const float4 x = *reinterpret_cast<const float4 *>(held + (t - t0));
-        const float xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (t + e >= t1) continue;
-            const bool inner = !all && t + e >= mid0 && t + e < mid1;
-            const uint32_t k = weight_key(xs[e]);
-            if (!inner || (!none && k > key)) bits |= 1u << e;
-            else if (!none && k == key) bits |= 16u << e;
-        }
-        return __popc(bits & 15u) | __popc(bits >> 4) << 16;
-    };
-    const int per = ((t1 - t0 + kSelWarps - 1) / kSelWarps + 127) & ~127;
+    // 32 consecutive tokens per step: those above the border (or first, or last), those on it
+    const int per = ((t1 - t0 + kSelWarps - 1) / kSelWarps + 31) & ~31;
     const int s0 = min(t0 + warp * per, t1), s1 = min(s0 + per, t1);
-    if (want == 0 || all || none) __syncthreads();       // (held is complete)
     int na = 0, no = 0;
-    for (int t = s0; t < s1; t += 128) {
-        uint32_t bits;
-        const uint32_t n = __reduce_add_sync(0xffffffffu, look(t + 4 * lane, bits));
-        na += n & 0xffffu;
-        no += n >> 16;
+#pragma unroll 2
+    for (int t = s0; t < s1; t += 32) {
+        const uint32_t k = weight_key(held[t + lane - t0]);
+        const bool outer = all || t + lane < mid0 || t + lane >= mid1, here = t + lane < t1;
+        const unsigned above = __ballot_sync(0xffffffffu, here && (outer || (!none && k > key)));
+        const unsigned on = __ballot_sync(0xffffffffu, here && !outer && !none && k == key);
+        if (lane == 0) sel[(t - t0) / 32] = make_uint2(above, on);
+        na += __popc(above);
+        no += __popc(on);
     }
     if (lane == 0) {
         warp_above[warp] = na;
         warp_on[warp] = no;
     }
     __syncthreads();
-    if (warp == 0) {
-        const int x = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? warp_above[lane] : 0);
-        const int y = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? warp_on[lane] : 0);
-        if (lane == 0) {
-            count[0] = x;
-            count[1] = y;
+    int before = lane < warp ? warp_above[lane] : 0, on_before = lane < warp ? warp_on[lane] : 0;
+    if (cluster > 1) {
+        if (warp == 0) {
+            const int x = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? warp_above[lane] : 0);
+            const int y = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? warp_on[lane] : 0);
+            if (lane < cluster) st_cluster(counts[rank], lane, x, y);
+        }
+        cluster_sync();                                  // (and every CTA holds its weights; the last meeting)
+        if (lane < rank) {
+            before += counts[lane][0];
+            on_before += counts[lane][1];
         }
     }
-    if (cluster > 1) cluster_sync();                     // (and every CTA holds its weights)
-    else __syncthreads();
-    // above the border and on it before this warp's stretch
-    int before = lane < warp ? warp_above[lane] : 0, on_before = lane < warp ? warp_on[lane] : 0;
-    if (lane < rank) {
-        before += ld_cluster(count, lane);
-        on_before += ld_cluster(count + 1, lane);
-    }
-    before = __reduce_add_sync(0xffffffffu, before);
+    // above the border and on it before this warp's stretch; those that stay
     on_before = __reduce_add_sync(0xffffffffu, on_before);
+    before = __reduce_add_sync(0xffffffffu, before) + min(on_before, want);
     grid_dep_launch();
-    const int chunk = kMovePieces * 8 / geo.D;           // rows (a power of two)
+    const int chunk = geo.D == 128 ? 5 : 6;              // rows of a chunk, as a power of two
+    static_assert(kMovePieces == 512, "");
     int32_t *kept = a.kept + (size_t)unit * a.budget;
     float *nw = a.new_weights + (size_t)unit * a.stride;
-    for (int t = s0; t < s1; t += 128) {
-        uint32_t bits, upto = look(t + 4 * lane, bits);
-        const uint32_t mine = upto;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
+    __syncwarp();                                        // (sel is this warp's own)
+    const unsigned below = (1u << lane) - 1;
+    int32_t *ends = need + (size_t)unit * marks * 16 - 1;
+#pragma unroll 2
+    for (int t = s0; t < s1; t += 32) {
+        const uint2 x = sel[(t - t0) / 32];
+        unsigned stay = x.x;
+        if (x.y && on_before < want) {                   // of those on the border the first ones
+            const int left = want - on_before;
+            stay |= __ballot_sync(0xffffffffu, (x.y >> lane & 1) && __popc(x.y & below) < left);
+            on_before += __popc(x.y);
         }
-        int ox = before + (int)((upto - mine) & 0xffffu), oy = on_before + (int)((upto - mine) >> 16);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool x = bits >> e & 1, y = bits >> (4 + e) & 1;
-            if (x || (y && oy < want)) {
-                const int at = ox + min(oy, want);
-                kept[at] = t + 4 * lane + e;
-                nw[at] = held[t + 4 * lane + e - t0];
-            }
-            ox += x;
-            oy += y;
-            // the rows that have to be read before the chunk that ends with this place is written
-            const int t1e = t + 4 * lane + e + 1;
-            if ((t1e & (chunk - 1)) == 0 && t1e <= rows && t1e <= t1) need[(size_t)unit * marks * 16 + t1e / chunk - 1] = ox + min(oy, want);
+        if (stay >> lane & 1) {
+            const int at = before + __popc(stay & below);
+            kept[at] = t + lane;
+            nw[at] = held[t + lane - t0];
         }
-        const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
-        before += total & 0xffffu;
-        on_before += total >> 16;
+        before += __popc(stay);
+        // the rows that have to be read before the chunk that ends here is written
+        if (lane == 0 && (t + 32 & (1 << chunk) - 1) == 0 && t + 32 <= min(rows, t1)) ends[(t + 32) >> chunk] = before;
     }
     // (the whole cluster writes the rest; nothing there is read again)
     for (int t = rows + rank * kThreads + tid; t < L; t += cluster * kThreads) nw[t] = 0.f;
     for (uint32_t t = rows + rank * kThreads + tid; t < (uint32_t)a.budget; t += cluster * kThreads) kept[t] = -1;
-    if (cluster > 1) cluster_sync();                     // (the counts are read)
 }
 
 constexpr int kMoveThreads = 128, kMoveCtas = 8;         // per SM
@@ -595,13 +569,13 @@ cudaError_t launch_evict(const EvictArgs &a) {
     static PerDeviceOnce once[2];
     const cudaError_t e = once[few].run([&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    KL_EVICT_MAX_TOKENS / kMostCluster * (int)sizeof(float));
+                                    KL_EVICT_MAX_TOKENS / kMostCluster / 4 * 17);
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(units * cluster));
     cfg.blockDim = dim3(few ? 1024 : 512);
-    cfg.dynamicSmemBytes = piece * sizeof(float);
+    cfg.dynamicSmemBytes = piece / 4 * 17;
     cfg.stream = a.stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
