@@ -386,16 +386,17 @@ size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t
  * (0 for the tokens behind a row's position). decay: finite and >= 0; with 0 the old weights are not read (and
  * may be NULL). weights, new_weights: [B][Hkv][weights_stride] fp32, dense; they may be the same.
  * Entries from seq_lens[b] on are neither read nor written; the old weight of a token that is new with this
- * call has to be there (0). A sequence with n_b = 0 gets decay * weights. A longer chunk goes in pieces of
+ * call has to be there (0). A sequence with n_b = 0 gets decay * weights (a call without any new token needs
+ * neither q, out nor a workspace). A longer chunk goes in pieces of
  * KL_WEIGHTS_MAX_ROWS with seq_lens of their own, decay 1 from the second on.
- * max_q_len <= KL_WEIGHTS_MAX_ROWS, num_seqs and num_kv_heads <= 65535 (KL_ERR_UNSUPPORTED otherwise); a sequence of more than weights_stride tokens
- * raises KL_FLAG_BAD_LENGTH and is skipped, like those of kl_window_attention; a bad page leaves the
- * sequence's outputs and weights unspecified. A row that is not finite makes the outputs of the positions
- * that see it NaN, and where their scores are not finite the weights that they add as well. Other arguments,
- * shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every run. One
- * launch, or two. The routed query carries 24 significant bits for either type of output, and so do the weights;
- * bf16 outputs that kl_window_attention would sum up from fp16 weights and values are so here as well. Workspace:
- * kl_weights_workspace_size bytes of the same arguments, 256-byte aligned.
+ * max_q_len <= KL_WEIGHTS_MAX_ROWS, num_seqs and num_kv_heads <= 65535 (KL_ERR_UNSUPPORTED otherwise); a sequence
+ * of more than weights_stride tokens raises KL_FLAG_BAD_LENGTH and is skipped, like those of kl_window_attention;
+ * a bad page leaves the sequence's outputs and weights unspecified. A row that is not finite makes the outputs of
+ * the positions that see it NaN, and where their scores are not finite the weights that they add as well. Other
+ * arguments, shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every
+ * run. One launch, or two. The routed query carries 24 significant bits for either type of output, and so do the
+ * weights; bf16 outputs that kl_window_attention would sum up from fp16 weights and values are so here as well.
+ * Workspace: kl_weights_workspace_size bytes of the same arguments, 256-byte aligned.
  */
 kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
                                const int32_t *block_table, const int32_t *seq_lens,

@@ -718,9 +718,24 @@ kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void 
     kl_status st = plan_weights_call(shape, total_q, max_q_len, weights_stride, num_splits, &c);
     if (st == KL_OK)
         st = check_causal(c.d.geo, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q, max_q_len, out, &some);
-    if (st != KL_OK || !some) return st;
+    if (st != KL_OK || c.d.geo.B == 0) return st;
     if (!new_weights || (!weights && decay != 0.f) || !aligned(new_weights, 4) || !aligned(weights, 4))
         return KL_ERR_INVALID_ARG;
+    if (!some) {                                         // (no new tokens: the weights fade)
+        if (!seq_lens || !cu_q_lens) return KL_ERR_INVALID_ARG;
+        DecodeArgs &d = c.d;
+        d.seq_lens = seq_lens;
+        d.tree.cu_q = cu_q_lens;
+        d.tree.total_q = total_q;
+        d.tree.max_q = max_q_len;
+        d.causal.stride = weights_stride;
+        d.causal.weights = weights;
+        d.causal.decay = decay;
+        d.causal.new_weights = new_weights;
+        d.err = err;
+        d.stream = reinterpret_cast<cudaStream_t>(stream);
+        return from_cuda(launch_weights_fade(d));
+    }
     if (!workspace || workspace_bytes < c.w.total || !aligned(workspace, 256)) return KL_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     if (!c.wide) {

@@ -344,6 +344,7 @@ cudaError_t launch_tree_wide(const DecodeArgs &a);
 cudaError_t launch_window_wide(const DecodeArgs &a);
 cudaError_t launch_window_tc(const PrefillArgs &a);
 cudaError_t launch_attention_weights(const DecodeArgs &a);
+cudaError_t launch_weights_fade(const DecodeArgs &a);   // a call without new tokens
 cudaError_t launch_weights_tc(const PrefillArgs &a);
 cudaError_t launch_evict(const EvictArgs &a);
 cudaError_t launch_tree_commit(const Geometry &g, const int32_t *cu_q, const int32_t *path,

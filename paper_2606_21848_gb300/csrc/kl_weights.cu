@@ -33,8 +33,12 @@ __global__ void __launch_bounds__(kAddThreads) add_weights_kernel(const DecodeAr
     const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
     const int q0 = a.tree.cu_q[b], q1 = a.tree.cu_q[b + 1], n = q1 - q0, L = a.seq_lens[b];
     if (q0 < 0 || n < 0 || q1 > a.tree.total_q || n > a.tree.max_q || L < n || L > a.causal.stride ||
-        L > geo.max_pages * geo.P)
-        return;                                          // (reported by the attention)
+        L > geo.max_pages * geo.P) {
+        // (reported by the attention where there is one)
+        if ((a.tree.total_q == 0 || a.tree.max_q == 0) && tid == 0 && blockIdx.x == 0 && g == 0)
+            raise_flag(a.err, KL_FLAG_BAD_LENGTH);
+        return;
+    }
     const int t0 = blockIdx.x * kAddTokens + tid;
     if (blockIdx.x * kAddTokens >= L) return;
     const size_t unit = (size_t)b * geo.Hkv + g;
@@ -127,28 +131,33 @@ cudaError_t launch_scores(const DecodeArgs &la, const CUtensorMap &vmap, const C
                                      : launch_kernel_wide<16, NG, false, kWeights, 3>(la, vmap, wmap, qmap);
 }
 
-}  // namespace
-
-cudaError_t launch_attention_weights(const DecodeArgs &a) {
-    DecodeArgs la = a;
-    Geometry &g = la.geo;
-    const int64_t sms = device_sm_count();
-    const bool two_per_sm = a.causal.two_per_sm;
-    g.qbox = a.causal.hp * a.causal.rpb;
-    CUtensorMap vmap, wmap, qmap;
-    if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
-    cudaError_t e = two_per_sm ? launch_scores<1>(la, vmap, wmap, qmap) : launch_scores<2>(la, vmap, wmap, qmap);
-    if (e != cudaSuccess || g.nhb == 1) return e;        // (one block per value head adds its weights itself)
+cudaError_t add_weights(const DecodeArgs &a) {
+    const Geometry &g = a.geo;
     cudaLaunchConfig_t cfg = {};
     const int64_t longest = (int64_t)g.max_pages * g.P < a.causal.stride ? (int64_t)g.max_pages * g.P : a.causal.stride;
     // (one token per thread while that leaves places empty)
-    const bool few = longest * g.Hkv * g.B <= 8 * kAddThreads * sms;
+    const bool few = longest * g.Hkv * g.B <= 8 * kAddThreads * (int64_t)device_sm_count();
     const int tokens = kAddThreads * (few ? 1 : 4);
     cfg.gridDim = dim3((unsigned)((longest + tokens - 1) / tokens), g.Hkv, g.B);
     cfg.blockDim = dim3(kAddThreads);
     cfg.stream = a.stream;
     const OverlapAttr overlap(cfg);
-    return cudaLaunchKernelEx(&cfg, few ? add_weights_kernel<1> : add_weights_kernel<4>, la);
+    return cudaLaunchKernelEx(&cfg, few ? add_weights_kernel<1> : add_weights_kernel<4>, a);
 }
+
+}  // namespace
+
+cudaError_t launch_attention_weights(const DecodeArgs &a) {
+    DecodeArgs la = a;
+    Geometry &g = la.geo;
+    const bool two_per_sm = a.causal.two_per_sm;
+    g.qbox = a.causal.hp * a.causal.rpb;
+    CUtensorMap vmap, wmap, qmap;
+    if (!rows_maps(a, a.causal.hp, a.causal.rpb, &vmap, &wmap, &qmap)) return cudaErrorInvalidValue;
+    cudaError_t e = two_per_sm ? launch_scores<1>(la, vmap, wmap, qmap) : launch_scores<2>(la, vmap, wmap, qmap);
+    return e != cudaSuccess || g.nhb == 1 ? e : add_weights(la);   // (one block per value head adds its weights itself)
+}
+
+cudaError_t launch_weights_fade(const DecodeArgs &a) { return add_weights(a); }
 
 }  // namespace kl

@@ -238,3 +238,8 @@ def test_a_graph_evicts_again_and_again():
         g["w"] += torch.arange(E, device="cuda").remainder(7)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, (g["v"], g["w"], lens, kept)))
+
+
+@pytest.mark.parametrize("spare", [0, 1])
+def test_many_sequences(spare):
+    check(case([1 + (7 * b) % 41 for b in range(2100)], Hkv=8, D=64, kind="ties", spare=spare), 19, 2, 5)

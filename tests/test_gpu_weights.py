@@ -183,3 +183,29 @@ def test_a_workspace_shared_with_a_graph_and_the_same_sums_on_every_run():
 def test_a_long_sequence(n):
     x = inputs((40000, 3), (n, 1), 8, 1, 64)
     check(x, 1.0)
+
+
+@pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (64, 1)])
+@pytest.mark.parametrize("max_q", [0, 1, 128])
+def test_a_call_without_new_tokens(decay, Hq, Hkv, max_q):
+    """The weights fade; what was not there stays, and a length that does not fit is reported."""
+    x = inputs((300, 5, 0, 1000), (0, 0, 0, 0), Hq, Hkv)
+    g = on(x)
+    for stride in (1003, 400):
+        old = torch.rand(4, Hkv, stride, generator=torch.Generator().manual_seed(2)).cuda()
+        for new in (torch.full_like(old, -7.0), old.clone()):
+            was, err = new.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+            kl.kl_attention_weights(shape_of(g), None, g["w_r"], g["v_cache"], g["block_table"], g["seq_lens"], g["cu_q"],
+                                    0, max_q, old if decay else None, stride, decay, new, 0, None, kl.KL_BF16, None, err)
+            torch.cuda.synchronize()
+            assert int(err) == (kl.KL_FLAG_BAD_LENGTH if stride < 1000 else 0)
+            for b, L in enumerate((300, 5, 0, 1000)):
+                L = L if L <= stride else 0
+                assert torch.equal(new[b, :, :L], old[b, :, :L] * decay) and torch.equal(new[b, :, L:], was[b, :, L:])
+
+
+@pytest.mark.parametrize("Hq,n", [(8, 1), (32, 1), (8, 20)])
+def test_more_units_than_shared_counters(Hq, n):
+    lens = [n + (7 * b) % 31 for b in range(2100)]
+    check(inputs(lens, [n if b % 5 else 0 for b in range(2100)], Hq, 8), 0.5, splits=0 if n == 1 else 3)

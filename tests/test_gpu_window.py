@@ -245,3 +245,10 @@ def test_a_long_cache_beyond_32_bits():
     g2["v_cache"] = v
     for dtype in TYPES:
         close(window(g2, 400, 4, dtype), want, dtype)
+
+
+@pytest.mark.parametrize("Hq,n", [(8, 1), (32, 1), (8, 20), (32, 40)])
+@pytest.mark.parametrize("splits", [0, 3])
+def test_more_units_than_shared_counters(Hq, n, splits):
+    lens = [n + (7 * b) % 331 for b in range(2100)]
+    both(inputs(lens, [n if b % 5 else 0 for b in range(2100)], Hq, 8), 150, 3, splits=splits)
