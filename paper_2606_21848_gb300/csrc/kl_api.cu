@@ -38,7 +38,6 @@ namespace {
 constexpr int kChunkQuantum = 128;  // split boundaries fall on multiples of 128 tokens
 constexpr int kSimtMaxGroup = 8;    // query heads per value head of the CUDA-core kernel
 constexpr int kMaxSplits = 1024;
-constexpr int kCausalMostRuns = 256;   // states of a block that one CTA merges
 
 bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 

@@ -6,6 +6,13 @@
 namespace kl {
 namespace {
 
+// merge_states puts 12 bytes per row and state and a state's rows into the ring.
+template <int NH, int NG, int T>
+constexpr bool merge_fits = ((12u * NH * kCausalMostRuns + 1023) & ~1023u) + NH * kD * sizeof(float) <=
+                            sizeof(WideSmem<NH, NG, T>::tiles);
+static_assert(kCausalMostRuns == kWideMaxRuns && merge_fits<16, 1, 2> && merge_fits<16, 1, 3> && merge_fits<16, 2, 2> &&
+                  merge_fits<16, 2, 3> && merge_fits<32, 2, 2>, "");
+
 // The maps of the cache, of W^R and of the queries ([total_q][Hq][128], one box = `rows` consecutive rows of
 // `heads` heads, 64 dims; rows past total_q and heads past Hq read as zeros).
 inline bool rows_maps(const DecodeArgs &a, int heads, int rows, CUtensorMap *vmap, CUtensorMap *wmap,

@@ -36,6 +36,9 @@ inline int window_rows(int64_t G, int64_t max_q, bool fine, bool per_qh) {
     return fine || per_qh ? 16 : 32;
 }
 
+// Most runs of a block: states that one CTA merges (their table and rows take the place of the ring's tiles).
+constexpr int kCausalMostRuns = 256;
+
 // How blocks of up to `tiles` tiles of 128 tokens are cut into runs, one per CTA.
 struct CausalRuns {
     int splits;      // pieces of a line, of `chunk` tokens each
@@ -43,8 +46,8 @@ struct CausalRuns {
     int spc;         // pieces per run
     int whole;       // the first units are one run each
 };
-// `units` blocks of rows on `slots` places; num_splits: most runs of a block, 0: chosen here. A CTA costs 8 tiles' time
-// by itself.
+// `units` blocks of rows on `slots` places; num_splits: most runs of a block, 0: chosen here; never more than most_states.
+// A CTA costs 8 tiles' time by itself.
 // - Fewer blocks than places: as many runs as fit one wave, or several waves of shorter runs where these are done a
 //   tenth sooner.
 // - More: the last wave's blocks alone are cut, where that is done sooner. (128 sequences with a window of 4160, 8 value
@@ -66,6 +69,7 @@ inline CausalRuns plan_runs(int64_t units, int64_t max_tokens, int num_splits, i
     if (num_splits > 0) {
         // (no more than four waves of CTAs, each of which pays a start)
         int64_t runs = num_splits < tiles ? num_splits : tiles;
+        if (runs > most_states) runs = most_states;
         while (runs > 1 && runs * units > 4 * slots) --runs;
         return cut(runs, 0);
     }
@@ -80,8 +84,8 @@ inline CausalRuns plan_runs(int64_t units, int64_t max_tokens, int num_splits, i
         if (cost(units, other) * 10 < one_wave * 9) best = other;
         return cut(best, 0);
     }
-    // long lines: runs of at most 8192 tokens, so that batches of any lengths balance
-    const int64_t cap = (max_tokens + 8191) / 8192;
+    // long lines: runs of at most 8192 tokens while these are not too many, so that batches of any lengths balance
+    const int64_t pieces = (max_tokens + 8191) / 8192, cap = pieces < most_states ? pieces : most_states;
     if (cap > 1) return cut(cap, 0);
     const int64_t rest = units % slots;
     for (int64_t runs = 2; runs <= 4 && runs <= most; ++runs)
