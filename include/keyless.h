@@ -428,10 +428,10 @@ size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, in
  * page size. min(max_pages_per_seq * P, weights_stride) at most KL_EVICT_MAX_TOKENS (KL_ERR_UNSUPPORTED). A
  * sequence whose length is negative, or more than weights_stride or max_pages_per_seq * P
  * (KL_FLAG_BAD_LENGTH), or one of whose pages, old or new, lies outside the pool (KL_FLAG_BAD_PAGE) is
- * left as it is, its entries of all outputs included. Two launches. Where a CTA of the move waits more than a second
- * for others to read what it is about to overwrite (few value heads, in place), it raises KL_FLAG_TIMEOUT and leaves
- * the rest of its rows unmoved; the cache is then undefined. Workspace: kl_evict_workspace_size bytes, 256-byte
- * aligned.
+ * left as it is, its entries of all outputs included. Two launches. Where a CTA of the move waits longer than
+ * kl_set_wait_timeout_ns allows (a second) for others to read what it is about to overwrite (few value heads, in
+ * place), it raises KL_FLAG_TIMEOUT and leaves the rest of its rows unmoved; the cache is then undefined. Workspace:
+ * kl_evict_workspace_size bytes, 256-byte aligned.
  */
 kl_status kl_evict(const kl_shape *shape, const float *weights, int32_t weights_stride, int32_t budget,
                    int32_t sinks, int32_t recent, const int32_t *block_table, const int32_t *seq_lens,
@@ -638,10 +638,10 @@ int32_t kl_decode_kernel_available(const kl_shape *shape, int32_t kernel, int32_
  * that limit, in nanoseconds, for every decode launched afterwards by kl_decode_attention(_ex),
  * kl_decode_step, kl_standard_decode, kl_decode_attention_noalloc, the latent decodes and the FP8
  * decodes, and in the same way for kl_tree_attention, for kl_attention_weights and kl_window_attention where they run on
- * the decodes' kernels (R <= 32 as defined there) and for the waits of kl_token_logprobs for its copies,
- * process-wide; 0 restores the default. Returns the limit in force before the call. A
- * small value makes the waits run out on purpose: this is how the timeout path is tested. The
- * paper has no counterpart.
+ * the decodes' kernels (R <= 32 as defined there), for the waits of kl_token_logprobs for its copies and for those of
+ * kl_evict between CTAs (whose workspace needs no zeros afterwards), process-wide; 0 restores the default. Returns
+ * the limit in force before the call. A small value makes the waits run out on purpose: this is how the timeout path is
+ * tested. The paper has no counterpart.
  */
 uint64_t kl_set_wait_timeout_ns(uint64_t ns);
 

@@ -826,6 +826,7 @@ kl_status kl_evict(const kl_shape *shape, const float *weights, int32_t weights_
     a.new_lens = new_lens;
     a.workspace = static_cast<char *>(workspace) + shared_layout(0, 0, 0).states;
     a.err = err;
+    a.wait_ns = current_wait_ns();
     a.stream = reinterpret_cast<cudaStream_t>(stream);
     return from_cuda(launch_evict(a));
 }

@@ -320,7 +320,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
 
 constexpr int kMoveThreads = 128, kMoveCtas = 8;         // per SM
 constexpr int64_t kEarlyBytes = 256 << 20;               // of rows: up to here the move starts early
-constexpr uint64_t kMoveWaitNs = 1000000000ull;          // bound of a wait for other CTAs' reads
 constexpr int kShareUnits = 48;                          // fewer units: share_kernel
 constexpr int kMoveDepth = kMovePieces / kMoveThreads;                            // 16-byte pieces per thread and turn
 
@@ -502,8 +501,9 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
                 const bool ok = n <= 0 || all_read(reinterpret_cast<const uint4 *>(mine + first) + lane, n);
                 const unsigned not_yet = ~__ballot_sync(0xffffffffu, ok);
                 known = not_yet ? max(known, first + 16 * (__ffs(not_yet) - 1)) : min(stop, first + 512);
-                if (known < stop && global_timer() - t0 > kMoveWaitNs) {
-                    gone = 1;
+                // (one lane's clock decides for the warp)
+                if (known < stop && __shfl_sync(0xffffffffu, global_timer() - t0 > a.wait_ns, 0)) {
+                    if (lane == 0) gone = 1;
                     break;
                 }
             }

@@ -118,6 +118,7 @@ struct EvictArgs {
     int32_t *new_lens;        // [B]
     void *workspace;
     int32_t *err;
+    uint64_t wait_ns;         // bound of a wait for other CTAs' reads
     cudaStream_t stream;
 };
 
