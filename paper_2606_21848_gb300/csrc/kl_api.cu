@@ -790,7 +790,7 @@ kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void 
 size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, int32_t budget) {
     Geometry g;
     if (resolve(shape, -1, &g) != KL_OK || weights_stride < 1 || budget < 1) return 0;
-    return shared_layout(0, (size_t)g.B * g.Hkv * (kEvictUnitBytes + 80 * (size_t)kl_evict_marks(budget)), 0).total;
+    return shared_layout(0, (size_t)g.B * g.Hkv * (kEvictUnitBytes + kEvictMarkBytes * (size_t)kl_evict_marks(budget)), 0).total;
 }
 
 kl_status kl_evict(const kl_shape *shape, const float *weights, int32_t weights_stride, int32_t budget, int32_t sinks,

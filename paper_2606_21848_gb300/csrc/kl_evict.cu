@@ -104,7 +104,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __flo
 // there are few units. Shared memory: the piece's weights, and two bits for each of them (above the border, on it).
 template <int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
-    select_kernel(const EvictArgs a, EvictUnit *units, uint4 *read, int32_t *need, int marks, int cluster, int piece) {
+    select_kernel(const EvictArgs a, EvictUnit *units, uint32_t *read, int32_t *need, int marks, int cluster, int piece) {
     constexpr int kSelWarps = kThreads / 32;
     extern __shared__ __align__(16) float held[];        // [piece], then the bits
     // of this CTA: the bins, and sums of 32 of them; the rounds take turns, since the cluster still reads the last one's
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
         }
     }
     for (int i = rank * kThreads + tid; i < marks; i += cluster * kThreads)      // (no chunk has been read)
-        read[(size_t)unit * marks + i] = make_uint4(0u, 0u, 0u, 0u);
+        read[(size_t)unit * marks + i] = 0u;
     fault = __syncthreads_or(fault);
     eq = __syncthreads_or(eq);
     if (tid == 0) {
@@ -329,20 +329,11 @@ __device__ __forceinline__ uint64_t global_timer() {
     return t;
 }
 
-// Whether the first n (or all 16) bytes at `p` are 1.
-__device__ __forceinline__ bool all_read(const uint4 *p, int n) {
-    bool all = true;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        uint32_t v;
-        asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];"
-                     : "=r"(v)
-                     : "l"(reinterpret_cast<const uint32_t *>(p) + e)
-                     : "memory");
-        const int m = min(4, n - 4 * e);
-        if (m > 0) all = all && ((v ^ 0x01010101u) & (0xffffffffu >> (32 - 8 * m))) == 0;
-    }
-    return all;
+// Whether the lowest n (or all 32) bits at `p` are set.
+__device__ __forceinline__ bool all_read(const uint32_t *p, int n) {
+    uint32_t v;
+    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return n >= 32 ? v == ~0u : (~v & ((1u << n) - 1)) == 0;
 }
 
 // t / P and t % P: P a power of two (its shift), or any (shift -1).
@@ -447,20 +438,21 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const Evi
     }
 }
 
-// CTA unit * team + t, whole rows: the CTAs of a unit take its chunks in order, from a counter. read[unit][chunk]: bytes,
-// 1 once its rows have been read (marks: 16 of them each); need[unit][chunk]: the first rows that have to be read before it
-// is written. The last warp keeps the books: it takes tickets, announces chunks and looks at the other CTAs' while the
+// CTA unit * team + t, whole rows: the CTAs of a unit take its chunks in order, from a counter. read[unit]: a
+// bit per chunk, set once its rows have been read; need[unit][chunk]: the first rows that have to be read before it is
+// written. The last warp keeps the books: it takes tickets, announces chunks and looks at the other CTAs' while the
 // movers' loads are on their way. A ticket is taken when there is room to read its chunk at once, so that no chunk waits
 // for another's write before it is read: the chunks below one that waits are with CTAs that read them.
-// The marks need no fences: what was announced has been read, since its values are here, and a write that follows a mark
-// in the program cannot be ahead of it. (3 sequences of 90000 rows to 40821, 2 heads: with fences, which wait for the
-// writes of all warps, 122 instead of 86 us; with a wait for all chunks ahead instead of those that are needed 86
-// instead of 29; with chunks in turns of the whole team instead of tickets 36.)
+// The marks are bits of words that are read as words, with a fence between a chunk's reads and its mark, and one between
+// the marks that a CTA has seen and its writes: what it overwrites has been read. (3 sequences of 90000 rows to 40821, 2
+// heads: the fences cost 4 of 33 us, since they wait for the writes of all warps; with a wait for all chunks ahead instead
+// of those that are needed 86 instead of 29 without them; with chunks in turns of the whole team instead of tickets 36.)
 constexpr int kShareThreads = kMoveThreads + 32, kShareCtas = 6;
 constexpr uint32_t kBarTake = 1, kBarRead = 2, kBarWrite = 3;    // a ticket is here; a chunk is; its place may be written
 __device__ __forceinline__ void bar(uint32_t id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kShareThreads) : "memory"); }
+__device__ __forceinline__ void gpu_fence() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
 
-__global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const EvictArgs a, EvictUnit *units, uint4 *read,
+__global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const EvictArgs a, EvictUnit *units, uint32_t *read,
                                                                           const int32_t *need, int marks, int team, int cshift,
                                                                           const Paging pg) {
     __shared__ volatile int ticket, gone;
@@ -472,7 +464,7 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
     if (unit % a.geo.Hkv == 0 && blockIdx.x % team == 0 && tid == 0) a.new_lens[unit / a.geo.Hkv] = rows;
     const int chunk = kMovePieces >> cshift;
     if (tid >= kMoveThreads) {
-        uint8_t *const mine = reinterpret_cast<uint8_t *>(read + (size_t)unit * marks);
+        uint32_t *const mine = read + (size_t)unit * marks;
         const int32_t *const first_rows = need + (size_t)unit * marks * 16;
         auto take = [&]() -> int {
             int c = 0;
@@ -489,24 +481,28 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
         bar(kBarTake);
         while (c0 * chunk < rows) {
             bar(kBarRead);
-            if (in_place && lane == 0)
-                asm volatile("st.relaxed.gpu.global.u8 [%0], %1;" ::"l"(mine + c0), "r"(1) : "memory");
+            if (in_place && lane == 0) {
+                gpu_fence();
+                asm volatile("red.relaxed.gpu.global.or.b32 [%0], %1;" ::"l"(mine + (c0 >> 5)), "r"(1u << (c0 & 31)) : "memory");
+            }
             const int c1 = take();
             bar(kBarTake);
             const int next = limit(c1);
             const uint64_t t0 = global_timer();
+            const bool looks = known < stop;
             while (known < stop) {
-                // 16 marks per lane from the last whole 16 on; as many as follow each other from there
-                const int first = known & ~15, n = min(16, stop - first - 16 * lane);
-                const bool ok = n <= 0 || all_read(reinterpret_cast<const uint4 *>(mine + first) + lane, n);
+                // a word of marks per lane from the last whole one on; as many as follow each other from there
+                const int first = known & ~31, n = min(32, stop - first - 32 * lane);
+                const bool ok = n <= 0 || all_read(mine + (first >> 5) + lane, n);
                 const unsigned not_yet = ~__ballot_sync(0xffffffffu, ok);
-                known = not_yet ? max(known, first + 16 * (__ffs(not_yet) - 1)) : min(stop, first + 512);
+                known = not_yet ? max(known, first + 32 * (__ffs(not_yet) - 1)) : min(stop, first + 1024);
                 // (one lane's clock decides for the warp)
                 if (known < stop && __shfl_sync(0xffffffffu, global_timer() - t0 > a.wait_ns, 0)) {
                     if (lane == 0) gone = 1;
                     break;
                 }
             }
+            if (looks) gpu_fence();
             __syncwarp();
             bar(kBarWrite);
             if (gone) {                                  // (rows that are still to be read may not be overwritten)
@@ -529,7 +525,8 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
     m.pages(c0 * chunk, id, page);
     m.load(c0 * chunk, id, page, x);
     while (c0 * chunk < rows) {
-        // (a word of every load goes into a branch, so that the rows are here and not only on their way)
+        // (a word of every load goes into a branch, so that the rows are here and not only on their way: the 16 bytes of
+        // a load come together)
         if ((x[0].x ^ x[1].x ^ x[2].x ^ x[3].x) == 0x9e3779b9u) __nanosleep(0);
         bar(kBarRead);
         bar(kBarTake);
@@ -559,9 +556,8 @@ cudaError_t launch_evict(const EvictArgs &a) {
             (2 * (int64_t)units * cluster <= sms && longest >= 4096 * (int64_t)cluster)))
         cluster *= 2;
     const int piece = (int)((longest + cluster - 1) / cluster + 127) & ~127;
-    // (the marks first: they are read 16 at a time)
     const int marks = kl_evict_marks(a.budget);
-    uint4 *read = static_cast<uint4 *>(a.workspace);
+    uint32_t *read = static_cast<uint32_t *>(a.workspace);
     int32_t *need = reinterpret_cast<int32_t *>(read + (size_t)units * marks);
     EvictUnit *info = reinterpret_cast<EvictUnit *>(need + (size_t)units * marks * 16);
     const bool few = units * cluster <= sms;

@@ -102,9 +102,9 @@ struct DecodeArgs {
     } causal;
 };
 
-// Arguments of a kl_evict launch. The workspace holds kEvictUnitBytes and 5 x 16 kl_evict_marks(budget) bytes for every
-// sequence and value head: five for each chunk of 32 rows or more.
-constexpr int kEvictUnitBytes = 16;
+// Arguments of a kl_evict launch. The workspace holds kEvictUnitBytes for every sequence and value head, and a word and 16
+// numbers for every 16 chunks of 32 rows or more.
+constexpr int kEvictUnitBytes = 16, kEvictMarkBytes = 4 + 16 * 4;
 inline int kl_evict_marks(int budget) { return budget / 512 + 1; }
 struct EvictArgs {
     Geometry geo;             // S and chunk unused
