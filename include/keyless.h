@@ -424,8 +424,9 @@ size_t kl_evict_workspace_size(const kl_shape *shape, int32_t weights_stride, in
  * [B][Hkv][weights_stride] fp32; kept: [B][Hkv][budget] int32; new_lens: [B] int32; new_weights may be weights
  * and new_lens may be seq_lens. block_table and new_block_table: [B][max_pages_per_seq]; page i of a sequence's
  * new table is its page i (rows then move in place; new_block_table may be block_table) or a page that no
- * sequence of the call reads. A page that is written must belong to one sequence alone. head_dim 64 or 128, any
- * page size. min(max_pages_per_seq * P, weights_stride) at most KL_EVICT_MAX_TOKENS (KL_ERR_UNSUPPORTED). A
+ * sequence of the call reads. A page that is written must belong to one sequence alone; where all of a sequence's pages
+ * stay, its rows ahead of the first one that goes are not written, and none of a sequence within its budget. head_dim
+ * 64 or 128, any page size. min(max_pages_per_seq * P, weights_stride) at most KL_EVICT_MAX_TOKENS (KL_ERR_UNSUPPORTED). A
  * sequence whose length is negative, or more than weights_stride or max_pages_per_seq * P
  * (KL_FLAG_BAD_LENGTH), or one of whose pages, old or new, lies outside the pool (KL_FLAG_BAD_PAGE) is
  * left as it is, its entries of all outputs included. Two launches. Where a CTA of the move waits longer than

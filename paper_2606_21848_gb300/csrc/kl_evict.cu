@@ -30,10 +30,13 @@ constexpr int kBins = 1 << kBits0;
 constexpr int kMostCluster = 8;
 constexpr int kMovePieces = 512;                         // 16-byte pieces of a chunk of rows: one CTA's turn of the move
 
-// What the move needs to know of a (sequence, value head): rows that stay (-1: it is left alone), whether its rows
-// may move within their pages, and the chunks that CTAs have taken.
+// What the move needs to know of a (sequence, value head): rows that stay (-1: it is left alone), whether none, some or all
+// of its pages stay, the chunks that CTAs have taken, and the first row that another row takes the place of.
+enum { kElsewhere = 0, kMixed = 1, kInPlace = 2 };
 struct EvictUnit {
-    int rows, in_place, taken, spare;
+    int rows, in_place, taken, gap;
+    // the first row that has to be written (rows: none)
+    __device__ __forceinline__ int first() const { return in_place == kInPlace ? min(gap, rows) : 0; }
 };
 static_assert(sizeof(EvictUnit) == kEvictUnitBytes, "");
 
@@ -112,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
     __shared__ __align__(8) int counts[kMostCluster][2]; // of the CTAs' pieces: above the border, on it
     __shared__ int warp_above[kSelWarps], warp_on[kSelWarps];
     __shared__ uint32_t border;
-    __shared__ __align__(8) int found[2];                // pages outside the pool; pages that stay where they are
+    __shared__ __align__(8) int found[2];                // pages outside the pool; 1: pages that stay, 2: that do not
     __shared__ int wanted, bad;
     uint2 *const sel = reinterpret_cast<uint2 *>(held + piece);
     const Geometry &geo = a.geo;
@@ -136,23 +139,29 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
         if (t0 + tid + k * kThreads < t1) ahead[k] = w[t0 + tid + k * kThreads];
-    int fault = 0, eq = 0;
+    int fault = 0, eq = 0, ne = 0;
     {
         const int pages = (L + geo.P - 1) / geo.P, new_pages = (rows + geo.P - 1) / geo.P;
 #pragma unroll 2
         for (int i = rank * kThreads + tid; i < pages; i += cluster * kThreads) {
             const int p = from[i], q = i < new_pages ? to[i] : 0;
             if (p < 0 || p >= geo.num_pages || q < 0 || q >= geo.num_pages) fault = 1;
-            if (i < new_pages && p == q) eq = 1;
+            if (i < new_pages) (p == q ? eq : ne) = 1;
         }
     }
     for (int i = rank * kThreads + tid; i < marks; i += cluster * kThreads)      // (no chunk has been read)
         read[(size_t)unit * marks + i] = 0u;
-    fault = __syncthreads_or(fault);
-    eq = __syncthreads_or(eq);
-    if (tid == 0) {
-        found[0] = fault;
-        found[1] = eq;
+    {
+        const unsigned seen = __reduce_or_sync(0xffffffffu, fault | eq << 1 | ne << 2);
+        if (lane == 0) warp_on[warp] = seen;
+        __syncthreads();
+        if (warp == 0) {
+            const unsigned any = __reduce_or_sync(0xffffffffu, lane < kSelWarps ? warp_on[lane] : 0);
+            if (lane == 0) {
+                found[0] = any & 1;
+                found[1] = any >> 1;
+            }
+        }
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
@@ -180,11 +189,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
             if (cluster > 1) ld_cluster(found, lane, x);
             else x[0] = found[0], x[1] = found[1];
         }
-        const bool fault = __any_sync(0xffffffffu, x[0]), eq = __any_sync(0xffffffffu, x[1]);
+        const bool fault = __any_sync(0xffffffffu, x[0]);
+        const int in_place = !__any_sync(0xffffffffu, x[1] & 1) ? kElsewhere : __any_sync(0xffffffffu, x[1] & 2) ? kMixed : kInPlace;
         if (lane > 0) return;
         bad = fault;
         if (tells && fault) raise_flag(a.err, KL_FLAG_BAD_PAGE);
-        if (first) units[unit] = EvictUnit{fault ? -1 : rows, eq, 0, 0};
+        if (first) units[unit] = EvictUnit{fault ? -1 : rows, in_place, 0, rows};
     };
     uint32_t key = 0;
     int shift = 31;
@@ -304,6 +314,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
             stay |= __ballot_sync(0xffffffffu, (x.y >> lane & 1) && __popc(x.y & below) < left);
             on_before += __popc(x.y);
         }
+        // (all rows before this one stay: here is the first that goes)
+        if (lane == 0 && before == t && ~stay && t + __ffs(~stay) <= L) units[unit].gap = t + __ffs(~stay) - 1;
         if (stay >> lane & 1) {
             const int at = before + __popc(stay & below);
             kept[at] = t + lane;
@@ -349,6 +361,7 @@ struct Mover {
     uint4 *v;
     int64_t page_pieces;     // 16-byte pieces of a page
     int head, cpr, c, first, rstep, rows;   // head: of the value head's first row in a page; c: of this thread in a row
+    int low;                 // the first row that is written
     Paging pg;
     __device__ __forceinline__ uint4 *piece(int page, int t) const {
         return v + page * page_pieces + head + pg.row(t) * cpr + c;
@@ -371,11 +384,13 @@ struct Mover {
         each(j, [&](int k, int) { x[k] = *piece(page[k], id[k]); });
     }
     __device__ __forceinline__ void store(int j, const uint4 (&x)[kMoveDepth]) const {
-        each(j, [&](int k, int at) { *piece(to[pg.page(at)], at) = x[k]; });
+        each(j, [&](int k, int at) {
+            if (at >= low) *piece(to[pg.page(at)], at) = x[k];
+        });
     }
 };
 // A stretch of 2^cshift pieces, number `slice`, of the rows of a unit.
-__device__ __forceinline__ Mover mover(const EvictArgs &a, int unit, int rows, int slice, int cshift, const Paging &pg) {
+__device__ __forceinline__ Mover mover(const EvictArgs &a, int unit, const EvictUnit &u, int slice, int cshift, const Paging &pg) {
     const Geometry &geo = a.geo;
     const int b = unit / geo.Hkv, g = unit % geo.Hkv, tid = threadIdx.x;
     Mover m;
@@ -389,14 +404,16 @@ __device__ __forceinline__ Mover mover(const EvictArgs &a, int unit, int rows, i
     m.c = (slice << cshift) + (tid & ((1 << cshift) - 1));
     m.first = tid >> cshift;
     m.rstep = kMoveThreads >> cshift;
-    m.rows = rows;
+    m.rows = u.rows;
+    m.low = u.first();
     m.pg = pg;
     return m;
 }
 
 // CTA ((unit * slices + slice) * groups + group) * team + rank: a cluster of `team` CTAs takes its chunks in turns, chunk
 // rank of each; `groups` of them share a unit that moves to other pages, in place the first does it alone. Three turns
-// ahead of the write a CTA reads which rows, two ahead their pages, one ahead the rows.
+// ahead of the write a CTA reads which rows, two ahead their pages, one ahead the rows. Rows ahead of the first that
+// goes are not written.
 __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const EvictArgs a, const EvictUnit *units, int slices,
                                                                        int cshift, int groups, int team, const Paging pg) {
     grid_dep_wait();
@@ -407,12 +424,13 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const Evi
     if (u.rows < 0) return;                              // (the whole cluster)
     if (unit % a.geo.Hkv == 0 && slice == 0 && group == 0 && rank == 0 && threadIdx.x == 0)
         a.new_lens[unit / a.geo.Hkv] = u.rows;
-    if (u.in_place && group > 0) return;
-    const Mover m = mover(a, unit, u.rows, slice, cshift, pg);
+    if ((u.in_place && group > 0) || u.first() >= u.rows) return;
+    const Mover m = mover(a, unit, u, slice, cshift, pg);
     const int chunk = kMovePieces >> cshift, step = chunk * team * (u.in_place ? 1 : groups);
+    const int j0 = u.first() & ~(chunk - 1);             // (a power of two)
     uint4 x[kMoveDepth], y[kMoveDepth];
     int id[kMoveDepth], page[kMoveDepth], next[kMoveDepth];
-    int j = (u.in_place ? rank : group * team + rank) * chunk;
+    int j = j0 + (u.in_place ? rank : group * team + rank) * chunk;
     m.ids(j, id);
     m.ids(j + step, next);
     m.pages(j, id, page);
@@ -421,7 +439,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const Evi
 #pragma unroll
     for (int k = 0; k < kMoveDepth; ++k) id[k] = next[k];
     m.ids(j + 2 * step, next);
-    const int turns = (u.rows + step - 1) / step;        // (as many in all CTAs: they meet)
+    const int turns = (u.rows - j0 + step - 1) / step;        // (as many in all CTAs: they meet)
     for (int s = 0; s < turns; ++s, j += step) {
         m.load(j + step, id, page, y);
         m.pages(j + 2 * step, next, page);
@@ -438,10 +456,10 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const Evi
     }
 }
 
-// CTA unit * team + t, whole rows: the CTAs of a unit take its chunks in order, from a counter. read[unit]: a
-// bit per chunk, set once its rows have been read; need[unit][chunk]: the first rows that have to be read before it is
-// written. The last warp keeps the books: it takes tickets, announces chunks and looks at the other CTAs' while the
-// movers' loads are on their way. A ticket is taken when there is room to read its chunk at once, so that no chunk waits
+// CTA unit * team + t, whole rows: the CTAs of a unit take its chunks in order, from a counter. read[unit]: a bit per chunk
+// from the first that is written on, set once its rows have been read; need[unit][chunk]: the first rows that have to be
+// read before it is written. The last warp keeps the books: it takes tickets, announces chunks and looks at the other CTAs'
+// while the movers' loads are on their way. A ticket is taken when there is room to read its chunk at once, so that no chunk waits
 // for another's write before it is read: the chunks below one that waits are with CTAs that read them.
 // The marks are bits of words that are read as words, with a fence between a chunk's reads and its mark, and one between
 // the marks that a CTA has seen and its writes: what it overwrites has been read. (3 sequences of 90000 rows to 40821, 2
@@ -459,31 +477,35 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
     grid_dep_wait();
     grid_dep_launch();
     const int unit = blockIdx.x / team, tid = threadIdx.x, lane = tid & 31;
-    const int rows = units[unit].rows, in_place = units[unit].in_place;
+    const EvictUnit u = units[unit];                     // (but for `taken`)
+    const int rows = u.rows, in_place = u.in_place;
     if (rows < 0) return;
     if (unit % a.geo.Hkv == 0 && blockIdx.x % team == 0 && tid == 0) a.new_lens[unit / a.geo.Hkv] = rows;
-    const int chunk = kMovePieces >> cshift;
+    const int chunk = kMovePieces >> cshift, base = u.first() / chunk;    // the first chunk that is written
+    if (u.first() >= rows) return;
     if (tid >= kMoveThreads) {
         uint32_t *const mine = read + (size_t)unit * marks;
         const int32_t *const first_rows = need + (size_t)unit * marks * 16;
         auto take = [&]() -> int {
             int c = 0;
-            if (lane == 0) ticket = c = atomicAdd(&units[unit].taken, 1);
+            if (lane == 0) ticket = c = base + atomicAdd(&units[unit].taken, 1);
             return __shfl_sync(0xffffffffu, c, 0);
         };
-        // chunk c may be written once those below this have been read
+        // chunk c may be written once those from base to below base + this have been read
         auto limit = [&](int c) -> int {
             if (!in_place || c * chunk >= rows) return 0;
-            return (c + 1) * chunk > rows ? c : min(c, (__ldcg(first_rows + c) + chunk - 1) / chunk);
+            return ((c + 1) * chunk > rows ? c : min(c, (__ldcg(first_rows + c) + chunk - 1) / chunk)) - base;
         };
         if (lane == 0) gone = 0;
-        int known = 0, c0 = take(), stop = limit(c0);    // known: all chunks below have been read
+        int known = 0, c0 = take(), stop = limit(c0);    // known: so many chunks from base on have been read
         bar(kBarTake);
         while (c0 * chunk < rows) {
             bar(kBarRead);
             if (in_place && lane == 0) {
                 gpu_fence();
-                asm volatile("red.relaxed.gpu.global.or.b32 [%0], %1;" ::"l"(mine + (c0 >> 5)), "r"(1u << (c0 & 31)) : "memory");
+                asm volatile("red.relaxed.gpu.global.or.b32 [%0], %1;" 
+                             ::"l"(mine + ((c0 - base) >> 5)), "r"(1u << ((c0 - base) & 31))
+                             : "memory");
             }
             const int c1 = take();
             bar(kBarTake);
@@ -514,7 +536,7 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
         }
         return;
     }
-    const Mover m = mover(a, unit, rows, 0, cshift, pg);
+    const Mover m = mover(a, unit, u, 0, cshift, pg);
     uint4 x[kMoveDepth], y[kMoveDepth];
 #pragma unroll
     for (int k = 0; k < kMoveDepth; ++k) x[k] = y[k] = make_uint4(0u, 0u, 0u, 0u);
