@@ -392,7 +392,8 @@ size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t
  * max_q_len <= KL_WEIGHTS_MAX_ROWS, num_seqs and num_kv_heads <= 65535 (KL_ERR_UNSUPPORTED otherwise); a sequence
  * of more than weights_stride tokens raises KL_FLAG_BAD_LENGTH and is skipped, like those of kl_window_attention;
  * a bad page leaves the sequence's outputs and weights unspecified. A row that is not finite makes the outputs of
- * the positions that see it NaN, and where their scores are not finite the weights that they add as well. Other
+ * the positions that see it NaN, and where their scores are not finite the weights that they add as well (a score of
+ * -inf may be a weight of 0); finite values past fp16's range reach the outputs alone. Other
  * arguments, shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every
  * run. One launch, or two. The routed query carries 24 significant bits for either type of output, and so do the
  * weights; bf16 outputs that kl_window_attention would sum up from fp16 weights and values are so here as well.

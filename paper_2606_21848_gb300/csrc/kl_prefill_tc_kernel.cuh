@@ -152,6 +152,7 @@ struct __align__(1024) PrefillSmem {
     // kWindow, kWeights: rows that some positions see and that are not finite as fp16: [0] of the tokens behind the block's
     // first position, [1] of those that leave the window within the block, each from its first
     uint32_t over[2][kBM / 32];
+    uint32_t infinite[2][kBM / 32];   // kWeights: of these, those that are not finite as bf16 either
     uint4 stage[kComputeWarps][32 * 4];   // kWindow: a warp's 32 rows of 32 outputs on their way
     uint32_t tmem_base;
     int abort;
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         sm.abort = 0;
         ptx::fence_mbar_init();
     }
-    if (kWindow && tid < 2 * kBM / 32) sm.over[0][tid] = 0;
+    if (kWindow && tid < 2 * kBM / 32) sm.over[0][tid] = sm.infinite[0][tid] = 0;
     if (warp == kMmaWarp) {
         ptx::tmem_alloc(&sm.tmem_base, kTmemCols);
         ptx::tmem_relinquish();
@@ -543,12 +544,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 0; c < 8; ++c) ld_shared_v4(v_s + ((c + lane) & 7) * 16, vr + 4 * c);
                 if (kWindow && some) {
-                    bool over = false;
+                    bool over = false, infinite = false;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) over |= PT == 1 ? past_fp16(vr[e]) : not_finite(vr[e]);
                     if (over) {
+                        if (kWeights)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) infinite |= not_finite(vr[e]);
                         const int t = t0 + (r & 63), bit = t > pos0 ? t - pos0 - 1 : t - (pos0 - window + 1);
                         atomicOr(&sm.over[t > pos0 ? 0 : 1][bit >> 5], 1u << (bit & 31));
+                        if (infinite) atomicOr(&sm.infinite[t > pos0 ? 0 : 1][bit >> 5], 1u << (bit & 31));
 #pragma unroll
                         for (int e = 0; e < 32; ++e) vr[e] = 0u;
                     }
@@ -770,20 +775,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool okp = ptx::bar_and(kWindow ? kBarWindow : pair_bar, kWindow ? 32 * kComputeWarps : 64, oke);
         float lt = l + sm.lsum[hf ^ 1][r];
         if constexpr (kWindow) {
-            // bit j of the first set: token pos0 + 1 + j; of the second: pos0 - window + 1 + j
-            const uint64_t o0 = sm.over[0][0] | (uint64_t)sm.over[0][1] << 32;
-            const uint64_t o1 = sm.over[0][2] | (uint64_t)sm.over[0][3] << 32;
-            const uint64_t w0 = sm.over[1][0] | (uint64_t)sm.over[1][1] << 32;
-            const uint64_t w1 = sm.over[1][2] | (uint64_t)sm.over[1][3] << 32;
-            if (o0 | o1 | w0 | w1) {
+            // whether the row sees a token of a set; bit j of its first half: token pos0 + 1 + j, of its second:
+            // pos0 - window + 1 + j
+            auto sees_one_of = [&](const uint32_t(&set)[2][kBM / 32]) -> bool {
+                const uint64_t o0 = set[0][0] | (uint64_t)set[0][1] << 32;
+                const uint64_t o1 = set[0][2] | (uint64_t)set[0][3] << 32;
+                const uint64_t w0 = set[1][0] | (uint64_t)set[1][1] << 32;
+                const uint64_t w1 = set[1][2] | (uint64_t)set[1][3] << 32;
+                if (!(o0 | o1 | w0 | w1)) return false;
                 const int i = pos_r - pos0, first = pos0 + 1;
                 auto sees = [&](int off) {       // 64 tokens from first + off on
                     return bits_below(i - off) & (~bits_below(i - window - off) | bits_below(sinks - first - off));
                 };
-                if ((sees(0) & o0) | (sees(64) & o1) | (~bits_below(i) & w0) | (~bits_below(i - 64) & w1)) lt = NAN;
-            }
+                return (sees(0) & o0) | (sees(64) & o1) | (~bits_below(i) & w0) | (~bits_below(i - 64) & w1);
+            };
+            // (a value past fp16's range is not finite for the outputs alone: the weights are those of its score)
+            if (kWeights && hf == 0)
+                a.stats[(blk * kBM + r) * 8 + rank] = make_float2(sm.mref[lb2][r], sees_one_of(sm.infinite) ? NAN : lt);
+            if (sees_one_of(sm.over)) lt = NAN;
         }
-        if (kWeights && hf == 0) a.stats[(blk * kBM + r) * 8 + rank] = make_float2(sm.mref[lb2][r], lt);
         if (kShared && cs > 1) {
             if (hf == 0) sm.ml[r] = okp ? make_float2(sm.mref[lb2][r], lt) : make_float2(-INFINITY, 0.f);
         } else if (okp) {
