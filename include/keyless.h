@@ -352,8 +352,9 @@ size_t kl_window_workspace_size(const kl_shape *shape, int32_t total_q, int32_t 
  * non-decreasing from 0; max_q_len: a host-side bound on every n_b (it chooses the kernel's blocks: a tight
  * one is faster); w_r (NULL: q is the composed query), v_cache, block_table, seq_lens, num_splits as in
  * kl_tree_attention. Workspace: kl_window_workspace_size bytes of the same arguments, 256-byte aligned. One
- * launch. head_dim 128, page size 16, 32, 64 or 128, compute capability
- * 10.3 (KL_ERR_UNSUPPORTED otherwise). A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or
+ * launch. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3; where R > 32 as defined below (with a W^R
+ * per query head: where max_q_len > 32), num_seqs <= 65535 and max_q_len <= 65535 * 128 (KL_ERR_UNSUPPORTED otherwise).
+ * A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or
  * seq_lens[b] <= max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine:
  * nothing is written); a bad id of a page that is read raises KL_FLAG_BAD_PAGE and leaves the affected
  * outputs unspecified (they may raise KL_FLAG_RANGE). A row that is not finite makes the outputs of the

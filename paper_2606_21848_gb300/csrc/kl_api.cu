@@ -652,8 +652,8 @@ kl_status kl_window_attention(const kl_shape *shape, const void *q, const void *
     bool some;
     if (out_dtype != KL_BF16 && out_dtype != KL_FP32) return KL_ERR_INVALID_ARG;
     kl_status st = plan_window_call(shape, total_q, max_q_len, window, sinks, num_splits, out_dtype == KL_FP32, &c);
-    // (blocks of 128 positions and more are the prefill's grid's z extent)
-    if (st == KL_OK && (int64_t)max_q_len > (int64_t)65535 * 128) st = KL_ERR_UNSUPPORTED;
+    // (sequences and blocks of 128 positions are extents of the prefill's grid)
+    if (st == KL_OK && !c.wide && (c.d.geo.B > 65535 || (int64_t)max_q_len > (int64_t)65535 * 128)) st = KL_ERR_UNSUPPORTED;
     if (st == KL_OK)
         st = check_causal(c.d.geo, q, w_r, v_cache, block_table, seq_lens, cu_q_lens, total_q, max_q_len, out, &some);
     if (st != KL_OK || !some) return st;
