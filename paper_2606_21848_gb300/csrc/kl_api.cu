@@ -634,7 +634,7 @@ extern "C" {
 
 size_t kl_window_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len, int32_t window,
                                 int32_t sinks, int32_t num_splits) {
-    size_t most = 0;
+    size_t most = 256;                                   // (0 means bad arguments, and blocks of 128 rows need nothing)
     for (int fp32 = 0; fp32 < 2; ++fp32) {
         WindowPlan c{};
         if (plan_window_call(shape, total_q, max_q_len, window, sinks, num_splits, fp32 != 0, &c) != KL_OK) return 0;
