@@ -17,9 +17,11 @@
 //   17 us).
 // - Fewer than 48: as many CTAs as the GPU holds take the chunks in order, from a counter, announce each that they have
 //   read, and ahead of a write wait for the chunks that read what it overwrites, whose number the selection has counted
-//   (3 sequences of 90000 rows to 40821, 2 heads, 29 us, in clusters 103; one of 131072 rows to 65536, one head, 17 and 140;
-//   88 units of 5300 rows to 3589 42 and 45, 64 of 2300 to 2048 36 and 17).
-// To other pages nothing waits.
+//   (3 sequences of 90000 rows to 40821, 2 heads, 35 us, in clusters 103; one of 131072 rows to 65536, one head, 16 and 140;
+//   before the fences between reads and writes, which cost up to a tenth, 88 units of 5300 rows to 3589 42, in clusters 45,
+//   64 of 2300 to 2048 36 and 17).
+// To other pages nothing waits. In place, rows ahead of the first that goes are where they belong and are not touched (64
+// sequences of 4096 rows within their budget, 8 heads: 18 us, all of it the selection; 182 to other pages).
 #include "kl_internal.cuh"
 
 namespace kl {
@@ -139,20 +141,20 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
         if (t0 + tid + k * kThreads < t1) ahead[k] = w[t0 + tid + k * kThreads];
-    int fault = 0, eq = 0, ne = 0;
+    unsigned seen = 0;                                   // 1: a page outside the pool, 2: one that stays, 4: one that does not
     {
         const int pages = (L + geo.P - 1) / geo.P, new_pages = (rows + geo.P - 1) / geo.P;
 #pragma unroll 2
         for (int i = rank * kThreads + tid; i < pages; i += cluster * kThreads) {
             const int p = from[i], q = i < new_pages ? to[i] : 0;
-            if (p < 0 || p >= geo.num_pages || q < 0 || q >= geo.num_pages) fault = 1;
-            if (i < new_pages) (p == q ? eq : ne) = 1;
+            if (p < 0 || p >= geo.num_pages || q < 0 || q >= geo.num_pages) seen |= 1;
+            if (i < new_pages) seen |= p == q ? 2 : 4;
         }
     }
     for (int i = rank * kThreads + tid; i < marks; i += cluster * kThreads)      // (no chunk has been read)
         read[(size_t)unit * marks + i] = 0u;
     {
-        const unsigned seen = __reduce_or_sync(0xffffffffu, fault | eq << 1 | ne << 2);
+        seen = __reduce_or_sync(0xffffffffu, seen);
         if (lane == 0) warp_on[warp] = seen;
         __syncthreads();
         if (warp == 0) {
@@ -315,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 4 : 1)
             on_before += __popc(x.y);
         }
         // (all rows before this one stay: here is the first that goes)
-        if (lane == 0 && before == t && ~stay && t + __ffs(~stay) <= L) units[unit].gap = t + __ffs(~stay) - 1;
+        if (before == t && lane == __ffs(~stay) - 1) units[unit].gap = t + lane;
         if (stay >> lane & 1) {
             const int at = before + __popc(stay & below);
             kept[at] = t + lane;
@@ -463,8 +465,8 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const Evi
 // for another's write before it is read: the chunks below one that waits are with CTAs that read them.
 // The marks are bits of words that are read as words, with a fence between a chunk's reads and its mark, and one between
 // the marks that a CTA has seen and its writes: what it overwrites has been read. (3 sequences of 90000 rows to 40821, 2
-// heads: the fences cost 4 of 33 us, since they wait for the writes of all warps; with a wait for all chunks ahead instead
-// of those that are needed 86 instead of 29 without them; with chunks in turns of the whole team instead of tickets 36.)
+// heads: the fences cost 4 of 35 us, since they wait for the writes of all warps. Without them, 29 us: 86 with a wait for
+// all chunks ahead instead of those that are needed, 36 with chunks in turns of the whole team instead of tickets.)
 constexpr int kShareThreads = kMoveThreads + 32, kShareCtas = 6;
 constexpr uint32_t kBarTake = 1, kBarRead = 2, kBarWrite = 3;    // a ticket is here; a chunk is; its place may be written
 __device__ __forceinline__ void bar(uint32_t id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kShareThreads) : "memory"); }
