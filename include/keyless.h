@@ -350,12 +350,12 @@ size_t kl_window_workspace_size(const kl_shape *shape, int32_t total_q, int32_t 
  * the block table may be anything.
  * q, out: [total_q][Hq][D] (q bf16, out of out_dtype); cu_q_lens: [B + 1] int32 on the device,
  * non-decreasing from 0; max_q_len: a host-side bound on every n_b (it chooses the kernel's blocks: a tight
- * one is faster); w_r (NULL: q is the composed query), v_cache, block_table, seq_lens, num_splits as in
- * kl_tree_attention. Workspace: kl_window_workspace_size bytes of the same arguments, 256-byte aligned. One
- * launch. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3; where R > 32 as defined below (with a W^R
+ * one is faster); w_r (NULL: q is the composed query), v_cache, block_table, seq_lens as in kl_tree_attention;
+ * num_splits: the parts that a block of rows is cut into at most, of which it makes 256 at most (0: chosen for the longest
+ * sequence that the table, and here the window, allow: a table little wider than the sequences is faster). Workspace:
+ * kl_window_workspace_size bytes of the same arguments, 256-byte aligned. One launch. head_dim 128, page size 16, 32, 64 or 128, compute capability 10.3; where R > 32 as defined below (with a W^R
  * per query head: where max_q_len > 32), num_seqs <= 65535 and max_q_len <= 65535 * 128 (KL_ERR_UNSUPPORTED otherwise).
- * A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or
- * seq_lens[b] <= max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine:
+ * A length that breaks 0 <= n_b <= min(max_q_len, seq_lens[b]) or seq_lens[b] <= max_pages_per_seq * P raises KL_FLAG_BAD_LENGTH and skips the sequence (n_b = 0 is fine:
  * nothing is written); a bad id of a page that is read raises KL_FLAG_BAD_PAGE and leaves the affected
  * outputs unspecified (they may raise KL_FLAG_RANGE). A row that is not finite makes the outputs of the
  * positions that see it NaN, and reaches no others.
@@ -375,7 +375,10 @@ kl_status kl_window_attention(const kl_shape *shape, const void *q, const void *
 #define KL_WEIGHTS_MAX_ROWS 128
 
 /* Bytes of device workspace kl_attention_weights needs (0 on bad arguments): the contract of
- * kl_decode_workspace_size. It holds the scores, 4 bytes for each row of a group and cached token. */
+ * kl_decode_workspace_size. It holds the scores of min(weights_stride, max_pages_per_seq * P) tokens of every sequence
+ * and value head, 4 bytes for each of them and each row: with R = (Hq / Hkv) * max_q_len up to 32 (with a W^R per query
+ * head: with max_q_len up to 32) the value head's R rows rounded up to whole blocks of at most 16, beyond that 128 rows
+ * for every block that kl_prefill_attention would form. */
 size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t max_q_len,
                                  int32_t weights_stride, int32_t num_splits);
 
@@ -396,8 +399,8 @@ size_t kl_weights_workspace_size(const kl_shape *shape, int32_t total_q, int32_t
  * the positions that see it NaN, and where their scores are not finite the weights that they add as well (a score of
  * -inf may be a weight of 0); finite values past fp16's range reach the outputs alone. Other
  * arguments, shapes and flags as in kl_window_attention. fp32 sums in a fixed order: the same weights on every
- * run. One launch, or two. The routed query carries 24 significant bits for either type of output, and so do the
- * weights; bf16 outputs that kl_window_attention would sum up from fp16 weights and values are so here as well.
+ * run. One launch, or two; num_splits 0 looks at min(weights_stride, max_pages_per_seq * P), not at the lengths. The
+ * routed query carries 24 significant bits for either type of output, and so do the weights; bf16 outputs that kl_window_attention would sum up from fp16 weights and values are so here as well.
  * Workspace: kl_weights_workspace_size bytes of the same arguments, 256-byte aligned.
  */
 kl_status kl_attention_weights(const kl_shape *shape, const void *q, const void *w_r, const void *v_cache,
