@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) move_kernel(const Evi
 #pragma unroll
     for (int k = 0; k < kMoveDepth; ++k) id[k] = next[k];
     m.ids(j + 2 * step, next);
-    const int turns = (u.rows - j0 + step - 1) / step;        // (as many in all CTAs: they meet)
+    const int turns = (u.rows - j0 + step - 1) / step;   // (as many in all CTAs: they meet)
     for (int s = 0; s < turns; ++s, j += step) {
         m.load(j + step, id, page, y);
         m.pages(j + 2 * step, next, page);
@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(kShareThreads, kShareCtas) share_kernel(const 
             bar(kBarRead);
             if (in_place && lane == 0) {
                 gpu_fence();
-                asm volatile("red.relaxed.gpu.global.or.b32 [%0], %1;" 
+                asm volatile("red.relaxed.gpu.global.or.b32 [%0], %1;"
                              ::"l"(mine + ((c0 - base) >> 5)), "r"(1u << ((c0 - base) & 31))
                              : "memory");
             }
